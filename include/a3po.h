@@ -109,7 +109,13 @@ typedef struct {
                                /* round trip); a value <= 0 selects this call's own token count         */
 } a3po_loss_options;
 
-enum { A3PO_WS_LOSS_FWD_BWD = 0, A3PO_WS_FUSED_LMHEAD = 1, A3PO_WS_FUSED_LMHEAD_LOSS = 2 };
+enum {
+    A3PO_WS_LOSS_FWD_BWD = 0,
+    A3PO_WS_FUSED_LMHEAD = 1,
+    A3PO_WS_FUSED_LMHEAD_LOSS = 2,
+    A3PO_WS_NORM_BWD = 3,     /* T and H */
+    A3PO_WS_ADJUST_LOGITS = 4 /* T and V */
+};
 
 /* Bytes of device workspace the given entry point needs (256-byte aligned base). */
 size_t a3po_workspace_bytes(int which, int64_t T, int64_t V, int64_t H);
@@ -389,6 +395,116 @@ int a3po_fused_lmhead_loss_fwd_bwd(const void *hidden, const void *weight, int64
                                    void *dhidden, void *dweight, float *logp_out, float *logp_prox_out,
                                    float *loss_out, a3po_stats *stats_out,
                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- operators around the log-probs ------------------------------------------------------------------
+ *
+ * What lies between the last layer's hidden states and the policy that tokens are drawn from, in rollouts and in
+ * training: the final norm with its gradient, the head of a rollout with its weight held in 4 bits, and the adjustment
+ * of logits with the gradient back through it.
+ */
+
+typedef enum {
+    A3PO_NORM_LAYER = 0, /* mean and variance of the row */
+    A3PO_NORM_RMS = 1    /* root mean square of the row: no mean, no bias */
+} a3po_norm_kind;
+
+#define A3PO_NORM_MAX_H 16384
+
+/*
+ * Layer norm, or its root-mean-square form, of every row:
+ *   kind: a3po_norm_kind.  mean_t = mean_h x[t,h] (RMS: 0),  rstd_t = 1 / sqrt(mean_h (x[t,h] - mean_t)^2 + eps),
+ *   y[t,h] = (x[t,h] - mean_t) rstd_t weight[h] + bias[h].
+ * x [T, H], dtype x_dt, row stride ldx; y [T, H], dtype y_dt, row stride ldy (strides >= H elements; rows may start at
+ * any element of their type).  y may alias x exactly when dtype and stride agree.  weight (nullable: 1) and bias
+ * (nullable: 0; NULL for A3PO_NORM_RMS) [H], dtype param_dt.  mean_out (A3PO_NORM_LAYER only) and rstd_out [T] float,
+ * nullable: what the backward pass takes.  1 <= H <= A3PO_NORM_MAX_H.  Statistics and products are fp32; y is rounded
+ * once.  Each row is read once.
+ */
+int a3po_norm_fwd(const void *x, a3po_dtype x_dt, int64_t T, int64_t H, int64_t ldx, const void *weight, const void *bias,
+                  a3po_dtype param_dt, float eps, int32_t kind, void *y, a3po_dtype y_dt, int64_t ldy,
+                  float *mean_out, float *rstd_out, void *stream);
+
+/*
+ * Gradient of a3po_norm_fwd.  With xhat = (x - mean) rstd and g = dy weight:
+ *   dx[t,h] = rstd_t (g - mean_h(g) - xhat mean_h(g xhat))   (RMS: without mean_h(g)),
+ *   dweight[h] = sum_t dy xhat,  dbias[h] = sum_t dy.
+ * dy [T, H] dtype y_dt, row stride lddy; x as in the forward call; mean (A3PO_NORM_LAYER) and rstd [T] float as the forward
+ * call wrote them.  dx [T, H], dtype x_dt, row stride lddx; it may alias x or dy exactly when dtype and stride agree.
+ * dweight, dbias [H] float, nullable; dbias is NULL for A3PO_NORM_RMS.  accumulate = 1 adds to what they hold
+ * (micro-batches of one update), 0 overwrites.  The sums over rows are taken in a fixed order: identical inputs give
+ * bit-identical outputs.  T == 0 clears dweight and dbias unless accumulating.
+ * workspace: a3po_workspace_bytes(A3PO_WS_NORM_BWD, T, 0, H) bytes, 256-byte aligned (not needed, and NULL, when neither
+ * dweight nor dbias is asked for).
+ */
+int a3po_norm_bwd(const void *dy, a3po_dtype y_dt, int64_t lddy, const void *x, a3po_dtype x_dt, int64_t T, int64_t H,
+                  int64_t ldx, const void *weight, a3po_dtype param_dt, const float *mean, const float *rstd,
+                  int32_t kind, void *dx, int64_t lddx, float *dweight, float *dbias, int32_t accumulate,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/* How the logits of each row are adjusted.  Host struct of device pointers, read during the call only; every array may be
+ * NULL (no such adjustment), and a zero-filled struct changes nothing. */
+typedef struct {
+    const int32_t *history;    /* token ids; row t's history is history[hist_start[t]] .. [hist_start[t] + hist_len[t] - 1]. */
+                               /* Rows may share or overlap: the tokens of one packed sequence have its start and growing    */
+                               /* lengths.  Ids outside [0,V) match no token; ranges are cut at the array's end, and a start */
+                               /* outside the array is an empty history.                                                     */
+    int64_t history_tokens;    /* elements of `history`                                                                      */
+    const int64_t *hist_start; /* [T], required with history                                                                 */
+    const int32_t *hist_len;   /* [T], required with history (<= 0: empty)                                                   */
+    const int32_t *prompt_len; /* [T]: the first prompt_len[t] tokens of the history are not output (NULL: all are)          */
+    const float *repetition;   /* [T]: u > 0 ? u / repetition : u * repetition for every token in the history (> 0)          */
+    const float *frequency;    /* [T]: u -= frequency * (how often the output holds the token)                               */
+    const float *presence;     /* [T]: u -= presence where the output holds the token                                        */
+    const float *temperature;  /* [T]: u /= temperature (> 0), after everything above and the bias                           */
+    const float *bias;         /* u += bias[t * bias_ld + v]; bias_ld = 0: one [V] row for all                               */
+    int64_t bias_ld;
+    const int32_t *allowed;    /* bit v % 32 of word allowed[t * allowed_ld + v / 32]: 0 makes u -inf; allowed_ld = 0: one   */
+    int64_t allowed_ld;        /* row of ceil(V / 32) words for all                                                          */
+} a3po_logit_adjustments;
+
+/*
+ * Logits of the policy that tokens are drawn from, with its log-sum-exp and the log-prob of a chosen token in the same read:
+ *   u[t,v] = logits[t,v] adjusted in the order of the struct's fields, bias before temperature, the mask last,
+ *   lse_out[t] = log sum_v exp u[t,v],  logp_out[t] = u[t, chosen[t]] - lse_out[t].
+ * logits [T, V] dtype dt, row stride ld.  out [T, V] dtype out_dt, row stride ld_out, nullable (log-probs only); it may
+ * alias logits exactly when dtype and stride agree.  chosen [T] int32, required with logp_out; an id outside [0,V) gives
+ * logp 0.  lse_out, logp_out [T] float, nullable; at least one output is required.  Everything is computed in fp32, and lse
+ * and logp are those of the fp32 values: out in float32 holds exactly these, out in bfloat16 rounds them once.
+ * A row with nothing allowed (or all -inf) has lse -inf; a chosen token with u = -inf has logp -inf.
+ * Masked entries are -inf whatever the logit holds, NaN included; an unmasked NaN or +inf makes the row's lse and logp NaN.
+ * V <= 2^31 - 1.  workspace: a3po_workspace_bytes(A3PO_WS_ADJUST_LOGITS, T, V, 0) bytes, 256-byte aligned (not needed, and
+ * NULL, when out alone is asked for).
+ */
+int a3po_adjust_logits(const void *logits, a3po_dtype dt, int64_t T, int64_t V, int64_t ld, const a3po_logit_adjustments *adj,
+                       const int32_t *chosen, void *out, a3po_dtype out_dt, int64_t ld_out, float *lse_out, float *logp_out,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient through a3po_adjust_logits: dout [T, V] (dtype out_dt, row stride ld_out) is the gradient with respect to the
+ * adjusted logits, as a3po_loss_fwd_bwd on them gives it;
+ *   dlogits[t,v] = dout[t,v] / temperature[t] * (v in the history: logits[t,v] > 0 ? 1 / repetition[t] : repetition[t]),
+ * 0 where v is not allowed.  logits as in the forward call (not overwritten by it): only entries in the history are read,
+ * and it may be NULL when there is no history or no repetition.  dlogits [T, V] dtype dt, row stride ld_d; it may alias
+ * dout exactly when dtype and stride agree.  Penalties, bias and temperature are constants of the policy: they get no
+ * gradient.
+ */
+int a3po_adjust_logits_bwd(const void *dout, a3po_dtype out_dt, int64_t ld_out, const void *logits, a3po_dtype dt, int64_t T,
+                           int64_t V, int64_t ld, const a3po_logit_adjustments *adj, void *dlogits, int64_t ld_d,
+                           void *stream);
+
+/*
+ * Products of a few tokens with a weight held as 4-bit codes (the head of a rollout; any linear layer):
+ *   out[t,n] = sum_k scale[n, k / group] (code[n,k] - zero[n, k / group]) x[t,k].
+ * x [T, H] bfloat16, row stride ldx (any element alignment).  codes [N, H / 2] bytes, row-major, contiguous, 16-byte
+ * aligned: byte j of a row holds code 2j in its low and 2j + 1 in its high half.  scales [N, H / group] dtype scale_dt,
+ * contiguous.  zeros [N, H / group] bytes, nullable (8 everywhere: codes are symmetric).  group 32, 64 or 128; H a multiple
+ * of it, at most 2^20.  out [T, N] dtype out_dt, row stride ld_out.
+ * T has no limit, but the weight is read once per 64 tokens: the kernel is made for single tokens and small batches.
+ * Products are exact and summed in fp32, out is rounded once.  x is expected to be finite (an infinity gives NaN).
+ */
+int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8_t *codes, const void *scales,
+                   a3po_dtype scale_dt, const uint8_t *zeros, int32_t group, int64_t N, void *out, a3po_dtype out_dt,
+                   int64_t ld_out, void *stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,9 @@ A3PO_PROX_INTERP, A3PO_PROX_GIVEN, A3PO_PROX_BEHAV = 0, 1, 2
 A3PO_WS_LOSS_FWD_BWD = 0
 A3PO_WS_FUSED_LMHEAD = 1
 A3PO_WS_FUSED_LMHEAD_LOSS = 2
+A3PO_WS_NORM_BWD = 3
+A3PO_WS_ADJUST_LOGITS = 4
+A3PO_NORM_LAYER, A3PO_NORM_RMS = 0, 1
 
 # layout of a3po_stats (include/a3po.h)
 STATS_DTYPE = np.dtype([("n_tokens", "<i8"), ("n_clipped", "<i8"), ("n_bad_index", "<i8"),
@@ -35,6 +38,15 @@ class LossOptions(ctypes.Structure):
                 ("entropy_out", ctypes.c_void_p), ("iw_out", ctypes.c_void_p), ("clipped_out", ctypes.c_void_p),
                 ("event_before_rows", ctypes.c_void_p), ("event_after_rows", ctypes.c_void_p),
                 ("denom_dev", ctypes.c_void_p)]
+
+
+class LogitAdjustments(ctypes.Structure):
+    """a3po_logit_adjustments (include/a3po.h)."""
+    _fields_ = [("history", ctypes.c_void_p), ("history_tokens", ctypes.c_int64), ("hist_start", ctypes.c_void_p),
+                ("hist_len", ctypes.c_void_p), ("prompt_len", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("bias_ld", ctypes.c_int64), ("allowed", ctypes.c_void_p),
+                ("allowed_ld", ctypes.c_int64)]
 
 
 _SIGNATURES = {
@@ -61,6 +73,16 @@ _SIGNATURES = {
                                            _P, _P, _F32, _F32, _P, _P, _P, _P, _P, _SZ, _P,
                                            ctypes.POINTER(LossOptions)]),
     "a3po_token_logprobs_entropy": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _P, _P, _P, _P]),
+    "a3po_norm_fwd": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I64, _I64, _P, _P, ctypes.c_int, _F32, _I32, _P,
+                                     ctypes.c_int, _I64, _P, _P, _P]),
+    "a3po_norm_bwd": (ctypes.c_int, [_P, ctypes.c_int, _I64, _P, ctypes.c_int, _I64, _I64, _I64, _P, ctypes.c_int, _P, _P,
+                                     _I32, _P, _I64, _P, _P, _I32, _P, _SZ, _P]),
+    "a3po_adjust_logits": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I64, _I64, ctypes.POINTER(LogitAdjustments), _P, _P,
+                                          ctypes.c_int, _I64, _P, _P, _P, _SZ, _P]),
+    "a3po_adjust_logits_bwd": (ctypes.c_int, [_P, ctypes.c_int, _I64, _P, ctypes.c_int, _I64, _I64, _I64,
+                                              ctypes.POINTER(LogitAdjustments), _P, _I64, _P]),
+    "a3po_w4_linear": (ctypes.c_int, [_P, _I64, _I64, _I64, _P, _P, ctypes.c_int, _P, _I32, _I64, _P, ctypes.c_int, _I64,
+                                      _P]),
 }
 
 _lib = None
@@ -447,6 +469,204 @@ def fused_lmhead_loss_fwd_bwd(hidden, weight, chosen, logp_behav, versions, curr
         _ptr(advantages), _ptr(loss_mask), float(clip_eps), float(denom), _ptr(dh), _ptr(dw), _ptr(logp), _ptr(prox),
         _ptr(loss), _ptr(stats), _ptr(workspace), workspace.numel(), _stream()), "a3po_fused_lmhead_loss_fwd_bwd")
     return dict(dhidden=dh, dweight=dw, logp=logp, logp_prox=prox, loss=loss, stats=stats, workspace=workspace)
+
+
+# ---- operators around the log-probs ----------------------------------------------------------------------------------
+
+
+def _dtype_code(t, name):
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return A3PO_BF16
+    if t.dtype == torch.float32:
+        return A3PO_F32
+    raise TypeError(f"{name} must be float32 or bfloat16")
+
+
+def _rows(t, name, shape=None):
+    """(dtype code, row stride) of a row-major matrix on the GPU."""
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), f"{name} must be a row-major CUDA matrix"
+    assert shape is None or tuple(t.shape) == shape, f"{name}: need shape {shape}"
+    return _dtype_code(t, name), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _params(weight, bias, H):
+    """The dtype code that weight and bias share."""
+    code = None
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            _vec(t, t.dtype, H, name)
+            assert code is None or code == _dtype_code(t, name), "weight and bias must have one dtype"
+            code = _dtype_code(t, name)
+    return A3PO_F32 if code is None else code
+
+
+def norm_fwd(x, weight=None, bias=None, eps: float = 1e-6, kind: int = A3PO_NORM_LAYER, out=None, out_dtype=None,
+             want_stats=True):
+    """a3po_norm_fwd -> (y[T, H], mean[T] f32 | None, rstd[T] f32 | None).  y goes to ``out`` (may be ``x`` itself), or to a
+    new tensor of ``out_dtype`` (x's by default).  The statistics are what norm_bwd takes; mean is None for A3PO_NORM_RMS."""
+    torch = _torch()
+    xd, ldx = _rows(x, "x")
+    T, H = x.shape
+    if out is None:
+        out = torch.empty((T, H), dtype=x.dtype if out_dtype is None else out_dtype, device=x.device)
+    yd, ldy = _rows(out, "out", (T, H))
+    mean = torch.empty(T, dtype=torch.float32, device=x.device) if want_stats and kind == A3PO_NORM_LAYER else None
+    rstd = torch.empty(T, dtype=torch.float32, device=x.device) if want_stats else None
+    _check(lib().a3po_norm_fwd(_ptr(x), xd, T, H, ldx, _ptr(weight), _ptr(bias), _params(weight, bias, H), float(eps),
+                               int(kind), _ptr(out), yd, ldy, _ptr(mean), _ptr(rstd), _stream()), "a3po_norm_fwd")
+    return out, mean, rstd
+
+
+def norm_bwd(dy, x, weight, rstd, mean=None, kind: int = A3PO_NORM_LAYER, dx=None, want_dweight=True, want_dbias=False,
+             dweight=None, dbias=None, accumulate=False, workspace=None):
+    """a3po_norm_bwd -> dict(dx (x's dtype), dweight f32[H] | None, dbias f32[H] | None, workspace).  ``dx`` may be ``x`` or
+    ``dy`` itself; with ``accumulate`` the sums are added to the given ``dweight`` / ``dbias``."""
+    torch = _torch()
+    yd, lddy = _rows(dy, "dy")
+    T, H = dy.shape
+    xd, ldx = _rows(x, "x", (T, H))
+    _vec(rstd, torch.float32, T, "rstd")
+    if mean is not None:
+        _vec(mean, torch.float32, T, "mean")
+    dev = x.device
+    if dx is None:
+        dx = torch.empty((T, H), dtype=x.dtype, device=dev)
+    assert dx.dtype == x.dtype, "dx must have x's dtype"
+    lddx = _rows(dx, "dx", (T, H))[1]
+    if accumulate and ((want_dweight and dweight is None) or (want_dbias and dbias is None)):
+        raise ValueError("accumulate needs the sums of the earlier calls in `dweight` / `dbias`")
+    if dweight is None and want_dweight:
+        dweight = torch.empty(H, dtype=torch.float32, device=dev)
+    if dbias is None and want_dbias:
+        dbias = torch.empty(H, dtype=torch.float32, device=dev)
+    for name, t in (("dweight", dweight), ("dbias", dbias)):
+        if t is not None:
+            _vec(t, torch.float32, H, name)
+    if workspace is None and (dweight is not None or dbias is not None):
+        workspace = torch.empty(workspace_bytes(T, 0, H, which=A3PO_WS_NORM_BWD), dtype=torch.uint8, device=dev)
+    _check(lib().a3po_norm_bwd(_ptr(dy), yd, lddy, _ptr(x), xd, T, H, ldx, _ptr(weight), _params(weight, None, H),
+                               _ptr(mean), _ptr(rstd), int(kind), _ptr(dx), lddx, _ptr(dweight), _ptr(dbias),
+                               int(bool(accumulate)), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                               _stream()), "a3po_norm_bwd")
+    return dict(dx=dx, dweight=dweight, dbias=dbias, workspace=workspace)
+
+
+def _adjustments(T, V, history, hist_start, hist_len, prompt_len, repetition, frequency, presence, temperature, bias,
+                 allowed):
+    torch = _torch()
+    adj = LogitAdjustments()
+    if history is not None:
+        adj.history, adj.history_tokens = _ptr(_vec(history, torch.int32, history.numel(), "history")), history.numel()
+        if hist_start is None or hist_len is None:
+            raise ValueError("history needs hist_start and hist_len")
+        adj.hist_start = _ptr(_vec(hist_start, torch.int64, T, "hist_start"))
+        adj.hist_len = _ptr(_vec(hist_len, torch.int32, T, "hist_len"))
+        if prompt_len is not None:
+            adj.prompt_len = _ptr(_vec(prompt_len, torch.int32, T, "prompt_len"))
+    if repetition is not None:
+        adj.repetition = _ptr(_vec(repetition, torch.float32, T, "repetition"))
+    if frequency is not None:
+        adj.frequency = _ptr(_vec(frequency, torch.float32, T, "frequency"))
+    if presence is not None:
+        adj.presence = _ptr(_vec(presence, torch.float32, T, "presence"))
+    if temperature is not None:
+        adj.temperature = _ptr(_vec(temperature, torch.float32, T, "temperature"))
+    if bias is not None:
+        adj.bias, adj.bias_ld = _shared_rows(bias, torch.float32, T, V, "bias")
+    if allowed is not None:
+        adj.allowed, adj.allowed_ld = _shared_rows(allowed, torch.int32, T, (V + 31) // 32, "allowed")
+    return adj
+
+
+def _shared_rows(t, dtype, T, width, name):
+    """(pointer, row stride) of [T, width], or of one [width] row for all (stride 0; also a row expanded to [T, width])."""
+    assert t.is_cuda and t.dtype == dtype and t.stride(-1) == 1 and t.shape[-1] == width, f"{name}: need {dtype}[..., {width}] on GPU"
+    if t.dim() == 1:
+        return t.data_ptr(), 0
+    assert t.dim() == 2 and t.shape[0] == T, f"{name}: need one row, or one for each of the {T}"
+    return t.data_ptr(), t.stride(0) if T > 1 else 0
+
+
+def adjust_logits(logits, V=None, *, history=None, hist_start=None, hist_len=None, prompt_len=None, repetition=None,
+                  frequency=None, presence=None, temperature=None, bias=None, allowed=None, chosen=None, out=None,
+                  out_dtype=None, write=True, want_lse=True, workspace=None):
+    """a3po_adjust_logits -> dict(out | None, lse[T] f32 | None, logp[T] f32 | None, workspace).
+
+    history int32 [tokens], hist_start int64 [T], hist_len / prompt_len int32 [T]; repetition, frequency, presence,
+    temperature float32 [T]; bias float32 [V] or [T, V]; allowed int32 [ceil(V/32)] or [T, ceil(V/32)] bits.  The adjusted
+    logits go to ``out`` (may be ``logits`` itself) or to a new tensor of ``out_dtype`` (logits' by default); ``write=False``
+    computes lse and, with ``chosen``, the log-probs alone."""
+    torch = _torch()
+    dt, T, V, ld = _logits_meta(logits, V)
+    dev = logits.device
+    adj = _adjustments(T, V, history, hist_start, hist_len, prompt_len, repetition, frequency, presence, temperature, bias,
+                       allowed)
+    od, ld_out = dt, 0
+    if not write:
+        out = None
+    else:
+        if out is None:
+            out = torch.empty((T, V), dtype=logits.dtype if out_dtype is None else out_dtype, device=dev)
+        od, ld_out = _rows(out, "out")
+        assert out.shape[0] == T and out.shape[1] >= V, f"out: need [{T}, {V}]"
+    lse = torch.empty(T, dtype=torch.float32, device=dev) if want_lse else None
+    logp = None
+    if chosen is not None:
+        _vec(chosen, torch.int32, T, "chosen")
+        logp = torch.empty(T, dtype=torch.float32, device=dev)
+    if workspace is None and (lse is not None or logp is not None):
+        workspace = torch.empty(workspace_bytes(T, V, which=A3PO_WS_ADJUST_LOGITS), dtype=torch.uint8, device=dev)
+    _check(lib().a3po_adjust_logits(_ptr(logits), dt, T, V, ld, ctypes.byref(adj), _ptr(chosen), _ptr(out), od, ld_out,
+                                    _ptr(lse), _ptr(logp), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                    _stream()), "a3po_adjust_logits")
+    return dict(out=out, lse=lse, logp=logp, workspace=workspace)
+
+
+def adjust_logits_bwd(dout, logits=None, V=None, *, history=None, hist_start=None, hist_len=None, prompt_len=None,
+                      repetition=None, frequency=None, presence=None, temperature=None, bias=None, allowed=None,
+                      dlogits=None, dtype=None):
+    """a3po_adjust_logits_bwd -> dlogits: ``dlogits`` itself (may be ``dout``), or a new tensor of ``dtype`` (logits', or
+    dout's without logits).  The adjustments are those of the forward call; logits are needed with history and repetition."""
+    torch = _torch()
+    od, T, V, ld_out = _logits_meta(dout, V)
+    adj = _adjustments(T, V, history, hist_start, hist_len, prompt_len, repetition, frequency, presence, temperature, bias,
+                       allowed)
+    ld = V
+    if logits is not None:
+        zd, zT, _, ld = _logits_meta(logits, V)
+        assert zT == T and logits.shape[1] >= V, f"logits: need [{T}, {V}]"
+    if dlogits is None:
+        dtype = dtype if dtype is not None else dout.dtype if logits is None else logits.dtype
+        dlogits = torch.empty((T, V), dtype=dtype, device=dout.device)
+    dd, ld_d = _rows(dlogits, "dlogits")
+    assert dlogits.shape[0] == T and dlogits.shape[1] >= V, f"dlogits: need [{T}, {V}]"
+    assert logits is None or dd == zd, "dlogits must have logits' dtype"
+    _check(lib().a3po_adjust_logits_bwd(_ptr(dout), od, ld_out, _ptr(logits), dd, T, V, ld, ctypes.byref(adj), _ptr(dlogits),
+                                        ld_d, _stream()), "a3po_adjust_logits_bwd")
+    return dlogits
+
+
+def w4_linear(x, codes, scales, zeros=None, group: int = 128, out=None, out_dtype=None):
+    """a3po_w4_linear -> out[T, N] (``out``, or a new tensor of ``out_dtype``, bfloat16 by default).  x bfloat16 [T, H];
+    codes uint8 [N, H/2] (low half: even k); scales bfloat16 or float32 [N, H/group]; zeros uint8 [N, H/group] or None (8)."""
+    torch = _torch()
+    assert x.dtype == torch.bfloat16, "x must be bfloat16"
+    ldx = _rows(x, "x")[1]
+    T, H = x.shape
+    N = codes.shape[0]
+    assert group in (32, 64, 128) and H % group == 0, "group must be 32, 64 or 128 and divide H"
+    _vec(codes, torch.uint8, N * (H // 2), "codes")
+    _vec(scales, scales.dtype, N * (H // group), "scales")
+    if zeros is not None:
+        _vec(zeros, torch.uint8, N * (H // group), "zeros")
+    if out is None:
+        out = torch.empty((T, N), dtype=torch.bfloat16 if out_dtype is None else out_dtype, device=x.device)
+    od, ld_out = _rows(out, "out", (T, N))
+    _check(lib().a3po_w4_linear(_ptr(x), T, H, ldx, _ptr(codes), _ptr(scales), _dtype_code(scales, "scales"), _ptr(zeros),
+                                int(group), N, _ptr(out), od, ld_out, _stream()), "a3po_w4_linear")
+    return out
+
 
 
 def stats_to_dict(stats_tensor) -> dict:

@@ -32,6 +32,53 @@ int check_logits(const void *logits, int dt, int64_t T, int64_t V, int64_t ld)
     return A3PO_OK;
 }
 
+uintptr_t elem(int dt) { return dt == A3PO_F32 ? 4 : 2; }
+
+int check_norm(int x_dt, int y_dt, int param_dt, int kind, int64_t T, int64_t H)
+{
+    for (int dt : {x_dt, y_dt, param_dt})
+        if (dt != A3PO_F32 && dt != A3PO_BF16) return A3PO_E_DTYPE;
+    if (T < 0 || T > kMaxRows || H <= 0 || H > A3PO_NORM_MAX_H) return A3PO_E_SIZE;
+    if (kind != A3PO_NORM_LAYER && kind != A3PO_NORM_RMS) return A3PO_E_VALUE;
+    return A3PO_OK;
+}
+
+int check_adjustments(const a3po_logit_adjustments *adj, int64_t T, int64_t V)
+{
+    if (!adj || T == 0) return A3PO_OK;
+    if (adj->history && (adj->history_tokens < 0 || adj->history_tokens > kMaxStride)) return A3PO_E_SIZE;
+    if (adj->history && (!adj->hist_start || !adj->hist_len)) return A3PO_E_NULL;
+    if (adj->bias && adj->bias_ld != 0 && (adj->bias_ld < V || adj->bias_ld > kMaxStride)) return A3PO_E_SIZE;
+    if (adj->allowed && adj->allowed_ld != 0 && (adj->allowed_ld < (V + 31) / 32 || adj->allowed_ld > kMaxStride))
+        return A3PO_E_SIZE;
+    const void *words[] = {adj->history, adj->hist_len, adj->prompt_len, adj->repetition, adj->frequency,
+                           adj->presence, adj->temperature, adj->bias, adj->allowed};
+    for (const void *p : words)
+        if (!aligned(p, 4)) return A3PO_E_ALIGN;
+    return aligned(adj->hist_start, 8) ? A3PO_OK : A3PO_E_ALIGN;
+}
+
+AdjustArgs adjust_args(const a3po_logit_adjustments *adj)
+{
+    AdjustArgs a = {};
+    if (!adj) return a;
+    // (a history changes nothing without a strength)
+    if (adj->repetition || adj->frequency || adj->presence) a.history = adj->history;
+    a.history_tokens = adj->history_tokens;
+    a.hist_start = adj->hist_start;
+    a.hist_len = adj->hist_len;
+    a.prompt_len = adj->prompt_len;
+    a.repetition = adj->repetition;
+    a.frequency = adj->frequency;
+    a.presence = adj->presence;
+    a.temperature = adj->temperature;
+    a.bias = adj->bias;
+    a.bias_ld = adj->bias_ld;
+    a.allowed = adj->allowed;
+    a.allowed_ld = adj->allowed_ld;
+    return a;
+}
+
 // ---- workspace of the entry point that allocates nothing ----------------------------------------------
 // One array per GPU, part of the loaded code object and held until the process ends.  In host code the
 // array's name is only a handle for hipGetSymbolAddress: the device address is looked up once per device,
@@ -64,6 +111,8 @@ size_t a3po_workspace_bytes(int which, int64_t T, int64_t V, int64_t H)
     if (which == A3PO_WS_LOSS_FWD_BWD) return loss_ws_layout(T).total;
     if (which == A3PO_WS_FUSED_LMHEAD) return lmhead_workspace_bytes(T);
     if (which == A3PO_WS_FUSED_LMHEAD_LOSS) return lmhead_bwd_workspace_bytes(T, V, H);
+    if (which == A3PO_WS_NORM_BWD) return norm_bwd_workspace_bytes(T, H);
+    if (which == A3PO_WS_ADJUST_LOGITS) return adjust_workspace_bytes(T, V);
     return 0;
 }
 
@@ -378,6 +427,157 @@ int a3po_shard_loss_bwd(const void *logits_shard, a3po_dtype dt, int64_t T, int6
     if (launch_shard_bwd_rows(b, v0, logp_theta, lse, s) != hipSuccess) return A3PO_E_LAUNCH;
     if (launch_loss_finish(a, s) != hipSuccess) return A3PO_E_LAUNCH;
     return A3PO_OK;
+}
+
+int a3po_norm_fwd(const void *x, a3po_dtype x_dt, int64_t T, int64_t H, int64_t ldx, const void *weight, const void *bias,
+                  a3po_dtype param_dt, float eps, int32_t kind, void *y, a3po_dtype y_dt, int64_t ldy,
+                  float *mean_out, float *rstd_out, void *stream)
+{
+    if (int rc = check_norm((int)x_dt, (int)y_dt, (int)param_dt, kind, T, H)) return rc;
+    if (ldx < H || ldy < H || ldx > kMaxStride || ldy > kMaxStride) return A3PO_E_SIZE;
+    if (!(eps >= 0.0f)) return A3PO_E_VALUE;
+    if (kind == A3PO_NORM_RMS && (bias || mean_out)) return A3PO_E_VALUE;
+    if (T == 0) return A3PO_OK;
+    if (!x || !y) return A3PO_E_NULL;
+    if (!aligned(x, elem(x_dt)) || !aligned(y, elem(y_dt)) || !aligned(weight, elem(param_dt)) || !aligned(bias, elem(param_dt)))
+        return A3PO_E_ALIGN;
+    NormArgs a = {};
+    a.x = x;
+    a.weight = weight;
+    a.bias = bias;
+    a.y = y;
+    a.x_dt = (int)x_dt;
+    a.y_dt = (int)y_dt;
+    a.param_f32 = param_dt == A3PO_F32;
+    a.center = kind == A3PO_NORM_LAYER;
+    a.T = T;
+    a.H = (int)H;
+    a.ldx = ldx;
+    a.ldy = ldy;
+    a.eps = eps;
+    a.mean = mean_out;
+    a.rstd = rstd_out;
+    return launch_norm_fwd(a, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+}
+
+int a3po_norm_bwd(const void *dy, a3po_dtype y_dt, int64_t lddy, const void *x, a3po_dtype x_dt, int64_t T, int64_t H,
+                  int64_t ldx, const void *weight, a3po_dtype param_dt, const float *mean, const float *rstd,
+                  int32_t kind, void *dx, int64_t lddx, float *dweight, float *dbias, int32_t accumulate,
+                  void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_norm((int)x_dt, (int)y_dt, (int)param_dt, kind, T, H)) return rc;
+    if (ldx < H || lddy < H || lddx < H || ldx > kMaxStride || lddy > kMaxStride || lddx > kMaxStride) return A3PO_E_SIZE;
+    if (accumulate != 0 && accumulate != 1) return A3PO_E_VALUE;
+    if (kind == A3PO_NORM_RMS && dbias) return A3PO_E_VALUE;
+    if (T > 0 && (!dy || !x || !rstd || !dx || (kind == A3PO_NORM_LAYER && !mean))) return A3PO_E_NULL;
+    if (!aligned(dy, elem(y_dt)) || !aligned(x, elem(x_dt)) || !aligned(dx, elem(x_dt)) || !aligned(weight, elem(param_dt)))
+        return A3PO_E_ALIGN;
+    if (T > 0 && (dweight || dbias)) {
+        if (!workspace || workspace_bytes < norm_bwd_workspace_bytes(T, H)) return A3PO_E_WORKSPACE;
+        if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
+    }
+    NormArgs a = {};
+    a.dy = dy;
+    a.x = x;
+    a.weight = weight;
+    a.dx = dx;
+    a.x_dt = (int)x_dt;
+    a.y_dt = (int)y_dt;
+    a.param_f32 = param_dt == A3PO_F32;
+    a.center = kind == A3PO_NORM_LAYER;
+    a.T = T;
+    a.H = (int)H;
+    a.ldx = ldx;
+    a.ldy = lddy;
+    a.lddx = lddx;
+    a.mean = const_cast<float *>(mean);
+    a.rstd = const_cast<float *>(rstd);
+    const hipError_t e = launch_norm_bwd(a, dweight, dbias, accumulate, workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+}
+
+int a3po_adjust_logits(const void *logits, a3po_dtype dt, int64_t T, int64_t V, int64_t ld, const a3po_logit_adjustments *adj,
+                       const int32_t *chosen, void *out, a3po_dtype out_dt, int64_t ld_out, float *lse_out, float *logp_out,
+                       void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_logits(logits, (int)dt, T, V, ld)) return rc;
+    if (int rc = check_logits(out, (int)out_dt, out ? T : 0, V, out ? ld_out : V)) return rc;
+    if (int rc = check_adjustments(adj, T, V)) return rc;
+    if (T == 0) return A3PO_OK;
+    if ((!out && !lse_out && !logp_out) || (logp_out && !chosen)) return A3PO_E_NULL;
+    AdjustArgs a = adjust_args(adj);
+    if (lse_out || logp_out) {
+        if (!workspace || workspace_bytes < adjust_workspace_bytes(T, V)) return A3PO_E_WORKSPACE;
+        if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
+        a.ws_chosen = static_cast<float *>(workspace);
+        a.ws_partials = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + adjust_partials_offset(T));
+        a.lse = lse_out;
+        a.logp = logp_out;
+        a.chosen = logp_out ? chosen : nullptr;
+    }
+    a.z = logits;
+    a.u = out;
+    a.z_dt = (int)dt;
+    a.u_dt = (int)out_dt;
+    a.T = T;
+    a.V = V;
+    a.ldz = ld;
+    a.ldu = ld_out;
+    return launch_adjust(a, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+}
+
+int a3po_adjust_logits_bwd(const void *dout, a3po_dtype out_dt, int64_t ld_out, const void *logits, a3po_dtype dt, int64_t T,
+                           int64_t V, int64_t ld, const a3po_logit_adjustments *adj, void *dlogits, int64_t ld_d, void *stream)
+{
+    const bool needs_logits = adj && adj->history && adj->repetition;
+    if (int rc = check_logits(dout, (int)out_dt, T, V, ld_out)) return rc;
+    if (int rc = check_logits(dlogits, (int)dt, T, V, ld_d)) return rc;
+    if (int rc = check_logits(logits, (int)dt, needs_logits ? T : 0, V, needs_logits ? ld : V)) return rc;
+    if (int rc = check_adjustments(adj, T, V)) return rc;
+    if (T == 0) return A3PO_OK;
+    AdjustArgs a = adjust_args(adj);
+    if (!needs_logits) a.history = nullptr;
+    a.z = logits;
+    a.du = dout;
+    a.dz = dlogits;
+    a.z_dt = (int)dt;
+    a.u_dt = (int)out_dt;
+    a.T = T;
+    a.V = V;
+    a.ldz = ld;
+    a.ldu = ld_out;
+    a.lddz = ld_d;
+    return launch_adjust(a, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+}
+
+int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8_t *codes, const void *scales,
+                   a3po_dtype scale_dt, const uint8_t *zeros, int32_t group, int64_t N, void *out, a3po_dtype out_dt,
+                   int64_t ld_out, void *stream)
+{
+    if ((scale_dt != A3PO_F32 && scale_dt != A3PO_BF16) || (out_dt != A3PO_F32 && out_dt != A3PO_BF16)) return A3PO_E_DTYPE;
+    if (group != 32 && group != 64 && group != 128) return A3PO_E_SIZE;
+    if (T < 0 || T > kW4MaxTokens || N <= 0 || N > (int64_t)0x7FFFFFFF || H <= 0 || H % group != 0 || H > (1 << 20) ||
+        ldx < H || ldx > kMaxStride || ld_out < N || ld_out > kMaxStride)
+        return A3PO_E_SIZE;
+    if (T == 0) return A3PO_OK;
+    if (!x || !codes || !scales || !out) return A3PO_E_NULL;
+    if (!aligned(x, 2) || !aligned(codes, 16) || !aligned(scales, elem(scale_dt)) || !aligned(out, elem(out_dt)))
+        return A3PO_E_ALIGN;
+    W4Args a;
+    a.x = x;
+    a.codes = codes;
+    a.scales = scales;
+    a.zeros = zeros;
+    a.out = out;
+    a.scale_dt = (int)scale_dt;
+    a.out_dt = (int)out_dt;
+    a.group = group;
+    a.T = T;
+    a.V = N;
+    a.ldx = ldx;
+    a.ldo = ld_out;
+    a.H = (int)H;
+    return launch_w4_linear(a, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
 }
 
 }  // extern "C"

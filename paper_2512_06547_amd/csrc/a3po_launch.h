@@ -394,4 +394,126 @@ hipError_t launch_lmhead_lse_finish(const void *hidden, const void *weight, int6
 
 size_t lmhead_bwd_workspace_bytes(int64_t T, int64_t V, int64_t H);
 
+// ---- operators around the log-probs: final norm, adjusted logits, head with 4-bit weights ------------------------------
+
+struct NormArgs {
+    const void *x, *dy, *weight, *bias;  // dy: backward pass only; weight, bias nullable
+    void *y, *dx;
+    int x_dt, y_dt;  // a3po_dtype of x, dx / of y, dy
+    bool param_f32, center;
+    int64_t T, ldx, ldy, lddx;
+    int H;
+    float eps;
+    float *mean, *rstd;    // [T]; written by the forward pass (nullable), read by the backward pass
+    int partial_rows = 2;  // backward pass: 2 with dbias, 1 without
+};
+
+constexpr int kNormMaxH = A3PO_NORM_MAX_H;
+
+// Lanes that share a row and the 16-byte vectors of x that each holds.  A wavefront alone needs no barrier; beyond what its
+// registers hold (the backward pass also keeps its sums there) four share a row, then sixteen.
+struct NormPlan {
+    int lanes, vectors;
+};
+inline NormPlan norm_plan(int64_t H, int x_bytes, bool backward)
+{
+    const int64_t full = H / (16 / x_bytes);
+    const int most = !backward || x_bytes == 4 ? 8 : 4;
+    auto up = [](int64_t a, int64_t b) { return (int)((a + b - 1) / b); };
+    NormPlan p;
+    if (full <= 64 * most) {
+        const int v = up(full, 64);
+        p = {64, v <= 4 ? (v > 1 ? v : 1) : v <= 6 ? 6 : 8};
+    } else if (full <= 1024) {
+        const int v = up(full, 256);
+        p = {256, v > 2 ? v : 2};
+    } else {
+        const int v = up(full, 1024);
+        p = {1024, v <= 2 ? 2 : 4};
+    }
+    return p;
+}
+// workgroups of the backward pass, each of which leaves its share of the sums over rows
+constexpr int kNormMaxBlocks = 512;
+inline int64_t norm_bwd_blocks(int64_t T, int64_t H, int x_bytes)
+{
+    const NormPlan p = norm_plan(H, x_bytes, true);
+    const int64_t rows = p.lanes >= 256 ? 1 : 256 / p.lanes, want = (T + rows - 1) / rows;
+    return want < kNormMaxBlocks ? want : kNormMaxBlocks;
+}
+inline size_t norm_bwd_workspace_bytes(int64_t T, int64_t H)
+{
+    if (T <= 0 || H <= 0 || H > kNormMaxH) return 256;
+    const int64_t a = norm_bwd_blocks(T, H, 2), b = norm_bwd_blocks(T, H, 4);
+    return ((size_t)(a > b ? a : b) * 8 * (size_t)H + 255) / 256 * 256;
+}
+hipError_t launch_norm_fwd(const NormArgs &a, hipStream_t s);
+hipError_t launch_norm_bwd(const NormArgs &a, float *dweight, float *dbias, int accumulate, void *workspace, hipStream_t s);
+
+struct AdjustArgs {
+    const void *z;
+    void *u;         // forward: the adjusted logits, nullable
+    const void *du;  // backward: gradient with respect to them
+    void *dz;        // backward: gradient with respect to z (set: this is the backward pass)
+    int z_dt, u_dt;  // a3po_dtype of z, dz / of u, du
+    int64_t T, V, ldz, ldu, lddz;
+    const int32_t *history;
+    int64_t history_tokens;
+    const int64_t *hist_start;
+    const int32_t *hist_len, *prompt_len;
+    const float *repetition, *frequency, *presence, *temperature, *bias;
+    int64_t bias_ld;
+    const int32_t *allowed;
+    int64_t allowed_ld;
+    const int32_t *chosen;
+    float *lse, *logp;
+    float2 *ws_partials;  // [T, parts], null: neither lse nor logp
+    float *ws_chosen;     // [T]
+    int parts, part, vectors;
+};
+
+// A row's parts: `part` entries each (a multiple of 512), `vectors` 16-byte vectors of z a thread.  As few parts as their
+// counts fit (62 KiB of LDS, so that two workgroups share a compute unit) if there are rows enough for four workgroups a
+// compute unit, and more otherwise, down to one vector a thread.
+constexpr int kAdjustThreads = 512;
+struct AdjustPlan {
+    int parts, part, vectors;
+};
+inline AdjustPlan adjust_plan(int64_t T, int64_t V, int z_bytes)
+{
+    const int64_t step = kAdjustThreads * (16 / z_bytes), most = z_bytes == 2 ? 4 * step - 512 : 4 * step;
+    const int64_t least = (V + most - 1) / most, widest = (V + step - 1) / step;
+    int64_t parts = (1024 + T - 1) / (T > 0 ? T : 1);
+    if (parts > widest) parts = widest;
+    if (parts < least) parts = least;
+    AdjustPlan p;
+    p.part = (int)(((V + parts - 1) / parts + 511) / 512 * 512);
+    p.parts = (int)((V + p.part - 1) / p.part);
+    p.vectors = (int)((p.part + step - 1) / step);
+    return p;
+}
+// workspace: the chosen tokens' adjusted logits, then a (max, sum) per part
+inline size_t adjust_partials_offset(int64_t T) { return ((size_t)T * 4 + 255) / 256 * 256; }
+inline size_t adjust_workspace_bytes(int64_t T, int64_t V)
+{
+    if (T <= 0 || V <= 0) return 256;
+    const int a = adjust_plan(T, V, 2).parts, b = adjust_plan(T, V, 4).parts;
+    return adjust_partials_offset(T) + ((size_t)T * 8 * (size_t)(a > b ? a : b) + 255) / 256 * 256;
+}
+hipError_t launch_adjust(AdjustArgs a, hipStream_t s);
+
+constexpr int kW4Waves = 8;
+constexpr int64_t kW4MaxTokens = 65535 * 64;  // (blocks of 64 tokens are the grid's second dimension)
+struct W4Args {
+    const void *x;
+    const uint8_t *codes;
+    const void *scales;
+    const uint8_t *zeros;  // nullable: every zero point is 8
+    void *out;
+    int scale_dt, out_dt, group;
+    int64_t T, V, ldx, ldo;
+    int H;
+};
+hipError_t launch_w4_linear(const W4Args &a, hipStream_t s);
+
 }  // namespace a3po

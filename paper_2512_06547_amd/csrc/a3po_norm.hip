@@ -1,0 +1,381 @@
+// Layer norm and its root-mean-square form over rows of hidden states, forward and backward.
+//
+//   c = x - mean (mean = 0 in the root-mean-square form),  rstd = 1 / sqrt(mean(c^2) + eps),  xhat = c rstd
+//   y = xhat w + b
+//   dx = rstd (g - mean(g) - xhat mean(g xhat)),  g = dy w   (without mean(g) in the root-mean-square form)
+//   dw = sum over rows of dy xhat,  db = sum over rows of dy
+//
+// Both passes read each row once and keep it in registers; statistics, products and sums are fp32, and every output is
+// rounded once.  The variance is the mean of (x - mean)^2, taken from the registers after the mean is known: the
+// difference of two sums loses all digits of rows whose mean is large against their spread.
+// The kernels are bound by memory.
+#include "a3po_common.h"
+#include "a3po_launch.h"
+
+namespace a3po {
+namespace {
+
+// LANES lanes share a row: each holds NV vectors of EPV elements (16 bytes of x), vector i at (i LANES + lane) EPV, and
+// one element of what is left of the row behind the last whole vector.  Rows may start at any element.
+template <typename XT>
+constexpr int kVec = 16 / XT::kBytes;
+
+// EPV consecutive elements of type DT, widened
+template <typename DT, int EPV>
+__device__ __forceinline__ void load_vec(const char *p, float *f)
+{
+    constexpr int kWords = EPV * DT::kBytes / 4;
+    typedef uint32_t words_t __attribute__((ext_vector_type(kWords < 4 ? kWords : 4), aligned(DT::kBytes)));
+    constexpr int kPer = kWords < 4 ? kWords : 4;
+#pragma unroll
+    for (int k = 0; k < kWords; k += kPer) {
+        const words_t w = *reinterpret_cast<const words_t *>(p + 4 * k);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if constexpr (DT::kBytes == 4) {
+                f[k + j] = __uint_as_float(w[j]);
+            } else {
+                f[2 * (k + j)] = __uint_as_float(w[j] << 16);
+                f[2 * (k + j) + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+            }
+        }
+    }
+}
+
+template <typename DT, int EPV>
+__device__ __forceinline__ void store_vec(char *p, const float *f)
+{
+    constexpr int kWords = EPV * DT::kBytes / 4;
+    constexpr int kPer = kWords < 4 ? kWords : 4;
+    typedef uint32_t words_t __attribute__((ext_vector_type(kPer), aligned(DT::kBytes)));
+#pragma unroll
+    for (int k = 0; k < kWords; k += kPer) {
+        words_t w;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if constexpr (DT::kBytes == 4) w[j] = __float_as_uint(f[k + j]);
+            else w[j] = pack_bf16x2(f[2 * (k + j)], f[2 * (k + j) + 1]);
+        }
+        *reinterpret_cast<words_t *>(p + 4 * k) = w;
+    }
+}
+
+// a weight or bias vector, whose type is the call's (one value for the whole grid); `none` where there is no array
+template <int EPV>
+__device__ __forceinline__ void load_param(const void *w, bool f32, int64_t e, float none, float *f)
+{
+    if (!w) {
+#pragma unroll
+        for (int k = 0; k < EPV; ++k) f[k] = none;
+    } else if (f32) {
+        load_vec<F32, EPV>(static_cast<const char *>(w) + 4 * e, f);
+    } else {
+        load_vec<Bf16, EPV>(static_cast<const char *>(w) + 2 * e, f);
+    }
+}
+__device__ __forceinline__ float load_param(const void *w, bool f32, int64_t e, float none)
+{
+    if (!w) return none;
+    return f32 ? load_elem<F32>(w, e) : load_elem<Bf16>(w, e);
+}
+
+// Sums over the LANES lanes of a row; every lane gets them.  With several wavefronts a row they pass through `red`,
+// which alternates between two halves from row to row, so that one barrier a sum is enough.
+template <int LANES, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[2 * (LANES / kWave)], int &phase)
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int off = kWave / 2; off > 0; off >>= 1) v[n] += __shfl_xor(v[n], off, kWave);
+    if constexpr (LANES > kWave) {
+        constexpr int kWaves = LANES / kWave;
+        const int wave = threadIdx.x / kWave;
+        if ((threadIdx.x & (kWave - 1)) == 0)
+#pragma unroll
+            for (int n = 0; n < N; ++n) red[phase][N * wave + n] = v[n];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+            for (int n = 0; n < N; ++n) v[n] += red[phase][N * w + n];
+        phase ^= 1;
+    }
+}
+
+template <typename XT, typename YT, int LANES, int NV, bool CENTER>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(NormArgs a)
+{
+    constexpr int EPV = kVec<XT>, kRows = LANES >= 256 ? 1 : 256 / LANES;
+    __shared__ float red[2][2 * (LANES / kWave)];
+    int phase = 0;
+    const int lane = threadIdx.x % LANES, full = a.H / EPV, rest = a.H - full * EPV;
+    const float inv_h = 1.0f / (float)a.H;
+    const bool last = lane < rest;
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    for (int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; t < a.T; t += stride) {
+        const char *row = static_cast<const char *>(a.x) + t * a.ldx * XT::kBytes;
+        char *out = static_cast<char *>(a.y) + t * a.ldy * YT::kBytes;
+        float f[NV][EPV], extra = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * LANES + lane;
+#pragma unroll
+            for (int k = 0; k < EPV; ++k) f[i][k] = 0.0f;
+            if (v < full) load_vec<XT, EPV>(row + (int64_t)v * EPV * XT::kBytes, f[i]);
+        }
+        if (last) extra = load_elem<XT>(row, full * EPV + lane);
+        float mean = 0.0f;
+        if constexpr (CENTER) {
+            float sum[1] = {extra};
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < EPV; ++k) sum[0] += f[i][k];
+            row_sum<LANES, 1>(sum, red, phase);
+            mean = sum[0] / (float)a.H;  // (divided: rows of equal values have that mean exactly)
+        }
+        float sq[1] = {last ? (extra - mean) * (extra - mean) : 0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool on = i * LANES + lane < full;
+#pragma unroll
+            for (int k = 0; k < EPV; ++k) {
+                f[i][k] = on ? f[i][k] - mean : 0.0f;
+                sq[0] = fmaf(f[i][k], f[i][k], sq[0]);
+            }
+        }
+        row_sum<LANES, 1>(sq, red, phase);
+        const float rstd = 1.0f / sqrtf(fmaf(sq[0], inv_h, a.eps));
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * LANES + lane;
+            if (v < full) {
+                float w[EPV], b[EPV];
+                load_param<EPV>(a.weight, a.param_f32, (int64_t)v * EPV, 1.0f, w);
+                load_param<EPV>(a.bias, a.param_f32, (int64_t)v * EPV, 0.0f, b);
+#pragma unroll
+                for (int k = 0; k < EPV; ++k) f[i][k] = fmaf(f[i][k] * rstd, w[k], b[k]);
+                store_vec<YT, EPV>(out + (int64_t)v * EPV * YT::kBytes, f[i]);
+            }
+        }
+        if (last) {
+            const int e = full * EPV + lane;
+            store_elem<YT>(out, e, fmaf((extra - mean) * rstd, load_param(a.weight, a.param_f32, e, 1.0f),
+                                        load_param(a.bias, a.param_f32, e, 0.0f)));
+        }
+        if (lane == 0) {
+            if (a.mean) a.mean[t] = mean;
+            if (a.rstd) a.rstd[t] = rstd;
+        }
+    }
+}
+
+// Each workgroup takes rows in turn and leaves its share of dw and db in partials [workgroup][dw | db][H]; a second
+// kernel adds the shares in one order, so that identical inputs give identical sums.
+template <typename XT, typename YT, int LANES, int NV, bool CENTER>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(NormArgs a, float *partials)
+{
+    constexpr int EPV = kVec<XT>, kRows = LANES >= 256 ? 1 : 256 / LANES;
+    __shared__ float red[2][2 * (LANES / kWave)];
+    int phase = 0;
+    const int lane = threadIdx.x % LANES, full = a.H / EPV, rest = a.H - full * EPV, group = threadIdx.x / LANES;
+    const float inv_h = 1.0f / (float)a.H;
+    const bool last = lane < rest;
+    const float w_extra = last ? load_param(a.weight, a.param_f32, full * EPV + lane, 1.0f) : 0.0f;
+    float dw[NV][EPV], db[NV][EPV], dw_extra = 0.0f, db_extra = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < EPV; ++k) dw[i][k] = db[i][k] = 0.0f;
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    for (int64_t t = (int64_t)blockIdx.x * kRows + group; t < a.T; t += stride) {
+        const char *row = static_cast<const char *>(a.x) + t * a.ldx * XT::kBytes;
+        const char *grow = static_cast<const char *>(a.dy) + t * a.ldy * YT::kBytes;
+        char *out = static_cast<char *>(a.dx) + t * a.lddx * XT::kBytes;
+        float x[NV][EPV], g[NV][EPV], x_extra = 0.0f, g_extra = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * LANES + lane;
+#pragma unroll
+            for (int k = 0; k < EPV; ++k) x[i][k] = g[i][k] = 0.0f;
+            if (v < full) {
+                load_vec<XT, EPV>(row + (int64_t)v * EPV * XT::kBytes, x[i]);
+                load_vec<YT, EPV>(grow + (int64_t)v * EPV * YT::kBytes, g[i]);
+            }
+        }
+        if (last) {
+            x_extra = load_elem<XT>(row, full * EPV + lane);
+            g_extra = load_elem<YT>(grow, full * EPV + lane);
+        }
+        const float rstd = a.rstd[t], mean = CENTER ? a.mean[t] : 0.0f;
+        float s[2] = {0.0f, 0.0f};  // sums of g xhat and of g
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * LANES + lane;
+            if (v < full) {
+                float w[EPV];
+                load_param<EPV>(a.weight, a.param_f32, (int64_t)v * EPV, 1.0f, w);
+#pragma unroll
+                for (int k = 0; k < EPV; ++k) {
+                    x[i][k] = (x[i][k] - mean) * rstd;
+                    dw[i][k] = fmaf(g[i][k], x[i][k], dw[i][k]);
+                    if constexpr (CENTER) db[i][k] += g[i][k];
+                    g[i][k] *= w[k];
+                    s[0] = fmaf(g[i][k], x[i][k], s[0]);
+                    if constexpr (CENTER) s[1] += g[i][k];
+                }
+            }
+        }
+        if (last) {
+            x_extra = (x_extra - mean) * rstd;
+            dw_extra = fmaf(g_extra, x_extra, dw_extra);
+            if constexpr (CENTER) db_extra += g_extra;
+            g_extra *= w_extra;
+            s[0] = fmaf(g_extra, x_extra, s[0]);
+            if constexpr (CENTER) s[1] += g_extra;
+        }
+        row_sum<LANES, 2>(s, red, phase);
+        const float along = s[0] * inv_h, level = CENTER ? s[1] * inv_h : 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * LANES + lane;
+            if (v < full) {
+#pragma unroll
+                for (int k = 0; k < EPV; ++k) g[i][k] = rstd * (g[i][k] - level - x[i][k] * along);
+                store_vec<XT, EPV>(out + (int64_t)v * EPV * XT::kBytes, g[i]);
+            }
+        }
+        if (last) store_elem<XT>(out, full * EPV + lane, rstd * (g_extra - level - x_extra * along));
+    }
+    if (!partials) return;
+    // the groups of lanes of this workgroup add their sums, one group after the other
+    extern __shared__ float sums[];  // [dw | db][H], kRows > 1 only
+    float *mine = partials + (int64_t)blockIdx.x * a.partial_rows * a.H;
+    for (int r = 0; r < kRows; ++r) {
+        if (r > 0) __syncthreads();
+        if (group == r) {
+            auto add = [&](int e, float p, float q) {
+                if (r > 0) {
+                    p += sums[e];
+                    q += sums[a.H + e];
+                }
+                float *to = r == kRows - 1 ? mine : sums;
+                to[e] = p;
+                if (r < kRows - 1 || a.partial_rows > 1) to[a.H + e] = q;
+            };
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = i * LANES + lane;
+                if (v < full)
+#pragma unroll
+                    for (int k = 0; k < EPV; ++k) add(v * EPV + k, dw[i][k], db[i][k]);
+            }
+            if (last) add(full * EPV + lane, dw_extra, db_extra);
+        }
+    }
+}
+
+// columns of the partials, summed in order: a workgroup takes 32 columns, 32 runs of workgroups' shares each
+__global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(const float *partials, int parts, int64_t width, int64_t H,
+                                                            float *dweight, float *dbias, int accumulate)
+{
+    __shared__ float part[32][33];
+    const int col = threadIdx.x & 31, run = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + col;
+    const int per = (parts + 31) / 32;
+    float s = 0.0f;
+    if (c < width) {
+        const int end = min(parts, (run + 1) * per);
+#pragma unroll 8
+        for (int p = run * per; p < end; ++p) s += partials[(int64_t)p * width + c];
+    }
+    part[run][col] = s;
+    __syncthreads();
+    if (run == 0 && c < width) {
+        float total = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 32; ++r) total += part[r][col];
+        float *to = c < H ? dweight : dbias;
+        if (to) {
+            to += c < H ? c : c - H;
+            *to = accumulate ? *to + total : total;
+        }
+    }
+}
+
+template <typename XT, typename YT, int LANES, int NV>
+hipError_t launch(const NormArgs &a, bool backward, float *partials, int64_t blocks, hipStream_t s)
+{
+    constexpr int kThreads = LANES > 256 ? LANES : 256;
+    const dim3 grid((unsigned)blocks), block(kThreads);
+    if (backward) {
+        const size_t lds = LANES < 256 && partials ? (size_t)8 * a.H : 0;
+        if (a.center) norm_bwd_kernel<XT, YT, LANES, NV, true><<<grid, block, lds, s>>>(a, partials);
+        else norm_bwd_kernel<XT, YT, LANES, NV, false><<<grid, block, lds, s>>>(a, partials);
+    } else {
+        if (a.center) norm_fwd_kernel<XT, YT, LANES, NV, true><<<grid, block, 0, s>>>(a);
+        else norm_fwd_kernel<XT, YT, LANES, NV, false><<<grid, block, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+template <typename XT, typename YT>
+hipError_t launch_of(const NormArgs &a, bool backward, float *partials, int64_t blocks, hipStream_t s)
+{
+    const NormPlan p = norm_plan(a.H, XT::kBytes, backward);
+    // (norm_plan gives no other pair)
+#define A3PO_NORM_CASE(L, N) \
+    if (p.lanes == L && p.vectors == N) return launch<XT, YT, L, N>(a, backward, partials, blocks, s)
+    A3PO_NORM_CASE(64, 1);
+    A3PO_NORM_CASE(64, 2);
+    A3PO_NORM_CASE(64, 3);
+    A3PO_NORM_CASE(64, 4);
+    A3PO_NORM_CASE(64, 6);
+    A3PO_NORM_CASE(64, 8);
+    A3PO_NORM_CASE(256, 2);
+    A3PO_NORM_CASE(256, 3);
+    A3PO_NORM_CASE(256, 4);
+    A3PO_NORM_CASE(1024, 2);
+    if constexpr (XT::kBytes == 4) A3PO_NORM_CASE(1024, 4);
+#undef A3PO_NORM_CASE
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_any(const NormArgs &a, bool backward, float *partials, int64_t blocks, hipStream_t s)
+{
+    if (a.x_dt == A3PO_F32)
+        return a.y_dt == A3PO_F32 ? launch_of<F32, F32>(a, backward, partials, blocks, s)
+                                  : launch_of<F32, Bf16>(a, backward, partials, blocks, s);
+    return a.y_dt == A3PO_F32 ? launch_of<Bf16, F32>(a, backward, partials, blocks, s)
+                              : launch_of<Bf16, Bf16>(a, backward, partials, blocks, s);
+}
+
+}  // namespace
+
+hipError_t launch_norm_fwd(const NormArgs &a, hipStream_t s)
+{
+    const NormPlan p = norm_plan(a.H, a.x_dt == A3PO_F32 ? 4 : 2, false);
+    const int rows = p.lanes >= 256 ? 1 : 256 / p.lanes;
+    const int64_t want = (a.T + rows - 1) / rows, most = 4096;
+    return launch_any(a, false, nullptr, want < most ? want : most, s);
+}
+
+hipError_t launch_norm_bwd(const NormArgs &a, float *dweight, float *dbias, int accumulate, void *workspace, hipStream_t s)
+{
+    const int64_t blocks = norm_bwd_blocks(a.T, a.H, a.x_dt == A3PO_F32 ? 4 : 2);
+    NormArgs b = a;
+    b.partial_rows = dbias ? 2 : 1;
+    float *partials = dweight || dbias ? static_cast<float *>(workspace) : nullptr;
+    if (a.T > 0)
+        if (const hipError_t e = launch_any(b, true, partials, blocks, s)) return e;
+    if (!dweight && !dbias) return hipSuccess;
+    const int64_t width = b.partial_rows * a.H;
+    norm_bwd_sum_kernel<<<dim3((unsigned)((width + 31) / 32)), dim3(1024), 0, s>>>(
+        partials, a.T > 0 ? (int)blocks : 0, width, a.H, dweight, dbias, accumulate);
+    return hipGetLastError();
+}
+
+}  // namespace a3po

@@ -1,0 +1,134 @@
+"""a3po_w4_linear against the product with the dequantised weight in 64 bits.
+
+Products of a bfloat16 and a code are exact; what is rounded is the fp32 sum.  A group's accumulator starts at
+-(16 + zero) sum x and adds (16 + code) x: at most 62 sum |x| in magnitude and some 32 roundings of 2^-24 of it, so an element
+is off by at most 2^-24 * 32 * 62 * sum_k scale |x|.  Roundings are random: over many elements the relative 2-norm of the
+errors is held to 4e-6 as well (estimated 6e-7).  Outputs in bfloat16 lie between the
+rounded ends of the bar."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def a3po():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2512_06547_amd as lib
+    lib.lib()
+    return lib
+
+
+def _weight(N, H, group, zeros, st, g):
+    q = torch.randint(0, 16, (N, H), generator=g, dtype=torch.uint8)
+    scales = (0.01 * (0.2 + torch.rand(N, H // group, generator=g))).to(st)
+    z = torch.randint(0, 16, (N, H // group), generator=g, dtype=torch.uint8) if zeros else None
+    w = q.double() - (z.double().repeat_interleave(group, 1) if zeros else 8.0)
+    s = scales.double().repeat_interleave(group, 1)
+    return q[:, 0::2] | (q[:, 1::2] << 4), scales, z, w * s, s
+
+
+def _check(a3po, T, N, H, group, zeros=False, st=torch.bfloat16, ot=torch.float32, seed=0, x=None, xg=None, out=None):
+    g = torch.Generator().manual_seed(seed)
+    codes, scales, z, w, s = _weight(N, H, group, zeros, st, g)
+    if x is None:
+        x = torch.randn(T, H, generator=g).to(torch.bfloat16)
+    got = a3po.w4_linear(x.cuda() if xg is None else xg, codes.cuda(), scales.cuda(), zeros=None if z is None else z.cuda(),
+                         group=group, out=out, out_dtype=ot)
+    torch.cuda.synchronize()
+    assert got.dtype == ot and got.shape == (T, N)
+    ref = x.double() @ w.t()
+    err = (got.cpu().double() - ref).abs()
+    bar = U * 32 * 62 * (x.double().abs() @ s.t())
+    assert (got.cpu() >= (ref - bar).to(ot)).all() and (got.cpu() <= (ref + bar).to(ot)).all()
+    if ot == torch.float32 and T * N >= 256:
+        assert err.norm() <= 4e-6 * ref.norm(), float(err.norm() / ref.norm())
+    return got
+
+
+@pytest.mark.parametrize("T", [1, 2, 3, 7, 8, 15, 16, 17, 31, 32, 33, 48, 63, 64, 65, 130])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_numbers_of_tokens(a3po, T, group, zeros):
+    _check(a3po, T, 300, 1536, group, zeros, seed=T)
+
+
+@pytest.mark.parametrize("H", [32, 64, 96, 128, 160, 224, 256, 288, 384, 896, 1056, 2080, 4128])
+@pytest.mark.parametrize("T", [1, 20, 50])
+@pytest.mark.parametrize("st", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_lengths_that_end_inside_a_unit(a3po, H, T, st, zeros):
+    for group in (32, 64, 128):
+        if H % group == 0:
+            _check(a3po, T, 77, H, group, zeros, st, seed=H)
+
+
+@pytest.mark.parametrize("N", [1, 2, 15, 16, 17, 63, 64, 127, 128, 129, 255, 257, 2000, 5003])
+@pytest.mark.parametrize("T", [1, 17, 40])
+@pytest.mark.parametrize("ot", [torch.float32, torch.bfloat16])
+def test_numbers_of_rows(a3po, N, T, ot):
+    _check(a3po, T, N, 256, 64, True, ot=ot, seed=N)
+
+
+def test_many_rows(a3po):
+    _check(a3po, 4, 70001, 128, 128, seed=3)
+    _check(a3po, 40, 40001, 160, 32, True, torch.float32, seed=4)
+
+
+def test_strided_unaligned_hidden_states_and_outputs(a3po):
+    g = torch.Generator().manual_seed(5)
+    for T in (3, 18, 61):
+        x = torch.randn(T, 256, generator=g).to(torch.bfloat16)
+        xg = torch.zeros(T * 267 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(T, 267)
+        xg[:, :256] = x.cuda()
+        out = torch.full((T, 103), 7.0, device="cuda")
+        _check(a3po, T, 100, 256, 128, seed=T, x=x, xg=xg[:, :256], out=out[:, :100])
+        assert (out[:, 100:] == 7.0).all()
+
+
+def test_every_code_and_zero_point_is_the_value_it_stands_for(a3po):
+    """One-hot hidden states read the weight itself, exactly: a code times a power of two."""
+    H, N = 128, 16 * 16
+    codes = torch.arange(N, dtype=torch.uint8)[:, None].expand(N, H // 2)      # every pair of codes
+    zeros = (torch.arange(N, dtype=torch.uint8) % 16)[:, None].expand(N, 4)
+    x = torch.zeros(64, H, dtype=torch.bfloat16)
+    x[torch.arange(64), torch.arange(64) * 2 + torch.arange(64) % 2] = 1.0
+    got = a3po.w4_linear(x.cuda(), codes.contiguous().cuda(), torch.full((N, 4), 0.5).cuda(), zeros=zeros.contiguous().cuda(),
+                         group=32, out_dtype=torch.float32).cpu()
+    n = torch.arange(N)
+    for t in range(64):
+        assert torch.equal(got[t], ((n >> 4 if t % 2 else n & 15) - n % 16).float() * 0.5), t
+
+
+def test_zero_hidden_states_large_scales_and_empty_calls(a3po):
+    g = torch.Generator().manual_seed(6)
+    codes, scales, _, _, _ = _weight(40, 256, 64, False, torch.float32, g)
+    x = torch.zeros(5, 256, dtype=torch.bfloat16, device="cuda")
+    assert not a3po.w4_linear(x, codes.cuda(), (scales * 1e30).cuda(), group=64).any()
+    assert a3po.w4_linear(x[:0], codes.cuda(), scales.cuda(), group=64).shape == (0, 40)
+
+
+def test_on_another_stream_and_in_a_graph(a3po):
+    g = torch.Generator().manual_seed(7)
+    codes, scales, _, _, _ = _weight(1000, 512, 128, False, torch.bfloat16, g)
+    codes, scales = codes.cuda(), scales.cuda()
+    x = torch.randn(4, 512, generator=g).to(torch.bfloat16).cuda()
+    out = torch.empty(4, 1000, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        a3po.w4_linear(x, codes, scales, out=out)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a3po.w4_linear(x, codes, scales, out=out)
+    for i in range(3):
+        x.copy_(torch.randn(4, 512, generator=g).to(torch.bfloat16))
+        want = a3po.w4_linear(x, codes, scales, out_dtype=torch.float32)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i

@@ -1,0 +1,186 @@
+"""Refusals and host-side plans of the operators around the log-probs (norm, adjusted logits, 4-bit head); no GPU needed:
+every call here returns at validation, before any device pointer is used."""
+import ctypes
+import os
+
+import pytest
+
+from test_launch_plans import run_on_host
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2512_06547_amd as a3po
+    if not os.path.exists(a3po.lib_path()):
+        from paper_2512_06547_amd import build
+        build.build(force=True)
+    return a3po.lib()
+
+
+P = lambda a=0x1000: ctypes.c_void_p(a)
+
+
+def caller(fn, base):
+    def call(**kw):
+        args = list(base)
+        for k, v in kw.items():
+            args[int(k[1:])] = v
+        return fn(*args)
+    return call
+
+
+def test_norm_fwd_refuses(lib):
+    # x, x_dt, T, H, ldx, weight, bias, param_dt, eps, kind, y, y_dt, ldy, mean, rstd, stream
+    call = caller(lib.a3po_norm_fwd, [P(), 1, 4, 64, 64, P(), P(), 1, 1e-6, 0, P(), 1, 64, P(), P(), None])
+    assert call(a2=0) == 0 and call(a2=0, a0=None, a10=None) == 0
+    for at in (1, 7, 11):
+        assert call(**{f"a{at}": 2}) == -3 and call(**{f"a{at}": -1}) == -3
+    assert call(a2=-1) == -2 and call(a2=(1 << 40) + 1) == -2
+    assert call(a3=0) == -2 and call(a3=16385, a4=20000, a12=20000) == -2
+    assert call(a4=63) == -2 and call(a12=63) == -2 and call(a4=(1 << 40) + 1) == -2
+    assert call(a8=-1e-6) == -7 and call(a8=float("nan")) == -7 and call(a9=2) == -7
+    assert call(a9=1) == -7 and call(a9=1, a6=None) == -7          # the RMS form has no bias and no mean
+    assert call(a0=None) == -1 and call(a10=None) == -1
+    for at in (0, 5, 6, 10):
+        assert call(**{f"a{at}": P(0x1001)}) == -4
+    assert call(a0=P(0x1002), a1=0) == -4 and call(a10=P(0x1002), a11=0) == -4
+
+
+def test_norm_bwd_refuses(lib):
+    # dy, y_dt, lddy, x, x_dt, T, H, ldx, weight, param_dt, mean, rstd, kind, dx, lddx, dweight, dbias, accumulate, ws, bytes, stream
+    need = lib.a3po_workspace_bytes(3, 4, 0, 64)
+    call = caller(lib.a3po_norm_bwd, [P(), 1, 64, P(), 1, 4, 64, 64, P(), 1, P(), P(), 0, P(), 64, P(), P(), 0, P(0x10000), need - 1,
+                                      None])
+    assert call() == -5 and call(a18=None, a19=1 << 30) == -5 and call(a18=P(0x10010), a19=need) == -4
+    assert call(a1=2) == -3 and call(a4=2) == -3 and call(a9=2) == -3
+    assert call(a5=-1) == -2 and call(a6=0) == -2 and call(a6=16385) == -2
+    assert call(a2=63) == -2 and call(a7=63) == -2 and call(a14=63) == -2
+    assert call(a12=2) == -7 and call(a17=2) == -7 and call(a12=1) == -7   # no dbias in the RMS form
+    assert call(a0=None) == -1 and call(a3=None) == -1 and call(a10=None) == -1 and call(a11=None) == -1 and call(a13=None) == -1
+    assert call(a13=P(0x1001)) == -4 and call(a8=P(0x1001)) == -4
+    assert call(a5=0, a15=None, a16=None, a18=None, a19=0) == 0            # nothing to do
+
+
+def test_adjust_logits_refuses(lib):
+    from paper_2512_06547_amd.binding import LogitAdjustments
+    need = lib.a3po_workspace_bytes(4, 4, 100, 0)
+    # logits, dt, T, V, ld, adj, chosen, out, out_dt, ld_out, lse, logp, ws, bytes, stream
+    call = caller(lib.a3po_adjust_logits, [P(), 1, 4, 100, 100, None, P(), P(), 0, 100, P(), P(), P(0x10000), need - 1, None])
+    assert call() == -5 and call(a12=None, a13=1 << 30) == -5 and call(a12=P(0x10010), a13=need) == -4
+    assert call(a1=2) == -3 and call(a8=2) == -3
+    assert call(a2=-1) == -2 and call(a3=0) == -2 and call(a4=99) == -2 and call(a9=99) == -2 and call(a3=1 << 31, a4=1 << 31) == -2
+    assert call(a0=None) == -1 and call(a6=None) == -1                     # log-probs need chosen tokens
+    assert call(a7=None, a10=None, a11=None) == -1                         # no output at all
+    assert call(a0=P(0x1001)) == -4 and call(a7=P(0x1002)) == -4
+    assert call(a2=0) == 0
+    adj = lambda **kw: ctypes.byref(LogitAdjustments(**kw))
+    assert call(a5=adj(history=0x1000, history_tokens=-1, hist_start=0x1000, hist_len=0x1000)) == -2
+    assert call(a5=adj(history=0x1000, history_tokens=5, hist_len=0x1000)) == -1
+    assert call(a5=adj(history=0x1000, history_tokens=5, hist_start=0x1000)) == -1
+    assert call(a5=adj(bias=0x1000, bias_ld=99)) == -2 and call(a5=adj(bias=0x1002)) == -4
+    assert call(a5=adj(allowed=0x1000, allowed_ld=3)) == -2 and call(a5=adj(allowed=0x1000, allowed_ld=4)) == -5
+    assert call(a5=adj(history=0x1000, history_tokens=5, hist_start=0x1004, hist_len=0x1000)) == -4
+    for name in ("repetition", "frequency", "presence", "temperature"):
+        assert call(a5=adj(**{name: 0x1002})) == -4
+
+
+def test_adjust_logits_bwd_refuses(lib):
+    from paper_2512_06547_amd.binding import LogitAdjustments
+    hist = lambda **kw: ctypes.byref(LogitAdjustments(history=0x1000, history_tokens=5, hist_start=0x1000, hist_len=0x1000, **kw))
+    # dout, out_dt, ld_out, logits, dt, T, V, ld, adj, dlogits, ld_d, stream
+    call = caller(lib.a3po_adjust_logits_bwd, [P(), 0, 100, P(), 1, 4, 100, 100, hist(repetition=0x1000), P(), 100, None])
+    assert call(a1=2) == -3 and call(a4=2) == -3
+    assert call(a2=99) == -2 and call(a7=99) == -2 and call(a10=99) == -2 and call(a5=-1) == -2 and call(a6=0) == -2
+    assert call(a0=None) == -1 and call(a9=None) == -1 and call(a3=None) == -1
+    assert call(a0=P(0x1002)) == -4 and call(a3=P(0x1001)) == -4 and call(a9=P(0x1001)) == -4
+    assert call(a5=0, a3=None) == 0
+
+
+def test_w4_linear_refuses(lib):
+    # x, T, H, ldx, codes, scales, scale_dt, zeros, group, N, out, out_dt, ld_out, stream
+    call = caller(lib.a3po_w4_linear, [P(), 4, 256, 256, P(), P(), 1, P(), 64, 100, P(), 0, 100, None])
+    assert call(a6=2) == -3 and call(a11=2) == -3
+    for group in (0, 16, 48, 256, -64):
+        assert call(a8=group) == -2
+    assert call(a2=0) == -2 and call(a2=224) == -2 and call(a2=(1 << 20) + 64, a3=1 << 21) == -2   # H: a multiple of the group
+    assert call(a1=-1) == -2 and call(a1=65535 * 64 + 1) == -2 and call(a9=0) == -2 and call(a9=1 << 31, a12=1 << 31) == -2
+    assert call(a3=255) == -2 and call(a12=99) == -2
+    assert call(a0=None) == -1 and call(a4=None) == -1 and call(a5=None) == -1 and call(a10=None) == -1
+    assert call(a0=P(0x1001)) == -4 and call(a4=P(0x1008)) == -4 and call(a5=P(0x1001)) == -4 and call(a10=P(0x1002)) == -4
+    assert call(a1=0, a0=None, a4=None) == 0
+
+
+def test_workspaces_grow_with_their_calls_and_take_any_size(lib):
+    ws = lib.a3po_workspace_bytes
+    for which in (3, 4):
+        sizes = [ws(which, T, 151936, 4096) for T in (-1, 0, 1, 7, 100, 10000, 65536)]
+        assert all(s % 256 == 0 and s > 0 for s in sizes) and sizes == sorted(sizes)
+    assert ws(3, 5, 0, -1) > 0 and ws(3, 5, 0, 1 << 40) > 0 and ws(4, 5, -1, 0) > 0
+
+
+def test_binding_refuses_what_the_library_cannot_see():
+    """Types and shapes of tensors (CPU tensors are refused before anything else is asked of them)."""
+    torch = pytest.importorskip("torch")
+    import paper_2512_06547_amd as a3po
+    x = torch.zeros(4, 64)
+    for call in (lambda: a3po.norm_fwd(x), lambda: a3po.norm_bwd(x, x, None, x[:, 0]), lambda: a3po.adjust_logits(x),
+                 lambda: a3po.adjust_logits_bwd(x), lambda: a3po.w4_linear(x, x, x),
+                 lambda: a3po.w4_linear(x.bfloat16(), x, x)):
+        with pytest.raises((AssertionError, TypeError)):
+            call()
+
+
+def test_norm_plan_holds_every_row(tmp_path):
+    """Every width has a kernel that holds its whole vectors, with no more than half of the lanes' vectors idle beyond the
+    narrowest one, and the workspace holds every workgroup's share."""
+    source = tmp_path / "norm.cpp"
+    source.write_text('''#include <cstdio>
+#include "a3po_common.h"
+#include "a3po_launch.h"
+using namespace a3po;
+int main()
+{
+    for (int bytes : {2, 4})
+        for (int back = 0; back < 2; ++back)
+            for (int64_t H = 1; H <= kNormMaxH; ++H) {
+                const NormPlan p = norm_plan(H, bytes, back);
+                const int64_t full = H / (16 / bytes), room = (int64_t)p.lanes * p.vectors;
+                const int v = p.vectors;
+                bool known = false;
+                if (p.lanes == 64) known = v == 1 || v == 2 || v == 3 || v == 4 || v == 6 || v == 8;
+                if (p.lanes == 256) known = v == 2 || v == 3 || v == 4;
+                if (p.lanes == 1024) known = v == 2 || (v == 4 && bytes == 4);
+                if (!known || full > room || (v > 1 && full * 2 <= room - p.lanes)) return std::printf("H %lld\\n", (long long)H), 1;
+                for (int64_t T : {1, 3, 5, 511, 513, 4096, 100000}) {
+                    const int64_t b = norm_bwd_blocks(T, H, bytes);
+                    if (b < 1 || b > T || (size_t)b * 8 * H > norm_bwd_workspace_bytes(T, H)) return std::printf("T %lld\\n", (long long)T), 1;
+                }
+            }
+    std::printf("ok\\n");
+}
+''')
+    assert run_on_host(str(source), tmp_path) == "ok\n"
+
+
+def test_adjust_plan_covers_every_row_within_lds(tmp_path):
+    source = tmp_path / "adjust.cpp"
+    source.write_text('''#include <cstdio>
+#include "a3po_common.h"
+#include "a3po_launch.h"
+using namespace a3po;
+int main()
+{
+    for (int bytes : {2, 4})
+        for (int64_t T : {1, 2, 5, 64, 300, 1023, 1024, 5000, 1 << 24})
+            for (int64_t V = 1; V < 0x7FFFFFFF; V += V < 70000 ? 1 : 1 + V / 9) {
+                const AdjustPlan p = adjust_plan(T, V, bytes);
+                const int64_t room = (int64_t)p.vectors * kAdjustThreads * (16 / bytes);
+                const bool ok = p.part % 512 == 0 && p.part > 0 && p.part * 4 + 256 <= 65536 && p.vectors >= 1 && p.vectors <= 4 &&
+                                p.part <= room && (int64_t)p.parts * p.part >= V && (int64_t)(p.parts - 1) * p.part < V &&
+                                adjust_partials_offset(T) + (size_t)T * p.parts * 8 <= adjust_workspace_bytes(T, V);
+                if (!ok) return std::printf("T %lld V %lld\\n", (long long)T, (long long)V), 1;
+            }
+    std::printf("ok\\n");
+}
+''')
+    assert run_on_host(str(source), tmp_path) == "ok\n"
