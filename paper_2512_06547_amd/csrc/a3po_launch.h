@@ -481,7 +481,7 @@ struct AdjustPlan {
 };
 inline AdjustPlan adjust_plan(int64_t T, int64_t V, int z_bytes)
 {
-    const int64_t step = kAdjustThreads * (16 / z_bytes), most = z_bytes == 2 ? 4 * step - 512 : 4 * step;
+    const int64_t step = kAdjustThreads * (16 / z_bytes), most = z_bytes == 2 ? 10752 : 4 * step;
     const int64_t least = (V + most - 1) / most, widest = (V + step - 1) / step;
     int64_t parts = (1024 + T - 1) / (T > 0 ? T : 1);
     if (parts > widest) parts = widest;
