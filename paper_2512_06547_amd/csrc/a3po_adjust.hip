@@ -7,13 +7,15 @@
 //   lse = log sum_j exp u_j,  logp = u_y - lse
 //   dz = du / temperature * (in the history: z > 0 ? 1 / repetition : repetition), 0 where not allowed
 //
-// A row is cut into parts, a workgroup each, whose entries are in flight while the row's history is read.  The history
-// becomes one number per entry of the part in LDS: what penalties add to the logit (forward) or what its gradient is
-// multiplied with (backward).  The part is then folded from registers at one addition or product an entry: a test per
-// entry for a token of the history, with its two divisions behind it, costs more than the exponential (scoring of 8,192 x
-// 50,001 bfloat16 with it 1,050 us).  Maximum and sum of exp are taken before the temperature, which then is part of the
-// exponent's scale.  All arithmetic is fp32; what is stored in bfloat16 is rounded once, and lse and logp are those of the
-// fp32 values.  The kernels are bound by memory.
+// A workgroup takes a row, or a part of one where rows are few.  The row's history becomes a bit per entry in LDS.  Forward,
+// entries without the bit are folded from registers as they stream by, and the others, few, are taken one a thread
+// afterwards: the bits number them, a second pass over the history's output counts them by those numbers (integers: no order
+// of additions), and they join the sum and the output.  A test per entry with the penalties behind it costs more than the
+// exponential, and the work on the history, the reductions and the row's parameters cost what some forty entries a thread do,
+// so that rows are not cut further than it takes to fill the chip (scoring of 8,192 x 50,001 bfloat16: a test per entry, four
+// parts a row 1,055 us; a penalty per entry in LDS 553; bits, four parts 735; bits, whole rows 312).
+// Maximum and sum of exp are taken before the temperature, which then is part of the exponent's scale.  All arithmetic is
+// fp32; what is stored in bfloat16 is rounded once, and lse and logp are those of the fp32 values.
 #include "a3po_common.h"
 #include "a3po_launch.h"
 
@@ -21,7 +23,6 @@ namespace a3po {
 namespace {
 
 constexpr int kThreads = kAdjustThreads;
-constexpr uint32_t kSeen = 0x80000000u;
 constexpr float kInf = __builtin_huge_valf(), kLowest = -3.402823466e38f;
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -55,29 +56,32 @@ __device__ __forceinline__ RowPolicy row_policy(const AdjustArgs &a, int64_t t)
     return p;
 }
 
-// f(place in the history, place in the part) for every token of the row's history that lies in [first, first + span); four
-// tokens a load, four loads of a thread in flight
+// f(places, valid, output) for the tokens of the row's history, four at a time: places[k] is the k-th one's entry in the part
+// if bit k of `valid` says that it lies there ([first, first + span)); bit k of `output`: it is behind the prompt
 template <typename F>
-__device__ __forceinline__ void each_token(const AdjustArgs &a, const RowPolicy &p, int64_t first, int span, F f)
+__device__ __forceinline__ void each_tokens(const AdjustArgs &a, const RowPolicy &p, int64_t first, int span, F f)
 {
     const int32_t *h = a.history + p.start;
-    const int base = (int)first;
-    auto one = [&](int i, int32_t id) {
-        // (ids and places are below 2^31: the difference of the bit patterns is below span only for those of the part)
-        const uint32_t at = (uint32_t)id - (uint32_t)base;
-        if (id >= 0 && at < (uint32_t)span) f(i, (int)at);
-    };
+    const uint32_t base = (uint32_t)first, width = (uint32_t)span;
     constexpr uint32_t kLoads = 4, kRound = kThreads * 4 * kLoads;
-    const uint32_t len = (uint32_t)p.len, lane = threadIdx.x;
+    const uint32_t len = (uint32_t)p.len, prompt = (uint32_t)max(p.prompt, 0), lane = threadIdx.x;
+    auto one = [&](int32_t id, uint32_t at_history, int k, uint32_t(&at)[4], uint32_t &valid, uint32_t &output) {
+        at[k] = (uint32_t)id - base;
+        valid |= (id >= 0 && at[k] < width ? 1u : 0u) << k;
+        output |= (at_history >= prompt ? 1u : 0u) << k;
+    };
     uint32_t i = 0;  // (unsigned: lengths end below 2^31, the places tried beyond them below 2^32)
     for (; len - i >= kRound; i += kRound) {
         i32x4_any v[kLoads];
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j) v[j] = *reinterpret_cast<const i32x4_any *>(h + i + (j * kThreads + lane) * 4);
 #pragma unroll
-        for (uint32_t j = 0; j < kLoads; ++j)
+        for (uint32_t j = 0; j < kLoads; ++j) {
+            uint32_t at[4], valid = 0, output = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) one((int)(i + (j * kThreads + lane) * 4) + k, v[j][k]);
+            for (int k = 0; k < 4; ++k) one(v[j][k], i + (j * kThreads + lane) * 4 + k, k, at, valid, output);
+            f(at, valid, output);
+        }
     }
     for (; i < len; i += kThreads * kLoads) {
         int32_t v[kLoads];
@@ -86,46 +90,90 @@ __device__ __forceinline__ void each_token(const AdjustArgs &a, const RowPolicy 
             const uint32_t at = i + j * kThreads + lane;
             v[j] = at < len ? h[at] : -1;
         }
+        uint32_t at[4], valid = 0, output = 0;
 #pragma unroll
-        for (uint32_t j = 0; j < kLoads; ++j) one((int)(i + j * kThreads + lane), v[j]);
+        for (int k = 0; k < 4; ++k) one(v[k], i + k * kThreads + lane, k, at, valid, output);
+        f(at, valid, output);
     }
 }
 
-__device__ __forceinline__ void fill(float *to, int span, float v)
-{
-    const int vecs = (span + 3) / 4;  // (parts end at multiples of 512: the last vector is there)
-    for (int i = threadIdx.x; i < vecs; i += kThreads) reinterpret_cast<float4 *>(to)[i] = make_float4(v, v, v, v);
-}
+// The part's entries that are in the row's history: a bit each, and the numbers of those entries.
+struct Seen {
+    static constexpr int kBlock = 16;  // words whose numbers share a base
+    uint32_t *words;                   // [part / 32]
+    uint32_t *bases;                   // [part / 512]
+    uint16_t *before;                  // [part / 32], within the block
+    int nwords;
 
-// What the penalties add to the entries [first, first + span) of row t, into `delta`.  Occurrences are counted there first
-// (integers: the order of the additions does not matter; the top bit stands for those in the prompt); whoever adds the
-// first one of a token notes its place, and each place noted is then turned into a difference.
-template <typename ZT>
-__device__ __forceinline__ void penalties(const AdjustArgs &a, const RowPolicy &p, const char *row, int64_t first, int span,
-                                          float *delta, uint16_t *places, int *noted)
-{
-    uint32_t *cnt = reinterpret_cast<uint32_t *>(delta);
-    __syncthreads();  // (the part before this one is done with the array)
-    fill(delta, span, 0.0f);
-    if (threadIdx.x == 0) *noted = 0;
-    __syncthreads();
-    each_token(a, p, first, span, [&](int i, int at) {
-        const uint32_t old = i < p.prompt ? atomicOr(&cnt[at], kSeen) : atomicAdd(&cnt[at], 1u);
-        if (old == 0) places[atomicAdd(noted, 1)] = (uint16_t)at;
-    });
-    __syncthreads();
-    const int n = *noted;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const int at = places[i];
-        const uint32_t out = cnt[at] & ~kSeen;
-        const float z = load_elem<ZT>(row, at);
-        float u = z > 0.0f ? z / p.repetition : z * p.repetition;
-        if (out) u -= fmaf(p.frequency, (float)out, p.presence);
-        delta[at] = fabsf(z) == kInf ? 0.0f : u - z;  // (an infinite logit stays what it is)
+    __device__ __forceinline__ Seen(char *lds, int part)
+        : words(reinterpret_cast<uint32_t *>(lds)), bases(words + part / 32),
+          before(reinterpret_cast<uint16_t *>(bases + part / 512)), nwords(part / 32)
+    {
     }
-    __syncthreads();
-}
 
+    __device__ __forceinline__ void mark(const AdjustArgs &a, const RowPolicy &p, int64_t first, int span)
+    {
+        __syncthreads();  // (the part before this one is done with the bits)
+        for (int w = threadIdx.x; w < nwords / 4; w += kThreads) reinterpret_cast<uint4 *>(words)[w] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        each_tokens(a, p, first, span, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t) {
+            // (most of a text's tokens are there already: looking first spares the atomics that all would aim at a few words)
+            uint32_t have[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) have[k] = valid >> k & 1 ? words[at[k] >> 5] : ~0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (!(have[k] >> (at[k] & 31) & 1)) atomicOr(&words[at[k] >> 5], 1u << (at[k] & 31));
+        });
+        __syncthreads();
+    }
+    // numbers the marked entries in ascending order; returns how many there are (numbers are there behind the next barrier)
+    __device__ __forceinline__ int count(int *waves)
+    {
+        const int tid = threadIdx.x, wave = tid / kWave, lane = tid & (kWave - 1);
+        int own = 0;
+        if (tid < nwords / kBlock)  // (a part has at most a block a thread)
+#pragma unroll
+            for (int k = 0; k < kBlock; k += 4) {
+                const uint4 w = reinterpret_cast<const uint4 *>(words)[(tid * kBlock + k) / 4];
+                uint16_t *to = before + tid * kBlock + k;
+                to[0] = (uint16_t)own, own += __popc(w.x);
+                to[1] = (uint16_t)own, own += __popc(w.y);
+                to[2] = (uint16_t)own, own += __popc(w.z);
+                to[3] = (uint16_t)own, own += __popc(w.w);
+            }
+        int sum = own;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+            const int up = __shfl_up(sum, off, kWave);
+            if (lane >= off) sum += up;
+        }
+        if (lane == kWave - 1) waves[wave] = sum;
+        __syncthreads();
+        int base = 0, total = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / kWave; ++w) {
+            base += w < wave ? waves[w] : 0;
+            total += waves[w];
+        }
+        if (tid < nwords / kBlock) bases[tid] = (uint32_t)(base + sum - own);
+        return total;
+    }
+    template <int EPV>
+    __device__ __forceinline__ uint32_t bits(int e) const  // of the EPV entries at e, a multiple of EPV
+    {
+        const uint32_t byte = reinterpret_cast<const uint8_t *>(words)[e >> 3];
+        return EPV == 8 ? byte : byte >> (e & 4) & 15u;
+    }
+    __device__ __forceinline__ bool bit(int e) const { return words[e >> 5] >> (e & 31) & 1; }
+    __device__ __forceinline__ int number_of_word(int w) const { return (int)bases[w / kBlock] + before[w]; }
+    __device__ __forceinline__ int number(uint32_t at) const
+    {
+        return number_of_word((int)(at >> 5)) + __popc(words[at >> 5] & ((1u << (at & 31)) - 1));
+    }
+};
+
+// (max, sum) pairs: sum_j exp((v_j - max) / temperature); nothing yet is (lowest, 0)
 __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float scale)
 {
     MaxSum o;
@@ -133,17 +181,16 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float scale)
     o.s = a.s * exp2_hw((a.m - o.m) * scale) + b.s * exp2_hw((b.m - o.m) * scale);
     return o;
 }
-
+template <int LANES = kWave>
 __device__ __forceinline__ MaxSum wave_join(MaxSum v, float scale)
 {
+    float m = v.m;
 #pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) {
-        MaxSum o;
-        o.m = __shfl_xor(v.m, off, kWave);
-        o.s = __shfl_xor(v.s, off, kWave);
-        v = join(v, o, scale);
-    }
-    return v;
+    for (int off = LANES / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+    float s = v.s * exp2_hw((v.m - m) * scale);
+#pragma unroll
+    for (int off = LANES / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, kWave);
+    return MaxSum{m, s};
 }
 
 template <typename UT, int EPV>
@@ -162,29 +209,34 @@ __device__ __forceinline__ void store_out(char *p, const float *f)
     }
 }
 
+// EPV elements of type UT as they are in memory, and widened
 template <typename UT, int EPV>
-__device__ __forceinline__ void load_in(const char *p, float *f)
-{
-    if constexpr (UT::kBytes * EPV >= 16) {
+struct Raw {
+    static constexpr int kWords = UT::kBytes * EPV / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const char *p)
+    {
+        if constexpr (kWords >= 4) {
 #pragma unroll
-        for (int k = 0; k < EPV; k += UT::kPerVec) unpack<UT>(row_load<true>(p + k * UT::kBytes), f + k);
-    } else {
-        const u32x2_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(p));
-        f[0] = __uint_as_float(t.x << 16), f[1] = __uint_as_float(t.x & 0xFFFF0000u);
-        f[2] = __uint_as_float(t.y << 16), f[3] = __uint_as_float(t.y & 0xFFFF0000u);
+            for (int k = 0; k < kWords; k += 4) {
+                const uint4 v = row_load<true>(p + 4 * k);
+                w[k] = v.x, w[k + 1] = v.y, w[k + 2] = v.z, w[k + 3] = v.w;
+            }
+        } else {
+            const u32x2_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(p));
+            w[0] = t.x, w[1] = t.y;
+        }
     }
-}
+    __device__ __forceinline__ void widen(float *f) const
+    {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) {
+            if constexpr (UT::kBytes == 4) f[k] = __uint_as_float(w[k]);
+            else f[2 * k] = __uint_as_float(w[k] << 16), f[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+        }
+    }
+};
 
-// EPV consecutive floats: from LDS (16-byte aligned), from memory (at any float)
-template <int EPV>
-__device__ __forceinline__ void load_lds(const float *p, float *f)
-{
-#pragma unroll
-    for (int k = 0; k < EPV; k += 4) {
-        const float4 w = *reinterpret_cast<const float4 *>(p + k);
-        f[k] = w.x, f[k + 1] = w.y, f[k + 2] = w.z, f[k + 3] = w.w;
-    }
-}
 template <int EPV>
 __device__ __forceinline__ void load_bias(const float *p, float *f)
 {
@@ -209,118 +261,188 @@ __device__ __forceinline__ float if_allowed(uint32_t bits, int k, float v, uint3
 }
 constexpr uint32_t kMinusInfBits = 0xFF800000u;
 
+// Entries of the history that are counted at a time, each with 8 bytes of LDS: all that a text has in a part, where the part's
+// bits leave room for them beside three other workgroups' (a second round reads the history again).
+constexpr int numbers_of(int part) { return part <= (1 << 16) ? 3072 : 1024; }
+
+// LDS of a part's bits, and with their numbers
+__device__ __host__ constexpr int seen_bytes(int part, bool numbers) { return part / 8 + (numbers ? part / 128 + part / 16 : 0); }
+
 template <typename ZT, typename UT, int NV>
 __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
 {
-    constexpr int EPV = ZT::kPerVec, kWaves = kThreads / kWave;
-    extern __shared__ __align__(16) float delta[];
+    constexpr int EPV = ZT::kPerVec, kWaves = kThreads / kWave, kStep = kThreads * EPV * NV;
+    constexpr uint32_t kAll = (1u << EPV) - 1;
+    extern __shared__ __align__(16) char lds[];
     __shared__ float red[2 * kWaves];
-    __shared__ int noted;
-    uint16_t *places = reinterpret_cast<uint16_t *>(delta + a.part);
+    __shared__ int waves[kWaves];
+    Seen seen(lds, a.part);
+    const int room = numbers_of(a.part);
+    uint32_t *counts = reinterpret_cast<uint32_t *>(lds + seen_bytes(a.part, true)), *places = counts + room;
     const int64_t items = a.T * a.parts;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t t = item / a.parts, first = (item - t * a.parts) * a.part;
-        const int span = (int)min((int64_t)a.part, a.V - first), full = span / EPV, rest = span - full * EPV;
+        const int span = (int)min((int64_t)a.part, a.V - first), whole = span / EPV * EPV, rest = span - whole;
         const char *row = static_cast<const char *>(a.z) + (t * a.ldz + first) * ZT::kBytes;
         char *out = a.u ? static_cast<char *>(a.u) + (t * a.ldu + first) * UT::kBytes : nullptr;
         const uint8_t *bits = a.allowed ? reinterpret_cast<const uint8_t *>(a.allowed + t * a.allowed_ld) + first / 8 : nullptr;
         const float *bias = a.bias ? a.bias + t * a.bias_ld + first : nullptr;
-        uint4 raw[NV];
-        uint32_t ok[NV];
+        Raw<ZT, EPV> next[NV];
+        uint32_t next_ok[NV];
+        auto fetch = [&](int at) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = i * kThreads + threadIdx.x;
-            raw[i] = neg_inf_vec<ZT>();
-            ok[i] = 0xFFu;
-            if (v < full) {
-                raw[i] = row_load<true>(row + (int64_t)v * 16);
-                if (bits) ok[i] = allowed_bits<EPV>(bits, v * EPV);
+            for (int i = 0; i < NV; ++i) {
+                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
+                if (e < whole) {
+                    next[i].load(row + (int64_t)e * ZT::kBytes);
+                    if (bits) next_ok[i] = allowed_bits<EPV>(bits, e) & kAll;
+                }
             }
-        }
+        };
+        fetch(0);
         // (one element of what is left of the row behind the last whole vector)
         const bool last = (int)threadIdx.x < rest;
-        const int le = full * EPV + threadIdx.x;
-        float extra = last ? load_elem<ZT>(row, le) : -kInf;
+        const int le = whole + threadIdx.x;
+        const float z_last = last ? load_elem<ZT>(row, le) : -kInf;
         const RowPolicy p = row_policy(a, t);
-        const bool hist = p.len > 0;
-        if (hist) penalties<ZT>(a, p, row, first, span, delta, places, &noted);
+        const int64_t y64 = a.logp ? (int64_t)a.chosen[t] - first : -1;
+        const int y = y64 >= 0 && y64 < span ? (int)y64 : -1;
         const float scale = p.inv_temperature * kLog2e;
-        float f[NV][EPV], m = kLowest;
+        const bool hist = p.len > 0 && (p.repetition != 1.0f || p.frequency != 0.0f || p.presence != 0.0f);
+        if (hist) seen.mark(a, p, first, span);
+
+        MaxSum acc = {kLowest, 0.0f};
+        for (int at = 0; at < whole; at += kStep) {
+            Raw<ZT, EPV> raw[NV];
+            uint32_t ok[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int e = (i * kThreads + threadIdx.x) * EPV;
-            unpack<ZT>(raw[i], f[i]);
-            if (e < full * EPV) {
-                if (hist) {
-                    float d[EPV];
-                    load_lds<EPV>(delta + e, d);
+            for (int i = 0; i < NV; ++i) raw[i] = next[i], ok[i] = next_ok[i];
+            if (at + kStep < whole) fetch(at + kStep);
+            float f[NV][EPV], m = acc.m;
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) f[i][k] += d[k];
+            for (int i = 0; i < NV; ++i) {
+                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
+                if (e >= whole) {
+#pragma unroll
+                    for (int k = 0; k < EPV; ++k) f[i][k] = -kInf;
+                    continue;
                 }
+                raw[i].widen(f[i]);
+                const uint32_t later = hist ? seen.bits<EPV>(e) : 0u;
                 if (bias) {
                     float b[EPV];
                     load_bias<EPV>(bias + e, b);
 #pragma unroll
                     for (int k = 0; k < EPV; ++k) f[i][k] += b[k];
                 }
-            }
-            if (bits && __any((~ok[i] & ((1u << EPV) - 1)) != 0))
+                if (bits && __any(ok[i] != kAll))
 #pragma unroll
-                for (int k = 0; k < EPV; ++k) f[i][k] = if_allowed(ok[i], k, f[i][k], kMinusInfBits);
-#pragma unroll
-            for (int k = 0; k < EPV; ++k) m = fmaxf(m, f[i][k]);
-        }
-        if (last) {
-            if (hist) extra += delta[le];
-            if (bias) extra += bias[le];
-            if (bits && !(bits[le >> 3] >> (le & 7) & 1)) extra = -kInf;
-            m = fmaxf(m, extra);
-        }
-        if (out) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int v = i * kThreads + threadIdx.x;
-                if (v < full) {
+                    for (int k = 0; k < EPV; ++k) f[i][k] = if_allowed(ok[i], k, f[i][k], kMinusInfBits);
+                if (out) {
                     float u[EPV];
 #pragma unroll
                     for (int k = 0; k < EPV; ++k) u[k] = f[i][k] * p.inv_temperature;
-                    store_out<UT, EPV>(out + (int64_t)v * EPV * UT::kBytes, u);
+                    if (later) {  // (their logits stay there for now: out may be the logits' own place)
+                        float z[EPV];
+                        raw[i].widen(z);
+#pragma unroll
+                        for (int k = 0; k < EPV; ++k) u[k] = later >> k & 1 ? z[k] : u[k];
+                    }
+                    store_out<UT, EPV>(out + (int64_t)e * UT::kBytes, u);
                 }
+                if (y >= e && y < e + EPV)
+#pragma unroll
+                    for (int k = 0; k < EPV; ++k)
+                        if (e + k == y && !(later >> k & 1)) a.ws_chosen[t] = f[i][k];
+                if (__any(later != 0))
+#pragma unroll
+                    for (int k = 0; k < EPV; ++k) f[i][k] = if_allowed(~later, k, f[i][k], kMinusInfBits);
+#pragma unroll
+                for (int k = 0; k < EPV; ++k) m = fmaxf(m, f[i][k]);
             }
-            if (last) store_elem<UT>(out, le, extra * p.inv_temperature);
+            acc.s *= exp2_hw((acc.m - m) * scale);
+            acc.m = m;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < EPV; ++k) acc.s += exp2_hw((f[i][k] - m) * scale);
+        }
+        auto bias_of = [&](int at) { return bias ? bias[at] : 0.0f; };
+        auto ok_of = [&](int at) { return !bits || (bits[at >> 3] >> (at & 7) & 1); };
+        auto put_out = [&](int at, float v) {
+            if (out) store_elem<UT>(out, at, v * p.inv_temperature);
+            if (at == y) a.ws_chosen[t] = v;
+        };
+        // (infinity and NaN make the sum NaN)
+        auto one_of = [](float v) { return v == -kInf ? 0.0f : v - v + 1.0f; };
+        if (last) {
+            if (!(hist && seen.bit(le))) {
+                const float v = ok_of(le) ? z_last + bias_of(le) : -kInf;
+                put_out(le, v);
+                acc = join(acc, MaxSum{fmaxf(v, kLowest), one_of(v)}, scale);
+            } else if (out) {
+                store_elem<UT>(out, le, z_last);
+            }
+        }
+        // the entries of the history, one a thread
+        const int numbers = hist ? seen.count(waves) : 0;
+        const float down = 1.0f / p.repetition;
+        for (int base = 0; base < numbers; base += room) {
+            const int many = min(numbers - base, room);
+            __syncthreads();  // (the numbers are there, the row is written, the counts before these are done with)
+            for (int i = threadIdx.x; i < many; i += kThreads) counts[i] = 0;
+            __syncthreads();
+            // (a token that is there more than once notes the same place)
+            each_tokens(a, p, first, span, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
+                int n[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) n[k] = valid >> k & 1 ? seen.number(at[k]) - base : -1;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (n[k] >= 0 && n[k] < room) {
+                        places[n[k]] = at[k];
+                        if (output >> k & 1) atomicAdd(&counts[n[k]], 1u);
+                    }
+            });
+            __syncthreads();
+            constexpr int kBatch = 4;  // (a thread's loads in flight)
+            for (int i = threadIdx.x; i < many; i += kThreads * kBatch) {
+                int at[kBatch];
+                float v[kBatch], b[kBatch], m = acc.m;
+                bool ok[kBatch];
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    at[k] = (int)places[min(i + k * kThreads, many - 1)];
+                    v[k] = load_elem<ZT>(row, at[k]);
+                    b[k] = bias_of(at[k]);
+                    ok[k] = ok_of(at[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const bool there = i + k * kThreads < many;
+                    const uint32_t n = there ? counts[i + k * kThreads] : 0;
+                    v[k] *= v[k] > 0.0f ? down : p.repetition;
+                    if (n) v[k] -= fmaf(p.frequency, (float)n, p.presence);
+                    v[k] = there && ok[k] ? v[k] + b[k] : -kInf;
+                    if (there) put_out(at[k], v[k]);
+                    m = fmaxf(m, v[k]);
+                }
+                acc.s *= exp2_hw((acc.m - m) * scale);
+                acc.m = m;
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) acc.s += exp2_hw((v[k] - m) * scale);
+            }
         }
         if (!a.ws_partials) continue;  // (neither log-sum-exp nor log-probs are asked for)
-        // the thread that holds the chosen token leaves it for the kernel that joins the parts
-        if (a.chosen) {
-            const int64_t y = (int64_t)a.chosen[t] - first;
-            if (y >= 0 && y < span) {
-                const int vy = (int)y / EPV, ky = (int)y - vy * EPV;
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (vy < full && i * kThreads + (int)threadIdx.x == vy)
-#pragma unroll
-                        for (int k = 0; k < EPV; ++k)
-                            if (k == ky) a.ws_chosen[t] = f[i][k];
-                if (last && le == (int)y) a.ws_chosen[t] = extra;
-            }
-        }
-        MaxSum acc = {m, exp2_hw((extra - m) * scale)};
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int k = 0; k < EPV; ++k) acc.s += exp2_hw((f[i][k] - m) * scale);
         acc = wave_join(acc, scale);
         const int wave = threadIdx.x / kWave;
         __syncthreads();
         if ((threadIdx.x & (kWave - 1)) == 0) put(red, kWaves, wave, acc);
         __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < kWaves; ++w) {
-                MaxSum o;
-                get(red, kWaves, w, o);
-                acc = join(acc, o, scale);
-            }
-            a.ws_partials[item] = make_float2(acc.m, acc.s);
+        if (threadIdx.x < kWaves) {
+            get(red, kWaves, threadIdx.x, acc);
+            acc = wave_join<kWaves>(acc, scale);
+            if (threadIdx.x == 0) a.ws_partials[item] = make_float2(acc.m, acc.s);
         }
     }
 }
@@ -356,88 +478,90 @@ __global__ __launch_bounds__(256) void adjust_finish_kernel(AdjustArgs a)
 template <typename ZT, typename UT, int NV>
 __global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
 {
-    constexpr int EPV = ZT::kPerVec;
-    extern __shared__ __align__(16) float factor[];
+    constexpr int EPV = ZT::kPerVec, kStep = kThreads * EPV * NV;
+    constexpr uint32_t kAll = (1u << EPV) - 1;
+    extern __shared__ __align__(16) char lds[];
+    Seen seen(lds, a.part);
     const int64_t items = a.T * a.parts;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t t = item / a.parts, first = (item - t * a.parts) * a.part;
-        const int span = (int)min((int64_t)a.part, a.V - first), full = span / EPV, rest = span - full * EPV;
+        const int span = (int)min((int64_t)a.part, a.V - first), whole = span / EPV * EPV, rest = span - whole;
         const char *row = static_cast<const char *>(a.z) + (t * a.ldz + first) * ZT::kBytes;
         const char *in = static_cast<const char *>(a.du) + (t * a.ldu + first) * UT::kBytes;
         char *out = static_cast<char *>(a.dz) + (t * a.lddz + first) * ZT::kBytes;
         const uint8_t *bits = a.allowed ? reinterpret_cast<const uint8_t *>(a.allowed + t * a.allowed_ld) + first / 8 : nullptr;
-        float g[NV][EPV];
-        uint32_t ok[NV];
+        Raw<UT, EPV> next[NV];
+        uint32_t next_ok[NV];
+        auto fetch = [&](int at) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = i * kThreads + threadIdx.x;
-            ok[i] = 0xFFu;
-            if (v < full) {
-                load_in<UT, EPV>(in + (int64_t)v * EPV * UT::kBytes, g[i]);
-                if (bits) ok[i] = allowed_bits<EPV>(bits, v * EPV);
+            for (int i = 0; i < NV; ++i) {
+                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
+                if (e < whole) {
+                    next[i].load(in + (int64_t)e * UT::kBytes);
+                    if (bits) next_ok[i] = allowed_bits<EPV>(bits, e) & kAll;
+                }
             }
-        }
+        };
+        fetch(0);
         const bool last = (int)threadIdx.x < rest;
-        const int le = full * EPV + threadIdx.x;
-        float extra = last ? load_elem<UT>(in, le) : 0.0f;
+        const int le = whole + threadIdx.x;
+        const float g_last = last ? load_elem<UT>(in, le) : 0.0f;
         const RowPolicy p = row_policy(a, t);
         const bool hist = p.len > 0 && p.repetition != 1.0f;
-        if (hist) {
-            const float up = p.inv_temperature * p.repetition, down = p.inv_temperature / p.repetition;
-            __syncthreads();  // (the part before this one is done with the array)
-            fill(factor, span, p.inv_temperature);
-            __syncthreads();
-            // (a token that is there twice is given the same factor twice)
-            each_token(a, p, first, span, [&](int, int at) { factor[at] = load_elem<ZT>(row, at) > 0.0f ? down : up; });
-            __syncthreads();
-        }
+        if (hist) seen.mark(a, p, first, span);
+        const float up = p.inv_temperature * p.repetition, down = p.inv_temperature / p.repetition;
+        for (int at = 0; at < whole; at += kStep) {
+            Raw<UT, EPV> raw[NV];
+            uint32_t ok[NV], hit[NV];
+            uint4 z[NV];
+            // logits of vectors that hold an entry of the history: asked for together, before the next gradients
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = i * kThreads + threadIdx.x, e = v * EPV;
-            if (v < full) {
-                if (hist) {
-                    float d[EPV];
-                    load_lds<EPV>(factor + e, d);
+            for (int i = 0; i < NV; ++i) {
+                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
+                raw[i] = next[i], ok[i] = next_ok[i];
+                hit[i] = hist && e < whole ? seen.bits<EPV>(e) : 0u;
+                if (hit[i]) z[i] = row_load<true, true>(row + (int64_t)e * ZT::kBytes);
+            }
+            if (at + kStep < whole) fetch(at + kStep);
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) g[i][k] *= d[k];
+            for (int i = 0; i < NV; ++i) {
+                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
+                if (e >= whole) continue;
+                float g[EPV];
+                raw[i].widen(g);
+                if (hit[i]) {
+                    float w[EPV];
+                    unpack<ZT>(z[i], w);
+#pragma unroll
+                    for (int k = 0; k < EPV; ++k) g[k] *= hit[i] >> k & 1 ? (w[k] > 0.0f ? down : up) : p.inv_temperature;
                 } else {
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) g[i][k] *= p.inv_temperature;
+                    for (int k = 0; k < EPV; ++k) g[k] *= p.inv_temperature;
                 }
-                if (bits && __any((~ok[i] & ((1u << EPV) - 1)) != 0))
+                if (bits && __any(ok[i] != kAll))
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) g[i][k] = if_allowed(ok[i], k, g[i][k], 0u);
-                store_out<ZT, EPV>(out + (int64_t)e * ZT::kBytes, g[i]);
+                    for (int k = 0; k < EPV; ++k) g[k] = if_allowed(ok[i], k, g[k], 0u);
+                store_out<ZT, EPV>(out + (int64_t)e * ZT::kBytes, g);
             }
         }
         if (last) {
-            extra *= hist ? factor[le] : p.inv_temperature;
-            if (bits && !(bits[le >> 3] >> (le & 7) & 1)) extra = 0.0f;
-            store_elem<ZT>(out, le, extra);
+            float f = g_last * p.inv_temperature;
+            if (hist && seen.bit(le)) f = g_last * (load_elem<ZT>(row, le) > 0.0f ? down : up);
+            if (bits && !(bits[le >> 3] >> (le & 7) & 1)) f = 0.0f;
+            store_elem<ZT>(out, le, f);
         }
     }
 }
 
-template <typename ZT, typename UT, int NV>
+template <typename ZT, typename UT>
 hipError_t launch(const AdjustArgs &a, hipStream_t s)
 {
     const int64_t items = a.T * a.parts, most = 1 << 20;
     const dim3 grid((unsigned)(items < most ? items : most)), block(kThreads);
-    const size_t lds = a.history ? (size_t)a.part * (a.dz ? 4 : 6) : 0;
-    if (a.dz) adjust_bwd_kernel<ZT, UT, NV><<<grid, block, lds, s>>>(a);
-    else adjust_kernel<ZT, UT, NV><<<grid, block, lds, s>>>(a);
+    const size_t lds = a.history ? seen_bytes(a.part, !a.dz) + (a.dz ? 0 : 8 * numbers_of(a.part)) : 0;
+    if (a.dz) adjust_bwd_kernel<ZT, UT, 2><<<grid, block, lds, s>>>(a);
+    else adjust_kernel<ZT, UT, 2><<<grid, block, lds, s>>>(a);
     return hipGetLastError();
-}
-
-template <typename ZT, typename UT>
-hipError_t launch_of(const AdjustArgs &a, hipStream_t s)
-{
-    switch (a.vectors) {
-        case 1: return launch<ZT, UT, 1>(a, s);
-        case 2: return launch<ZT, UT, 2>(a, s);
-        case 3: return launch<ZT, UT, 3>(a, s);
-        default: return launch<ZT, UT, 4>(a, s);
-    }
 }
 
 }  // namespace
@@ -447,10 +571,9 @@ hipError_t launch_adjust(AdjustArgs a, hipStream_t s)
     const AdjustPlan p = adjust_plan(a.T, a.V, a.z_dt == A3PO_F32 ? 4 : 2);
     a.parts = p.parts;
     a.part = p.part;
-    a.vectors = p.vectors;
     hipError_t e;
-    if (a.z_dt == A3PO_F32) e = a.u_dt == A3PO_F32 ? launch_of<F32, F32>(a, s) : launch_of<F32, Bf16>(a, s);
-    else e = a.u_dt == A3PO_F32 ? launch_of<Bf16, F32>(a, s) : launch_of<Bf16, Bf16>(a, s);
+    if (a.z_dt == A3PO_F32) e = a.u_dt == A3PO_F32 ? launch<F32, F32>(a, s) : launch<F32, Bf16>(a, s);
+    else e = a.u_dt == A3PO_F32 ? launch<Bf16, F32>(a, s) : launch<Bf16, Bf16>(a, s);
     if (e != hipSuccess || a.dz || !a.ws_partials) return e;
     const int64_t want = (a.T + 3) / 4, most = 1 << 20;
     adjust_finish_kernel<<<dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s>>>(a);

@@ -469,27 +469,25 @@ struct AdjustArgs {
     float *lse, *logp;
     float2 *ws_partials;  // [T, parts], null: neither lse nor logp
     float *ws_chosen;     // [T]
-    int parts, part, vectors;
+    int parts, part;
 };
 
-// A row's parts: `part` entries each (a multiple of 512), `vectors` 16-byte vectors of z a thread.  As few parts as their
-// counts fit (62 KiB of LDS, so that two workgroups share a compute unit) if there are rows enough for four workgroups a
-// compute unit, and more otherwise, down to one vector a thread.
-constexpr int kAdjustThreads = 512;
+// A row's parts, `part` entries each: whole rows if they are enough for two workgroups a compute unit, more parts
+// otherwise, down to a 16-byte vector a thread; a part's bits and their numbers have to fit 64 KiB of LDS.
+constexpr int kAdjustThreads = 512, kAdjustMaxPart = 1 << 18;
 struct AdjustPlan {
-    int parts, part, vectors;
+    int parts, part;
 };
 inline AdjustPlan adjust_plan(int64_t T, int64_t V, int z_bytes)
 {
-    const int64_t step = kAdjustThreads * (16 / z_bytes), most = z_bytes == 2 ? 10752 : 4 * step;
-    const int64_t least = (V + most - 1) / most, widest = (V + step - 1) / step;
-    int64_t parts = (1024 + T - 1) / (T > 0 ? T : 1);
+    const int64_t step = kAdjustThreads * (16 / z_bytes);
+    const int64_t least = (V + kAdjustMaxPart - 1) / kAdjustMaxPart, widest = (V + step - 1) / step;
+    int64_t parts = (512 + T - 1) / (T > 0 ? T : 1);
     if (parts > widest) parts = widest;
     if (parts < least) parts = least;
     AdjustPlan p;
     p.part = (int)(((V + parts - 1) / parts + 511) / 512 * 512);
     p.parts = (int)((V + p.part - 1) / p.part);
-    p.vectors = (int)((p.part + step - 1) / step);
     return p;
 }
 // workspace: the chosen tokens' adjusted logits, then a (max, sum) per part

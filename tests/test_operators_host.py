@@ -174,9 +174,8 @@ int main()
         for (int64_t T : {1, 2, 5, 64, 300, 1023, 1024, 5000, 1 << 24})
             for (int64_t V = 1; V < 0x7FFFFFFF; V += V < 70000 ? 1 : 1 + V / 9) {
                 const AdjustPlan p = adjust_plan(T, V, bytes);
-                const int64_t room = (int64_t)p.vectors * kAdjustThreads * (16 / bytes);
-                const bool ok = p.part % 512 == 0 && p.part > 0 && p.part * 4 + 256 <= 65536 && p.vectors >= 1 && p.vectors <= 4 &&
-                                p.part <= room && (int64_t)p.parts * p.part >= V && (int64_t)(p.parts - 1) * p.part < V &&
+                const bool ok = p.part % 512 == 0 && p.part > 0 && p.part <= kAdjustMaxPart &&
+                                (int64_t)p.parts * p.part >= V && (int64_t)(p.parts - 1) * p.part < V &&
                                 adjust_partials_offset(T) + (size_t)T * p.parts * 8 <= adjust_workspace_bytes(T, V);
                 if (!ok) return std::printf("T %lld V %lld\\n", (long long)T, (long long)V), 1;
             }
