@@ -512,6 +512,44 @@ struct W4Args {
     int64_t T, V, ldx, ldo;
     int H;
 };
+// How the kernel that keeps all hidden values in LDS goes about a call (units == 0: they do not fit, or rows end inside a unit
+// of 128 codes; the call takes the kernel that passes them through LDS in chunks).
+struct W4Plan {
+    int units;               // of a row, a wavefront
+    int blocks16;            // of 16 tokens
+    int wk_shift, tp_shift;  // log2 of the wavefronts that share a row, of the tokens in LDS (at least four)
+    int sets, blocks;
+    int lds;
+};
+constexpr int kW4MaxLds = 160 * 1024;
+inline W4Plan w4_plan(int64_t T, int64_t H, int64_t N, int group, bool scale_f32, int64_t cus)
+{
+    W4Plan p = {};
+    if (T > 32 || H % 128 != 0 || H < 256 || H > 8192) return p;
+    p.blocks16 = T <= 16 ? 1 : 2;
+    p.tp_shift = T <= 4 ? 2 : T <= 8 ? 3 : T <= 16 ? 4 : 5;
+    const int64_t tp = (int64_t)1 << p.tp_shift, units = H / 128;
+    const int64_t lds = tp * H * 2 + H / group * tp * 4 + 16 * 1024 * p.blocks16;
+    if (lds > kW4MaxLds) return p;
+    p.lds = (int)lds;
+    // the split of rows over wavefronts that leaves the busiest compute unit the fewest units in turn (a set's joining counts
+    // for one)
+    int64_t best = 0;
+    for (int shift = 0; shift <= 4; ++shift) {
+        const int64_t upw = (units + (1 << shift) - 1) >> shift;
+        if (upw > (group == 32 && scale_f32 ? 3 : 4)) continue;  // (scales of a unit take registers too)
+        if (units < (upw < 2 ? 2 : upw)) continue;
+        const int64_t rows = 16 * (16 >> shift), sets = (N + rows - 1) / rows, rounds = (sets + cus - 1) / cus;
+        const int64_t held = upw < 2 ? 2 : upw, cost = rounds * (held + 1);
+        if (best && cost >= best) continue;
+        best = cost;
+        p.units = (int)held;
+        p.wk_shift = shift;
+        p.sets = (int)sets;
+        p.blocks = (int)(sets < cus ? sets : cus);
+    }
+    return p;
+}
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t s);
 
 }  // namespace a3po

@@ -66,13 +66,14 @@ struct Scales {
         if (have >= kPerUnit) {
             if constexpr (kBytes * kPerUnit == 2) {
                 w[0] = *reinterpret_cast<const uint16_t *>(p);
+            } else if constexpr (kWords == 1) {
+                typedef uint32_t word_t __attribute__((aligned(2)));
+                w[0] = *reinterpret_cast<const word_t *>(p);
             } else {
                 typedef uint32_t words_t __attribute__((ext_vector_type(kWords), aligned(kBytes)));
                 const words_t v = *reinterpret_cast<const words_t *>(p);
-                if constexpr (kWords == 1) w[0] = v[0];
-                else
 #pragma unroll
-                    for (int i = 0; i < kWords; ++i) w[i] = v[i];
+                for (int i = 0; i < kWords; ++i) w[i] = v[i];
             }
             if constexpr (ZEROS) {
                 if constexpr (kPerUnit == 1) {
@@ -265,6 +266,231 @@ __global__ __launch_bounds__(kThreads) void w4_kernel(W4Args a)
     }
 }
 
+// ---- few tokens: hidden values resident -------------------------------------------------------------------------------
+//
+// All hidden values lie in LDS, in the order of the matrix instructions, for as long as the workgroup lives: one workgroup a
+// compute unit, sixteen wavefronts.  A set of 16 x (16 / WK) rows is taken at a time: WK wavefronts share the 16 rows, a run of
+// UPW units each, and add their sums through LDS.  A wavefront's weight is loaded NB sets ahead into registers (eight units or
+// more in flight, 128 KiB a compute unit) and waits for nobody else's.
+
+// BYTES consecutive bytes, at any address
+template <int BYTES>
+__device__ __forceinline__ void load_run(const char *p, uint32_t (&w)[(BYTES + 3) / 4])
+{
+    typedef uint32_t v4_t __attribute__((ext_vector_type(4), aligned(1)));
+    typedef uint32_t v2_t __attribute__((ext_vector_type(2), aligned(1)));
+    typedef uint32_t v1_t __attribute__((aligned(1)));
+    typedef uint16_t half_t __attribute__((aligned(1)));
+    constexpr int kFours = BYTES / 16, kTwos = BYTES / 8 % 2, kOnes = BYTES / 4 % 2, kRest = BYTES % 4;
+#pragma unroll
+    for (int i = 0; i < kFours; ++i) {
+        const v4_t v = *reinterpret_cast<const v4_t *>(p + 16 * i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
+    }
+    if constexpr (kTwos) {
+        const v2_t v = *reinterpret_cast<const v2_t *>(p + 16 * kFours);
+        w[4 * kFours] = v.x, w[4 * kFours + 1] = v.y;
+    }
+    if constexpr (kOnes) w[4 * kFours + 2 * kTwos] = *reinterpret_cast<const v1_t *>(p + 16 * kFours + 8 * kTwos);
+    if constexpr (kRest) {
+        constexpr int kAt = BYTES - kRest;
+        uint32_t v = kRest >= 2 ? *reinterpret_cast<const half_t *>(p + kAt) : 0u;
+        if constexpr (kRest & 1) v |= (uint32_t)*reinterpret_cast<const uint8_t *>(p + BYTES - 1) << (8 * (kRest - 1));
+        w[BYTES / 4] = v;
+    }
+}
+
+// a row's codes of UPW units in a row, with their scales and zero points
+template <int UPW, int GROUP, bool ZEROS, bool SCALE_F32>
+struct Run {
+    static constexpr int kGroups = UPW * 128 / GROUP, kScaleBytes = kGroups * (SCALE_F32 ? 4 : 2);
+    uint4 codes[UPW];
+    uint32_t scales[(kScaleBytes + 3) / 4], zeros[ZEROS ? (kGroups + 3) / 4 : 1];
+    __device__ __forceinline__ void load(const char *c, const char *s, const char *z)
+    {
+#pragma unroll
+        for (int u = 0; u < UPW; ++u) {
+            const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(c + u * 64));
+            codes[u] = make_uint4(v.x, v.y, v.z, v.w);
+        }
+        load_run<kScaleBytes>(s, scales);
+        if constexpr (ZEROS) load_run<kGroups>(z, zeros);
+    }
+    __device__ __forceinline__ float scale(int g) const
+    {
+        if constexpr (SCALE_F32) return __uint_as_float(scales[g]);
+        else return __uint_as_float(g & 1 ? scales[g / 2] & 0xFFFF0000u : scales[g / 2] << 16);
+    }
+    __device__ __forceinline__ float zero(int g) const { return (float)(zeros[g / 4] >> (8 * (g % 4)) & 0xFFu); }
+};
+
+// a value in a scalar / vector register that the compiler knows nothing of (it would fold a constant into every instruction,
+// of which an and-or can hold one only)
+__device__ __forceinline__ uint32_t opaque_scalar(uint32_t v)
+{
+    asm("s_mov_b32 %0, %1" : "=s"(v) : "i"(0x00780078));
+    return v;
+}
+
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(waitcnt_imm(kNoVmWait, 0));
+    __builtin_amdgcn_s_barrier();  // (bare: the weight stays in flight)
+    asm volatile("" ::: "memory");
+}
+
+template <int MT, int UPW, int NB, int GROUP, bool ZEROS, bool SCALE_F32>
+__global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shift, int tp_shift, int sets)
+{
+    constexpr int S = 128 / GROUP, BLOCKS = GROUP / 32, kAll = 16;
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int n16 = lane & 15, q = lane >> 4;
+    const int WK = 1 << wk_shift, WR = kAll >> wk_shift, wk = wave & (WK - 1), wr = wave >> wk_shift;
+    const int TP = MT > 1 ? 16 * MT : 1 << tp_shift;
+    // (the last wavefronts' runs move down to end with the row; units that another one has as well count for nothing here)
+    const int units = a.H >> 7, u0 = min(wk * UPW, units - UPW), skip = wk * UPW - u0;
+    const int64_t groups = a.H / GROUP, row_bytes = a.H / 2;
+    char *xs = lds;                                                             // [units][4][4][TP] 16 bytes
+    float *sums = reinterpret_cast<float *>(lds + (size_t)a.H * TP * 2);        // [groups][TP]
+    char *red = reinterpret_cast<char *>(sums + groups * TP);                   // [16 wavefronts][MT][64] 16 bytes
+
+    // lane offsets from a set's first row (fewer than 16 rows in all: the last one again)
+    const uint32_t row_lane = (uint32_t)min((int64_t)n16, a.V - 1);
+    const uint32_t code_lane = row_lane * (uint32_t)row_bytes + q * 16, group_lane = row_lane * (uint32_t)groups;
+    constexpr uint32_t kScale = SCALE_F32 ? 4 : 2;
+    Run<UPW, GROUP, ZEROS, SCALE_F32> run[NB];
+    // first row of this wavefront's block in a set; the last block moves up to end with the weight
+    auto first_row = [&](int set) { return min(((int64_t)set * WR + wr) * 16, max(a.V - 16, (int64_t)0)); };
+    // (no branch around the loads: at one the compiler waits for all that are in flight; sets beyond the last are the last)
+    auto fetch = [&](int set, Run<UPW, GROUP, ZEROS, SCALE_F32> &to) {
+        const int64_t row = first_row(min(set, sets - 1));
+        const char *codes = reinterpret_cast<const char *>(a.codes) + row * row_bytes + u0 * 64;
+        const int64_t group = row * groups + u0 * S;
+        to.load(codes + code_lane, static_cast<const char *>(a.scales) + group * kScale + group_lane * kScale,
+                ZEROS ? reinterpret_cast<const char *>(a.zeros) + group + group_lane : nullptr);
+        __builtin_amdgcn_sched_barrier(0);  // (in this order: what is waited for first is issued first)
+    };
+#pragma unroll
+    for (int b = 0; b < NB; ++b) fetch((int)blockIdx.x + b * (int)gridDim.x, run[b]);
+
+    for (int p = threadIdx.x; p < units * 16 * TP; p += 1024) {
+        const int token = p & (TP - 1), k8 = p / TP;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (token < a.T) {
+            const u32x4_half h = *reinterpret_cast<const u32x4_half *>(static_cast<const char *>(a.x) + (token * a.ldx + k8 * 8) * 2);
+            v = make_uint4(h.x, h.y, h.z, h.w);
+        }
+        // groups of a whole unit: the lanes of a block of codes keep it, and the quarter of the unit that they multiply is theirs
+        const int at = GROUP == 128 ? (k8 & ~15) | (k8 & 3) << 2 | (k8 >> 2 & 3) : k8;
+        *reinterpret_cast<uint4 *>(xs + ((size_t)at * TP + token) * 16) = order_like_codes(v);
+    }
+    meet();
+    for (int p = threadIdx.x; p < (int)groups * TP; p += 1024) {
+        const int token = p & (TP - 1), g = p / TP;
+        float total = 0.0f;
+#pragma unroll
+        for (int k = 0; k < GROUP / 8; ++k) {
+            float f[8];
+            unpack<Bf16>(*reinterpret_cast<const uint4 *>(xs + ((size_t)(g * (GROUP / 8) + k) * TP + token) * 16), f);
+            total += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+        }
+        sums[p] = ZEROS ? -total : -24.0f * total;  // (the codes' excess: 16 + 8 without zero points)
+    }
+    meet();
+
+    const uint32_t mask = opaque_scalar(0);
+    uint32_t sixteen;
+    asm("v_mov_b32 %0, %1" : "=v"(sixteen) : "i"(0x41804180));
+    auto widen_fast = [&](uint32_t d) {
+        const u32x4_t v = {((d << 3) & mask) | sixteen, ((d >> 1) & mask) | sixteen, ((d >> 5) & mask) | sixteen,
+                           ((d >> 9) & mask) | sixteen};
+        return __builtin_bit_cast(bf16x8_t, v);
+    };
+    // (with fewer than 16 tokens the lanes of the others read these again; their products are not stored)
+    const char *x_lane = xs + (q * TP + (n16 & (TP - 1))) * 16;
+    const float *sum_lane = sums + ((q * 4) & (TP - 1));
+
+    auto multiply = [&](const Run<UPW, GROUP, ZEROS, SCALE_F32> &from, f32x4_t (&acc)[MT]) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < UPW; ++u) {
+            uint32_t d[4] = {from.codes[u].x, from.codes[u].y, from.codes[u].z, from.codes[u].w};
+            if constexpr (GROUP < 128) transpose_blocks(d);
+            const char *x = x_lane + (size_t)(u0 + u) * 16 * TP * 16;
+            const float *sum = sum_lane + (u0 + u) * S * TP;
+            f32x4_t part[MT];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int gi = g / BLOCKS;
+                if (g % BLOCKS == 0)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        part[m] = *reinterpret_cast<const f32x4_t *>(sum + gi * TP + m * 16);
+                        if (ZEROS) part[m] *= 16.0f + from.zero(u * S + gi);
+                    }
+                const bf16x8_t wide = widen_fast(d[g]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    part[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        *reinterpret_cast<const bf16x8_t *>(x + ((size_t)g * 4 * TP + m * 16) * 16), wide, part[m], 0, 0, 0);
+                if (g % BLOCKS == BLOCKS - 1) {
+                    const float scale = u < skip ? 0.0f : from.scale(u * S + gi);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) acc[m] += part[m] * scale;
+                }
+            }
+        }
+    };
+    auto put_out = [&](int64_t t, int64_t n, float v) {
+        if (a.out_dt == A3PO_F32) static_cast<float *>(a.out)[t * a.ldo + n] = v;
+        else store_elem<Bf16>(a.out, t * a.ldo + n, v);
+    };
+    auto finish = [&](int set, f32x4_t (&acc)[MT]) {
+        meet();  // (the sums of the set before are read)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) *reinterpret_cast<f32x4_t *>(red + ((wave * MT + m) * kWave + lane) * 16) = acc[m];
+        meet();
+        for (int o = threadIdx.x; o < WR * MT * 256; o += 1024) {
+            const int block = o / (MT * 256), token = o / 16 % (MT * 16), n = o & 15;
+            if (token >= a.T) continue;
+            const char *from = red + (((block << wk_shift) * MT + token / 16) * kWave + (token / 4 % 4) * 16 + n) * 16 + token % 4 * 4;
+            constexpr int kFrom = MT * kWave * 16;
+            float total = 0.0f;
+            for (int k = 0; k < WK; k += 4) {  // (four reads in flight; beyond the last wavefront its sum again, for nothing)
+                float v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float *>(from + min(k + j, WK - 1) * kFrom);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) total += k + j < WK ? v[j] : 0.0f;
+            }
+            const int64_t want = ((int64_t)set * WR + block) * 16, row = min(want, max(a.V - 16, (int64_t)0)) + n;
+            if (row >= want && row < a.V) put_out(token, row, total);
+        }
+    };
+
+    const int step = (int)gridDim.x;
+    int set = blockIdx.x, left = (sets - 1 - set) / step + 1;
+    for (; left >= NB; left -= NB)
+#pragma unroll
+        for (int b = 0; b < NB; ++b, set += step) {
+            f32x4_t acc[MT];
+            multiply(run[b], acc);
+            fetch(set + NB * step, run[b]);
+            finish(set, acc);
+        }
+#pragma unroll
+    for (int b = 0; b < NB - 1; ++b, set += step)
+        if (b < left) {
+            f32x4_t acc[MT];
+            multiply(run[b], acc);
+            finish(set, acc);
+        }
+}
+
 template <int MT, int R, int GROUP, bool ZEROS, bool SCALE_F32>
 hipError_t launch(const W4Args &a, hipStream_t s)
 {
@@ -274,9 +500,34 @@ hipError_t launch(const W4Args &a, hipStream_t s)
     return hipGetLastError();
 }
 
+template <int MT, int UPW, int NB, int GROUP, bool ZEROS, bool SCALE_F32>
+hipError_t launch_resident(const W4Args &a, const W4Plan &p, hipStream_t s)
+{
+    static LdsLimitState lds_limit;
+    auto *kernel = w4_resident_kernel<MT, UPW, NB, GROUP, ZEROS, SCALE_F32>;
+    if (const hipError_t e = ensure_lds_limit(reinterpret_cast<const void *>(kernel), kW4MaxLds, lds_limit)) return e;
+    kernel<<<dim3((unsigned)p.blocks), dim3(1024), p.lds, s>>>(a, p.wk_shift, p.tp_shift, p.sets);
+    return hipGetLastError();
+}
+
+template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
+hipError_t launch_units(const W4Args &a, const W4Plan &p, hipStream_t s)
+{
+    // registers of a unit in flight; as many units ahead as the 128 registers of sixteen wavefronts hold
+    constexpr int kRegs = 4 + Scales<GROUP, SCALE_F32>::kWords + (ZEROS ? 1 : 0), kAhead = kRegs >= 8 ? 6 : kRegs == 7 && MT == 2 ? 8 : 9;
+    if (p.units == 2) return launch_resident<MT, 2, kAhead / 2, GROUP, ZEROS, SCALE_F32>(a, p, s);
+    if (p.units == 3) return launch_resident<MT, 3, kAhead / 3, GROUP, ZEROS, SCALE_F32>(a, p, s);
+    if constexpr (kAhead >= 8) return launch_resident<MT, 4, kAhead / 4, GROUP, ZEROS, SCALE_F32>(a, p, s);
+    return hipErrorInvalidValue;  // (w4_plan gives no such call four units)
+}
+
 template <int GROUP, bool ZEROS, bool SCALE_F32>
 hipError_t launch_tokens(const W4Args &a, hipStream_t s)
 {
+    const GemmGrid chip = gemm_grid();
+    const W4Plan p = w4_plan(a.T, a.H, a.V, a.group, SCALE_F32, (int64_t)chip.nxcd * chip.per_xcd);
+    if (p.units && p.blocks16 == 1) return launch_units<1, GROUP, ZEROS, SCALE_F32>(a, p, s);
+    if (p.units) return launch_units<2, GROUP, ZEROS, SCALE_F32>(a, p, s);
     if (a.T <= 16) return launch<1, 1, GROUP, ZEROS, SCALE_F32>(a, s);
     if (a.T <= 32) return launch<2, 1, GROUP, ZEROS, SCALE_F32>(a, s);
     return launch<4, 2, GROUP, ZEROS, SCALE_F32>(a, s);
