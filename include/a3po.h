@@ -114,7 +114,8 @@ enum {
     A3PO_WS_FUSED_LMHEAD = 1,
     A3PO_WS_FUSED_LMHEAD_LOSS = 2,
     A3PO_WS_NORM_BWD = 3,     /* T and H */
-    A3PO_WS_ADJUST_LOGITS = 4 /* T and V */
+    A3PO_WS_ADJUST_LOGITS = 4, /* T and V */
+    A3PO_WS_W4_LINEAR = 5      /* T and H */
 };
 
 /* Bytes of device workspace the given entry point needs (256-byte aligned base). */
@@ -499,12 +500,14 @@ int a3po_adjust_logits_bwd(const void *dout, a3po_dtype out_dt, int64_t ld_out, 
  * aligned: byte j of a row holds code 2j in its low and 2j + 1 in its high half.  scales [N, H / group] dtype scale_dt,
  * contiguous.  zeros [N, H / group] bytes, nullable (8 everywhere: codes are symmetric).  group 32, 64 or 128; H a multiple
  * of it, at most 2^20.  out [T, N] dtype out_dt, row stride ld_out.
- * T has no limit, but the weight is read once per 64 tokens: the kernel is made for single tokens and small batches.
+ * T <= 64 * 65,535; the weight is read once per 64 tokens: the kernels are made for single tokens and small batches.
+ * workspace: a3po_workspace_bytes(A3PO_WS_W4_LINEAR, T, 0, H) bytes, 256-byte aligned; 0 (and NULL) for up to 16 tokens
+ * with H a multiple of 128 from 256 to 4,096, whose hidden values stay on chip.
  * Products are exact and summed in fp32, out is rounded once.  x is expected to be finite (an infinity gives NaN).
  */
 int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8_t *codes, const void *scales,
                    a3po_dtype scale_dt, const uint8_t *zeros, int32_t group, int64_t N, void *out, a3po_dtype out_dt,
-                   int64_t ld_out, void *stream);
+                   int64_t ld_out, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

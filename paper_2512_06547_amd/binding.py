@@ -21,6 +21,7 @@ A3PO_WS_FUSED_LMHEAD = 1
 A3PO_WS_FUSED_LMHEAD_LOSS = 2
 A3PO_WS_NORM_BWD = 3
 A3PO_WS_ADJUST_LOGITS = 4
+A3PO_WS_W4_LINEAR = 5
 A3PO_NORM_LAYER, A3PO_NORM_RMS = 0, 1
 
 # layout of a3po_stats (include/a3po.h)
@@ -82,7 +83,7 @@ _SIGNATURES = {
     "a3po_adjust_logits_bwd": (ctypes.c_int, [_P, ctypes.c_int, _I64, _P, ctypes.c_int, _I64, _I64, _I64,
                                               ctypes.POINTER(LogitAdjustments), _P, _I64, _P]),
     "a3po_w4_linear": (ctypes.c_int, [_P, _I64, _I64, _I64, _P, _P, ctypes.c_int, _P, _I32, _I64, _P, ctypes.c_int, _I64,
-                                      _P]),
+                                      _P, _SZ, _P]),
 }
 
 _lib = None
@@ -647,7 +648,7 @@ def adjust_logits_bwd(dout, logits=None, V=None, *, history=None, hist_start=Non
     return dlogits
 
 
-def w4_linear(x, codes, scales, zeros=None, group: int = 128, out=None, out_dtype=None):
+def w4_linear(x, codes, scales, zeros=None, group: int = 128, out=None, out_dtype=None, workspace=None):
     """a3po_w4_linear -> out[T, N] (``out``, or a new tensor of ``out_dtype``, bfloat16 by default).  x bfloat16 [T, H];
     codes uint8 [N, H/2] (low half: even k); scales bfloat16 or float32 [N, H/group]; zeros uint8 [N, H/group] or None (8)."""
     torch = _torch()
@@ -663,8 +664,12 @@ def w4_linear(x, codes, scales, zeros=None, group: int = 128, out=None, out_dtyp
     if out is None:
         out = torch.empty((T, N), dtype=torch.bfloat16 if out_dtype is None else out_dtype, device=x.device)
     od, ld_out = _rows(out, "out", (T, N))
+    if workspace is None:
+        need = workspace_bytes(T, 0, H, which=A3PO_WS_W4_LINEAR)
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     _check(lib().a3po_w4_linear(_ptr(x), T, H, ldx, _ptr(codes), _ptr(scales), _dtype_code(scales, "scales"), _ptr(zeros),
-                                int(group), N, _ptr(out), od, ld_out, _stream()), "a3po_w4_linear")
+                                int(group), N, _ptr(out), od, ld_out, _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                _stream()), "a3po_w4_linear")
     return out
 
 

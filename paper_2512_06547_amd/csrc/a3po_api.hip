@@ -113,6 +113,7 @@ size_t a3po_workspace_bytes(int which, int64_t T, int64_t V, int64_t H)
     if (which == A3PO_WS_FUSED_LMHEAD_LOSS) return lmhead_bwd_workspace_bytes(T, V, H);
     if (which == A3PO_WS_NORM_BWD) return norm_bwd_workspace_bytes(T, H);
     if (which == A3PO_WS_ADJUST_LOGITS) return adjust_workspace_bytes(T, V);
+    if (which == A3PO_WS_W4_LINEAR) return T > kW4MaxTokens || H > (1 << 20) ? 0 : w4_workspace_bytes(T, H);
     return 0;
 }
 
@@ -552,7 +553,7 @@ int a3po_adjust_logits_bwd(const void *dout, a3po_dtype out_dt, int64_t ld_out, 
 
 int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8_t *codes, const void *scales,
                    a3po_dtype scale_dt, const uint8_t *zeros, int32_t group, int64_t N, void *out, a3po_dtype out_dt,
-                   int64_t ld_out, void *stream)
+                   int64_t ld_out, void *workspace, size_t workspace_bytes, void *stream)
 {
     if ((scale_dt != A3PO_F32 && scale_dt != A3PO_BF16) || (out_dt != A3PO_F32 && out_dt != A3PO_BF16)) return A3PO_E_DTYPE;
     if (group != 32 && group != 64 && group != 128) return A3PO_E_SIZE;
@@ -563,6 +564,10 @@ int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8
     if (!x || !codes || !scales || !out) return A3PO_E_NULL;
     if (!aligned(x, 2) || !aligned(codes, 16) || !aligned(scales, elem(scale_dt)) || !aligned(out, elem(out_dt)))
         return A3PO_E_ALIGN;
+    if (const size_t need = w4_workspace_bytes(T, H)) {
+        if (!workspace || workspace_bytes < need) return A3PO_E_WORKSPACE;
+        if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
+    }
     W4Args a;
     a.x = x;
     a.codes = codes;
@@ -577,7 +582,7 @@ int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8
     a.ldx = ldx;
     a.ldo = ld_out;
     a.H = (int)H;
-    return launch_w4_linear(a, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+    return launch_w4_linear(a, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
 }
 
 }  // extern "C"

@@ -500,7 +500,7 @@ inline size_t adjust_workspace_bytes(int64_t T, int64_t V)
 }
 hipError_t launch_adjust(AdjustArgs a, hipStream_t s);
 
-constexpr int kW4Waves = 8;
+constexpr int kW4UnitBytes = 4096 + 256;  // of 16 tokens' hidden values of a unit (128) and of their sums
 constexpr int64_t kW4MaxTokens = 65535 * 64;  // (blocks of 64 tokens are the grid's second dimension)
 struct W4Args {
     const void *x;
@@ -550,6 +550,13 @@ inline W4Plan w4_plan(int64_t T, int64_t H, int64_t N, int group, bool scale_f32
     }
     return p;
 }
-hipError_t launch_w4_linear(const W4Args &a, hipStream_t s);
+// workspace of the kernel that streams them (none for a call that never takes it: see w4_plan)
+inline size_t w4_workspace_bytes(int64_t T, int64_t H)
+{
+    if (T <= 0 || H <= 0 || (T <= 16 && H % 128 == 0 && H >= 256 && H <= 4096)) return 0;
+    const int64_t tokens = T <= 16 ? 16 : T <= 32 ? 32 : (T + 63) / 64 * 64;
+    return (size_t)(tokens / 16) * (size_t)((H + 127) / 128) * kW4UnitBytes;
+}
+hipError_t launch_w4_linear(const W4Args &a, void *workspace, hipStream_t s);
 
 }  // namespace a3po

@@ -15,16 +15,28 @@
 namespace a3po {
 namespace {
 
-constexpr int kWaves = kW4Waves, kThreads = kWaves * kWave;
-
 typedef uint32_t u32x4_half __attribute__((ext_vector_type(4), aligned(2)));
 
-// codes of dword d, as bfloat16 16 + n, in the order 0 4 1 5 2 6 3 7
-__device__ __forceinline__ bf16x8_t widen(uint32_t d)
+// Constants in registers that the compiler knows nothing of: it would fold them into an instruction each, of which an and-or
+// holds one at most.
+__device__ __forceinline__ uint32_t opaque_scalar()
 {
-    constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
-    const u32x4_t w = {((d << 3) & kMask) | kSixteen, ((d >> 1) & kMask) | kSixteen, ((d >> 5) & kMask) | kSixteen,
-                       ((d >> 9) & kMask) | kSixteen};
+    uint32_t v;
+    asm("s_mov_b32 %0, %1" : "=s"(v) : "i"(0x00780078));
+    return v;
+}
+__device__ __forceinline__ uint32_t opaque_vector()
+{
+    uint32_t v;
+    asm("v_mov_b32 %0, %1" : "=v"(v) : "i"(0x41804180));
+    return v;
+}
+
+// codes of dword d, as bfloat16 16 + n, in the order 0 4 1 5 2 6 3 7 (mask, sixteen: the two constants)
+__device__ __forceinline__ bf16x8_t widen(uint32_t d, uint32_t mask, uint32_t sixteen)
+{
+    const u32x4_t w = {((d << 3) & mask) | sixteen, ((d >> 1) & mask) | sixteen, ((d >> 5) & mask) | sixteen,
+                       ((d >> 9) & mask) | sixteen};
     return __builtin_bit_cast(bf16x8_t, w);
 }
 // eight hidden values in the same order
@@ -45,233 +57,13 @@ __device__ __forceinline__ void transpose_blocks(uint32_t (&d)[4])
     d[0] = t0[0], d[1] = t0[1], d[2] = t1[0], d[3] = t1[1];
 }
 
-template <int GROUP, bool SCALE_F32>
-struct Scales {
-    static constexpr int kPerUnit = 128 / GROUP, kWords = SCALE_F32 ? kPerUnit : (kPerUnit + 1) / 2;
-    uint32_t w[kWords];
-    uint32_t zeros;
-    __device__ __forceinline__ float scale(int g) const
-    {
-        if constexpr (SCALE_F32) return __uint_as_float(w[g]);
-        else return __uint_as_float(g & 1 ? w[g / 2] & 0xFFFF0000u : w[g / 2] << 16);
-    }
-    __device__ __forceinline__ float zero(int g) const { return (float)(zeros >> (8 * g) & 0xFFu); }
-
-    // the groups of one unit; `have` of them exist (the last unit of a row may be cut short)
-    template <bool ZEROS>
-    __device__ __forceinline__ void load(const void *s, const uint8_t *z, int64_t first, int have)
-    {
-        constexpr int kBytes = SCALE_F32 ? 4 : 2;
-        const char *p = static_cast<const char *>(s) + first * kBytes;
-        if (have >= kPerUnit) {
-            if constexpr (kBytes * kPerUnit == 2) {
-                w[0] = *reinterpret_cast<const uint16_t *>(p);
-            } else if constexpr (kWords == 1) {
-                typedef uint32_t word_t __attribute__((aligned(2)));
-                w[0] = *reinterpret_cast<const word_t *>(p);
-            } else {
-                typedef uint32_t words_t __attribute__((ext_vector_type(kWords), aligned(kBytes)));
-                const words_t v = *reinterpret_cast<const words_t *>(p);
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) w[i] = v[i];
-            }
-            if constexpr (ZEROS) {
-                if constexpr (kPerUnit == 1) {
-                    zeros = z[first];
-                } else if constexpr (kPerUnit == 2) {
-                    typedef uint16_t half_t __attribute__((aligned(1)));
-                    zeros = *reinterpret_cast<const half_t *>(z + first);
-                } else {
-                    typedef uint32_t word_t __attribute__((aligned(1)));
-                    zeros = *reinterpret_cast<const word_t *>(z + first);
-                }
-            }
-            return;
-        }
-        zeros = 0;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) w[i] = 0;
-#pragma unroll
-        for (int g = 0; g < kPerUnit; ++g)
-            if (g < have) {
-                if constexpr (SCALE_F32) w[g] = reinterpret_cast<const uint32_t *>(p)[g];
-                else w[g / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[g] << (g & 1 ? 16 : 0);
-                if constexpr (ZEROS) zeros |= (uint32_t)z[first + g] << (8 * g);
-            }
-    }
-};
-
-// MT: blocks of 16 tokens; R: blocks of 16 rows a wavefront.  The hidden values pass through LDS in chunks of 8 / MT units,
-// two chunks at a time: one is read while the next arrives.
-template <int MT, int R, int GROUP, bool ZEROS, bool SCALE_F32>
-__global__ __launch_bounds__(kThreads) void w4_kernel(W4Args a)
+__device__ __forceinline__ void meet()
 {
-    constexpr int UC = kWaves / MT, S = 128 / GROUP, BLOCKS = GROUP / 32;
-    using Sc = Scales<GROUP, SCALE_F32>;
-    __shared__ __align__(16) char xs[2][kWaves * 4 * kWave * 16];
-    __shared__ __align__(16) float sums[2][kWaves * 4 * 16];
-    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int n16 = lane & 15, q = lane >> 4;
-    const int units = (a.H + 127) / 128, chunks = (units + UC - 1) / UC;
-    const int64_t t0 = (int64_t)blockIdx.y * (16 * MT), groups = a.H / GROUP;
-    const int64_t n0 = (int64_t)blockIdx.x * (kWaves * R * 16) + wave * (R * 16);
-
-    const char *codes[R];
-    int64_t gbase[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t n = min(n0 + r * 16 + n16, a.V - 1);
-        codes[r] = reinterpret_cast<const char *>(a.codes) + n * (a.H / 2);
-        gbase[r] = n * groups;
-    }
-    // the unit and the 16 tokens of a chunk that this wavefront brings to LDS
-    const int xu = wave / MT, xt = wave % MT;
-    const int64_t token = t0 + xt * 16 + n16;
-    const bool live = token < a.T;
-    const char *xrow = reinterpret_cast<const char *>(a.x) + (live ? token : 0) * a.ldx * 2;
-
-    uint4 xr[4];
-    auto fetch_x = [&](int c) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int k = (c * UC + xu) * 128 + g * 32 + q * 8;
-            xr[g] = make_uint4(0, 0, 0, 0);
-            if (live && k < a.H) {
-                const u32x4_half v = *reinterpret_cast<const u32x4_half *>(xrow + (int64_t)k * 2);
-                xr[g] = make_uint4(v.x, v.y, v.z, v.w);
-            }
-        }
-    };
-    auto store_x = [&](int half) {
-        float total = 0.0f;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            *reinterpret_cast<uint4 *>(xs[half] + (((xu * 4 + g) * MT + xt) * kWave + lane) * 16) = order_like_codes(xr[g]);
-            float f[8], s;
-            unpack<Bf16>(xr[g], f);
-            s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-            s += __shfl_xor(s, 16, kWave);
-            s += __shfl_xor(s, 32, kWave);
-            total = g % BLOCKS == 0 ? s : total + s;
-            // (the codes' excess: 16 + 8 without zero points)
-            if (g % BLOCKS == BLOCKS - 1 && q == 0)
-                sums[half][(xu * S + g / BLOCKS) * (16 * MT) + xt * 16 + n16] = ZEROS ? -total : -24.0f * total;
-        }
-    };
-
-    uint4 wa[UC * R], wb[UC * R];
-    Sc sa[UC * R], sb[UC * R];
-    auto fetch_w = [&](int c, uint4 (&w)[UC * R], Sc (&s)[UC * R]) {
-#pragma unroll
-        for (int i = 0; i < UC; ++i) {
-            const int u = c * UC + i;
-            if (u < units) {
-                const int left = (a.H - u * 128) / 32;  // blocks of this unit that exist
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const u32x4_t v = __builtin_nontemporal_load(
-                        reinterpret_cast<const u32x4_t *>(codes[r] + (int64_t)u * 64 + min(q, left - 1) * 16));
-                    w[i * R + r] = make_uint4(v.x, v.y, v.z, v.w);
-                    s[i * R + r].template load<ZEROS>(a.scales, a.zeros, gbase[r] + (int64_t)u * S, left / BLOCKS);
-                }
-            }
-        }
-    };
-
-    f32x4_t acc[R][MT];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[r][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-
-    auto multiply = [&](int c, int half, uint4 (&w)[UC * R], Sc (&s)[UC * R]) {
-#pragma unroll
-        for (int i = 0; i < UC; ++i) {
-            if (c * UC + i >= units) break;
-            uint32_t d[R][4];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const uint4 v = w[i * R + r];
-                d[r][0] = v.x, d[r][1] = v.y, d[r][2] = v.z, d[r][3] = v.w;
-                transpose_blocks(d[r]);
-            }
-            f32x4_t part[R][MT];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int gi = g / BLOCKS;
-                if (g % BLOCKS == 0)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        const f32x4_t e =
-                            *reinterpret_cast<const f32x4_t *>(&sums[half][(i * S + gi) * (16 * MT) + m * 16 + q * 4]);
-#pragma unroll
-                        for (int r = 0; r < R; ++r) part[r][m] = ZEROS ? e * (16.0f + s[i * R + r].zero(gi)) : e;
-                    }
-                bf16x8_t wide[R];
-#pragma unroll
-                for (int r = 0; r < R; ++r) wide[r] = widen(d[r][g]);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const bf16x8_t x = *reinterpret_cast<const bf16x8_t *>(xs[half] + (((i * 4 + g) * MT + m) * kWave + lane) * 16);
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-                        part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, wide[r], part[r][m], 0, 0, 0);
-                }
-                if (g % BLOCKS == BLOCKS - 1)
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) acc[r][m] += part[r][m] * s[i * R + r].scale(gi);
-            }
-        }
-    };
-
-    fetch_x(0);
-    fetch_w(0, wa, sa);
-    store_x(0);
-    __syncthreads();
-    for (int c = 0; c < chunks; c += 2) {
-        if (c + 1 < chunks) {
-            fetch_x(c + 1);
-            fetch_w(c + 1, wb, sb);
-        }
-        multiply(c, 0, wa, sa);
-        if (c + 1 >= chunks) break;
-        store_x(1);
-        __syncthreads();
-        if (c + 2 < chunks) {
-            fetch_x(c + 2);
-            fetch_w(c + 2, wa, sa);
-        }
-        multiply(c + 1, 1, wb, sb);
-        if (c + 2 >= chunks) break;
-        store_x(0);
-        __syncthreads();
-    }
-
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t n = n0 + r * 16 + n16;
-        if (n >= a.V) continue;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t t = t0 + m * 16 + q * 4 + i;
-                if (t < a.T) {
-                    if (a.out_dt == A3PO_F32) static_cast<float *>(a.out)[t * a.ldo + n] = acc[r][m][i];
-                    else store_elem<Bf16>(a.out, t * a.ldo + n, acc[r][m][i]);
-                }
-            }
-    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(waitcnt_imm(kNoVmWait, 0));
+    __builtin_amdgcn_s_barrier();  // (bare: the weight stays in flight)
+    asm volatile("" ::: "memory");
 }
-
-// ---- few tokens: hidden values resident -------------------------------------------------------------------------------
-//
-// All hidden values lie in LDS, in the order of the matrix instructions, for as long as the workgroup lives: one workgroup a
-// compute unit, sixteen wavefronts.  A set of 16 x (16 / WK) rows is taken at a time: WK wavefronts share the 16 rows, a run of
-// UPW units each, and add their sums through LDS.  A wavefront's weight is loaded NB sets ahead into registers (eight units or
-// more in flight, 128 KiB a compute unit) and waits for nobody else's.
 
 // BYTES consecutive bytes, at any address
 template <int BYTES>
@@ -301,6 +93,67 @@ __device__ __forceinline__ void load_run(const char *p, uint32_t (&w)[(BYTES + 3
     }
 }
 
+// the scales and zero points of a row's groups in one unit of 128 codes
+template <int GROUP, bool SCALE_F32>
+struct Scales {
+    static constexpr int kPerUnit = 128 / GROUP, kBytes = SCALE_F32 ? 4 : 2, kWords = (kPerUnit * kBytes + 3) / 4;
+    // (vectors: the compiler keeps an array of them in registers, an array of arrays not always)
+    typedef uint32_t words_t __attribute__((ext_vector_type(kWords > 2 ? 4 : 2)));
+    words_t w;
+    uint32_t z;
+    __device__ __forceinline__ float scale(int g) const
+    {
+        if constexpr (SCALE_F32) return __uint_as_float(w[g]);
+        else return __uint_as_float(g & 1 ? w[g / 2] & 0xFFFF0000u : w[g / 2] << 16);
+    }
+    // scale (16 + zero) of group g, which may differ from lane to lane; 0 beyond the unit's groups
+    __device__ __forceinline__ float excess_of(int g) const
+    {
+        float s = scale(0);
+#pragma unroll
+        for (int k = 1; k < kPerUnit; ++k) s = g == k ? scale(k) : s;
+        return g < kPerUnit ? s * (16.0f + (float)(z >> (8 * g & 31) & 0xFFu)) : 0.0f;
+    }
+    // groups first .. of a row (whose own begin at `row`); CUT: the unit may be the row's last and cut short, the groups that
+    // it lacks are the last one again (their hidden values are zeros)
+    template <bool ZEROS, bool CUT>
+    __device__ __forceinline__ void load(const void *s, const uint8_t *zeros, int64_t row, int first, int groups)
+    {
+        if constexpr (!CUT) {
+            uint32_t v[kWords], b[1];
+            load_run<kPerUnit * kBytes>(static_cast<const char *>(s) + (row + first) * kBytes, v);
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) w[k] = v[k];
+            if constexpr (ZEROS) {
+                load_run<kPerUnit>(reinterpret_cast<const char *>(zeros) + row + first, b);
+                z = b[0];
+            }
+        } else {
+            uint32_t v[kPerUnit], b[kPerUnit];
+#pragma unroll
+            for (int g = 0; g < kPerUnit; ++g) {
+                const int64_t at = row + min(first + g, groups - 1);
+                if constexpr (SCALE_F32) v[g] = static_cast<const uint32_t *>(s)[at];
+                else v[g] = static_cast<const uint16_t *>(s)[at];
+                b[g] = ZEROS ? zeros[at] : 0;
+            }
+#pragma unroll
+            for (int g = 0; g < kPerUnit; ++g) {
+                if constexpr (SCALE_F32) w[g] = v[g];
+                else w[g / 2] = g & 1 ? w[g / 2] | v[g] << 16 : v[g];
+                z = g == 0 ? b[g] : z | b[g] << (8 * g);
+            }
+        }
+    }
+};
+
+// ---- few tokens: hidden values resident -------------------------------------------------------------------------------
+//
+// All hidden values lie in LDS, in the order of the matrix instructions, for as long as the workgroup lives: one workgroup a
+// compute unit, sixteen wavefronts.  A set of 16 x (16 / WK) rows is taken at a time: WK wavefronts share the 16 rows, a run of
+// UPW units each, and add their sums through LDS.  A wavefront's weight is loaded NB sets ahead into registers (eight units or
+// more in flight, 128 KiB a compute unit) and waits for nobody else's.
+
 // a row's codes of UPW units in a row, with their scales and zero points
 template <int UPW, int GROUP, bool ZEROS, bool SCALE_F32>
 struct Run {
@@ -324,22 +177,6 @@ struct Run {
     }
     __device__ __forceinline__ float zero(int g) const { return (float)(zeros[g / 4] >> (8 * (g % 4)) & 0xFFu); }
 };
-
-// a value in a scalar / vector register that the compiler knows nothing of (it would fold a constant into every instruction,
-// of which an and-or can hold one only)
-__device__ __forceinline__ uint32_t opaque_scalar(uint32_t v)
-{
-    asm("s_mov_b32 %0, %1" : "=s"(v) : "i"(0x00780078));
-    return v;
-}
-
-__device__ __forceinline__ void meet()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(waitcnt_imm(kNoVmWait, 0));
-    __builtin_amdgcn_s_barrier();  // (bare: the weight stays in flight)
-    asm volatile("" ::: "memory");
-}
 
 template <int MT, int UPW, int NB, int GROUP, bool ZEROS, bool SCALE_F32>
 __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shift, int tp_shift, int sets)
@@ -401,14 +238,7 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
     }
     meet();
 
-    const uint32_t mask = opaque_scalar(0);
-    uint32_t sixteen;
-    asm("v_mov_b32 %0, %1" : "=v"(sixteen) : "i"(0x41804180));
-    auto widen_fast = [&](uint32_t d) {
-        const u32x4_t v = {((d << 3) & mask) | sixteen, ((d >> 1) & mask) | sixteen, ((d >> 5) & mask) | sixteen,
-                           ((d >> 9) & mask) | sixteen};
-        return __builtin_bit_cast(bf16x8_t, v);
-    };
+    const uint32_t mask = opaque_scalar(), sixteen = opaque_vector();
     // (with fewer than 16 tokens the lanes of the others read these again; their products are not stored)
     const char *x_lane = xs + (q * TP + (n16 & (TP - 1))) * 16;
     const float *sum_lane = sums + ((q * 4) & (TP - 1));
@@ -432,7 +262,7 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
                         part[m] = *reinterpret_cast<const f32x4_t *>(sum + gi * TP + m * 16);
                         if (ZEROS) part[m] *= 16.0f + from.zero(u * S + gi);
                     }
-                const bf16x8_t wide = widen_fast(d[g]);
+                const bf16x8_t wide = widen(d[g], mask, sixteen);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
                     part[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
@@ -491,12 +321,215 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
         }
 }
 
-template <int MT, int R, int GROUP, bool ZEROS, bool SCALE_F32>
-hipError_t launch(const W4Args &a, hipStream_t s)
+// ---- more tokens, long or odd rows: hidden values stream through LDS ----------------------------------------------------
+//
+// A first kernel writes the hidden values in the order of the matrix instructions, with the sums of each group, so that the
+// second copies them to LDS as they are: [pass of 16 MT tokens][unit][4 blocks of codes][MT][64 lanes] 16 bytes, then
+// [4 groups][16 MT] sums.
+
+constexpr int unit_bytes(int mt) { return kW4UnitBytes * mt; }
+
+template <int MT>
+__global__ __launch_bounds__(256) void w4_order_kernel(W4Args a, char *to, int units, bool zeros)
 {
-    constexpr int64_t kRows = kWaves * R * 16;
-    const dim3 grid((unsigned)((a.V + kRows - 1) / kRows), (unsigned)((a.T + 16 * MT - 1) / (16 * MT)));
-    w4_kernel<MT, R, GROUP, ZEROS, SCALE_F32><<<grid, dim3(kThreads), 0, s>>>(a);
+    const int unit = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t pass = blockIdx.y;
+    char *out = to + (pass * units + unit) * unit_bytes(MT);
+    float *sums = reinterpret_cast<float *>(out + 4096 * MT);
+    const int q = lane >> 4, n16 = lane & 15, S = 128 / a.group, per = 4 / S;
+    for (int m = wave; m < MT; m += 4) {
+        const int64_t token = pass * (16 * MT) + m * 16 + n16;
+        const char *row = static_cast<const char *>(a.x) + token * a.ldx * 2;
+        float total = 0.0f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int k = unit * 128 + g * 32 + q * 8;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (token < a.T && k < a.H) {
+                const u32x4_half h = *reinterpret_cast<const u32x4_half *>(row + (int64_t)k * 2);
+                v = make_uint4(h.x, h.y, h.z, h.w);
+            }
+            *reinterpret_cast<uint4 *>(out + ((g * MT + m) * kWave + lane) * 16) = order_like_codes(v);
+            float f[8], s;
+            unpack<Bf16>(v, f);
+            s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+            s += __shfl_xor(s, 16, kWave);
+            s += __shfl_xor(s, 32, kWave);
+            total = g % per == 0 ? s : total + s;
+            // (the codes' excess: 16 + 8 without zero points)
+            if (g % per == per - 1 && q == 0) sums[(g / per) * (16 * MT) + m * 16 + n16] = zeros ? -total : -24.0f * total;
+        }
+        if (q == 0)
+            for (int g = S; g < 4; ++g) sums[g * (16 * MT) + m * 16 + n16] = 0.0f;
+    }
+}
+
+// Four wavefronts of 32 rows each.  Two units a chunk: chunk c is multiplied from LDS while chunk c + 1 of the hidden values
+// and chunks c + 1 and c + 2 of the codes arrive in registers.  TAIL: rows end inside a unit.
+// With zero points the excess leaves by a matrix instruction of its own (fp32 operands: a group's sum times scale (16 + zero)):
+// as a start value of each group's accumulators it took as many instructions as the scales themselves.
+template <int MT, int GROUP, bool ZEROS, bool SCALE_F32, bool TAIL>
+__global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char *ordered, int units)
+{
+    constexpr int UC = 2, R = 2, S = 128 / GROUP, BLOCKS = GROUP / 32, kChunk = UC * unit_bytes(MT);
+    constexpr int kCopies = (kChunk + 4095) / 4096;
+    using Sc = Scales<GROUP, SCALE_F32>;
+    __shared__ __align__(16) char xs[2][kChunk];
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int n16 = lane & 15, q = lane >> 4;
+    const int chunks = (units + UC - 1) / UC, groups = a.H / GROUP, left = (a.H - (units - 1) * 128) / 32;
+    const int64_t row_bytes = a.H / 2, n0 = ((int64_t)blockIdx.x * 4 + wave) * (R * 16);
+    const char *x = ordered + (int64_t)blockIdx.y * units * unit_bytes(MT);
+    const int x_bytes = units * unit_bytes(MT);
+
+    const char *codes[R];
+    int64_t gbase[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int64_t n = min(n0 + r * 16 + n16, a.V - 1);
+        codes[r] = reinterpret_cast<const char *>(a.codes) + n * row_bytes;
+        gbase[r] = n * groups;
+    }
+    struct Chunk {
+        u32x4_t w[UC * R];
+        Sc s[UC * R];
+    };
+    // (no branch around loads: at one the compiler waits for all that are in flight; beyond the last unit it is the last again)
+    auto fetch_w = [&](int c, Chunk &to) {
+#pragma unroll
+        for (int i = 0; i < UC; ++i) {
+            const int u = min(c * UC + i, units - 1);
+            const int block = TAIL && u == units - 1 ? min(q, left - 1) : q;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                to.w[i * R + r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(codes[r] + u * 64 + block * 16));
+                to.s[i * R + r].template load<ZEROS, TAIL>(a.scales, a.zeros, gbase[r], u * S, groups);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    u32x4_t xr[kCopies];
+    const int x_lane = threadIdx.x * 16;
+    auto fetch_x = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i)
+            xr[i] = *reinterpret_cast<const u32x4_t *>(x + min(c * kChunk + min(i * 4096 + x_lane, kChunk - 16), x_bytes - 16));
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto store_x = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) *reinterpret_cast<u32x4_t *>(xs[half] + min(i * 4096 + x_lane, kChunk - 16)) = xr[i];
+    };
+
+    const uint32_t mask = opaque_scalar();
+    const uint32_t sixteen = opaque_vector();
+    f32x4_t acc[R][MT];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[r][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+    auto multiply = [&](int c, const Chunk &from) {
+        const char *half = xs[c & 1];
+#pragma unroll
+        for (int i = 0; i < UC; ++i) {
+            if (c * UC + i >= units) break;
+            const char *unit = half + i * unit_bytes(MT);
+            const float *sums = reinterpret_cast<const float *>(unit + 4096 * MT);
+            uint32_t d[R][4];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) d[r][k] = from.w[i * R + r][k];
+                transpose_blocks(d[r]);
+            }
+            if constexpr (ZEROS) {
+                float excess[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) excess[r] = from.s[i * R + r].excess_of(q);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const float e = sums[q * (16 * MT) + m * 16 + n16];
+#pragma unroll
+                    for (int r = 0; r < R; ++r) acc[r][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(e, excess[r], acc[r][m], 0, 0, 0);
+                }
+            }
+            f32x4_t part[R][MT];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                bf16x8_t wide[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) wide[r] = widen(d[r][g], mask, sixteen);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const bf16x8_t xv = *reinterpret_cast<const bf16x8_t *>(unit + ((g * MT + m) * kWave + lane) * 16);
+                    f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (!ZEROS && g % BLOCKS == 0)
+                        start = *reinterpret_cast<const f32x4_t *>(sums + (g / BLOCKS) * (16 * MT) + m * 16 + q * 4);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wide[r], g % BLOCKS == 0 ? start : part[r][m], 0, 0, 0);
+                        if (g % BLOCKS == BLOCKS - 1) acc[r][m] += part[r][m] * from.s[i * R + r].scale(g / BLOCKS);
+                    }
+                }
+            }
+        }
+    };
+
+    auto step = [&](int c, const Chunk &now, Chunk &ahead) {
+        fetch_x(c + 1);
+        fetch_w(c + 2, ahead);
+        multiply(c, now);
+        store_x((c + 1) & 1);
+        meet();
+    };
+    Chunk k0, k1, k2;
+    fetch_x(0);
+    fetch_w(0, k0);
+    fetch_w(1, k1);
+    store_x(0);
+    meet();
+    for (int c = 0;;) {
+        step(c, k0, k2);
+        if (++c >= chunks) break;
+        step(c, k1, k0);
+        if (++c >= chunks) break;
+        step(c, k2, k1);
+        if (++c >= chunks) break;
+    }
+
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int64_t n = n0 + r * 16 + n16;
+        if (n >= a.V) continue;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t t = (int64_t)blockIdx.y * (16 * MT) + m * 16 + q * 4 + i;
+                if (t < a.T) {
+                    if (a.out_dt == A3PO_F32) static_cast<float *>(a.out)[t * a.ldo + n] = acc[r][m][i];
+                    else store_elem<Bf16>(a.out, t * a.ldo + n, acc[r][m][i]);
+                }
+            }
+    }
+}
+
+template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
+hipError_t launch_stream(const W4Args &a, void *workspace, hipStream_t s)
+{
+    const int units = (a.H + 127) / 128;
+    const unsigned passes = (unsigned)((a.T + 16 * MT - 1) / (16 * MT));
+    char *ordered = static_cast<char *>(workspace);
+    w4_order_kernel<MT><<<dim3(units, passes), dim3(256), 0, s>>>(a, ordered, units, ZEROS);
+    if (const hipError_t e = hipGetLastError()) return e;
+    const dim3 grid((unsigned)((a.V + 127) / 128), passes);
+    if constexpr (GROUP < 128)
+        if (a.H % 128) {
+            w4_stream_kernel<MT, GROUP, ZEROS, SCALE_F32, true><<<grid, dim3(256), 0, s>>>(a, ordered, units);
+            return hipGetLastError();
+        }
+    w4_stream_kernel<MT, GROUP, ZEROS, SCALE_F32, false><<<grid, dim3(256), 0, s>>>(a, ordered, units);
     return hipGetLastError();
 }
 
@@ -514,7 +547,7 @@ template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
 hipError_t launch_units(const W4Args &a, const W4Plan &p, hipStream_t s)
 {
     // registers of a unit in flight; as many units ahead as the 128 registers of sixteen wavefronts hold
-    constexpr int kRegs = 4 + Scales<GROUP, SCALE_F32>::kWords + (ZEROS ? 1 : 0), kAhead = kRegs >= 8 ? 6 : kRegs == 7 && MT == 2 ? 8 : 9;
+    constexpr int kRegs = 4 + (128 / GROUP * (SCALE_F32 ? 4 : 2) + 3) / 4 + (ZEROS ? 1 : 0), kAhead = kRegs >= 8 ? 6 : kRegs == 7 && MT == 2 ? 8 : 9;
     if (p.units == 2) return launch_resident<MT, 2, kAhead / 2, GROUP, ZEROS, SCALE_F32>(a, p, s);
     if (p.units == 3) return launch_resident<MT, 3, kAhead / 3, GROUP, ZEROS, SCALE_F32>(a, p, s);
     if constexpr (kAhead >= 8) return launch_resident<MT, 4, kAhead / 4, GROUP, ZEROS, SCALE_F32>(a, p, s);
@@ -522,31 +555,32 @@ hipError_t launch_units(const W4Args &a, const W4Plan &p, hipStream_t s)
 }
 
 template <int GROUP, bool ZEROS, bool SCALE_F32>
-hipError_t launch_tokens(const W4Args &a, hipStream_t s)
+hipError_t launch_tokens(const W4Args &a, void *workspace, hipStream_t s)
 {
     const GemmGrid chip = gemm_grid();
     const W4Plan p = w4_plan(a.T, a.H, a.V, a.group, SCALE_F32, (int64_t)chip.nxcd * chip.per_xcd);
     if (p.units && p.blocks16 == 1) return launch_units<1, GROUP, ZEROS, SCALE_F32>(a, p, s);
     if (p.units) return launch_units<2, GROUP, ZEROS, SCALE_F32>(a, p, s);
-    if (a.T <= 16) return launch<1, 1, GROUP, ZEROS, SCALE_F32>(a, s);
-    if (a.T <= 32) return launch<2, 1, GROUP, ZEROS, SCALE_F32>(a, s);
-    return launch<4, 2, GROUP, ZEROS, SCALE_F32>(a, s);
+    if (a.T <= 16) return launch_stream<1, GROUP, ZEROS, SCALE_F32>(a, workspace, s);
+    if (a.T <= 32) return launch_stream<2, GROUP, ZEROS, SCALE_F32>(a, workspace, s);
+    return launch_stream<4, GROUP, ZEROS, SCALE_F32>(a, workspace, s);
 }
 
 template <int GROUP>
-hipError_t launch_group(const W4Args &a, hipStream_t s)
+hipError_t launch_group(const W4Args &a, void *ws, hipStream_t s)
 {
-    if (a.zeros) return a.scale_dt == A3PO_F32 ? launch_tokens<GROUP, true, true>(a, s) : launch_tokens<GROUP, true, false>(a, s);
-    return a.scale_dt == A3PO_F32 ? launch_tokens<GROUP, false, true>(a, s) : launch_tokens<GROUP, false, false>(a, s);
+    const bool f32 = a.scale_dt == A3PO_F32;
+    if (a.zeros) return f32 ? launch_tokens<GROUP, true, true>(a, ws, s) : launch_tokens<GROUP, true, false>(a, ws, s);
+    return f32 ? launch_tokens<GROUP, false, true>(a, ws, s) : launch_tokens<GROUP, false, false>(a, ws, s);
 }
 
 }  // namespace
 
-hipError_t launch_w4_linear(const W4Args &a, hipStream_t s)
+hipError_t launch_w4_linear(const W4Args &a, void *workspace, hipStream_t s)
 {
-    if (a.group == 32) return launch_group<32>(a, s);
-    if (a.group == 64) return launch_group<64>(a, s);
-    return launch_group<128>(a, s);
+    if (a.group == 32) return launch_group<32>(a, workspace, s);
+    if (a.group == 64) return launch_group<64>(a, workspace, s);
+    return launch_group<128>(a, workspace, s);
 }
 
 }  // namespace a3po

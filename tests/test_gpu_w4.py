@@ -132,3 +132,20 @@ def test_on_another_stream_and_in_a_graph(a3po):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want), i
+
+
+@pytest.mark.parametrize("T,H", [(16, 4224), (16, 4608), (9, 4480), (8, 8192), (3, 8192), (1, 8320), (4, 16384), (32, 2048), (32, 2176), (20, 1664),
+                                 (17, 256), (1, 256), (1, 128), (5, 384), (12, 3968), (64, 4096), (65, 2432)])
+@pytest.mark.parametrize("group,zeros,st", [(128, False, torch.bfloat16), (64, True, torch.float32), (32, True, torch.float32),
+                                            (32, False, torch.bfloat16), (32, False, torch.float32), (64, False, torch.float32)])
+def test_hidden_values_resident_and_streamed(a3po, T, H, group, zeros, st):
+    """Every split of a row over wavefronts, runs that move down to end with the row, hidden values too many for LDS."""
+    for N in (5, 530):
+        _check(a3po, T, N, H, group, zeros, st, seed=T + H)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+def test_more_sets_than_compute_units(a3po, zeros):
+    """Workgroups take several sets of rows each, the last of them not all."""
+    for T, N, H in ((2, 33333, 256), (16, 20011, 512), (30, 9001, 768), (5, 12345, 384)):
+        _check(a3po, T, N, H, 128, zeros, seed=N)

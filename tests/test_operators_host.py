@@ -97,8 +97,11 @@ def test_adjust_logits_bwd_refuses(lib):
 
 
 def test_w4_linear_refuses(lib):
-    # x, T, H, ldx, codes, scales, scale_dt, zeros, group, N, out, out_dt, ld_out, stream
-    call = caller(lib.a3po_w4_linear, [P(), 4, 256, 256, P(), P(), 1, P(), 64, 100, P(), 0, 100, None])
+    # x, T, H, ldx, codes, scales, scale_dt, zeros, group, N, out, out_dt, ld_out, workspace, bytes, stream
+    need = lib.a3po_workspace_bytes(5, 40, 0, 256)
+    call = caller(lib.a3po_w4_linear, [P(), 40, 256, 256, P(), P(), 1, P(), 64, 100, P(), 0, 100, P(0x10000), need - 1, None])
+    assert call() == -5 and call(a13=None, a14=1 << 30) == -5 and call(a13=P(0x10010), a14=need) == -4
+    assert lib.a3po_workspace_bytes(5, 16, 0, 4096) == 0 and need % 256 == 0 and need > 40 * 256 * 2
     assert call(a6=2) == -3 and call(a11=2) == -3
     for group in (0, 16, 48, 256, -64):
         assert call(a8=group) == -2
@@ -112,9 +115,9 @@ def test_w4_linear_refuses(lib):
 
 def test_workspaces_grow_with_their_calls_and_take_any_size(lib):
     ws = lib.a3po_workspace_bytes
-    for which in (3, 4):
+    for which in (3, 4, 5):
         sizes = [ws(which, T, 151936, 4096) for T in (-1, 0, 1, 7, 100, 10000, 65536)]
-        assert all(s % 256 == 0 and s > 0 for s in sizes) and sizes == sorted(sizes)
+        assert all(s % 256 == 0 and (s > 0 or which == 5) for s in sizes) and sizes == sorted(sizes)
     assert ws(3, 5, 0, -1) > 0 and ws(3, 5, 0, 1 << 40) > 0 and ws(4, 5, -1, 0) > 0
 
 
