@@ -114,25 +114,25 @@ struct Scales {
         for (int k = 1; k < kPerUnit; ++k) s = g == k ? scale(k) : s;
         return g < kPerUnit ? s * (16.0f + (float)(z >> (8 * g & 31) & 0xFFu)) : 0.0f;
     }
-    // groups first .. of a row (whose own begin at `row`); CUT: the unit may be the row's last and cut short, the groups that
+    // groups first .. of a row (whose own begin at `row` + `lane`, the lane's part of it); CUT: the unit may be the row's last and cut short, the groups that
     // it lacks are the last one again (their hidden values are zeros)
     template <bool ZEROS, bool CUT>
-    __device__ __forceinline__ void load(const void *s, const uint8_t *zeros, int64_t row, int first, int groups)
+    __device__ __forceinline__ void load(const void *s, const uint8_t *zeros, int64_t row, uint32_t lane, int first, int groups)
     {
         if constexpr (!CUT) {
             uint32_t v[kWords], b[1];
-            load_run<kPerUnit * kBytes>(static_cast<const char *>(s) + (row + first) * kBytes, v);
+            load_run<kPerUnit * kBytes>(static_cast<const char *>(s) + (row + first) * kBytes + lane * kBytes, v);
 #pragma unroll
             for (int k = 0; k < kWords; ++k) w[k] = v[k];
             if constexpr (ZEROS) {
-                load_run<kPerUnit>(reinterpret_cast<const char *>(zeros) + row + first, b);
+                load_run<kPerUnit>(reinterpret_cast<const char *>(zeros) + (row + first) + lane, b);
                 z = b[0];
             }
         } else {
             uint32_t v[kPerUnit], b[kPerUnit];
 #pragma unroll
             for (int g = 0; g < kPerUnit; ++g) {
-                const int64_t at = row + min(first + g, groups - 1);
+                const int64_t at = row + lane + min(first + g, groups - 1);
                 if constexpr (SCALE_F32) v[g] = static_cast<const uint32_t *>(s)[at];
                 else v[g] = static_cast<const uint16_t *>(s)[at];
                 b[g] = ZEROS ? zeros[at] : 0;
@@ -325,7 +325,8 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
 //
 // A first kernel writes the hidden values in the order of the matrix instructions, with the sums of each group, so that the
 // second copies them to LDS as they are: [pass of 16 MT tokens][unit][4 blocks of codes][MT][64 lanes] 16 bytes, then
-// [4 groups][16 MT] sums.
+// [4 groups][16 MT] sums.  Units are even in number: one beyond the row holds zeros (a branch around it would cost the wait that
+// loads are kept out of branches for).
 
 constexpr int unit_bytes(int mt) { return kW4UnitBytes * mt; }
 
@@ -377,18 +378,20 @@ __global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char 
     __shared__ __align__(16) char xs[2][kChunk];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int n16 = lane & 15, q = lane >> 4;
-    const int chunks = (units + UC - 1) / UC, groups = a.H / GROUP, left = (a.H - (units - 1) * 128) / 32;
+    const int chunks = units / UC, last = (a.H - 1) / 128, groups = a.H / GROUP, left = (a.H - last * 128) / 32;
     const int64_t row_bytes = a.H / 2, n0 = ((int64_t)blockIdx.x * 4 + wave) * (R * 16);
     const char *x = ordered + (int64_t)blockIdx.y * units * unit_bytes(MT);
     const int x_bytes = units * unit_bytes(MT);
 
-    const char *codes[R];
-    int64_t gbase[R];
+    // the wavefront's first row, and each lane's bytes and groups from there (rows beyond the last are the last)
+    const int64_t first = min(n0, a.V - 1), row_groups = first * groups;
+    const char *codes = reinterpret_cast<const char *>(a.codes) + first * row_bytes;
+    uint32_t code_lane[R], group_lane[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int64_t n = min(n0 + r * 16 + n16, a.V - 1);
-        codes[r] = reinterpret_cast<const char *>(a.codes) + n * row_bytes;
-        gbase[r] = n * groups;
+        const uint32_t n = (uint32_t)(min(n0 + r * 16 + n16, a.V - 1) - first);
+        code_lane[r] = n * (uint32_t)row_bytes;
+        group_lane[r] = n * (uint32_t)groups;
     }
     struct Chunk {
         u32x4_t w[UC * R];
@@ -398,12 +401,12 @@ __global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char 
     auto fetch_w = [&](int c, Chunk &to) {
 #pragma unroll
         for (int i = 0; i < UC; ++i) {
-            const int u = min(c * UC + i, units - 1);
-            const int block = TAIL && u == units - 1 ? min(q, left - 1) : q;
+            const int u = min(c * UC + i, last);
+            const uint32_t block = TAIL && u == last ? min(q, left - 1) : q;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                to.w[i * R + r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(codes[r] + u * 64 + block * 16));
-                to.s[i * R + r].template load<ZEROS, TAIL>(a.scales, a.zeros, gbase[r], u * S, groups);
+                to.w[i * R + r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(codes + u * 64 + (code_lane[r] + block * 16)));
+                to.s[i * R + r].template load<ZEROS, TAIL>(a.scales, a.zeros, row_groups, group_lane[r], u * S, groups);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -433,7 +436,6 @@ __global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char 
         const char *half = xs[c & 1];
 #pragma unroll
         for (int i = 0; i < UC; ++i) {
-            if (c * UC + i >= units) break;
             const char *unit = half + i * unit_bytes(MT);
             const float *sums = reinterpret_cast<const float *>(unit + 4096 * MT);
             uint32_t d[R][4];
@@ -467,11 +469,15 @@ __global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char 
                     if (!ZEROS && g % BLOCKS == 0)
                         start = *reinterpret_cast<const f32x4_t *>(sums + (g / BLOCKS) * (16 * MT) + m * 16 + q * 4);
 #pragma unroll
-                    for (int r = 0; r < R; ++r) {
+                    for (int r = 0; r < R; ++r)
                         part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wide[r], g % BLOCKS == 0 ? start : part[r][m], 0, 0, 0);
-                        if (g % BLOCKS == BLOCKS - 1) acc[r][m] += part[r][m] * from.s[i * R + r].scale(g / BLOCKS);
-                    }
                 }
+                // (behind the products of all tokens: a sum that is read at once holds the wavefront up for its whole length)
+                if (g % BLOCKS == BLOCKS - 1)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) acc[r][m] += part[r][m] * from.s[i * R + r].scale(g / BLOCKS);
             }
         }
     };
@@ -518,7 +524,7 @@ __global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char 
 template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
 hipError_t launch_stream(const W4Args &a, void *workspace, hipStream_t s)
 {
-    const int units = (a.H + 127) / 128;
+    const int units = (a.H + 255) / 256 * 2;
     const unsigned passes = (unsigned)((a.T + 16 * MT - 1) / (16 * MT));
     char *ordered = static_cast<char *>(workspace);
     w4_order_kernel<MT><<<dim3(units, passes), dim3(256), 0, s>>>(a, ordered, units, ZEROS);
