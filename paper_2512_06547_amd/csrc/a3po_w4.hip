@@ -57,6 +57,20 @@ __device__ __forceinline__ void transpose_blocks(uint32_t (&d)[4])
     d[0] = t0[0], d[1] = t0[1], d[2] = t1[0], d[3] = t1[1];
 }
 
+// Two units of 16 rows are loaded as 8 rows x 128 bytes twice: whole lines, half as many requests as 16 rows x 64 bytes (what
+// a compute unit can ask for is counted in lines).  Lane (n, q) of a holds row n % 8, unit n / 8, of b row 8 + n % 8; afterwards
+// a is the first unit's row n, b the second's.
+__device__ __forceinline__ void sort_units(uint32_t (&a)[4], uint32_t (&b)[4])
+{
+    constexpr int kRor8 = 0x128;  // lane i of 16 takes lane i - 8
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int x = (int)a[k], y = (int)b[k];
+        a[k] = (uint32_t)__builtin_amdgcn_update_dpp(x, y, kRor8, 0xF, 0xC, false);
+        b[k] = (uint32_t)__builtin_amdgcn_update_dpp(y, x, kRor8, 0xF, 0x3, false);
+    }
+}
+
 __device__ __forceinline__ void meet()
 {
     asm volatile("" ::: "memory");
@@ -158,15 +172,17 @@ struct Scales {
 template <int UPW, int GROUP, bool ZEROS, bool SCALE_F32>
 struct Run {
     static constexpr int kGroups = UPW * 128 / GROUP, kScaleBytes = kGroups * (SCALE_F32 ? 4 : 2);
-    uint4 codes[UPW];
+    u32x4_t codes[UPW];
     uint32_t scales[(kScaleBytes + 3) / 4], zeros[ZEROS ? (kGroups + 3) / 4 : 1];
-    __device__ __forceinline__ void load(const char *c, const char *s, const char *z)
+    // c: the block's first row and unit; a, b: a lane's place in pairs of units (see sort_units), one: in a single unit
+    __device__ __forceinline__ void load(const char *c, uint32_t a, uint32_t b, uint32_t one, const char *s, const char *z)
     {
 #pragma unroll
-        for (int u = 0; u < UPW; ++u) {
-            const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(c + u * 64));
-            codes[u] = make_uint4(v.x, v.y, v.z, v.w);
+        for (int u = 0; u + 1 < UPW; u += 2) {
+            codes[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(c + u * 64 + a));
+            codes[u + 1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(c + u * 64 + b));
         }
+        if constexpr (UPW % 2) codes[UPW - 1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(c + (UPW - 1) * 64 + one));
         load_run<kScaleBytes>(s, scales);
         if constexpr (ZEROS) load_run<kGroups>(z, zeros);
     }
@@ -196,7 +212,9 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
 
     // lane offsets from a set's first row (fewer than 16 rows in all: the last one again)
     const uint32_t row_lane = (uint32_t)min((int64_t)n16, a.V - 1);
-    const uint32_t code_lane = row_lane * (uint32_t)row_bytes + q * 16, group_lane = row_lane * (uint32_t)groups;
+    const uint32_t one_lane = row_lane * (uint32_t)row_bytes + q * 16, group_lane = row_lane * (uint32_t)groups;
+    auto pair_lane = [&](int row) { return (uint32_t)min((int64_t)row, a.V - 1) * (uint32_t)row_bytes + (n16 >> 3) * 64 + q * 16; };
+    const uint32_t a_lane = pair_lane(n16 & 7), b_lane = pair_lane(8 + (n16 & 7));
     constexpr uint32_t kScale = SCALE_F32 ? 4 : 2;
     Run<UPW, GROUP, ZEROS, SCALE_F32> run[NB];
     // first row of this wavefront's block in a set; the last block moves up to end with the weight
@@ -206,7 +224,7 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
         const int64_t row = first_row(min(set, sets - 1));
         const char *codes = reinterpret_cast<const char *>(a.codes) + row * row_bytes + u0 * 64;
         const int64_t group = row * groups + u0 * S;
-        to.load(codes + code_lane, static_cast<const char *>(a.scales) + group * kScale + group_lane * kScale,
+        to.load(codes, a_lane, b_lane, one_lane, static_cast<const char *>(a.scales) + group * kScale + group_lane * kScale,
                 ZEROS ? reinterpret_cast<const char *>(a.zeros) + group + group_lane : nullptr);
         __builtin_amdgcn_sched_barrier(0);  // (in this order: what is waited for first is issued first)
     };
@@ -246,9 +264,16 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
     auto multiply = [&](const Run<UPW, GROUP, ZEROS, SCALE_F32> &from, f32x4_t (&acc)[MT]) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        uint32_t codes[UPW][4];
+#pragma unroll
+        for (int u = 0; u < UPW; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) codes[u][k] = from.codes[u][k];
+#pragma unroll
+        for (int u = 0; u + 1 < UPW; u += 2) sort_units(codes[u], codes[u + 1]);
 #pragma unroll
         for (int u = 0; u < UPW; ++u) {
-            uint32_t d[4] = {from.codes[u].x, from.codes[u].y, from.codes[u].z, from.codes[u].w};
+            uint32_t(&d)[4] = codes[u];
             if constexpr (GROUP < 128) transpose_blocks(d);
             const char *x = x_lane + (size_t)(u0 + u) * 16 * TP * 16;
             const float *sum = sum_lane + (u0 + u) * S * TP;
