@@ -550,12 +550,28 @@ inline W4Plan w4_plan(int64_t T, int64_t H, int64_t N, int group, bool scale_f32
     }
     return p;
 }
-// workspace of the kernel that streams them (none for a call that never takes it: see w4_plan)
+// Tiles of the kernel that streams them: of 256 rows, in rounds over the compute units, and of 128 rows for what is left if
+// that is no more than a round of those (or nothing but those, where even they do not fill a round).
+struct W4Tiles {
+    int wide, narrow, blocks;
+};
+inline W4Tiles w4_tiles(int64_t N, int64_t cus)
+{
+    const int64_t rounds = N / (256 * cus), left = N - rounds * 256 * cus;
+    W4Tiles t;
+    const bool half = left <= 128 * cus;
+    t.wide = (int)(rounds * cus + (half ? 0 : (left + 255) / 256));
+    t.narrow = half ? (int)((left + 127) / 128) : 0;
+    t.blocks = (int)(t.wide > cus ? cus : t.wide > t.narrow ? t.wide : t.narrow);
+    return t;
+}
+constexpr int kW4ShortBytes = 128;
+// its workspace (none for a call that never takes it: see w4_plan)
 inline size_t w4_workspace_bytes(int64_t T, int64_t H)
 {
     if (T <= 0 || H <= 0 || (T <= 16 && H % 128 == 0 && H >= 256 && H <= 4096)) return 0;
     const int64_t tokens = T <= 16 ? 16 : T <= 32 ? 32 : (T + 63) / 64 * 64;
-    return (size_t)(tokens / 16) * (size_t)((H + 255) / 256 * 2) * kW4UnitBytes;
+    return (size_t)(tokens / 16) * (size_t)((H + 255) / 256 * 2) * kW4UnitBytes + 2 * kW4ShortBytes;
 }
 hipError_t launch_w4_linear(const W4Args &a, void *workspace, hipStream_t s);
 

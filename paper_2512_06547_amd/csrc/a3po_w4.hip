@@ -8,6 +8,8 @@
 // (16 + zero) * sum x is what the fp32 accumulator of a group starts from, and the group's scale multiplies the sum.
 // Products are exact, sums are fp32, the output is rounded once.
 // With up to 16 tokens the kernel is bound by the weight's bytes: the matrix cores take a seventh of that time.
+#include <type_traits>
+
 #include "a3po_common.h"
 #include "a3po_direct.h"
 #include "a3po_launch.h"
@@ -106,60 +108,6 @@ __device__ __forceinline__ void load_run(const char *p, uint32_t (&w)[(BYTES + 3
         w[BYTES / 4] = v;
     }
 }
-
-// the scales and zero points of a row's groups in one unit of 128 codes
-template <int GROUP, bool SCALE_F32>
-struct Scales {
-    static constexpr int kPerUnit = 128 / GROUP, kBytes = SCALE_F32 ? 4 : 2, kWords = (kPerUnit * kBytes + 3) / 4;
-    // (vectors: the compiler keeps an array of them in registers, an array of arrays not always)
-    typedef uint32_t words_t __attribute__((ext_vector_type(kWords > 2 ? 4 : 2)));
-    words_t w;
-    uint32_t z;
-    __device__ __forceinline__ float scale(int g) const
-    {
-        if constexpr (SCALE_F32) return __uint_as_float(w[g]);
-        else return __uint_as_float(g & 1 ? w[g / 2] & 0xFFFF0000u : w[g / 2] << 16);
-    }
-    // scale (16 + zero) of group g, which may differ from lane to lane; 0 beyond the unit's groups
-    __device__ __forceinline__ float excess_of(int g) const
-    {
-        float s = scale(0);
-#pragma unroll
-        for (int k = 1; k < kPerUnit; ++k) s = g == k ? scale(k) : s;
-        return g < kPerUnit ? s * (16.0f + (float)(z >> (8 * g & 31) & 0xFFu)) : 0.0f;
-    }
-    // groups first .. of a row (whose own begin at `row` + `lane`, the lane's part of it); CUT: the unit may be the row's last and cut short, the groups that
-    // it lacks are the last one again (their hidden values are zeros)
-    template <bool ZEROS, bool CUT>
-    __device__ __forceinline__ void load(const void *s, const uint8_t *zeros, int64_t row, uint32_t lane, int first, int groups)
-    {
-        if constexpr (!CUT) {
-            uint32_t v[kWords], b[1];
-            load_run<kPerUnit * kBytes>(static_cast<const char *>(s) + (row + first) * kBytes + lane * kBytes, v);
-#pragma unroll
-            for (int k = 0; k < kWords; ++k) w[k] = v[k];
-            if constexpr (ZEROS) {
-                load_run<kPerUnit>(reinterpret_cast<const char *>(zeros) + (row + first) + lane, b);
-                z = b[0];
-            }
-        } else {
-            uint32_t v[kPerUnit], b[kPerUnit];
-#pragma unroll
-            for (int g = 0; g < kPerUnit; ++g) {
-                const int64_t at = row + lane + min(first + g, groups - 1);
-                if constexpr (SCALE_F32) v[g] = static_cast<const uint32_t *>(s)[at];
-                else v[g] = static_cast<const uint16_t *>(s)[at];
-                b[g] = ZEROS ? zeros[at] : 0;
-            }
-#pragma unroll
-            for (int g = 0; g < kPerUnit; ++g) {
-                if constexpr (SCALE_F32) w[g] = v[g];
-                else w[g / 2] = g & 1 ? w[g / 2] | v[g] << 16 : v[g];
-                z = g == 0 ? b[g] : z | b[g] << (8 * g);
-            }
-        }
-    }
-};
 
 // ---- few tokens: hidden values resident -------------------------------------------------------------------------------
 //
@@ -390,90 +338,239 @@ __global__ __launch_bounds__(256) void w4_order_kernel(W4Args a, char *to, int u
     }
 }
 
-// Four wavefronts of 32 rows each.  Two units a chunk: chunk c is multiplied from LDS while chunk c + 1 of the hidden values
-// and chunks c + 1 and c + 2 of the codes arrive in registers.  TAIL: rows end inside a unit.
+// arrays of scales or zero points too short for the loads of the second kernel, with zeros behind them
+__global__ __launch_bounds__(kW4ShortBytes) void w4_short_kernel(const uint8_t *from, int bytes, uint8_t *to)
+{
+    to[threadIdx.x] = (int)threadIdx.x < bytes ? from[threadIdx.x] : 0;
+}
+
+// 16 bytes of an array, `over` of which would lie behind its end: loaded that much earlier, the others moved to the front
+__device__ __forceinline__ u32x4_t load_piece(const char *p)
+{
+    typedef uint32_t v4_t __attribute__((ext_vector_type(4), aligned(1)));
+    return *reinterpret_cast<const v4_t *>(p);
+}
+__device__ __forceinline__ u32x4_t move_piece(u32x4_t v, int over)
+{
+    if (__any(over > 0)) {
+        uint64_t lo = (uint64_t)v.y << 32 | v.x, hi = (uint64_t)v.w << 32 | v.z;
+        const int bits = min(over, 15) * 8;
+        if (over >= 8) {
+            lo = hi >> (bits - 64);
+            hi = 0;
+        } else if (over > 0) {
+            lo = lo >> bits | hi << (64 - bits);
+            hi >>= bits;
+        }
+        v.x = (uint32_t)lo, v.y = (uint32_t)(lo >> 32), v.z = (uint32_t)hi, v.w = (uint32_t)(hi >> 32);
+    }
+    return v;
+}
+
+// The blocks of scales (128 bytes of a row at a time, a line) and zero points that a wavefront's 16 R rows need for the next
+// units: from memory into registers, from there into the wavefront's own LDS.
+template <int R, int GROUP, bool ZEROS, bool SCALE_F32>
+struct GroupBlocks {
+    static constexpr int S = 128 / GROUP, kBytes = SCALE_F32 ? 4 : 2, kUnits = 128 / (S * kBytes), kZeroBytes = kUnits * S;
+    static constexpr int kStride = 144, kZeroStride = kZeroBytes + 16;  // (rows on different banks)
+    static constexpr int kLds = 32 * (kStride + (ZEROS ? kZeroStride : 0));
+    static constexpr int kPieces = 2 * R, kZeroLanes = kZeroBytes / 16, kZeroPieces = (16 * R * kZeroLanes + kWave - 1) / kWave;
+    u32x4_t s[kPieces], z[kZeroPieces];
+
+    // a row's bytes, the block's first byte of the wavefront's first row, and how far a piece may begin from there
+    struct Place {
+        const char *from;
+        int last;
+    };
+    __device__ __forceinline__ static Place place(const void *array, int64_t array_rows, int64_t row, int row_len, int64_t at)
+    {
+        Place p;
+        p.from = static_cast<const char *>(array) + row * row_len + at;
+        p.last = (int)min(array_rows * row_len - 16 - (row * row_len + at), (int64_t)0x7FFFFFFF);
+        return p;
+    }
+    __device__ __forceinline__ static int lane_at(int row, int rows, int row_len, int byte) { return min(row, rows - 1) * row_len + byte; }
+
+    // row, rows: the wavefront's first row and their number; groups: of a row
+    __device__ __forceinline__ void fetch(const W4Args &a, int64_t row, int rows, int groups, int block, int lane)
+    {
+        const Place p = place(a.scales, a.V, row, groups * kBytes, (int64_t)block * 128);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+            s[i] = load_piece(p.from + min(lane_at(i * 8 + lane / 8, rows, groups * kBytes, lane % 8 * 16), p.last));
+        if constexpr (ZEROS) {
+            const Place zp = place(a.zeros, a.V, row, groups, (int64_t)block * kZeroBytes);
+#pragma unroll
+            for (int i = 0; i < kZeroPieces; ++i)
+                z[i] = load_piece(zp.from + min(lane_at(i * (kWave / kZeroLanes) + lane / kZeroLanes, rows, groups, lane % kZeroLanes * 16), zp.last));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __device__ __forceinline__ void store(const W4Args &a, char *lds, int64_t row, int rows, int groups, int block, int lane)
+    {
+        const int row_bytes = groups * kBytes;
+        const Place p = place(a.scales, a.V, row, row_bytes, (int64_t)block * 128);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            u32x4_t v = move_piece(s[i], lane_at(i * 8 + lane / 8, rows, row_bytes, lane % 8 * 16) - p.last);
+            if ((block + 1) * 128 > row_bytes) {  // what lies behind the row's end is another row's: no scale at all here
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int left = row_bytes - (block * 128 + lane % 8 * 16 + 4 * k);
+                    v[k] = left >= 4 ? v[k] : left == 2 ? v[k] & 0xFFFFu : 0u;
+                }
+            }
+            *reinterpret_cast<u32x4_t *>(lds + (i * 8 + lane / 8) * kStride + lane % 8 * 16) = v;
+        }
+        if constexpr (ZEROS) {
+            const Place zp = place(a.zeros, a.V, row, groups, (int64_t)block * kZeroBytes);
+#pragma unroll
+            for (int i = 0; i < kZeroPieces; ++i) {
+                const int r = i * (kWave / kZeroLanes) + lane / kZeroLanes;
+                const u32x4_t v = move_piece(z[i], lane_at(r, rows, groups, lane % kZeroLanes * 16) - zp.last);
+                if (r < 16 * R) *reinterpret_cast<u32x4_t *>(lds + 32 * kStride + r * kZeroStride + lane % kZeroLanes * 16) = v;
+            }
+        }
+    }
+    // of row r, unit u of the block
+    __device__ __forceinline__ static void scales(const char *lds, int r, int u, float (&out)[S])
+    {
+        const char *p = lds + r * kStride + u * (S * kBytes);
+        if constexpr (SCALE_F32) {
+            typedef float v_t __attribute__((ext_vector_type(S > 1 ? S : 2)));
+            if constexpr (S == 1) out[0] = *reinterpret_cast<const float *>(p);
+            else {
+                const v_t v = *reinterpret_cast<const v_t *>(p);
+#pragma unroll
+                for (int g = 0; g < S; ++g) out[g] = v[g];
+            }
+        } else {
+            uint32_t w[(S + 1) / 2];
+            if constexpr (S == 1) w[0] = *reinterpret_cast<const uint16_t *>(p);
+            else
+#pragma unroll
+                for (int k = 0; k < S / 2; ++k) w[k] = reinterpret_cast<const uint32_t *>(p)[k];
+#pragma unroll
+            for (int g = 0; g < S; ++g) out[g] = __uint_as_float(g & 1 ? w[g / 2] & 0xFFFF0000u : w[g / 2] << 16);
+        }
+    }
+    // scale (16 + zero) of the unit's group g, which differs from lane to lane; 0 beyond its groups
+    __device__ __forceinline__ static float excess(const char *lds, int r, int u, int g)
+    {
+        const int at = u * S + min(g, S - 1);
+        const float s = load_elem<std::conditional_t<SCALE_F32, F32, Bf16>>(lds + r * kStride, at);
+        const float z = (float)*reinterpret_cast<const uint8_t *>(lds + 32 * kStride + r * kZeroStride + at);
+        return S == 4 || g < S ? s * (16.0f + z) : 0.0f;
+    }
+};
+
+// Eight wavefronts of 16 R rows each, tile after tile.  Two units a chunk: chunk c is multiplied from LDS while chunk c + 1 of the
+// hidden values and chunks c + 1 and c + 2 of the codes arrive in registers, the next tile's among them.
 // With zero points the excess leaves by a matrix instruction of its own (fp32 operands: a group's sum times scale (16 + zero)):
 // as a start value of each group's accumulators it took as many instructions as the scales themselves.
-template <int MT, int GROUP, bool ZEROS, bool SCALE_F32, bool TAIL>
-__global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char *ordered, int units)
+template <int MT, int R, int GROUP, bool ZEROS, bool SCALE_F32>
+__device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int units, int64_t first_row, int tiles, int64_t t0, char *xs,
+                                             char *own)
 {
-    constexpr int UC = 2, R = 2, S = 128 / GROUP, BLOCKS = GROUP / 32, kChunk = UC * unit_bytes(MT);
-    constexpr int kCopies = (kChunk + 4095) / 4096;
-    using Sc = Scales<GROUP, SCALE_F32>;
-    __shared__ __align__(16) char xs[2][kChunk];
+    constexpr int UC = 2, S = 128 / GROUP, BLOCKS = GROUP / 32, kChunk = UC * unit_bytes(MT), kRows = 8 * 16 * R;
+    constexpr int kCopies = (kChunk + 8191) / 8192;
+    using Groups = GroupBlocks<R, GROUP, ZEROS, SCALE_F32>;
+    constexpr int kPerBlock = Groups::kUnits / UC;  // chunks of a block of scales
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int n16 = lane & 15, q = lane >> 4;
-    const int chunks = units / UC, last = (a.H - 1) / 128, groups = a.H / GROUP, left = (a.H - last * 128) / 32;
-    const int64_t row_bytes = a.H / 2, n0 = ((int64_t)blockIdx.x * 4 + wave) * (R * 16);
-    const char *x = ordered + (int64_t)blockIdx.y * units * unit_bytes(MT);
-    const int x_bytes = units * unit_bytes(MT);
-
-    // the wavefront's first row, and each lane's bytes and groups from there (rows beyond the last are the last)
-    const int64_t first = min(n0, a.V - 1), row_groups = first * groups;
-    const char *codes = reinterpret_cast<const char *>(a.codes) + first * row_bytes;
-    uint32_t code_lane[R], group_lane[R];
+    const int n16 = lane & 15, q = lane >> 4, step = (int)gridDim.x;
+    const int chunks = units / UC, groups = a.H / GROUP, row_bytes = a.H / 2;
+    const int mine = tiles > (int)blockIdx.x ? (tiles - 1 - (int)blockIdx.x) / step + 1 : 0;
+    if (mine == 0) return;
+    // rows of this wavefront in its i-th tile; those beyond the last move up to end with the weight
+    const int rows = (int)min((int64_t)(16 * R), a.V);
+    auto wanted = [&](int i) { return first_row + ((int64_t)blockIdx.x + (int64_t)i * step) * kRows + wave * (16 * R); };
+    auto row_of = [&](int i) { return min(wanted(i), max(a.V - 16 * R, (int64_t)0)); };
+    uint32_t a_lane[R], b_lane[R];
+    const uint32_t in_row = (n16 >> 3) * 64 + q * 16;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const uint32_t n = (uint32_t)(min(n0 + r * 16 + n16, a.V - 1) - first);
-        code_lane[r] = n * (uint32_t)row_bytes;
-        group_lane[r] = n * (uint32_t)groups;
+        a_lane[r] = (uint32_t)min(r * 16 + (n16 & 7), rows - 1) * (uint32_t)row_bytes;
+        b_lane[r] = (uint32_t)min(r * 16 + 8 + (n16 & 7), rows - 1) * (uint32_t)row_bytes;
     }
     struct Chunk {
         u32x4_t w[UC * R];
-        Sc s[UC * R];
     };
-    // (no branch around loads: at one the compiler waits for all that are in flight; beyond the last unit it is the last again)
-    auto fetch_w = [&](int c, Chunk &to) {
+    // the place of what is fetched next: tile, chunk
+    auto advance = [&](int &i, int &c) {
+        ++c;
+        const bool over = c == chunks;
+        c = over ? 0 : c;
+        i = over ? min(i + 1, mine - 1) : i;  // (beyond the last tile it is the last again: no branch around loads, at one the
+    };                                        // compiler waits for all that are in flight)
+    int wi = 0, wc = 0, xc = 0;
+    auto fetch_w = [&](Chunk &to) {
+        const char *codes = reinterpret_cast<const char *>(a.codes) + row_of(wi) * row_bytes;
+        // (a row that ends inside the pair of units: its last 16 bytes again, against hidden values of zero)
+        const uint32_t at = min(wc * 128 + in_row, (uint32_t)row_bytes - 16);
 #pragma unroll
-        for (int i = 0; i < UC; ++i) {
-            const int u = min(c * UC + i, last);
-            const uint32_t block = TAIL && u == last ? min(q, left - 1) : q;
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                to.w[i * R + r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(codes + u * 64 + (code_lane[r] + block * 16)));
-                to.s[i * R + r].template load<ZEROS, TAIL>(a.scales, a.zeros, row_groups, group_lane[r], u * S, groups);
-            }
+        for (int r = 0; r < R; ++r) {
+            to.w[2 * r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(codes + (a_lane[r] + at)));
+            to.w[2 * r + 1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(codes + (b_lane[r] + at)));
         }
+        advance(wi, wc);
         __builtin_amdgcn_sched_barrier(0);
     };
     u32x4_t xr[kCopies];
     const int x_lane = threadIdx.x * 16;
-    auto fetch_x = [&](int c) {
+    auto fetch_x = [&]() {
 #pragma unroll
         for (int i = 0; i < kCopies; ++i)
-            xr[i] = *reinterpret_cast<const u32x4_t *>(x + min(c * kChunk + min(i * 4096 + x_lane, kChunk - 16), x_bytes - 16));
+            xr[i] = *reinterpret_cast<const u32x4_t *>(x + (int64_t)xc * kChunk + min(i * 8192 + x_lane, kChunk - 16));
+        xc = xc + 1 == chunks ? 0 : xc + 1;
         __builtin_amdgcn_sched_barrier(0);
     };
     auto store_x = [&](int half) {
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) *reinterpret_cast<u32x4_t *>(xs[half] + min(i * 4096 + x_lane, kChunk - 16)) = xr[i];
+        for (int i = 0; i < kCopies; ++i) *reinterpret_cast<u32x4_t *>(xs + half * kChunk + min(i * 8192 + x_lane, kChunk - 16)) = xr[i];
+    };
+    // blocks of scales: the one in registers
+    Groups next;
+    int gi = 0, gb = 0;
+    const int blocks = (chunks + kPerBlock - 1) / kPerBlock;
+    auto fetch_groups = [&]() { next.fetch(a, row_of(gi), rows, groups, gb, lane); };
+    auto store_groups = [&]() {
+        next.store(a, own, row_of(gi), rows, groups, gb, lane);
+        gb = gb + 1 == blocks ? 0 : gb + 1;
+        gi = gb == 0 ? min(gi + 1, mine - 1) : gi;
     };
 
-    const uint32_t mask = opaque_scalar();
-    const uint32_t sixteen = opaque_vector();
+    const uint32_t mask = opaque_scalar(), sixteen = opaque_vector();
     f32x4_t acc[R][MT];
+    auto clear = [&]() {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) acc[r][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-
-    auto multiply = [&](int c, const Chunk &from) {
-        const char *half = xs[c & 1];
+            for (int m = 0; m < MT; ++m) acc[r][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    auto multiply = [&](int half, int in_block, const Chunk &from) {
+        uint32_t d[R][UC][4];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int i = 0; i < UC; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) d[r][i][k] = from.w[2 * r + i][k];
+            sort_units(d[r][0], d[r][1]);
+        }
 #pragma unroll
         for (int i = 0; i < UC; ++i) {
-            const char *unit = half + i * unit_bytes(MT);
+            const char *unit = xs + half * kChunk + i * unit_bytes(MT);
             const float *sums = reinterpret_cast<const float *>(unit + 4096 * MT);
-            uint32_t d[R][4];
+            float scale[R][S];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) d[r][k] = from.w[i * R + r][k];
-                transpose_blocks(d[r]);
+                transpose_blocks(d[r][i]);
+                Groups::scales(own, r * 16 + n16, in_block * UC + i, scale[r]);
             }
             if constexpr (ZEROS) {
                 float excess[R];
 #pragma unroll
-                for (int r = 0; r < R; ++r) excess[r] = from.s[i * R + r].excess_of(q);
+                for (int r = 0; r < R; ++r) excess[r] = Groups::excess(own, r * 16 + n16, in_block * UC + i, q);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     const float e = sums[q * (16 * MT) + m * 16 + n16];
@@ -486,7 +583,7 @@ __global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char 
             for (int g = 0; g < 4; ++g) {
                 bf16x8_t wide[R];
 #pragma unroll
-                for (int r = 0; r < R; ++r) wide[r] = widen(d[r][g], mask, sixteen);
+                for (int r = 0; r < R; ++r) wide[r] = widen(d[r][i][g], mask, sixteen);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     const bf16x8_t xv = *reinterpret_cast<const bf16x8_t *>(unit + ((g * MT + m) * kWave + lane) * 16);
@@ -502,65 +599,110 @@ __global__ __launch_bounds__(256, 2) void w4_stream_kernel(W4Args a, const char 
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
 #pragma unroll
-                        for (int r = 0; r < R; ++r) acc[r][m] += part[r][m] * from.s[i * R + r].scale(g / BLOCKS);
+                        for (int r = 0; r < R; ++r) acc[r][m] += part[r][m] * scale[r][g / BLOCKS];
             }
         }
     };
+    auto put_out = [&](int i) {
+        const int64_t want = wanted(i), at = row_of(i);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t n = at + r * 16 + n16;
+            if (n < want || n >= a.V) continue;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t t = t0 + m * 16 + q * 4 + k;
+                    if (t < a.T) {
+                        if (a.out_dt == A3PO_F32) static_cast<float *>(a.out)[t * a.ldo + n] = acc[r][m][k];
+                        else store_elem<Bf16>(a.out, t * a.ldo + n, acc[r][m][k]);
+                    }
+                }
+        }
+    };
 
-    auto step = [&](int c, const Chunk &now, Chunk &ahead) {
-        fetch_x(c + 1);
-        fetch_w(c + 2, ahead);
-        multiply(c, now);
-        store_x((c + 1) & 1);
+    int tile = 0, c = 0, in_block = 0, half = 0;
+    const int64_t total = (int64_t)mine * chunks;
+    auto one = [&](const Chunk &now, Chunk &ahead) {
+        if (in_block == 0) {
+            store_groups();
+            fetch_groups();
+        }
+        fetch_x();
+        fetch_w(ahead);
+        multiply(half, in_block, now);
+        half ^= 1;
+        store_x(half);
+        if (++in_block == kPerBlock) in_block = 0;
+        if (++c == chunks) {
+            put_out(tile);
+            clear();
+            ++tile;
+            c = in_block = 0;
+        }
         meet();
     };
     Chunk k0, k1, k2;
-    fetch_x(0);
-    fetch_w(0, k0);
-    fetch_w(1, k1);
+    fetch_groups();
+    fetch_x();
+    fetch_w(k0);
+    fetch_w(k1);
+    clear();
+    meet();  // (the tiles before these are read)
     store_x(0);
     meet();
-    for (int c = 0;;) {
-        step(c, k0, k2);
-        if (++c >= chunks) break;
-        step(c, k1, k0);
-        if (++c >= chunks) break;
-        step(c, k2, k1);
-        if (++c >= chunks) break;
-    }
-
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t n = n0 + r * 16 + n16;
-        if (n >= a.V) continue;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t t = (int64_t)blockIdx.y * (16 * MT) + m * 16 + q * 4 + i;
-                if (t < a.T) {
-                    if (a.out_dt == A3PO_F32) static_cast<float *>(a.out)[t * a.ldo + n] = acc[r][m][i];
-                    else store_elem<Bf16>(a.out, t * a.ldo + n, acc[r][m][i]);
-                }
-            }
+    for (int64_t s = 0;;) {
+        one(k0, k2);
+        if (++s >= total) break;
+        one(k1, k0);
+        if (++s >= total) break;
+        one(k2, k1);
+        if (++s >= total) break;
     }
 }
 
+// Tiles of 256 rows first, then a last round of 128 rows where no more are left for it: a compute unit is done with those in
+// half the time.
 template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
-hipError_t launch_stream(const W4Args &a, void *workspace, hipStream_t s)
+__global__ __launch_bounds__(512) void w4_stream_kernel(W4Args a, const char *ordered, int units, int wide_tiles, int narrow_tiles)
 {
+    constexpr int kOwn = GroupBlocks<2, GROUP, ZEROS, SCALE_F32>::kLds;
+    extern __shared__ __align__(16) char lds[];
+    char *own = lds + 4 * unit_bytes(MT) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kOwn;
+    const char *x = ordered + (int64_t)blockIdx.y * units * unit_bytes(MT);
+    const int64_t t0 = (int64_t)blockIdx.y * (16 * MT);
+    stream_tiles<MT, 2, GROUP, ZEROS, SCALE_F32>(a, x, units, 0, wide_tiles, t0, lds, own);
+    stream_tiles<MT, 1, GROUP, ZEROS, SCALE_F32>(a, x, units, (int64_t)wide_tiles * 256, narrow_tiles, t0, lds, own);
+}
+
+template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
+hipError_t launch_stream(W4Args a, void *workspace, int cus, hipStream_t s)
+{
+    static LdsLimitState lds_limit;
+    auto *kernel = w4_stream_kernel<MT, GROUP, ZEROS, SCALE_F32>;
+    if (const hipError_t e = ensure_lds_limit(reinterpret_cast<const void *>(kernel), kW4MaxLds, lds_limit)) return e;
     const int units = (a.H + 255) / 256 * 2;
     const unsigned passes = (unsigned)((a.T + 16 * MT - 1) / (16 * MT));
     char *ordered = static_cast<char *>(workspace);
     w4_order_kernel<MT><<<dim3(units, passes), dim3(256), 0, s>>>(a, ordered, units, ZEROS);
     if (const hipError_t e = hipGetLastError()) return e;
-    const dim3 grid((unsigned)((a.V + 127) / 128), passes);
-    if constexpr (GROUP < 128)
-        if (a.H % 128) {
-            w4_stream_kernel<MT, GROUP, ZEROS, SCALE_F32, true><<<grid, dim3(256), 0, s>>>(a, ordered, units);
-            return hipGetLastError();
-        }
-    w4_stream_kernel<MT, GROUP, ZEROS, SCALE_F32, false><<<grid, dim3(256), 0, s>>>(a, ordered, units);
+    // scales and zero points are loaded 16 bytes at a time: short arrays from a copy behind the hidden values
+    uint8_t *spare = static_cast<uint8_t *>(workspace) + (size_t)passes * units * unit_bytes(MT);
+    const int64_t groups = a.V * (a.H / GROUP), bytes = groups * (SCALE_F32 ? 4 : 2);
+    if (bytes < 16) {
+        w4_short_kernel<<<1, kW4ShortBytes, 0, s>>>(static_cast<const uint8_t *>(a.scales), (int)bytes, spare);
+        if (const hipError_t e = hipGetLastError()) return e;
+        a.scales = spare;
+    }
+    if (ZEROS && groups < 16) {
+        w4_short_kernel<<<1, kW4ShortBytes, 0, s>>>(a.zeros, (int)groups, spare + kW4ShortBytes);
+        if (const hipError_t e = hipGetLastError()) return e;
+        a.zeros = spare + kW4ShortBytes;
+    }
+    const W4Tiles p = w4_tiles(a.V, cus);
+    const int lds = 4 * unit_bytes(MT) + 8 * GroupBlocks<2, GROUP, ZEROS, SCALE_F32>::kLds;
+    kernel<<<dim3((unsigned)p.blocks, passes), dim3(512), lds, s>>>(a, ordered, units, p.wide, p.narrow);
     return hipGetLastError();
 }
 
@@ -589,12 +731,13 @@ template <int GROUP, bool ZEROS, bool SCALE_F32>
 hipError_t launch_tokens(const W4Args &a, void *workspace, hipStream_t s)
 {
     const GemmGrid chip = gemm_grid();
-    const W4Plan p = w4_plan(a.T, a.H, a.V, a.group, SCALE_F32, (int64_t)chip.nxcd * chip.per_xcd);
+    const int cus = chip.nxcd * chip.per_xcd;
+    const W4Plan p = w4_plan(a.T, a.H, a.V, a.group, SCALE_F32, cus);
     if (p.units && p.blocks16 == 1) return launch_units<1, GROUP, ZEROS, SCALE_F32>(a, p, s);
     if (p.units) return launch_units<2, GROUP, ZEROS, SCALE_F32>(a, p, s);
-    if (a.T <= 16) return launch_stream<1, GROUP, ZEROS, SCALE_F32>(a, workspace, s);
-    if (a.T <= 32) return launch_stream<2, GROUP, ZEROS, SCALE_F32>(a, workspace, s);
-    return launch_stream<4, GROUP, ZEROS, SCALE_F32>(a, workspace, s);
+    if (a.T <= 16) return launch_stream<1, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
+    if (a.T <= 32) return launch_stream<2, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
+    return launch_stream<4, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
 }
 
 template <int GROUP>
