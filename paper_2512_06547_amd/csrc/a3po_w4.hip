@@ -8,8 +8,6 @@
 // (16 + zero) * sum x is what the fp32 accumulator of a group starts from, and the group's scale multiplies the sum.
 // Products are exact, sums are fp32, the output is rounded once.
 // With up to 16 tokens the kernel is bound by the weight's bytes: the matrix cores take a seventh of that time.
-#include <type_traits>
-
 #include "a3po_common.h"
 #include "a3po_direct.h"
 #include "a3po_launch.h"
@@ -367,14 +365,15 @@ __device__ __forceinline__ u32x4_t move_piece(u32x4_t v, int over)
     return v;
 }
 
-// The blocks of scales (128 bytes of a row at a time, a line) and zero points that a wavefront's 16 R rows need for the next
+// The blocks of scales (64 bytes of a row at a time) and zero points that a wavefront's 16 R rows need for the next
 // units: from memory into registers, from there into the wavefront's own LDS.
 template <int R, int GROUP, bool ZEROS, bool SCALE_F32>
 struct GroupBlocks {
-    static constexpr int S = 128 / GROUP, kBytes = SCALE_F32 ? 4 : 2, kUnits = 128 / (S * kBytes), kZeroBytes = kUnits * S;
-    static constexpr int kStride = 144, kZeroStride = kZeroBytes + 16;  // (rows on different banks)
+    static constexpr int S = 128 / GROUP, kBytes = SCALE_F32 ? 4 : 2, kBlock = 64, kUnits = kBlock / (S * kBytes), kZeroBytes = kUnits * S;
+    static constexpr int kLanes = kBlock / 16, kTogether = kWave / kLanes;  // lanes a row, rows a load
+    static constexpr int kStride = kBlock + 16, kZeroStride = kZeroBytes + 16;  // (rows on different banks)
     static constexpr int kLds = 32 * (kStride + (ZEROS ? kZeroStride : 0));
-    static constexpr int kPieces = 2 * R, kZeroLanes = kZeroBytes / 16, kZeroPieces = (16 * R * kZeroLanes + kWave - 1) / kWave;
+    static constexpr int kPieces = 16 * R / kTogether, kZeroLanes = kZeroBytes / 16, kZeroPieces = (16 * R * kZeroLanes + kWave - 1) / kWave;
     u32x4_t s[kPieces], z[kZeroPieces];
 
     // a row's bytes, the block's first byte of the wavefront's first row, and how far a piece may begin from there
@@ -394,10 +393,10 @@ struct GroupBlocks {
     // row, rows: the wavefront's first row and their number; groups: of a row
     __device__ __forceinline__ void fetch(const W4Args &a, int64_t row, int rows, int groups, int block, int lane)
     {
-        const Place p = place(a.scales, a.V, row, groups * kBytes, (int64_t)block * 128);
+        const Place p = place(a.scales, a.V, row, groups * kBytes, (int64_t)block * kBlock);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
-            s[i] = load_piece(p.from + min(lane_at(i * 8 + lane / 8, rows, groups * kBytes, lane % 8 * 16), p.last));
+            s[i] = load_piece(p.from + min(lane_at(i * kTogether + lane / kLanes, rows, groups * kBytes, lane % kLanes * 16), p.last));
         if constexpr (ZEROS) {
             const Place zp = place(a.zeros, a.V, row, groups, (int64_t)block * kZeroBytes);
 #pragma unroll
@@ -409,18 +408,18 @@ struct GroupBlocks {
     __device__ __forceinline__ void store(const W4Args &a, char *lds, int64_t row, int rows, int groups, int block, int lane)
     {
         const int row_bytes = groups * kBytes;
-        const Place p = place(a.scales, a.V, row, row_bytes, (int64_t)block * 128);
+        const Place p = place(a.scales, a.V, row, row_bytes, (int64_t)block * kBlock);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            u32x4_t v = move_piece(s[i], lane_at(i * 8 + lane / 8, rows, row_bytes, lane % 8 * 16) - p.last);
-            if ((block + 1) * 128 > row_bytes) {  // what lies behind the row's end is another row's: no scale at all here
+            u32x4_t v = move_piece(s[i], lane_at(i * kTogether + lane / kLanes, rows, row_bytes, lane % kLanes * 16) - p.last);
+            if ((block + 1) * kBlock > row_bytes) {  // what lies behind the row's end is another row's: no scale at all here
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int left = row_bytes - (block * 128 + lane % 8 * 16 + 4 * k);
+                    const int left = row_bytes - (block * kBlock + lane % kLanes * 16 + 4 * k);
                     v[k] = left >= 4 ? v[k] : left == 2 ? v[k] & 0xFFFFu : 0u;
                 }
             }
-            *reinterpret_cast<u32x4_t *>(lds + (i * 8 + lane / 8) * kStride + lane % 8 * 16) = v;
+            lds_put(lds + (i * kTogether + lane / kLanes) * kStride + lane % kLanes * 16, v);
         }
         if constexpr (ZEROS) {
             const Place zp = place(a.zeros, a.V, row, groups, (int64_t)block * kZeroBytes);
@@ -428,7 +427,7 @@ struct GroupBlocks {
             for (int i = 0; i < kZeroPieces; ++i) {
                 const int r = i * (kWave / kZeroLanes) + lane / kZeroLanes;
                 const u32x4_t v = move_piece(z[i], lane_at(r, rows, groups, lane % kZeroLanes * 16) - zp.last);
-                if (r < 16 * R) *reinterpret_cast<u32x4_t *>(lds + 32 * kStride + r * kZeroStride + lane % kZeroLanes * 16) = v;
+                if (r < 16 * R) lds_put(lds + 32 * kStride + r * kZeroStride + lane % kZeroLanes * 16, v);
             }
         }
     }
@@ -438,18 +437,18 @@ struct GroupBlocks {
         const char *p = lds + r * kStride + u * (S * kBytes);
         if constexpr (SCALE_F32) {
             typedef float v_t __attribute__((ext_vector_type(S > 1 ? S : 2)));
-            if constexpr (S == 1) out[0] = *reinterpret_cast<const float *>(p);
+            if constexpr (S == 1) out[0] = lds_get<float>(p);
             else {
-                const v_t v = *reinterpret_cast<const v_t *>(p);
+                const v_t v = lds_get<v_t>(p);
 #pragma unroll
                 for (int g = 0; g < S; ++g) out[g] = v[g];
             }
         } else {
             uint32_t w[(S + 1) / 2];
-            if constexpr (S == 1) w[0] = *reinterpret_cast<const uint16_t *>(p);
+            if constexpr (S == 1) w[0] = lds_get<uint16_t>(p);
             else
 #pragma unroll
-                for (int k = 0; k < S / 2; ++k) w[k] = reinterpret_cast<const uint32_t *>(p)[k];
+                for (int k = 0; k < S / 2; ++k) w[k] = lds_get<uint32_t>(p + 4 * k);
 #pragma unroll
             for (int g = 0; g < S; ++g) out[g] = __uint_as_float(g & 1 ? w[g / 2] & 0xFFFF0000u : w[g / 2] << 16);
         }
@@ -458,14 +457,18 @@ struct GroupBlocks {
     __device__ __forceinline__ static float excess(const char *lds, int r, int u, int g)
     {
         const int at = u * S + min(g, S - 1);
-        const float s = load_elem<std::conditional_t<SCALE_F32, F32, Bf16>>(lds + r * kStride, at);
-        const float z = (float)*reinterpret_cast<const uint8_t *>(lds + 32 * kStride + r * kZeroStride + at);
+        const char *p = lds + r * kStride + at * kBytes;
+        float s;
+        if constexpr (SCALE_F32) s = lds_get<float>(p);
+        else s = bf16_bits_to_float(lds_get<uint16_t>(p));
+        const float z = (float)lds_get<uint8_t>(lds + 32 * kStride + r * kZeroStride + at);
         return S == 4 || g < S ? s * (16.0f + z) : 0.0f;
     }
 };
 
-// Eight wavefronts of 16 R rows each, tile after tile.  Two units a chunk: chunk c is multiplied from LDS while chunk c + 1 of the
-// hidden values and chunks c + 1 and c + 2 of the codes arrive in registers, the next tile's among them.
+// Eight wavefronts of 16 R rows each, tile after tile.  Two units a chunk: chunk c is multiplied from LDS while chunks c + 1 and
+// c + 2 of the hidden values arrive in LDS (direct loads) and of the codes in registers, the next tile's among them.  What is
+// waited for before a barrier is counted by hand: everything but the operations issued behind the next chunk's direct loads.
 // With zero points the excess leaves by a matrix instruction of its own (fp32 operands: a group's sum times scale (16 + zero)):
 // as a start value of each group's accumulators it took as many instructions as the scales themselves.
 template <int MT, int R, int GROUP, bool ZEROS, bool SCALE_F32>
@@ -473,7 +476,8 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
                                              char *own)
 {
     constexpr int UC = 2, S = 128 / GROUP, BLOCKS = GROUP / 32, kChunk = UC * unit_bytes(MT), kRows = 8 * 16 * R;
-    constexpr int kCopies = (kChunk + 8191) / 8192;
+    constexpr int kCopies = (kChunk + 8191) / 8192;                 // direct loads of 1 KiB a wavefront and chunk
+    constexpr int kBehind = UC * R + kCopies + UC * R;              // operations behind the next chunk's
     using Groups = GroupBlocks<R, GROUP, ZEROS, SCALE_F32>;
     constexpr int kPerBlock = Groups::kUnits / UC;  // chunks of a block of scales
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -513,20 +517,19 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
             to.w[2 * r + 1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(codes + (b_lane[r] + at)));
         }
         advance(wi, wc);
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    u32x4_t xr[kCopies];
-    const int x_lane = threadIdx.x * 16;
-    auto fetch_x = [&]() {
+    const __amdgpu_buffer_rsrc_t x_buffer = dma_buffer(x, (uint32_t)(units * unit_bytes(MT)));
+    auto fetch_x = [&](int to) {
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i)
-            xr[i] = *reinterpret_cast<const u32x4_t *>(x + (int64_t)xc * kChunk + min(i * 8192 + x_lane, kChunk - 16));
+        for (int i = 0; i < kCopies; ++i) {
+            const int at = min(i * 8192 + wave * 1024, kChunk - 1024);  // (the last piece overlaps: the same bytes again)
+            dma16(x_buffer, lane * 16, (uint32_t)(xc * kChunk + at), xs + to * kChunk + at);
+        }
         xc = xc + 1 == chunks ? 0 : xc + 1;
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-    };
-    auto store_x = [&](int half) {
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) *reinterpret_cast<u32x4_t *>(xs + half * kChunk + min(i * 8192 + x_lane, kChunk - 16)) = xr[i];
     };
     // blocks of scales: the one in registers
     Groups next;
@@ -547,7 +550,7 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
 #pragma unroll
             for (int m = 0; m < MT; ++m) acc[r][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     };
-    auto multiply = [&](int half, int in_block, const Chunk &from) {
+    auto multiply = [&](int which, int in_block, const Chunk &from) {
         uint32_t d[R][UC][4];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -559,7 +562,7 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
         }
 #pragma unroll
         for (int i = 0; i < UC; ++i) {
-            const char *unit = xs + half * kChunk + i * unit_bytes(MT);
+            const char *unit = xs + which * kChunk + i * unit_bytes(MT);
             const float *sums = reinterpret_cast<const float *>(unit + 4096 * MT);
             float scale[R][S];
 #pragma unroll
@@ -573,7 +576,7 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
                 for (int r = 0; r < R; ++r) excess[r] = Groups::excess(own, r * 16 + n16, in_block * UC + i, q);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    const float e = sums[q * (16 * MT) + m * 16 + n16];
+                    const float e = lds_get<float>(sums + q * (16 * MT) + m * 16 + n16);
 #pragma unroll
                     for (int r = 0; r < R; ++r) acc[r][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(e, excess[r], acc[r][m], 0, 0, 0);
                 }
@@ -585,21 +588,23 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
 #pragma unroll
                 for (int r = 0; r < R; ++r) wide[r] = widen(d[r][i][g], mask, sixteen);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const bf16x8_t xv = *reinterpret_cast<const bf16x8_t *>(unit + ((g * MT + m) * kWave + lane) * 16);
-                    f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if (!ZEROS && g % BLOCKS == 0)
-                        start = *reinterpret_cast<const f32x4_t *>(sums + (g / BLOCKS) * (16 * MT) + m * 16 + q * 4);
+                for (int m0 = 0; m0 < MT; m0 += 2) {
 #pragma unroll
-                    for (int r = 0; r < R; ++r)
-                        part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wide[r], g % BLOCKS == 0 ? start : part[r][m], 0, 0, 0);
+                    for (int m = m0; m < (m0 + 2 < MT ? m0 + 2 : MT); ++m) {
+                        const bf16x8_t xv = lds_get<bf16x8_t>(unit + ((g * MT + m) * kWave + lane) * 16);
+                        f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
+                        if (!ZEROS && g % BLOCKS == 0) start = lds_get<f32x4_t>(sums + (g / BLOCKS) * (16 * MT) + m * 16 + q * 4);
+#pragma unroll
+                        for (int r = 0; r < R; ++r)
+                            part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wide[r], g % BLOCKS == 0 ? start : part[r][m], 0, 0, 0);
+                    }
+                    // (behind the products of 32 tokens: a sum that is read at once holds the wavefront up for its whole length)
+                    if (g % BLOCKS == BLOCKS - 1)
+#pragma unroll
+                        for (int m = m0; m < (m0 + 2 < MT ? m0 + 2 : MT); ++m)
+#pragma unroll
+                            for (int r = 0; r < R; ++r) acc[r][m] += part[r][m] * scale[r][g / BLOCKS];
                 }
-                // (behind the products of all tokens: a sum that is read at once holds the wavefront up for its whole length)
-                if (g % BLOCKS == BLOCKS - 1)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m)
-#pragma unroll
-                        for (int r = 0; r < R; ++r) acc[r][m] += part[r][m] * scale[r][g / BLOCKS];
             }
         }
     };
@@ -622,18 +627,22 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
         }
     };
 
-    int tile = 0, c = 0, in_block = 0, half = 0;
+    int tile = 0, c = 0, in_block = 0;
     const int64_t total = (int64_t)mine * chunks;
-    auto one = [&](const Chunk &now, Chunk &ahead) {
+    auto meet_next = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(waitcnt_imm(kBehind, 0));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto one = [&](int which, const Chunk &now, Chunk &ahead) {
         if (in_block == 0) {
             store_groups();
             fetch_groups();
         }
-        fetch_x();
+        fetch_x((which + 2) % 3);
         fetch_w(ahead);
-        multiply(half, in_block, now);
-        half ^= 1;
-        store_x(half);
+        multiply(which, in_block, now);
         if (++in_block == kPerBlock) in_block = 0;
         if (++c == chunks) {
             put_out(tile);
@@ -641,25 +650,26 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
             ++tile;
             c = in_block = 0;
         }
-        meet();
+        meet_next();
     };
     Chunk k0, k1, k2;
+    meet();  // (the tiles before these are read)
     fetch_groups();
-    fetch_x();
+    fetch_x(0);
     fetch_w(k0);
+    fetch_x(1);
     fetch_w(k1);
     clear();
-    meet();  // (the tiles before these are read)
-    store_x(0);
-    meet();
+    meet_next();
     for (int64_t s = 0;;) {
-        one(k0, k2);
+        one(0, k0, k2);
         if (++s >= total) break;
-        one(k1, k0);
+        one(1, k1, k0);
         if (++s >= total) break;
-        one(k2, k1);
+        one(2, k2, k1);
         if (++s >= total) break;
     }
+    __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));  // (nothing may arrive in LDS that the next tiles, or workgroup, use)
 }
 
 // Tiles of 256 rows first, then a last round of 128 rows where no more are left for it: a compute unit is done with those in
@@ -669,7 +679,7 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4Args a, const char *or
 {
     constexpr int kOwn = GroupBlocks<2, GROUP, ZEROS, SCALE_F32>::kLds;
     extern __shared__ __align__(16) char lds[];
-    char *own = lds + 4 * unit_bytes(MT) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kOwn;
+    char *own = lds + 6 * unit_bytes(MT) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kOwn;
     const char *x = ordered + (int64_t)blockIdx.y * units * unit_bytes(MT);
     const int64_t t0 = (int64_t)blockIdx.y * (16 * MT);
     stream_tiles<MT, 2, GROUP, ZEROS, SCALE_F32>(a, x, units, 0, wide_tiles, t0, lds, own);
@@ -701,7 +711,7 @@ hipError_t launch_stream(W4Args a, void *workspace, int cus, hipStream_t s)
         a.zeros = spare + kW4ShortBytes;
     }
     const W4Tiles p = w4_tiles(a.V, cus);
-    const int lds = 4 * unit_bytes(MT) + 8 * GroupBlocks<2, GROUP, ZEROS, SCALE_F32>::kLds;
+    const int lds = 6 * unit_bytes(MT) + 8 * GroupBlocks<2, GROUP, ZEROS, SCALE_F32>::kLds;
     kernel<<<dim3((unsigned)p.blocks, passes), dim3(512), lds, s>>>(a, ordered, units, p.wide, p.narrow);
     return hipGetLastError();
 }
