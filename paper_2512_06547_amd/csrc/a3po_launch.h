@@ -571,7 +571,7 @@ inline size_t w4_workspace_bytes(int64_t T, int64_t H)
 {
     if (T <= 0 || H <= 0 || (T <= 16 && H % 128 == 0 && H >= 256 && H <= 4096)) return 0;
     const int64_t tokens = T <= 16 ? 16 : T <= 32 ? 32 : (T + 63) / 64 * 64;
-    return (size_t)(tokens / 16) * (size_t)((H + 255) / 256 * 2) * kW4UnitBytes + 2 * kW4ShortBytes;
+    return (size_t)(tokens / 16) * (size_t)((H + 511) / 512 * 4) * kW4UnitBytes + 2 * kW4ShortBytes;
 }
 hipError_t launch_w4_linear(const W4Args &a, void *workspace, hipStream_t s);
 

@@ -296,8 +296,8 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
 //
 // A first kernel writes the hidden values in the order of the matrix instructions, with the sums of each group, so that the
 // second copies them to LDS as they are: [pass of 16 MT tokens][unit][4 blocks of codes][MT][64 lanes] 16 bytes, then
-// [4 groups][16 MT] sums.  Units are even in number: one beyond the row holds zeros (a branch around it would cost the wait that
-// loads are kept out of branches for).
+// [4 groups][16 MT] sums.  Units are a multiple of four, those beyond the row hold zeros (a branch around them would cost the wait
+// that loads are kept out of branches for).
 
 constexpr int unit_bytes(int mt) { return kW4UnitBytes * mt; }
 
@@ -480,6 +480,7 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
     constexpr int kBehind = UC * R + kCopies + UC * R;              // operations behind the next chunk's
     using Groups = GroupBlocks<R, GROUP, ZEROS, SCALE_F32>;
     constexpr int kPerBlock = Groups::kUnits / UC;  // chunks of a block of scales
+    static_assert(kPerBlock % 2 == 0, "chunks go in pairs");
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int n16 = lane & 15, q = lane >> 4, step = (int)gridDim.x;
     const int chunks = units / UC, groups = a.H / GROUP, row_bytes = a.H / 2;
@@ -550,8 +551,8 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
 #pragma unroll
             for (int m = 0; m < MT; ++m) acc[r][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     };
-    auto multiply = [&](int which, int in_block, const Chunk &from) {
-        uint32_t d[R][UC][4];
+    // (a chunk's registers are free for the next but one as soon as its lanes are sorted)
+    auto sort = [&](const Chunk &from, uint32_t (&d)[R][UC][4]) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -560,6 +561,10 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
                 for (int k = 0; k < 4; ++k) d[r][i][k] = from.w[2 * r + i][k];
             sort_units(d[r][0], d[r][1]);
         }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](int which, int in_block, uint32_t (&d)[R][UC][4]) {
 #pragma unroll
         for (int i = 0; i < UC; ++i) {
             const char *unit = xs + which * kChunk + i * unit_bytes(MT);
@@ -588,23 +593,20 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
 #pragma unroll
                 for (int r = 0; r < R; ++r) wide[r] = widen(d[r][i][g], mask, sixteen);
 #pragma unroll
-                for (int m0 = 0; m0 < MT; m0 += 2) {
+                for (int m = 0; m < MT; ++m) {
+                    const bf16x8_t xv = lds_get<bf16x8_t>(unit + ((g * MT + m) * kWave + lane) * 16);
+                    f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (!ZEROS && g % BLOCKS == 0) start = lds_get<f32x4_t>(sums + (g / BLOCKS) * (16 * MT) + m * 16 + q * 4);
 #pragma unroll
-                    for (int m = m0; m < (m0 + 2 < MT ? m0 + 2 : MT); ++m) {
-                        const bf16x8_t xv = lds_get<bf16x8_t>(unit + ((g * MT + m) * kWave + lane) * 16);
-                        f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
-                        if (!ZEROS && g % BLOCKS == 0) start = lds_get<f32x4_t>(sums + (g / BLOCKS) * (16 * MT) + m * 16 + q * 4);
-#pragma unroll
-                        for (int r = 0; r < R; ++r)
-                            part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wide[r], g % BLOCKS == 0 ? start : part[r][m], 0, 0, 0);
-                    }
-                    // (behind the products of 32 tokens: a sum that is read at once holds the wavefront up for its whole length)
-                    if (g % BLOCKS == BLOCKS - 1)
-#pragma unroll
-                        for (int m = m0; m < (m0 + 2 < MT ? m0 + 2 : MT); ++m)
-#pragma unroll
-                            for (int r = 0; r < R; ++r) acc[r][m] += part[r][m] * scale[r][g / BLOCKS];
+                    for (int r = 0; r < R; ++r)
+                        part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wide[r], g % BLOCKS == 0 ? start : part[r][m], 0, 0, 0);
                 }
+                // (behind the products of all tokens: a sum that is read at once holds the wavefront up for its whole length)
+                if (g % BLOCKS == BLOCKS - 1)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) acc[r][m] += part[r][m] * scale[r][g / BLOCKS];
             }
         }
     };
@@ -635,24 +637,18 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    auto one = [&](int which, const Chunk &now, Chunk &ahead) {
-        if (in_block == 0) {
-            store_groups();
-            fetch_groups();
-        }
-        fetch_x((which + 2) % 3);
-        fetch_w(ahead);
-        multiply(which, in_block, now);
-        if (++in_block == kPerBlock) in_block = 0;
-        if (++c == chunks) {
-            put_out(tile);
-            clear();
-            ++tile;
-            c = in_block = 0;
-        }
-        meet_next();
+    int which = 0;  // the third of the hidden values' LDS that is multiplied
+    auto one = [&](Chunk &now) {
+        uint32_t d[R][UC][4];
+        sort(now, d);
+        fetch_x(which == 0 ? 2 : which - 1);
+        fetch_w(now);
+        multiply(which, in_block, d);
+        which = which == 2 ? 0 : which + 1;
+        ++in_block;
+        ++c;
     };
-    Chunk k0, k1, k2;
+    Chunk k0, k1;
     meet();  // (the tiles before these are read)
     fetch_groups();
     fetch_x(0);
@@ -661,13 +657,22 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
     fetch_w(k1);
     clear();
     meet_next();
-    for (int64_t s = 0;;) {
-        one(0, k0, k2);
-        if (++s >= total) break;
-        one(1, k1, k0);
-        if (++s >= total) break;
-        one(2, k2, k1);
-        if (++s >= total) break;
+    for (int64_t s = 0; s < total; s += 2) {
+        if (in_block == 0) {
+            store_groups();
+            fetch_groups();
+        }
+        one(k0);
+        meet_next();
+        one(k1);
+        if (in_block == kPerBlock) in_block = 0;
+        if (c == chunks) {
+            put_out(tile);
+            clear();
+            ++tile;
+            c = in_block = 0;
+        }
+        meet_next();
     }
     __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));  // (nothing may arrive in LDS that the next tiles, or workgroup, use)
 }
@@ -692,7 +697,7 @@ hipError_t launch_stream(W4Args a, void *workspace, int cus, hipStream_t s)
     static LdsLimitState lds_limit;
     auto *kernel = w4_stream_kernel<MT, GROUP, ZEROS, SCALE_F32>;
     if (const hipError_t e = ensure_lds_limit(reinterpret_cast<const void *>(kernel), kW4MaxLds, lds_limit)) return e;
-    const int units = (a.H + 255) / 256 * 2;
+    const int units = (a.H + 511) / 512 * 4;
     const unsigned passes = (unsigned)((a.T + 16 * MT - 1) / (16 * MT));
     char *ordered = static_cast<char *>(workspace);
     w4_order_kernel<MT><<<dim3(units, passes), dim3(256), 0, s>>>(a, ordered, units, ZEROS);
