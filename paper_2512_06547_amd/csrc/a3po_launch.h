@@ -410,26 +410,30 @@ struct NormArgs {
 
 constexpr int kNormMaxH = A3PO_NORM_MAX_H;
 
-// Lanes that share a row and the 16-byte vectors of x that each holds.  A wavefront alone needs no barrier; beyond what its
-// registers hold (the backward pass also keeps its sums there) four share a row, then sixteen.
+// Lanes that share a row and the 16-byte vectors of x that each holds.  A wavefront alone needs no barrier, four have a quarter
+// of the registers and of the latency each: one where it holds the row with registers to spare for other wavefronts, four for
+// longer rows and where rows are fewer than compute units, eight beyond those.  One / four, us: backward of 20,000 rows bf16 x
+// 1,024 26 / 53, x 2,048 47 / 62, fp32 x 1,024 37 / 55, x 1,536 65 / 64, x 2,048 78 / 73, of 64 x 1,536 bf16 5.7 / 4.0; forward
+// of 20,000 bf16 x 700 15 / 20, x 1,536 22 / 21, x 2,048 42 / 35, fp32 x 1,024 21 / 23, x 1,536 46 / 46, x 2,048 49 / 47, of
+// 64 x 1,536 bf16 4.3 / 3.5.
 struct NormPlan {
     int lanes, vectors;
 };
-inline NormPlan norm_plan(int64_t H, int x_bytes, bool backward)
+constexpr int64_t kNormFewRows = 256;
+inline NormPlan norm_plan(int64_t T, int64_t H, int x_bytes, bool backward)
 {
     const int64_t full = H / (16 / x_bytes);
-    const int most = !backward || x_bytes == 4 ? 8 : 4;
+    const int most = x_bytes == 4 ? 6 : backward ? 4 : 3;
     auto up = [](int64_t a, int64_t b) { return (int)((a + b - 1) / b); };
     NormPlan p;
-    if (full <= 64 * most) {
+    if (full <= 64 || (full <= 64 * most && T > kNormFewRows)) {
         const int v = up(full, 64);
-        p = {64, v <= 4 ? (v > 1 ? v : 1) : v <= 6 ? 6 : 8};
-    } else if (full <= 1024) {
-        const int v = up(full, 256);
-        p = {256, v > 2 ? v : 2};
+        p = {64, v <= 4 ? (v > 1 ? v : 1) : 6};
+    } else if (full <= 256 * 4) {
+        p = {256, up(full, 256)};
     } else {
-        const int v = up(full, 1024);
-        p = {1024, v <= 2 ? 2 : 4};
+        const int v = up(full, 512);
+        p = {512, x_bytes == 4 ? (v <= 4 ? 4 : v <= 6 ? 6 : 8) : v <= 3 ? 3 : 4};
     }
     return p;
 }
@@ -437,7 +441,7 @@ inline NormPlan norm_plan(int64_t H, int x_bytes, bool backward)
 constexpr int kNormMaxBlocks = 512;
 inline int64_t norm_bwd_blocks(int64_t T, int64_t H, int x_bytes)
 {
-    const NormPlan p = norm_plan(H, x_bytes, true);
+    const NormPlan p = norm_plan(T, H, x_bytes, true);
     const int64_t rows = p.lanes >= 256 ? 1 : 256 / p.lanes, want = (T + rows - 1) / rows;
     return want < kNormMaxBlocks ? want : kNormMaxBlocks;
 }

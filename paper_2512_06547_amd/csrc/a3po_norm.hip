@@ -21,7 +21,7 @@ template <typename XT>
 constexpr int kVec = 16 / XT::kBytes;
 
 // EPV consecutive elements of type DT, widened
-template <typename DT, int EPV>
+template <typename DT, int EPV, bool STREAM = false>
 __device__ __forceinline__ void load_vec(const char *p, float *f)
 {
     constexpr int kWords = EPV * DT::kBytes / 4;
@@ -29,7 +29,9 @@ __device__ __forceinline__ void load_vec(const char *p, float *f)
     constexpr int kPer = kWords < 4 ? kWords : 4;
 #pragma unroll
     for (int k = 0; k < kWords; k += kPer) {
-        const words_t w = *reinterpret_cast<const words_t *>(p + 4 * k);
+        words_t w;
+        if constexpr (STREAM) w = __builtin_nontemporal_load(reinterpret_cast<const words_t *>(p + 4 * k));
+        else w = *reinterpret_cast<const words_t *>(p + 4 * k);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             if constexpr (DT::kBytes == 4) {
@@ -42,7 +44,7 @@ __device__ __forceinline__ void load_vec(const char *p, float *f)
     }
 }
 
-template <typename DT, int EPV>
+template <typename DT, int EPV, bool STREAM = false>
 __device__ __forceinline__ void store_vec(char *p, const float *f)
 {
     constexpr int kWords = EPV * DT::kBytes / 4;
@@ -56,7 +58,8 @@ __device__ __forceinline__ void store_vec(char *p, const float *f)
             if constexpr (DT::kBytes == 4) w[j] = __float_as_uint(f[k + j]);
             else w[j] = pack_bf16x2(f[2 * (k + j)], f[2 * (k + j) + 1]);
         }
-        *reinterpret_cast<words_t *>(p + 4 * k) = w;
+        if constexpr (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<words_t *>(p + 4 * k));
+        else *reinterpret_cast<words_t *>(p + 4 * k) = w;
     }
 }
 
@@ -105,28 +108,42 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[2 * (LANES /
     }
 }
 
+// Vectors beyond the row's last whole one read that one again and count for nothing: with a branch around each vector's load
+// its use waits for it alone, one after the other.  (Rows shorter than a vector have none.)
 template <typename XT, typename YT, int LANES, int NV, bool CENTER>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(NormArgs a)
 {
     constexpr int EPV = kVec<XT>, kRows = LANES >= 256 ? 1 : 256 / LANES;
     __shared__ float red[2][2 * (LANES / kWave)];
     int phase = 0;
-    const int lane = threadIdx.x % LANES, full = a.H / EPV, rest = a.H - full * EPV;
+    const int lane = threadIdx.x % LANES, full = a.H / EPV, rest = a.H - full * EPV, e_last = full * EPV + lane;
     const float inv_h = 1.0f / (float)a.H;
     const bool last = lane < rest;
+    float w[NV][EPV], b[CENTER ? NV : 1][EPV], w_last = 0.0f, b_last = 0.0f;
+    if (full)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int64_t e = (int64_t)min(i * LANES + lane, full - 1) * EPV;
+            load_param<EPV>(a.weight, a.param_f32, e, 1.0f, w[i]);
+            if constexpr (CENTER) load_param<EPV>(a.bias, a.param_f32, e, 0.0f, b[i]);
+        }
+    if (last) {
+        w_last = load_param(a.weight, a.param_f32, e_last, 1.0f);
+        b_last = load_param(a.bias, a.param_f32, e_last, 0.0f);
+    }
     const int64_t stride = (int64_t)gridDim.x * kRows;
     for (int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; t < a.T; t += stride) {
         const char *row = static_cast<const char *>(a.x) + t * a.ldx * XT::kBytes;
         char *out = static_cast<char *>(a.y) + t * a.ldy * YT::kBytes;
         float f[NV][EPV], extra = 0.0f;
+        if (full)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = i * LANES + lane;
+            for (int i = 0; i < NV; ++i) load_vec<XT, EPV>(row + min(i * LANES + lane, full - 1) * EPV * XT::kBytes, f[i]);
+        if (last) extra = load_elem<XT>(row, e_last);
 #pragma unroll
-            for (int k = 0; k < EPV; ++k) f[i][k] = 0.0f;
-            if (v < full) load_vec<XT, EPV>(row + (int64_t)v * EPV * XT::kBytes, f[i]);
-        }
-        if (last) extra = load_elem<XT>(row, full * EPV + lane);
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < EPV; ++k) f[i][k] = i * LANES + lane < full ? f[i][k] : 0.0f;
         float mean = 0.0f;
         if constexpr (CENTER) {
             float sum[1] = {extra};
@@ -143,7 +160,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(Nor
             const bool on = i * LANES + lane < full;
 #pragma unroll
             for (int k = 0; k < EPV; ++k) {
-                f[i][k] = on ? f[i][k] - mean : 0.0f;
+                if constexpr (CENTER) f[i][k] = on ? f[i][k] - mean : 0.0f;
                 sq[0] = fmaf(f[i][k], f[i][k], sq[0]);
             }
         }
@@ -153,19 +170,12 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(Nor
         for (int i = 0; i < NV; ++i) {
             const int v = i * LANES + lane;
             if (v < full) {
-                float w[EPV], b[EPV];
-                load_param<EPV>(a.weight, a.param_f32, (int64_t)v * EPV, 1.0f, w);
-                load_param<EPV>(a.bias, a.param_f32, (int64_t)v * EPV, 0.0f, b);
 #pragma unroll
-                for (int k = 0; k < EPV; ++k) f[i][k] = fmaf(f[i][k] * rstd, w[k], b[k]);
-                store_vec<YT, EPV>(out + (int64_t)v * EPV * YT::kBytes, f[i]);
+                for (int k = 0; k < EPV; ++k) f[i][k] = fmaf(f[i][k] * rstd, w[i][k], CENTER ? b[i][k] : 0.0f);
+                store_vec<YT, EPV>(out + v * EPV * YT::kBytes, f[i]);
             }
         }
-        if (last) {
-            const int e = full * EPV + lane;
-            store_elem<YT>(out, e, fmaf((extra - mean) * rstd, load_param(a.weight, a.param_f32, e, 1.0f),
-                                        load_param(a.bias, a.param_f32, e, 0.0f)));
-        }
+        if (last) store_elem<YT>(out, e_last, fmaf((extra - mean) * rstd, w_last, b_last));
         if (lane == 0) {
             if (a.mean) a.mean[t] = mean;
             if (a.rstd) a.rstd[t] = rstd;
@@ -182,10 +192,15 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(Nor
     __shared__ float red[2][2 * (LANES / kWave)];
     int phase = 0;
     const int lane = threadIdx.x % LANES, full = a.H / EPV, rest = a.H - full * EPV, group = threadIdx.x / LANES;
+    const int e_last = full * EPV + lane;
     const float inv_h = 1.0f / (float)a.H;
     const bool last = lane < rest;
-    const float w_extra = last ? load_param(a.weight, a.param_f32, full * EPV + lane, 1.0f) : 0.0f;
-    float dw[NV][EPV], db[NV][EPV], dw_extra = 0.0f, db_extra = 0.0f;
+    float w[NV][EPV], dw[NV][EPV], db[NV][EPV], w_last = 0.0f, dw_last = 0.0f, db_last = 0.0f;
+    if (full)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            load_param<EPV>(a.weight, a.param_f32, (int64_t)min(i * LANES + lane, full - 1) * EPV, 1.0f, w[i]);
+    if (last) w_last = load_param(a.weight, a.param_f32, e_last, 1.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -195,47 +210,41 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(Nor
         const char *row = static_cast<const char *>(a.x) + t * a.ldx * XT::kBytes;
         const char *grow = static_cast<const char *>(a.dy) + t * a.ldy * YT::kBytes;
         char *out = static_cast<char *>(a.dx) + t * a.lddx * XT::kBytes;
-        float x[NV][EPV], g[NV][EPV], x_extra = 0.0f, g_extra = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = i * LANES + lane;
-#pragma unroll
-            for (int k = 0; k < EPV; ++k) x[i][k] = g[i][k] = 0.0f;
-            if (v < full) {
-                load_vec<XT, EPV>(row + (int64_t)v * EPV * XT::kBytes, x[i]);
-                load_vec<YT, EPV>(grow + (int64_t)v * EPV * YT::kBytes, g[i]);
-            }
-        }
-        if (last) {
-            x_extra = load_elem<XT>(row, full * EPV + lane);
-            g_extra = load_elem<YT>(grow, full * EPV + lane);
-        }
         const float rstd = a.rstd[t], mean = CENTER ? a.mean[t] : 0.0f;
+        float x[NV][EPV], g[NV][EPV], x_last = 0.0f, g_last = 0.0f;
+        if (full)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = min(i * LANES + lane, full - 1);
+                load_vec<XT, EPV, true>(row + v * EPV * XT::kBytes, x[i]);
+                load_vec<YT, EPV, true>(grow + v * EPV * YT::kBytes, g[i]);
+            }
+        if (last) {
+            x_last = load_elem<XT>(row, e_last);
+            g_last = load_elem<YT>(grow, e_last);
+        }
         float s[2] = {0.0f, 0.0f};  // sums of g xhat and of g
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = i * LANES + lane;
-            if (v < full) {
-                float w[EPV];
-                load_param<EPV>(a.weight, a.param_f32, (int64_t)v * EPV, 1.0f, w);
+            const bool on = i * LANES + lane < full;
 #pragma unroll
-                for (int k = 0; k < EPV; ++k) {
-                    x[i][k] = (x[i][k] - mean) * rstd;
-                    dw[i][k] = fmaf(g[i][k], x[i][k], dw[i][k]);
-                    if constexpr (CENTER) db[i][k] += g[i][k];
-                    g[i][k] *= w[k];
-                    s[0] = fmaf(g[i][k], x[i][k], s[0]);
-                    if constexpr (CENTER) s[1] += g[i][k];
-                }
+            for (int k = 0; k < EPV; ++k) {
+                x[i][k] = on ? (CENTER ? x[i][k] - mean : x[i][k]) * rstd : 0.0f;
+                g[i][k] = on ? g[i][k] : 0.0f;
+                dw[i][k] = fmaf(g[i][k], x[i][k], dw[i][k]);
+                if constexpr (CENTER) db[i][k] += g[i][k];
+                g[i][k] = on ? g[i][k] * w[i][k] : 0.0f;
+                s[0] = fmaf(g[i][k], x[i][k], s[0]);
+                if constexpr (CENTER) s[1] += g[i][k];
             }
         }
         if (last) {
-            x_extra = (x_extra - mean) * rstd;
-            dw_extra = fmaf(g_extra, x_extra, dw_extra);
-            if constexpr (CENTER) db_extra += g_extra;
-            g_extra *= w_extra;
-            s[0] = fmaf(g_extra, x_extra, s[0]);
-            if constexpr (CENTER) s[1] += g_extra;
+            x_last = (x_last - mean) * rstd;
+            dw_last = fmaf(g_last, x_last, dw_last);
+            if constexpr (CENTER) db_last += g_last;
+            g_last *= w_last;
+            s[0] = fmaf(g_last, x_last, s[0]);
+            if constexpr (CENTER) s[1] += g_last;
         }
         row_sum<LANES, 2>(s, red, phase);
         const float along = s[0] * inv_h, level = CENTER ? s[1] * inv_h : 0.0f;
@@ -245,35 +254,47 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(Nor
             if (v < full) {
 #pragma unroll
                 for (int k = 0; k < EPV; ++k) g[i][k] = rstd * (g[i][k] - level - x[i][k] * along);
-                store_vec<XT, EPV>(out + (int64_t)v * EPV * XT::kBytes, g[i]);
+                store_vec<XT, EPV, true>(out + v * EPV * XT::kBytes, g[i]);
             }
         }
-        if (last) store_elem<XT>(out, full * EPV + lane, rstd * (g_extra - level - x_extra * along));
+        if (last) store_elem<XT>(out, e_last, rstd * (g_last - level - x_last * along));
     }
     if (!partials) return;
     // the groups of lanes of this workgroup add their sums, one group after the other
-    extern __shared__ float sums[];  // [dw | db][H], kRows > 1 only
+    extern __shared__ __align__(16) float sums[];  // [dw | db][H rounded up to vectors], kRows > 1 only
     float *mine = partials + (int64_t)blockIdx.x * a.partial_rows * a.H;
+    const int half = (a.H + 3) / 4 * 4;
     for (int r = 0; r < kRows; ++r) {
         if (r > 0) __syncthreads();
-        if (group == r) {
-            auto add = [&](int e, float p, float q) {
-                if (r > 0) {
-                    p += sums[e];
-                    q += sums[a.H + e];
+        if (group != r) continue;
+        const bool first = r == 0, leave = r == kRows - 1;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = i * LANES + lane, e = v * EPV;
+            if (v >= full) continue;
+#pragma unroll
+            for (int k = 0; k < EPV; k += 4) {
+                typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+                f32x4_any p = {dw[i][k], dw[i][k + 1], dw[i][k + 2], dw[i][k + 3]};
+                f32x4_any q = {db[i][k], db[i][k + 1], db[i][k + 2], db[i][k + 3]};
+                if (!first) {
+                    p += *reinterpret_cast<const f32x4_any *>(sums + e + k);
+                    if constexpr (CENTER) q += *reinterpret_cast<const f32x4_any *>(sums + half + e + k);
                 }
-                float *to = r == kRows - 1 ? mine : sums;
-                to[e] = p;
-                if (r < kRows - 1 || a.partial_rows > 1) to[a.H + e] = q;
-            };
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int v = i * LANES + lane;
-                if (v < full)
-#pragma unroll
-                    for (int k = 0; k < EPV; ++k) add(v * EPV + k, dw[i][k], db[i][k]);
+                if (leave) {
+                    *reinterpret_cast<f32x4_any *>(mine + e + k) = p;
+                    if (CENTER && a.partial_rows > 1) *reinterpret_cast<f32x4_any *>(mine + a.H + e + k) = q;
+                } else {
+                    *reinterpret_cast<f32x4_any *>(sums + e + k) = p;
+                    if constexpr (CENTER) *reinterpret_cast<f32x4_any *>(sums + half + e + k) = q;
+                }
             }
-            if (last) add(full * EPV + lane, dw_extra, db_extra);
+        }
+        if (last) {
+            const float p = dw_last + (first ? 0.0f : sums[e_last]), q = db_last + (first ? 0.0f : sums[half + e_last]);
+            (leave ? mine : sums)[e_last] = p;
+            if (!leave) sums[half + e_last] = q;
+            else if (a.partial_rows > 1) mine[a.H + e_last] = q;
         }
     }
 }
@@ -312,10 +333,10 @@ hipError_t launch(const NormArgs &a, bool backward, float *partials, int64_t blo
     constexpr int kThreads = LANES > 256 ? LANES : 256;
     const dim3 grid((unsigned)blocks), block(kThreads);
     if (backward) {
-        const size_t lds = LANES < 256 && partials ? (size_t)8 * a.H : 0;
+        const size_t lds = LANES < 256 && partials ? (size_t)8 * ((a.H + 3) / 4 * 4) : 0;
         if (a.center) norm_bwd_kernel<XT, YT, LANES, NV, true><<<grid, block, lds, s>>>(a, partials);
         else norm_bwd_kernel<XT, YT, LANES, NV, false><<<grid, block, lds, s>>>(a, partials);
-    } else {
+    } else if constexpr (XT::kBytes == 4 || LANES > 64 || NV < 4) {  // (the plan gives the forward pass no four of bf16)
         if (a.center) norm_fwd_kernel<XT, YT, LANES, NV, true><<<grid, block, 0, s>>>(a);
         else norm_fwd_kernel<XT, YT, LANES, NV, false><<<grid, block, 0, s>>>(a);
     }
@@ -325,7 +346,7 @@ hipError_t launch(const NormArgs &a, bool backward, float *partials, int64_t blo
 template <typename XT, typename YT>
 hipError_t launch_of(const NormArgs &a, bool backward, float *partials, int64_t blocks, hipStream_t s)
 {
-    const NormPlan p = norm_plan(a.H, XT::kBytes, backward);
+    const NormPlan p = norm_plan(a.T, a.H, XT::kBytes, backward);
     // (norm_plan gives no other pair)
 #define A3PO_NORM_CASE(L, N) \
     if (p.lanes == L && p.vectors == N) return launch<XT, YT, L, N>(a, backward, partials, blocks, s)
@@ -333,13 +354,15 @@ hipError_t launch_of(const NormArgs &a, bool backward, float *partials, int64_t 
     A3PO_NORM_CASE(64, 2);
     A3PO_NORM_CASE(64, 3);
     A3PO_NORM_CASE(64, 4);
-    A3PO_NORM_CASE(64, 6);
-    A3PO_NORM_CASE(64, 8);
+    if constexpr (XT::kBytes == 4) A3PO_NORM_CASE(64, 6);
+    A3PO_NORM_CASE(256, 1);
     A3PO_NORM_CASE(256, 2);
     A3PO_NORM_CASE(256, 3);
     A3PO_NORM_CASE(256, 4);
-    A3PO_NORM_CASE(1024, 2);
-    if constexpr (XT::kBytes == 4) A3PO_NORM_CASE(1024, 4);
+    if constexpr (XT::kBytes == 2) A3PO_NORM_CASE(512, 3);
+    A3PO_NORM_CASE(512, 4);
+    if constexpr (XT::kBytes == 4) A3PO_NORM_CASE(512, 6);
+    if constexpr (XT::kBytes == 4) A3PO_NORM_CASE(512, 8);
 #undef A3PO_NORM_CASE
     return hipErrorInvalidValue;
 }
@@ -357,7 +380,7 @@ hipError_t launch_any(const NormArgs &a, bool backward, float *partials, int64_t
 
 hipError_t launch_norm_fwd(const NormArgs &a, hipStream_t s)
 {
-    const NormPlan p = norm_plan(a.H, a.x_dt == A3PO_F32 ? 4 : 2, false);
+    const NormPlan p = norm_plan(a.T, a.H, a.x_dt == A3PO_F32 ? 4 : 2, false);
     const int rows = p.lanes >= 256 ? 1 : 256 / p.lanes;
     const int64_t want = (a.T + rows - 1) / rows, most = 4096;
     return launch_any(a, false, nullptr, want < most ? want : most, s);

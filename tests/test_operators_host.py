@@ -144,20 +144,20 @@ using namespace a3po;
 int main()
 {
     for (int bytes : {2, 4})
-        for (int back = 0; back < 2; ++back)
-            for (int64_t H = 1; H <= kNormMaxH; ++H) {
-                const NormPlan p = norm_plan(H, bytes, back);
-                const int64_t full = H / (16 / bytes), room = (int64_t)p.lanes * p.vectors;
+        for (int64_t T : {1, 3, 5, 256, 257, 511, 513, 4096, 100000})
+            for (int64_t k = 2; k <= 2 * kNormMaxH + 1; ++k) {
+                const int64_t H = k / 2;
+                const bool back = k % 2;
+                const NormPlan p = norm_plan(T, H, bytes, back);
+                const int64_t full = H / (16 / bytes), room = (int64_t)p.lanes * p.vectors, b = norm_bwd_blocks(T, H, bytes);
                 const int v = p.vectors;
                 bool known = false;
-                if (p.lanes == 64) known = v == 1 || v == 2 || v == 3 || v == 4 || v == 6 || v == 8;
-                if (p.lanes == 256) known = v == 2 || v == 3 || v == 4;
-                if (p.lanes == 1024) known = v == 2 || (v == 4 && bytes == 4);
-                if (!known || full > room || (v > 1 && full * 2 <= room - p.lanes)) return std::printf("H %lld\\n", (long long)H), 1;
-                for (int64_t T : {1, 3, 5, 511, 513, 4096, 100000}) {
-                    const int64_t b = norm_bwd_blocks(T, H, bytes);
-                    if (b < 1 || b > T || (size_t)b * 8 * H > norm_bwd_workspace_bytes(T, H)) return std::printf("T %lld\\n", (long long)T), 1;
-                }
+                if (p.lanes == 64) known = v == 1 || v == 2 || v == 3 || (v == 4 && (bytes == 4 || back)) || (v == 6 && bytes == 4);
+                if (p.lanes == 256) known = v >= 1 && v <= 4;
+                if (p.lanes == 512) known = v == 4 || (v == 3 && bytes == 2) || ((v == 6 || v == 8) && bytes == 4);
+                if (!known || full > room || (v > 1 && full * 2 <= room - p.lanes) || b < 1 || b > T ||
+                    (size_t)b * 8 * H > norm_bwd_workspace_bytes(T, H))
+                    return std::printf("T %lld H %lld\\n", (long long)T, (long long)H), 1;
             }
     std::printf("ok\\n");
 }
