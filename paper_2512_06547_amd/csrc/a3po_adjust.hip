@@ -56,18 +56,39 @@ __device__ __forceinline__ RowPolicy row_policy(const AdjustArgs &a, int64_t t)
     return p;
 }
 
+// A part of a row: every 2^shift-th block of 512 entries from the `index`-th on.  (Runs of entries would leave most of a
+// history, which holds the vocabulary's first tokens by far the most often, to the first part.)  Parts number their entries
+// by themselves; `id` is an entry's place in the row.
+struct Part {
+    static constexpr int kBlock = 512;
+    int shift, index;
+    int span;  // entries
+    __device__ __forceinline__ Part(const AdjustArgs &a, int part) : shift(a.parts_shift), index(part)
+    {
+        const int64_t blocks = (a.V + kBlock - 1) / kBlock, mine = (blocks - part + (1 << shift) - 1) >> shift;
+        const bool holds_last = ((blocks - 1) & ((1 << shift) - 1)) == part;
+        span = mine > 0 ? (int)(mine * kBlock - (holds_last ? blocks * kBlock - a.V : 0)) : 0;
+    }
+    __device__ __forceinline__ uint32_t id(int at) const { return ((((uint32_t)at >> 9) << shift | index) << 9) | (at & (kBlock - 1)); }
+    // the entry of token `token`, if it is one of the part's (V: the row's length)
+    __device__ __forceinline__ bool has(int32_t token, int64_t V, uint32_t &at) const
+    {
+        const uint32_t t = (uint32_t)token, block = t >> 9;
+        at = (block >> shift) << 9 | (t & (kBlock - 1));
+        return t < (uint32_t)V && (block & ((1u << shift) - 1)) == (uint32_t)index;
+    }
+};
+
 // f(places, valid, output) for the tokens of the row's history, four at a time: places[k] is the k-th one's entry in the part
-// if bit k of `valid` says that it lies there ([first, first + span)); bit k of `output`: it is behind the prompt
+// if bit k of `valid` says that it is one of the part's; bit k of `output`: it is behind the prompt
 template <typename F>
-__device__ __forceinline__ void each_tokens(const AdjustArgs &a, const RowPolicy &p, int64_t first, int span, F f)
+__device__ __forceinline__ void each_tokens(const AdjustArgs &a, const RowPolicy &p, const Part &part, F f)
 {
     const int32_t *h = a.history + p.start;
-    const uint32_t base = (uint32_t)first, width = (uint32_t)span;
     constexpr uint32_t kLoads = 4, kRound = kThreads * 4 * kLoads;
     const uint32_t len = (uint32_t)p.len, prompt = (uint32_t)max(p.prompt, 0), lane = threadIdx.x;
     auto one = [&](int32_t id, uint32_t at_history, int k, uint32_t(&at)[4], uint32_t &valid, uint32_t &output) {
-        at[k] = (uint32_t)id - base;
-        valid |= (id >= 0 && at[k] < width ? 1u : 0u) << k;
+        valid |= (part.has(id, a.V, at[k]) ? 1u : 0u) << k;
         output |= (at_history >= prompt ? 1u : 0u) << k;
     };
     uint32_t i = 0;  // (unsigned: lengths end below 2^31, the places tried beyond them below 2^32)
@@ -111,12 +132,12 @@ struct Seen {
     {
     }
 
-    __device__ __forceinline__ void mark(const AdjustArgs &a, const RowPolicy &p, int64_t first, int span)
+    __device__ __forceinline__ void mark(const AdjustArgs &a, const RowPolicy &p, const Part &part)
     {
         __syncthreads();  // (the part before this one is done with the bits)
         for (int w = threadIdx.x; w < nwords / 4; w += kThreads) reinterpret_cast<uint4 *>(words)[w] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        each_tokens(a, p, first, span, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t) {
+        each_tokens(a, p, part, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t) {
             // (most of a text's tokens are there already: looking first spares the atomics that all would aim at a few words)
             uint32_t have[4];
 #pragma unroll
@@ -269,7 +290,7 @@ constexpr int numbers_of(int part) { return part <= (1 << 16) ? 3072 : 1024; }
 __device__ __host__ constexpr int seen_bytes(int part, bool numbers) { return part / 8 + (numbers ? part / 128 + part / 16 : 0); }
 
 template <typename ZT, typename UT, int NV>
-__global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
+__global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
 {
     constexpr int EPV = ZT::kPerVec, kWaves = kThreads / kWave, kStep = kThreads * EPV * NV;
     constexpr uint32_t kAll = (1u << EPV) - 1;
@@ -279,23 +300,28 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
     Seen seen(lds, a.part);
     const int room = numbers_of(a.part);
     uint32_t *counts = reinterpret_cast<uint32_t *>(lds + seen_bytes(a.part, true)), *places = counts + room;
-    const int64_t items = a.T * a.parts;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane_e = (threadIdx.x & (kWave - 1)) * EPV;
+    const int64_t items = a.T << a.parts_shift;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t t = item / a.parts, first = (item - t * a.parts) * a.part;
-        const int span = (int)min((int64_t)a.part, a.V - first), whole = span / EPV * EPV, rest = span - whole;
-        const char *row = static_cast<const char *>(a.z) + (t * a.ldz + first) * ZT::kBytes;
-        char *out = a.u ? static_cast<char *>(a.u) + (t * a.ldu + first) * UT::kBytes : nullptr;
-        const uint8_t *bits = a.allowed ? reinterpret_cast<const uint8_t *>(a.allowed + t * a.allowed_ld) + first / 8 : nullptr;
-        const float *bias = a.bias ? a.bias + t * a.bias_ld + first : nullptr;
+        const int64_t t = item >> a.parts_shift;
+        const Part part(a, (int)(item & ((1 << a.parts_shift) - 1)));
+        const int whole = part.span / EPV * EPV, rest = part.span - whole;
+        const char *row = static_cast<const char *>(a.z) + t * a.ldz * ZT::kBytes;
+        char *out = a.u ? static_cast<char *>(a.u) + t * a.ldu * UT::kBytes : nullptr;
+        const uint8_t *bits = a.allowed ? reinterpret_cast<const uint8_t *>(a.allowed + t * a.allowed_ld) : nullptr;
+        const float *bias = a.bias ? a.bias + t * a.bias_ld : nullptr;
         Raw<ZT, EPV> next[NV];
         uint32_t next_ok[NV];
+        // (a wavefront's vectors lie in one block: its place in the row is one number)
+        auto first_of = [&](int at, int i) { return at + (i * kWaves + wave) * (kWave * EPV); };
         auto fetch = [&](int at) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
-                if (e < whole) {
-                    next[i].load(row + (int64_t)e * ZT::kBytes);
-                    if (bits) next_ok[i] = allowed_bits<EPV>(bits, e) & kAll;
+                const int e = first_of(at, i);
+                if (e + lane_e < whole) {
+                    const uint32_t id = part.id(e);
+                    next[i].load(row + (uint64_t)id * ZT::kBytes + lane_e * ZT::kBytes);
+                    if (bits) next_ok[i] = allowed_bits<EPV>(bits + id / 8, lane_e) & kAll;
                 }
             }
         };
@@ -303,13 +329,14 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
         // (one element of what is left of the row behind the last whole vector)
         const bool last = (int)threadIdx.x < rest;
         const int le = whole + threadIdx.x;
-        const float z_last = last ? load_elem<ZT>(row, le) : -kInf;
+        const uint32_t id_last = part.id(le);
+        const float z_last = last ? load_elem<ZT>(row, id_last) : -kInf;
         const RowPolicy p = row_policy(a, t);
-        const int64_t y64 = a.logp ? (int64_t)a.chosen[t] - first : -1;
-        const int y = y64 >= 0 && y64 < span ? (int)y64 : -1;
+        uint32_t y_at = 0;
+        const int y = a.logp && part.has(a.chosen[t], a.V, y_at) ? (int)y_at : -1;
         const float scale = p.inv_temperature * kLog2e;
         const bool hist = p.len > 0 && (p.repetition != 1.0f || p.frequency != 0.0f || p.presence != 0.0f);
-        if (hist) seen.mark(a, p, first, span);
+        if (hist) seen.mark(a, p, part);
 
         MaxSum acc = {kLowest, 0.0f};
         for (int at = 0; at < whole; at += kStep) {
@@ -321,7 +348,8 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
             float f[NV][EPV], m = acc.m;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
+                const int first = first_of(at, i), e = first + lane_e;
+                const uint32_t id = part.id(first);
                 if (e >= whole) {
 #pragma unroll
                     for (int k = 0; k < EPV; ++k) f[i][k] = -kInf;
@@ -331,7 +359,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
                 const uint32_t later = hist ? seen.bits<EPV>(e) : 0u;
                 if (bias) {
                     float b[EPV];
-                    load_bias<EPV>(bias + e, b);
+                    load_bias<EPV>(bias + id + lane_e, b);
 #pragma unroll
                     for (int k = 0; k < EPV; ++k) f[i][k] += b[k];
                 }
@@ -348,7 +376,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
 #pragma unroll
                         for (int k = 0; k < EPV; ++k) u[k] = later >> k & 1 ? z[k] : u[k];
                     }
-                    store_out<UT, EPV>(out + (int64_t)e * UT::kBytes, u);
+                    store_out<UT, EPV>(out + (uint64_t)id * UT::kBytes + lane_e * UT::kBytes, u);
                 }
                 if (y >= e && y < e + EPV)
 #pragma unroll
@@ -367,21 +395,21 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
 #pragma unroll
                 for (int k = 0; k < EPV; ++k) acc.s += exp2_hw((f[i][k] - m) * scale);
         }
-        auto bias_of = [&](int at) { return bias ? bias[at] : 0.0f; };
-        auto ok_of = [&](int at) { return !bits || (bits[at >> 3] >> (at & 7) & 1); };
+        auto bias_of = [&](uint32_t id) { return bias ? bias[id] : 0.0f; };
+        auto ok_of = [&](uint32_t id) { return !bits || (bits[id >> 3] >> (id & 7) & 1); };
         auto put_out = [&](int at, float v) {
-            if (out) store_elem<UT>(out, at, v * p.inv_temperature);
+            if (out) store_elem<UT>(out, part.id(at), v * p.inv_temperature);
             if (at == y) a.ws_chosen[t] = v;
         };
         // (infinity and NaN make the sum NaN)
         auto one_of = [](float v) { return v == -kInf ? 0.0f : v - v + 1.0f; };
         if (last) {
             if (!(hist && seen.bit(le))) {
-                const float v = ok_of(le) ? z_last + bias_of(le) : -kInf;
+                const float v = ok_of(id_last) ? z_last + bias_of(id_last) : -kInf;
                 put_out(le, v);
                 acc = join(acc, MaxSum{fmaxf(v, kLowest), one_of(v)}, scale);
             } else if (out) {
-                store_elem<UT>(out, le, z_last);
+                store_elem<UT>(out, id_last, z_last);
             }
         }
         // the entries of the history, one a thread
@@ -393,7 +421,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
             for (int i = threadIdx.x; i < many; i += kThreads) counts[i] = 0;
             __syncthreads();
             // (a token that is there more than once notes the same place)
-            each_tokens(a, p, first, span, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
+            each_tokens(a, p, part, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
                 int n[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) n[k] = valid >> k & 1 ? seen.number(at[k]) - base : -1;
@@ -413,9 +441,10 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
                     at[k] = (int)places[min(i + k * kThreads, many - 1)];
-                    v[k] = load_elem<ZT>(row, at[k]);
-                    b[k] = bias_of(at[k]);
-                    ok[k] = ok_of(at[k]);
+                    const uint32_t id = part.id(at[k]);
+                    v[k] = load_elem<ZT>(row, id);
+                    b[k] = bias_of(id);
+                    ok[k] = ok_of(id);
                 }
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
@@ -435,7 +464,6 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a)
         }
         if (!a.ws_partials) continue;  // (neither log-sum-exp nor log-probs are asked for)
         acc = wave_join(acc, scale);
-        const int wave = threadIdx.x / kWave;
         __syncthreads();
         if ((threadIdx.x & (kWave - 1)) == 0) put(red, kWaves, wave, acc);
         __syncthreads();
@@ -454,8 +482,8 @@ __global__ __launch_bounds__(256) void adjust_finish_kernel(AdjustArgs a)
     for (int64_t t = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; t < a.T; t += (int64_t)gridDim.x * 4) {
         const float inv = a.temperature ? 1.0f / a.temperature[t] : 1.0f, scale = inv * kLog2e;
         MaxSum v = {kLowest, 0.0f};
-        for (int p = lane; p < a.parts; p += kWave) {
-            const float2 w = a.ws_partials[t * a.parts + p];
+        for (int p = lane; p < 1 << a.parts_shift; p += kWave) {
+            const float2 w = a.ws_partials[(t << a.parts_shift) + p];
             v = join(v, MaxSum{w.x, w.y}, scale);
         }
         v = wave_join(v, scale);
@@ -478,37 +506,42 @@ __global__ __launch_bounds__(256) void adjust_finish_kernel(AdjustArgs a)
 template <typename ZT, typename UT, int NV>
 __global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
 {
-    constexpr int EPV = ZT::kPerVec, kStep = kThreads * EPV * NV;
+    constexpr int EPV = ZT::kPerVec, kWaves = kThreads / kWave, kStep = kThreads * EPV * NV;
     constexpr uint32_t kAll = (1u << EPV) - 1;
     extern __shared__ __align__(16) char lds[];
     Seen seen(lds, a.part);
-    const int64_t items = a.T * a.parts;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane_e = (threadIdx.x & (kWave - 1)) * EPV;
+    const int64_t items = a.T << a.parts_shift;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t t = item / a.parts, first = (item - t * a.parts) * a.part;
-        const int span = (int)min((int64_t)a.part, a.V - first), whole = span / EPV * EPV, rest = span - whole;
-        const char *row = static_cast<const char *>(a.z) + (t * a.ldz + first) * ZT::kBytes;
-        const char *in = static_cast<const char *>(a.du) + (t * a.ldu + first) * UT::kBytes;
-        char *out = static_cast<char *>(a.dz) + (t * a.lddz + first) * ZT::kBytes;
-        const uint8_t *bits = a.allowed ? reinterpret_cast<const uint8_t *>(a.allowed + t * a.allowed_ld) + first / 8 : nullptr;
+        const int64_t t = item >> a.parts_shift;
+        const Part part(a, (int)(item & ((1 << a.parts_shift) - 1)));
+        const int whole = part.span / EPV * EPV, rest = part.span - whole;
+        const char *row = static_cast<const char *>(a.z) + t * a.ldz * ZT::kBytes;
+        const char *in = static_cast<const char *>(a.du) + t * a.ldu * UT::kBytes;
+        char *out = static_cast<char *>(a.dz) + t * a.lddz * ZT::kBytes;
+        const uint8_t *bits = a.allowed ? reinterpret_cast<const uint8_t *>(a.allowed + t * a.allowed_ld) : nullptr;
         Raw<UT, EPV> next[NV];
         uint32_t next_ok[NV];
+        auto first_of = [&](int at, int i) { return at + (i * kWaves + wave) * (kWave * EPV); };
         auto fetch = [&](int at) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
-                if (e < whole) {
-                    next[i].load(in + (int64_t)e * UT::kBytes);
-                    if (bits) next_ok[i] = allowed_bits<EPV>(bits, e) & kAll;
+                const int e = first_of(at, i);
+                if (e + lane_e < whole) {
+                    const uint32_t id = part.id(e);
+                    next[i].load(in + (uint64_t)id * UT::kBytes + lane_e * UT::kBytes);
+                    if (bits) next_ok[i] = allowed_bits<EPV>(bits + id / 8, lane_e) & kAll;
                 }
             }
         };
         fetch(0);
         const bool last = (int)threadIdx.x < rest;
         const int le = whole + threadIdx.x;
-        const float g_last = last ? load_elem<UT>(in, le) : 0.0f;
+        const uint32_t id_last = part.id(le);
+        const float g_last = last ? load_elem<UT>(in, id_last) : 0.0f;
         const RowPolicy p = row_policy(a, t);
         const bool hist = p.len > 0 && p.repetition != 1.0f;
-        if (hist) seen.mark(a, p, first, span);
+        if (hist) seen.mark(a, p, part);
         const float up = p.inv_temperature * p.repetition, down = p.inv_temperature / p.repetition;
         for (int at = 0; at < whole; at += kStep) {
             Raw<UT, EPV> raw[NV];
@@ -517,16 +550,16 @@ __global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
             // logits of vectors that hold an entry of the history: asked for together, before the next gradients
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
+                const int first = first_of(at, i), e = first + lane_e;
                 raw[i] = next[i], ok[i] = next_ok[i];
                 hit[i] = hist && e < whole ? seen.bits<EPV>(e) : 0u;
-                if (hit[i]) z[i] = row_load<true, true>(row + (int64_t)e * ZT::kBytes);
+                if (hit[i]) z[i] = row_load<true, true>(row + (uint64_t)part.id(first) * ZT::kBytes + lane_e * ZT::kBytes);
             }
             if (at + kStep < whole) fetch(at + kStep);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int e = at + (i * kThreads + (int)threadIdx.x) * EPV;
-                if (e >= whole) continue;
+                const int first = first_of(at, i);
+                if (first + lane_e >= whole) continue;
                 float g[EPV];
                 raw[i].widen(g);
                 if (hit[i]) {
@@ -541,14 +574,14 @@ __global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
                 if (bits && __any(ok[i] != kAll))
 #pragma unroll
                     for (int k = 0; k < EPV; ++k) g[k] = if_allowed(ok[i], k, g[k], 0u);
-                store_out<ZT, EPV>(out + (int64_t)e * ZT::kBytes, g);
+                store_out<ZT, EPV>(out + (uint64_t)part.id(first) * ZT::kBytes + lane_e * ZT::kBytes, g);
             }
         }
         if (last) {
             float f = g_last * p.inv_temperature;
-            if (hist && seen.bit(le)) f = g_last * (load_elem<ZT>(row, le) > 0.0f ? down : up);
-            if (bits && !(bits[le >> 3] >> (le & 7) & 1)) f = 0.0f;
-            store_elem<ZT>(out, le, f);
+            if (hist && seen.bit(le)) f = g_last * (load_elem<ZT>(row, id_last) > 0.0f ? down : up);
+            if (bits && !(bits[id_last >> 3] >> (id_last & 7) & 1)) f = 0.0f;
+            store_elem<ZT>(out, id_last, f);
         }
     }
 }
@@ -556,7 +589,7 @@ __global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
 template <typename ZT, typename UT>
 hipError_t launch(const AdjustArgs &a, hipStream_t s)
 {
-    const int64_t items = a.T * a.parts, most = 1 << 20;
+    const int64_t items = a.T << a.parts_shift, most = 1 << 20;
     const dim3 grid((unsigned)(items < most ? items : most)), block(kThreads);
     const size_t lds = a.history ? seen_bytes(a.part, !a.dz) + (a.dz ? 0 : 8 * numbers_of(a.part)) : 0;
     if (a.dz) adjust_bwd_kernel<ZT, UT, 2><<<grid, block, lds, s>>>(a);
@@ -569,7 +602,7 @@ hipError_t launch(const AdjustArgs &a, hipStream_t s)
 hipError_t launch_adjust(AdjustArgs a, hipStream_t s)
 {
     const AdjustPlan p = adjust_plan(a.T, a.V, a.z_dt == A3PO_F32 ? 4 : 2);
-    a.parts = p.parts;
+    a.parts_shift = p.shift;
     a.part = p.part;
     hipError_t e;
     if (a.z_dt == A3PO_F32) e = a.u_dt == A3PO_F32 ? launch<F32, F32>(a, s) : launch<F32, Bf16>(a, s);

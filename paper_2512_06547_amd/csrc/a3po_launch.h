@@ -473,25 +473,22 @@ struct AdjustArgs {
     float *lse, *logp;
     float2 *ws_partials;  // [T, parts], null: neither lse nor logp
     float *ws_chosen;     // [T]
-    int parts, part;
+    int parts_shift, part;
 };
 
-// A row's parts, `part` entries each: whole rows if they are enough for two workgroups a compute unit, more parts
-// otherwise, down to a 16-byte vector a thread; a part's bits and their numbers have to fit 64 KiB of LDS.
-constexpr int kAdjustThreads = 512, kAdjustMaxPart = 1 << 18;
+// A row's parts, 2^shift of up to `part` entries each: whole rows if they are enough for two workgroups a compute unit, more
+// parts otherwise, down to a 16-byte vector a thread; a part's bits and their numbers have to fit 64 KiB of LDS.
+constexpr int kAdjustThreads = 512, kAdjustMaxPart = 1 << 18, kAdjustItems = 512;
 struct AdjustPlan {
-    int parts, part;
+    int shift, part;
 };
 inline AdjustPlan adjust_plan(int64_t T, int64_t V, int z_bytes)
 {
-    const int64_t step = kAdjustThreads * (16 / z_bytes);
-    const int64_t least = (V + kAdjustMaxPart - 1) / kAdjustMaxPart, widest = (V + step - 1) / step;
-    int64_t parts = (512 + T - 1) / (T > 0 ? T : 1);
-    if (parts > widest) parts = widest;
-    if (parts < least) parts = least;
-    AdjustPlan p;
-    p.part = (int)(((V + parts - 1) / parts + 511) / 512 * 512);
-    p.parts = (int)((V + p.part - 1) / p.part);
+    const int64_t step = kAdjustThreads * (16 / z_bytes), blocks = (V + 511) / 512;
+    AdjustPlan p = {0, 0};
+    while (((blocks + (1 << p.shift) - 1) >> p.shift) * 512 > kAdjustMaxPart) ++p.shift;
+    while ((T << p.shift) < kAdjustItems && (V >> p.shift) > step) ++p.shift;
+    p.part = (int)((blocks + (1 << p.shift) - 1) >> p.shift) * 512;
     return p;
 }
 // workspace: the chosen tokens' adjusted logits, then a (max, sum) per part
@@ -499,8 +496,8 @@ inline size_t adjust_partials_offset(int64_t T) { return ((size_t)T * 4 + 255) /
 inline size_t adjust_workspace_bytes(int64_t T, int64_t V)
 {
     if (T <= 0 || V <= 0) return 256;
-    const int a = adjust_plan(T, V, 2).parts, b = adjust_plan(T, V, 4).parts;
-    return adjust_partials_offset(T) + ((size_t)T * 8 * (size_t)(a > b ? a : b) + 255) / 256 * 256;
+    const int a = adjust_plan(T, V, 2).shift, b = adjust_plan(T, V, 4).shift;
+    return adjust_partials_offset(T) + (((size_t)T * 8 << (a > b ? a : b)) + 255) / 256 * 256;
 }
 hipError_t launch_adjust(AdjustArgs a, hipStream_t s);
 
