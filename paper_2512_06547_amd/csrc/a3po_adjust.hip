@@ -275,12 +275,42 @@ __device__ __forceinline__ uint32_t allowed_bits(const uint8_t *bits, int e)
     const uint32_t byte = bits[e >> 3];
     return EPV == 8 ? byte : byte >> (e & 4);
 }
-__device__ __forceinline__ float if_allowed(uint32_t bits, int k, float v, uint32_t other)
+// (two instructions; from a comparison or a mask in C the compiler makes three)
+__device__ __forceinline__ float if_allowed(uint32_t bits, int k, float v, float other)
 {
-    const uint32_t on = (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1);
-    return __uint_as_float((__float_as_uint(v) & on) | (other & ~on));
+    const int on = __builtin_amdgcn_sbfe((int)bits, k, 1);
+    float r;
+    asm("v_bfi_b32 %0, %1, %2, %3" : "=v"(r) : "v"(on), "v"(v), "v"(other));
+    return r;
 }
-constexpr uint32_t kMinusInfBits = 0xFF800000u;
+// the largest of three (fmaxf makes a quiet NaN of each operand first, an instruction each; a NaN shows in the sums)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// Folds a thread's values into its (max, sum), m being the new maximum.  exp2(f s - c) is one instruction less than
+// exp2((f - m) s) and, with c = m s rounded, differs from it by the factor 2^(m s - c) alone, which the sum is freed of
+// at once: the exponent is rounded relative to f - m as before.  Where m s is too large for that (nothing but -inf and the
+// type's lowest values yet) the difference comes first.
+template <int N>
+__device__ __forceinline__ void fold_values(MaxSum &acc, const float (&f)[N], float m, float scale)
+{
+    const float c = m * scale;
+    float s = 0.0f;
+    if (__any(!(fabsf(c) < 1e37f))) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) s += exp2_hw((f[k] - m) * scale);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) s += exp2_hw(fmaf(f[k], scale, -c));
+        s *= exp2_hw(-fmaf(m, scale, -c));
+    }
+    acc.s = fmaf(acc.s, exp2_hw((acc.m - m) * scale), s);
+    acc.m = m;
+}
 
 // Entries of the history that are counted at a time, each with 8 bytes of LDS: all that a text has in a part, where the part's
 // bits leave room for them beside three other workgroups' (a second round reads the history again).
@@ -345,31 +375,31 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
 #pragma unroll
             for (int i = 0; i < NV; ++i) raw[i] = next[i], ok[i] = next_ok[i];
             if (at + kStep < whole) fetch(at + kStep);
-            float f[NV][EPV], m = acc.m;
+            float f[NV * EPV], m = acc.m;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int first = first_of(at, i), e = first + lane_e;
                 const uint32_t id = part.id(first);
                 if (e >= whole) {
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) f[i][k] = -kInf;
+                    for (int k = 0; k < EPV; ++k) f[i * EPV + k] = -kInf;
                     continue;
                 }
-                raw[i].widen(f[i]);
+                raw[i].widen(f + i * EPV);
                 const uint32_t later = hist ? seen.bits<EPV>(e) : 0u;
                 if (bias) {
                     float b[EPV];
                     load_bias<EPV>(bias + id + lane_e, b);
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) f[i][k] += b[k];
+                    for (int k = 0; k < EPV; ++k) f[i * EPV + k] += b[k];
                 }
                 if (bits && __any(ok[i] != kAll))
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) f[i][k] = if_allowed(ok[i], k, f[i][k], kMinusInfBits);
+                    for (int k = 0; k < EPV; ++k) f[i * EPV + k] = if_allowed(ok[i], k, f[i * EPV + k], -kInf);
                 if (out) {
                     float u[EPV];
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) u[k] = f[i][k] * p.inv_temperature;
+                    for (int k = 0; k < EPV; ++k) u[k] = f[i * EPV + k] * p.inv_temperature;
                     if (later) {  // (their logits stay there for now: out may be the logits' own place)
                         float z[EPV];
                         raw[i].widen(z);
@@ -381,19 +411,14 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
                 if (y >= e && y < e + EPV)
 #pragma unroll
                     for (int k = 0; k < EPV; ++k)
-                        if (e + k == y && !(later >> k & 1)) a.ws_chosen[t] = f[i][k];
+                        if (e + k == y && !(later >> k & 1)) a.ws_chosen[t] = f[i * EPV + k];
                 if (__any(later != 0))
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) f[i][k] = if_allowed(~later, k, f[i][k], kMinusInfBits);
+                    for (int k = 0; k < EPV; ++k) f[i * EPV + k] = if_allowed(~later, k, f[i * EPV + k], -kInf);
 #pragma unroll
-                for (int k = 0; k < EPV; ++k) m = fmaxf(m, f[i][k]);
+                for (int k = 0; k < EPV; k += 2) m = max3(m, f[i * EPV + k], f[i * EPV + k + 1]);
             }
-            acc.s *= exp2_hw((acc.m - m) * scale);
-            acc.m = m;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int k = 0; k < EPV; ++k) acc.s += exp2_hw((f[i][k] - m) * scale);
+            fold_values(acc, f, m, scale);
         }
         auto bias_of = [&](uint32_t id) { return bias ? bias[id] : 0.0f; };
         auto ok_of = [&](uint32_t id) { return !bits || (bits[id >> 3] >> (id & 7) & 1); };
@@ -456,10 +481,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
                     if (there) put_out(at[k], v[k]);
                     m = fmaxf(m, v[k]);
                 }
-                acc.s *= exp2_hw((acc.m - m) * scale);
-                acc.m = m;
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k) acc.s += exp2_hw((v[k] - m) * scale);
+                fold_values(acc, v, m, scale);
             }
         }
         if (!a.ws_partials) continue;  // (neither log-sum-exp nor log-probs are asked for)
@@ -573,7 +595,7 @@ __global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
                 }
                 if (bits && __any(ok[i] != kAll))
 #pragma unroll
-                    for (int k = 0; k < EPV; ++k) g[k] = if_allowed(ok[i], k, g[k], 0u);
+                    for (int k = 0; k < EPV; ++k) g[k] = if_allowed(ok[i], k, g[k], 0.0f);
                 store_out<ZT, EPV>(out + (uint64_t)part.id(first) * ZT::kBytes + lane_e * ZT::kBytes, g);
             }
         }
