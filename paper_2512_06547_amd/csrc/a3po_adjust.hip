@@ -293,14 +293,14 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 
 // Folds a thread's values into its (max, sum), m being the new maximum.  exp2(f s - c) is one instruction less than
 // exp2((f - m) s) and, with c = m s rounded, differs from it by the factor 2^(m s - c) alone, which the sum is freed of
-// at once: the exponent is rounded relative to f - m as before.  Where m s is too large for that (nothing but -inf and the
-// type's lowest values yet) the difference comes first.
+// at once: the exponent is rounded relative to f - m as before.  From |m s| = 2^23 on, where that factor could leave the range
+// (values masked by large numbers, all but greedy temperatures, infinities), the difference comes first.
 template <int N>
 __device__ __forceinline__ void fold_values(MaxSum &acc, const float (&f)[N], float m, float scale)
 {
     const float c = m * scale;
     float s = 0.0f;
-    if (__any(!(fabsf(c) < 1e37f))) {
+    if (__any(!(fabsf(c) < 8388608.0f))) {
 #pragma unroll
         for (int k = 0; k < N; ++k) s += exp2_hw((f[k] - m) * scale);
     } else {

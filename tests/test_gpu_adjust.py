@@ -354,3 +354,16 @@ def test_empty_calls(a3po):
     r = a3po.adjust_logits(e, temperature=torch.empty(0, device="cuda"))
     assert r["out"].shape == (0, 100) and r["lse"].shape == (0,)
     assert a3po.adjust_logits_bwd(e).shape == (0, 100)
+
+
+@pytest.mark.parametrize("zt", ["f32", "bf16"])
+@pytest.mark.parametrize("level,temperature", [(-1e30, 1.0), (1e9, 1.0), (-3e7, 1e-3), (7.0, 1e-12), (1e6, 1.0)])
+def test_values_far_from_zero_whose_scaled_maximum_rounds_coarsely(a3po, zt, level, temperature):
+    T, V = 4, 1500
+    g = torch.Generator().manual_seed(3)
+    z = (level * (1 + 1e-2 * torch.rand(T, V, generator=g))).to(DT[zt])
+    z[1] = level                                    # ties throughout
+    z[2, V // 2] = level + abs(level) / 2           # one ahead of the others
+    p = dict(history=None, hist_start=None, hist_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
+             temperature=torch.full((T,), temperature), bias=None, allowed=None)
+    check_forward(a3po, z, p, None, torch.float32)
