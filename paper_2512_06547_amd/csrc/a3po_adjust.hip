@@ -132,12 +132,16 @@ struct Seen {
     {
     }
 
-    __device__ __forceinline__ void mark(const AdjustArgs &a, const RowPolicy &p, const Part &part)
+    // With a `list` of `room` tokens for the wavefront, its tokens that are the part's are noted there, the output's with the
+    // top bit; returns how many they are, those behind the list's end included.
+    template <bool LIST>
+    __device__ __forceinline__ int mark(const AdjustArgs &a, const RowPolicy &p, const Part &part, uint32_t *list, int room)
     {
+        int listed = 0;
         __syncthreads();  // (the part before this one is done with the bits)
         for (int w = threadIdx.x; w < nwords / 4; w += kThreads) reinterpret_cast<uint4 *>(words)[w] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        each_tokens(a, p, part, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t) {
+        each_tokens(a, p, part, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
             // (most of a text's tokens are there already: looking first spares the atomics that all would aim at a few words)
             uint32_t have[4];
 #pragma unroll
@@ -145,8 +149,17 @@ struct Seen {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (!(have[k] >> (at[k] & 31) & 1)) atomicOr(&words[at[k] >> 5], 1u << (at[k] & 31));
+            if constexpr (LIST)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint64_t mine = __ballot(valid >> k & 1);
+                    const int to = listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(mine >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mine, 0));
+                    if ((valid >> k & 1) && to < room) list[to] = at[k] | (output >> k) << 31;
+                    listed += __popcll(mine);
+                }
         });
         __syncthreads();
+        return listed;
     }
     // numbers the marked entries in ascending order; returns how many there are (numbers are there behind the next barrier)
     __device__ __forceinline__ int count(int *waves)
@@ -222,11 +235,11 @@ __device__ __forceinline__ void store_out(char *p, const float *f)
         for (int k = 0; k < EPV; k += UT::kPerVec) {
             const uint4 v = pack<UT>(f + k);
             const u32x4_t t = {v.x, v.y, v.z, v.w};
-            __builtin_nontemporal_store(t, reinterpret_cast<u32x4_elem_t *>(p + k * UT::kBytes));
+            *reinterpret_cast<u32x4_elem_t *>(p + k * UT::kBytes) = t;
         }
     } else {
         const u32x2_t t = {pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
-        __builtin_nontemporal_store(t, reinterpret_cast<u32x2_t *>(p));
+        *reinterpret_cast<u32x2_t *>(p) = t;
     }
 }
 
@@ -240,11 +253,11 @@ struct Raw {
         if constexpr (kWords >= 4) {
 #pragma unroll
             for (int k = 0; k < kWords; k += 4) {
-                const uint4 v = row_load<true>(p + 4 * k);
+                const uint4 v = row_load<true, true>(p + 4 * k);
                 w[k] = v.x, w[k + 1] = v.y, w[k + 2] = v.z, w[k + 3] = v.w;
             }
         } else {
-            const u32x2_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(p));
+            const u32x2_t t = *reinterpret_cast<const u32x2_t *>(p);
             w[0] = t.x, w[1] = t.y;
         }
     }
@@ -314,10 +327,16 @@ __device__ __forceinline__ void fold_values(MaxSum &acc, const float (&f)[N], fl
 
 // Entries of the history that are counted at a time, each with 8 bytes of LDS: all that a text has in a part, where the part's
 // bits leave room for them beside three other workgroups' (a second round reads the history again).
-constexpr int numbers_of(int part) { return part <= (1 << 16) ? 3072 : 1024; }
-
+__device__ __host__ constexpr int numbers_of(int part) { return part <= (1 << 16) ? 2048 : 1024; }
 // LDS of a part's bits, and with their numbers
 __device__ __host__ constexpr int seen_bytes(int part, bool numbers) { return part / 8 + (numbers ? part / 128 + part / 16 : 0); }
+// Tokens that a wavefront notes while it marks them, 4 bytes each, so that they are counted from there: what four workgroups
+// a compute unit leave of the LDS.
+__device__ __host__ constexpr int listed_of(int part)
+{
+    const int left = 160 * 1024 / 4 - 512 - seen_bytes(part, true) - 8 * numbers_of(part);
+    return left > 4096 ? left / (4 * kThreads / kWave) & ~1 : 128;
+}
 
 template <typename ZT, typename UT, int NV>
 __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
@@ -329,8 +348,10 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
     __shared__ int waves[kWaves];
     Seen seen(lds, a.part);
     const int room = numbers_of(a.part);
-    uint32_t *counts = reinterpret_cast<uint32_t *>(lds + seen_bytes(a.part, true)), *places = counts + room;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane_e = (threadIdx.x & (kWave - 1)) * EPV;
+    uint32_t *counts = reinterpret_cast<uint32_t *>(lds + seen_bytes(a.part, true)), *places = counts + room;
+    const int list_room = listed_of(a.part);
+    uint32_t *list = places + room + wave * list_room;
     const int64_t items = a.T << a.parts_shift;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t t = item >> a.parts_shift;
@@ -366,7 +387,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
         const int y = a.logp && part.has(a.chosen[t], a.V, y_at) ? (int)y_at : -1;
         const float scale = p.inv_temperature * kLog2e;
         const bool hist = p.len > 0 && (p.repetition != 1.0f || p.frequency != 0.0f || p.presence != 0.0f);
-        if (hist) seen.mark(a, p, part);
+        const int listed = hist ? __builtin_amdgcn_readfirstlane(seen.mark<true>(a, p, part, list, list_room)) : 0;
 
         MaxSum acc = {kLowest, 0.0f};
         for (int at = 0; at < whole; at += kStep) {
@@ -446,7 +467,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
             for (int i = threadIdx.x; i < many; i += kThreads) counts[i] = 0;
             __syncthreads();
             // (a token that is there more than once notes the same place)
-            each_tokens(a, p, part, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
+            auto count_tokens = [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
                 int n[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) n[k] = valid >> k & 1 ? seen.number(at[k]) - base : -1;
@@ -456,7 +477,23 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
                         places[n[k]] = at[k];
                         if (output >> k & 1) atomicAdd(&counts[n[k]], 1u);
                     }
-            });
+            };
+            if (listed <= list_room) {
+                for (int i = threadIdx.x & (kWave - 1); i < listed; i += 4 * kWave) {
+                    uint32_t at[4], valid = 0, output = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int from = i + k * kWave;
+                        const uint32_t v = list[min(from, listed - 1)];
+                        at[k] = v & 0x7FFFFFFFu;
+                        valid |= (from < listed ? 1u : 0u) << k;
+                        output |= v >> 31 << k;
+                    }
+                    count_tokens(at, valid, output);
+                }
+            } else {
+                each_tokens(a, p, part, count_tokens);
+            }
             __syncthreads();
             constexpr int kBatch = 4;  // (a thread's loads in flight)
             for (int i = threadIdx.x; i < many; i += kThreads * kBatch) {
@@ -563,7 +600,7 @@ __global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
         const float g_last = last ? load_elem<UT>(in, id_last) : 0.0f;
         const RowPolicy p = row_policy(a, t);
         const bool hist = p.len > 0 && p.repetition != 1.0f;
-        if (hist) seen.mark(a, p, part);
+        if (hist) seen.mark<false>(a, p, part, nullptr, 0);
         const float up = p.inv_temperature * p.repetition, down = p.inv_temperature / p.repetition;
         for (int at = 0; at < whole; at += kStep) {
             Raw<UT, EPV> raw[NV];
@@ -613,7 +650,7 @@ hipError_t launch(const AdjustArgs &a, hipStream_t s)
 {
     const int64_t items = a.T << a.parts_shift, most = 1 << 20;
     const dim3 grid((unsigned)(items < most ? items : most)), block(kThreads);
-    const size_t lds = a.history ? seen_bytes(a.part, !a.dz) + (a.dz ? 0 : 8 * numbers_of(a.part)) : 0;
+    const size_t lds = a.history ? seen_bytes(a.part, !a.dz) + (a.dz ? 0 : 8 * numbers_of(a.part) + 4 * listed_of(a.part) * (kThreads / kWave)) : 0;
     if (a.dz) adjust_bwd_kernel<ZT, UT, 2><<<grid, block, lds, s>>>(a);
     else adjust_kernel<ZT, UT, 2><<<grid, block, lds, s>>>(a);
     return hipGetLastError();
