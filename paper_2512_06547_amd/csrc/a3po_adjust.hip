@@ -338,6 +338,17 @@ __device__ __host__ constexpr int listed_of(int part)
     return left > 4096 ? left / (4 * kThreads / kWave) & ~1 : 128;
 }
 
+// what is told of a row: of its (max, sum), and of the chosen token's adjusted logit before the temperature
+__device__ __forceinline__ void finish_row(const AdjustArgs &a, int64_t t, MaxSum v, float inv_temperature, float u)
+{
+    const float log_s = logf(v.s);  // (-inf where nothing is left of the row)
+    if (a.lse) a.lse[t] = fmaf(v.m, inv_temperature, log_s);
+    if (a.logp) {
+        const int64_t y = a.chosen[t];
+        a.logp[t] = y < 0 || y >= a.V ? 0.0f : u == -kInf ? -kInf : (u - v.m) * inv_temperature - log_s;
+    }
+}
+
 template <typename ZT, typename UT, int NV>
 __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
 {
@@ -346,6 +357,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
     extern __shared__ __align__(16) char lds[];
     __shared__ float red[2 * kWaves];
     __shared__ int waves[kWaves];
+    __shared__ float u_chosen;
     Seen seen(lds, a.part);
     const int room = numbers_of(a.part);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane_e = (threadIdx.x & (kWave - 1)) * EPV;
@@ -432,7 +444,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
                 if (y >= e && y < e + EPV)
 #pragma unroll
                     for (int k = 0; k < EPV; ++k)
-                        if (e + k == y && !(later >> k & 1)) a.ws_chosen[t] = f[i * EPV + k];
+                        if (e + k == y && !(later >> k & 1)) u_chosen = f[i * EPV + k];
                 if (__any(later != 0))
 #pragma unroll
                     for (int k = 0; k < EPV; ++k) f[i * EPV + k] = if_allowed(~later, k, f[i * EPV + k], -kInf);
@@ -445,7 +457,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
         auto ok_of = [&](uint32_t id) { return !bits || (bits[id >> 3] >> (id & 7) & 1); };
         auto put_out = [&](int at, float v) {
             if (out) store_elem<UT>(out, part.id(at), v * p.inv_temperature);
-            if (at == y) a.ws_chosen[t] = v;
+            if (at == y) u_chosen = v;
         };
         // (infinity and NaN make the sum NaN)
         auto one_of = [](float v) { return v == -kInf ? 0.0f : v - v + 1.0f; };
@@ -529,8 +541,16 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
         if (threadIdx.x < kWaves) {
             get(red, kWaves, threadIdx.x, acc);
             acc = wave_join<kWaves>(acc, scale);
-            if (threadIdx.x == 0) a.ws_partials[item] = make_float2(acc.m, acc.s);
+            if (threadIdx.x == 0) {
+                if (a.parts_shift == 0) {
+                    finish_row(a, t, acc, p.inv_temperature, u_chosen);
+                } else {
+                    a.ws_partials[item] = make_float2(acc.m, acc.s);
+                    if (y >= 0) a.ws_chosen[t] = u_chosen;
+                }
+            }
         }
+        if (item + gridDim.x < items) __syncthreads();  // (u_chosen is read)
     }
 }
 
@@ -546,19 +566,7 @@ __global__ __launch_bounds__(256) void adjust_finish_kernel(AdjustArgs a)
             v = join(v, MaxSum{w.x, w.y}, scale);
         }
         v = wave_join(v, scale);
-        if (lane == 0) {
-            const float log_s = logf(v.s);  // (-inf where nothing is left of the row)
-            if (a.lse) a.lse[t] = fmaf(v.m, inv, log_s);
-            if (a.logp) {
-                const int64_t y = a.chosen[t];
-                float r = 0.0f;
-                if (y >= 0 && y < a.V) {
-                    const float u = a.ws_chosen[t];
-                    r = u == -kInf ? -kInf : (u - v.m) * inv - log_s;
-                }
-                a.logp[t] = r;
-            }
-        }
+        if (lane == 0) finish_row(a, t, v, inv, a.ws_chosen[t]);
     }
 }
 
@@ -666,7 +674,7 @@ hipError_t launch_adjust(AdjustArgs a, hipStream_t s)
     hipError_t e;
     if (a.z_dt == A3PO_F32) e = a.u_dt == A3PO_F32 ? launch<F32, F32>(a, s) : launch<F32, Bf16>(a, s);
     else e = a.u_dt == A3PO_F32 ? launch<Bf16, F32>(a, s) : launch<Bf16, Bf16>(a, s);
-    if (e != hipSuccess || a.dz || !a.ws_partials) return e;
+    if (e != hipSuccess || a.dz || !a.ws_partials || a.parts_shift == 0) return e;
     const int64_t want = (a.T + 3) / 4, most = 1 << 20;
     adjust_finish_kernel<<<dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s>>>(a);
     return hipGetLastError();

@@ -472,7 +472,7 @@ struct AdjustArgs {
     const int32_t *chosen;
     float *lse, *logp;
     float2 *ws_partials;  // [T, parts], null: neither lse nor logp
-    float *ws_chosen;     // [T]
+    float *ws_chosen;     // [T] (both: where a row has several parts)
     int parts_shift, part;
 };
 

@@ -367,3 +367,16 @@ def test_values_far_from_zero_whose_scaled_maximum_rounds_coarsely(a3po, zt, lev
     p = dict(history=None, hist_start=None, hist_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
              temperature=torch.full((T,), temperature), bias=None, allowed=None)
     check_forward(a3po, z, p, None, torch.float32)
+
+
+def test_more_rows_than_workgroups(a3po):
+    T, V = (1 << 20) + 700, 9
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = 4 * torch.randn(T, V, device="cuda", generator=g)
+    y = torch.randint(-1, V, (T,), device="cuda", generator=g, dtype=torch.int32)
+    temperature = 0.5 + torch.rand(T, device="cuda", generator=g)
+    r = a3po.adjust_logits(z, chosen=y, temperature=temperature, write=False)
+    u = z.double() / temperature.double()[:, None]
+    ref = torch.log_softmax(u, 1).gather(1, y.clamp(min=0).long()[:, None])[:, 0].masked_fill(y < 0, 0.0)
+    for got, ref in ((r["logp"], ref), (r["lse"], torch.logsumexp(u, 1))):
+        assert ((got.double() - ref).abs() <= 1e-5 * (1 + ref.abs())).all()
