@@ -750,8 +750,11 @@ hipError_t launch_tokens(const W4Args &a, void *workspace, hipStream_t s)
     const W4Plan p = w4_plan(a.T, a.H, a.V, a.group, SCALE_F32, cus);
     if (p.units && p.blocks16 == 1) return launch_units<1, GROUP, ZEROS, SCALE_F32>(a, p, s);
     if (p.units) return launch_units<2, GROUP, ZEROS, SCALE_F32>(a, p, s);
-    if (a.T <= 16) return launch_stream<1, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
-    if (a.T <= 32) return launch_stream<2, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
+    // (more than 64 tokens: shared out evenly among as many readings of the weight as 64 at a time take)
+    const int64_t passes = (a.T + 63) / 64, tokens = (a.T + passes - 1) / passes;
+    if (tokens <= 16) return launch_stream<1, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
+    if (tokens <= 32) return launch_stream<2, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
+    if (tokens <= 48) return launch_stream<3, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
     return launch_stream<4, GROUP, ZEROS, SCALE_F32>(a, workspace, cus, s);
 }
 
