@@ -9,11 +9,16 @@
 //
 // A workgroup takes a row, or a part of one where rows are few.  The row's history becomes a bit per entry in LDS.  Forward,
 // entries without the bit are folded from registers as they stream by, and the others, few, are taken one a thread
-// afterwards: the bits number them, a second pass over the history's output counts them by those numbers (integers: no order
-// of additions), and they join the sum and the output.  A test per entry with the penalties behind it costs more than the
-// exponential, and the work on the history, the reductions and the row's parameters cost what some forty entries a thread do,
-// so that rows are not cut further than it takes to fill the chip (scoring of 8,192 x 50,001 bfloat16: a test per entry, four
-// parts a row 1,055 us; a penalty per entry in LDS 553; bits, four parts 735; bits, whole rows 312).
+// afterwards: the bits number them, the part's tokens, noted while they were marked, are counted by those numbers (integers: no
+// order of additions), and the entries join the sum and the output.  A test per entry with the penalties behind it costs more
+// than the exponential, and the work on the history, the reductions and the row's parameters cost what some forty entries a
+// thread do, so that rows are not cut further than it takes to fill the chip (scoring of 8,192 x 50,001 bfloat16: a test per
+// entry, four parts a row 1,055 us; a penalty per entry in LDS 553; bits, four parts 735; bits, whole rows 306; now 280).
+// What bounds it: scoring, 819 MB in 280 us, the vector instructions (212 us without a history, 31 for the bits, 16 for the
+// counts, 36 for the entries); decoding, 64 x 151,936 to fp32 with 16,384 tokens of history, 33 us, the passes over the history
+// (18 us without one); the gradient, two streams and little else, memory: 8,192 x 151,936 4.98 GB in 1,050 us (4.7 TB/s, what a large copy reaches).
+// Rows are read and written through the caches: the entries of the history are fetched a second time (non-temporal: scoring
+// 301 us, decoding 38), and the next kernel reads what is written here.
 // Maximum and sum of exp are taken before the temperature, which then is part of the exponent's scale.  All arithmetic is
 // fp32; what is stored in bfloat16 is rounded once, and lse and logp are those of the fp32 values.
 #include "a3po_common.h"
@@ -326,7 +331,7 @@ __device__ __forceinline__ void fold_values(MaxSum &acc, const float (&f)[N], fl
 }
 
 // Entries of the history that are counted at a time, each with 8 bytes of LDS: all that a text has in a part, where the part's
-// bits leave room for them beside three other workgroups' (a second round reads the history again).
+// bits leave room for them beside three other workgroups' (further rounds go over the tokens again).
 __device__ __host__ constexpr int numbers_of(int part) { return part <= (1 << 16) ? 2048 : 1024; }
 // LDS of a part's bits, and with their numbers
 __device__ __host__ constexpr int seen_bytes(int part, bool numbers) { return part / 8 + (numbers ? part / 128 + part / 16 : 0); }
@@ -668,7 +673,7 @@ hipError_t launch(const AdjustArgs &a, hipStream_t s)
 
 hipError_t launch_adjust(AdjustArgs a, hipStream_t s)
 {
-    const AdjustPlan p = adjust_plan(a.T, a.V, a.z_dt == A3PO_F32 ? 4 : 2);
+    const AdjustPlan p = adjust_plan(a.T, a.V, a.z_dt == A3PO_F32 ? 4 : 2, a.dz != nullptr);
     a.parts_shift = p.shift;
     a.part = p.part;
     hipError_t e;

@@ -476,18 +476,29 @@ struct AdjustArgs {
     int parts_shift, part;
 };
 
-// A row's parts, 2^shift of up to `part` entries each: whole rows if they are enough for two workgroups a compute unit, more
-// parts otherwise, down to a 16-byte vector a thread; a part's bits and their numbers have to fit 64 KiB of LDS.
-constexpr int kAdjustThreads = 512, kAdjustMaxPart = 1 << 18, kAdjustItems = 512;
+// A row's parts, 2^shift of up to `part` entries each; a part's bits and their numbers have to fit 64 KiB of LDS.  Parts of the
+// forward pass each go over the row's history and are joined by another kernel; those of the backward pass only mark it, and
+// more of them even out how the workgroups end.  So rows are cut down to a 16-byte vector a thread until there is a workgroup for
+// every compute unit (backward in fp32 two), to 16,384 entries until there are four (backward: sixteen), and backward to 32,768
+// whatever their number.
+// Forward, workgroups and us, history of 4,000: 16 x 151,936 256 / 512 13 / 14, 150 x 151,936 300 / 600 / 1,200 / 2,400 61 / 55 /
+// 52 / 64, 300 x 151,936 131 / 106 / 100 / 103, 300 x 32,000 22 / 30 / 35 / 50, 1,036 x 87,709 1,036 / 2,072 64 / 79; 64 x 151,936
+// with 16,384 tokens 256 / 512 / 1,024 37 / 32 / 41.  Backward: 300 x 32,000 300 / 600 14 / 16 (fp32 19 / 16), 700 x 151,936
+// 700 / 1,400 / 2,800 144 / 132 / 126, 2,100 x 151,936 4,200 / 8,400 / 16,800 290 / 278 / 293, 8,192 x 151,936 8,192 / 32,768
+// 1,127 / 1,050, 7,000 x 50,001 7,000 / 14,000 391 / 437.
+constexpr int kAdjustThreads = 512, kAdjustMaxPart = 1 << 18, kAdjustItems = 256, kAdjustMany = 1024, kAdjustManyBwd = 4096;
 struct AdjustPlan {
     int shift, part;
 };
-inline AdjustPlan adjust_plan(int64_t T, int64_t V, int z_bytes)
+inline AdjustPlan adjust_plan(int64_t T, int64_t V, int z_bytes, bool backward = false)
 {
     const int64_t step = kAdjustThreads * (16 / z_bytes), blocks = (V + 511) / 512;
     AdjustPlan p = {0, 0};
     while (((blocks + (1 << p.shift) - 1) >> p.shift) * 512 > kAdjustMaxPart) ++p.shift;
-    while ((T << p.shift) < kAdjustItems && (V >> p.shift) > step) ++p.shift;
+    const int64_t fill = backward && z_bytes == 4 ? 2 * kAdjustItems : kAdjustItems;
+    while ((T << p.shift) < fill && (V >> p.shift) > step) ++p.shift;
+    while ((T << p.shift) < (backward ? kAdjustManyBwd : kAdjustMany) && (V >> p.shift) > 2 * 16384) ++p.shift;
+    while (backward && (V >> p.shift) > 2 * 32768) ++p.shift;
     p.part = (int)((blocks + (1 << p.shift) - 1) >> p.shift) * 512;
     return p;
 }

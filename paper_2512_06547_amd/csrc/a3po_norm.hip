@@ -8,7 +8,9 @@
 // Both passes read each row once and keep it in registers; statistics, products and sums are fp32, and every output is
 // rounded once.  The variance is the mean of (x - mean)^2, taken from the registers after the mean is known: the
 // difference of two sums loses all digits of rows whose mean is large against their spread.
-// The kernels are bound by memory.
+// The kernels are bound by memory where there are rows enough: the gradient of 65,536 x 4,096 bfloat16 moves 1.61 GB in 280 us
+// (5.8 TB/s), the forward pass of 10,240 x 2,049 fp32 to bfloat16 126 MB in 25.  Fewer rows are a chain of latencies, a load, two
+// reductions and a store: 64 x 1,536 forward 3.5 us, 1,000 x 1,536 backward 7.5 and 3.4 for the sums over rows.
 #include "a3po_common.h"
 #include "a3po_launch.h"
 

@@ -173,14 +173,14 @@ def test_adjust_plan_covers_every_row_within_lds(tmp_path):
 using namespace a3po;
 int main()
 {
-    for (int bytes : {2, 4})
+    for (int bytes : {2, 4, -2, -4})  // (negative: the backward pass, without a workspace)
         for (int64_t T : {1, 2, 5, 64, 300, 1023, 1024, 5000, 1 << 24})
             for (int64_t V = 1; V < 0x7FFFFFFF; V += V < 70000 ? 1 : 1 + V / 9) {
-                const AdjustPlan p = adjust_plan(T, V, bytes);
+                const AdjustPlan p = adjust_plan(T, V, bytes < 0 ? -bytes : bytes, bytes < 0);
                 const int64_t parts = (int64_t)1 << p.shift;
                 const bool ok = p.part % 512 == 0 && p.part > 0 && p.part <= kAdjustMaxPart && parts * p.part >= V &&
                                 (parts == 1 || V > parts * 512 / 2) &&
-                                adjust_partials_offset(T) + (size_t)T * parts * 8 <= adjust_workspace_bytes(T, V);
+                                (bytes < 0 || adjust_partials_offset(T) + (size_t)T * parts * 8 <= adjust_workspace_bytes(T, V));
                 if (!ok) return std::printf("T %lld V %lld\\n", (long long)T, (long long)V), 1;
             }
     std::printf("ok\\n");
