@@ -410,6 +410,9 @@ typedef enum {
 } a3po_norm_kind;
 
 #define A3PO_NORM_MAX_H 16384
+/* a3po_norm_bwd is one launch, and needs no workspace, for T up to the first, T * H up to the second, and dx neither x nor dy */
+#define A3PO_NORM_ONE_LAUNCH_ROWS 1024
+#define A3PO_NORM_ONE_LAUNCH_ELEMENTS (3 << 20)
 
 /*
  * Layer norm, or its root-mean-square form, of every row:
@@ -434,8 +437,9 @@ int a3po_norm_fwd(const void *x, a3po_dtype x_dt, int64_t T, int64_t H, int64_t 
  * dweight, dbias [H] float, nullable; dbias is NULL for A3PO_NORM_RMS.  accumulate = 1 adds to what they hold
  * (micro-batches of one update), 0 overwrites.  The sums over rows are taken in a fixed order: identical inputs give
  * bit-identical outputs.  T == 0 clears dweight and dbias unless accumulating.
- * workspace: a3po_workspace_bytes(A3PO_WS_NORM_BWD, T, 0, H) bytes, 256-byte aligned (not needed, and NULL, when neither
- * dweight nor dbias is asked for).
+ * workspace: a3po_workspace_bytes(A3PO_WS_NORM_BWD, T, 0, H) bytes, 256-byte aligned.  Not needed, and NULL, when neither
+ * dweight nor dbias is asked for, nor for few rows (A3PO_NORM_ONE_LAUNCH_ROWS,
+ * A3PO_NORM_ONE_LAUNCH_ELEMENTS) whose dx is neither x nor dy: one launch then takes the sums straight from x and dy.
  */
 int a3po_norm_bwd(const void *dy, a3po_dtype y_dt, int64_t lddy, const void *x, a3po_dtype x_dt, int64_t T, int64_t H,
                   int64_t ldx, const void *weight, a3po_dtype param_dt, const float *mean, const float *rstd,

@@ -23,6 +23,7 @@ A3PO_WS_NORM_BWD = 3
 A3PO_WS_ADJUST_LOGITS = 4
 A3PO_WS_W4_LINEAR = 5
 A3PO_NORM_LAYER, A3PO_NORM_RMS = 0, 1
+A3PO_NORM_ONE_LAUNCH_ROWS, A3PO_NORM_ONE_LAUNCH_ELEMENTS = 1024, 3 << 20
 
 # layout of a3po_stats (include/a3po.h)
 STATS_DTYPE = np.dtype([("n_tokens", "<i8"), ("n_clipped", "<i8"), ("n_bad_index", "<i8"),
@@ -521,8 +522,8 @@ def norm_fwd(x, weight=None, bias=None, eps: float = 1e-6, kind: int = A3PO_NORM
 
 def norm_bwd(dy, x, weight, rstd, mean=None, kind: int = A3PO_NORM_LAYER, dx=None, want_dweight=True, want_dbias=False,
              dweight=None, dbias=None, accumulate=False, workspace=None):
-    """a3po_norm_bwd -> dict(dx (x's dtype), dweight f32[H] | None, dbias f32[H] | None, workspace).  ``dx`` may be ``x`` or
-    ``dy`` itself; with ``accumulate`` the sums are added to the given ``dweight`` / ``dbias``."""
+    """a3po_norm_bwd -> dict(dx (x's dtype), dweight f32[H] | None, dbias f32[H] | None, workspace | None).  ``dx`` may be ``x``
+    or ``dy`` itself; with ``accumulate`` the sums are added to the given ``dweight`` / ``dbias``."""
     torch = _torch()
     yd, lddy = _rows(dy, "dy")
     T, H = dy.shape
@@ -544,7 +545,9 @@ def norm_bwd(dy, x, weight, rstd, mean=None, kind: int = A3PO_NORM_LAYER, dx=Non
     for name, t in (("dweight", dweight), ("dbias", dbias)):
         if t is not None:
             _vec(t, torch.float32, H, name)
-    if workspace is None and (dweight is not None or dbias is not None):
+    if workspace is None and (dweight is not None or dbias is not None) and not (
+            T <= A3PO_NORM_ONE_LAUNCH_ROWS and T * H <= A3PO_NORM_ONE_LAUNCH_ELEMENTS
+            and dx.data_ptr() not in (x.data_ptr(), dy.data_ptr())):
         workspace = torch.empty(workspace_bytes(T, 0, H, which=A3PO_WS_NORM_BWD), dtype=torch.uint8, device=dev)
     _check(lib().a3po_norm_bwd(_ptr(dy), yd, lddy, _ptr(x), xd, T, H, ldx, _ptr(weight), _params(weight, None, H),
                                _ptr(mean), _ptr(rstd), int(kind), _ptr(dx), lddx, _ptr(dweight), _ptr(dbias),

@@ -473,7 +473,7 @@ int a3po_norm_bwd(const void *dy, a3po_dtype y_dt, int64_t lddy, const void *x, 
     if (T > 0 && (!dy || !x || !rstd || !dx || (kind == A3PO_NORM_LAYER && !mean))) return A3PO_E_NULL;
     if (!aligned(dy, elem(y_dt)) || !aligned(x, elem(x_dt)) || !aligned(dx, elem(x_dt)) || !aligned(weight, elem(param_dt)))
         return A3PO_E_ALIGN;
-    if (T > 0 && (dweight || dbias)) {
+    if (T > 0 && (dweight || dbias) && !norm_bwd_in_one(T, H, x, dy, dx)) {
         if (!workspace || workspace_bytes < norm_bwd_workspace_bytes(T, H)) return A3PO_E_WORKSPACE;
         if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
     }

@@ -445,6 +445,13 @@ inline int64_t norm_bwd_blocks(int64_t T, int64_t H, int x_bytes)
     const int64_t rows = p.lanes >= 256 ? 1 : 256 / p.lanes, want = (T + rows - 1) / rows;
     return want < kNormMaxBlocks ? want : kNormMaxBlocks;
 }
+// Few rows: the sums over rows are taken by workgroups of the same launch that read x and dy a second time, which dx must
+// therefore leave alone.  Against two kernels, us: fp32 300 x 1,536 4.3 / 9.2, 1,000 x 1,536 8.4 / 10.7, 1,000 x 4,096 17.4 / 15.9;
+// bf16 16 x 4,096 3.7 / 7.0, 300 x 8,192 7.7 / 14.6, 1,000 x 1,536 9.5 / 10.2, 1,000 x 4,096 19.0 / 14.1; a launch less for the host.
+inline bool norm_bwd_in_one(int64_t T, int64_t H, const void *x, const void *dy, const void *dx)
+{
+    return T > 0 && T <= A3PO_NORM_ONE_LAUNCH_ROWS && T * H <= A3PO_NORM_ONE_LAUNCH_ELEMENTS && dx != x && dx != dy;
+}
 inline size_t norm_bwd_workspace_bytes(int64_t T, int64_t H)
 {
     if (T <= 0 || H <= 0 || H > kNormMaxH) return 256;

@@ -10,7 +10,7 @@
 // difference of two sums loses all digits of rows whose mean is large against their spread.
 // The kernels are bound by memory where there are rows enough: the gradient of 65,536 x 4,096 bfloat16 moves 1.61 GB in 280 us
 // (5.8 TB/s), the forward pass of 10,240 x 2,049 fp32 to bfloat16 126 MB in 25.  Fewer rows are a chain of latencies, a load, two
-// reductions and a store: 64 x 1,536 forward 3.5 us, 1,000 x 1,536 backward 7.5 and 3.4 for the sums over rows.
+// reductions and a store: 64 x 1,536 forward 3.5 us, 1,000 x 1,536 backward 8.4.
 #include "a3po_common.h"
 #include "a3po_launch.h"
 
@@ -187,9 +187,83 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(Nor
 
 // Each workgroup takes rows in turn and leaves its share of dw and db in partials [workgroup][dw | db][H]; a second
 // kernel adds the shares in one order, so that identical inputs give identical sums.
-template <typename XT, typename YT, int LANES, int NV, bool CENTER>
-__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(NormArgs a, float *partials)
+// The sums over rows of 4 vectors of columns, straight from x and dy (mean and rstd are known): four lanes read a row's 64 bytes,
+// so that a workgroup takes 64 rows at a time (32 rows of 128 bytes: 1,000 x 1,536 10.3 us, 64: 8.4), three or four rows each in
+// flight; lanes and wavefronts add theirs in a fixed order.  A vector at the end moves down to end with
+// the row, its first columns are another lane's.
+struct ColumnSums {
+    float *dweight, *dbias;
+    int accumulate, blocks;
+};
+constexpr int kColumnLanes = 4;
+template <typename XT, typename YT, int THREADS, bool CENTER>
+__device__ __forceinline__ void column_sums(const NormArgs &a, const ColumnSums &to, int block)
 {
+    constexpr int EPV = kVec<XT>, kInFlight = EPV == 8 ? 3 : 4, kGroups = THREADS / kColumnLanes, kWaves = THREADS / kWave, kCols = kColumnLanes * EPV;
+    __shared__ float part[kWaves][2][kCols];
+    auto first_of = [&](int lane) { return (block * kColumnLanes + lane) * EPV; };
+    auto at_of = [&](int lane) { return max(min(first_of(lane), a.H - EPV), 0); };
+    const int lane = threadIdx.x % kColumnLanes, group = threadIdx.x / kColumnLanes, at = at_of(lane);
+    float dw[EPV], db[EPV];
+#pragma unroll
+    for (int k = 0; k < EPV; ++k) dw[k] = db[k] = 0.0f;
+    for (int64_t t0 = group; t0 < a.T; t0 += kGroups * kInFlight) {
+        float x[kInFlight][EPV], g[kInFlight][EPV], rstd[kInFlight], mean[kInFlight];
+#pragma unroll
+        for (int j = 0; j < kInFlight; ++j) {
+            const int64_t t = min(t0 + j * kGroups, a.T - 1);
+            const char *row = static_cast<const char *>(a.x) + t * a.ldx * XT::kBytes;
+            const char *grow = static_cast<const char *>(a.dy) + t * a.ldy * YT::kBytes;
+            rstd[j] = a.rstd[t];
+            mean[j] = CENTER ? a.mean[t] : 0.0f;
+            if (a.H >= EPV) {
+                load_vec<XT, EPV>(row + at * XT::kBytes, x[j]);
+                load_vec<YT, EPV>(grow + at * YT::kBytes, g[j]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < EPV; ++k) {
+                    x[j][k] = load_elem<XT>(row, min(k, a.H - 1));
+                    g[j][k] = load_elem<YT>(grow, min(k, a.H - 1));
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kInFlight; ++j)
+#pragma unroll
+            for (int k = 0; k < EPV; ++k) {
+                const float v = t0 + j * kGroups < a.T ? g[j][k] : 0.0f;
+                dw[k] = fmaf(v, (CENTER ? x[j][k] - mean[j] : x[j][k]) * rstd[j], dw[k]);
+                if constexpr (CENTER) db[k] += v;
+            }
+    }
+#pragma unroll
+    for (int k = 0; k < EPV; ++k)
+#pragma unroll
+        for (int off = kColumnLanes; off < kWave; off <<= 1) {
+            dw[k] += __shfl_xor(dw[k], off, kWave);
+            if constexpr (CENTER) db[k] += __shfl_xor(db[k], off, kWave);
+        }
+    if (threadIdx.x % kWave < kColumnLanes)
+#pragma unroll
+        for (int k = 0; k < EPV; ++k) {
+            part[threadIdx.x / kWave][0][lane * EPV + k] = dw[k];
+            if constexpr (CENTER) part[threadIdx.x / kWave][1][lane * EPV + k] = db[k];
+        }
+    __syncthreads();
+    const int which = threadIdx.x / kCols, i = threadIdx.x % kCols, first = first_of(i / EPV), column = at_of(i / EPV) + i % EPV;
+    float *out = which == 0 ? to.dweight : to.dbias;
+    if (which > (CENTER ? 1 : 0) || !out || column < first || column >= a.H) return;
+    float total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total += part[w][which][i];
+    out[column] = to.accumulate ? out[column] + total : total;
+}
+
+// With to.blocks, that many workgroups come first that take the sums over rows, and no partial sums are left.
+template <typename XT, typename YT, int LANES, int NV, bool CENTER>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(NormArgs a, float *partials, ColumnSums to)
+{
+    if ((int)blockIdx.x < to.blocks) return column_sums<XT, YT, (LANES > 256 ? LANES : 256), CENTER>(a, to, (int)blockIdx.x);
     constexpr int EPV = kVec<XT>, kRows = LANES >= 256 ? 1 : 256 / LANES;
     __shared__ float red[2][2 * (LANES / kWave)];
     int phase = 0;
@@ -207,8 +281,8 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(Nor
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int k = 0; k < EPV; ++k) dw[i][k] = db[i][k] = 0.0f;
-    const int64_t stride = (int64_t)gridDim.x * kRows;
-    for (int64_t t = (int64_t)blockIdx.x * kRows + group; t < a.T; t += stride) {
+    const int64_t stride = (int64_t)(gridDim.x - to.blocks) * kRows;
+    for (int64_t t = (int64_t)(blockIdx.x - to.blocks) * kRows + group; t < a.T; t += stride) {
         const char *row = static_cast<const char *>(a.x) + t * a.ldx * XT::kBytes;
         const char *grow = static_cast<const char *>(a.dy) + t * a.ldy * YT::kBytes;
         char *out = static_cast<char *>(a.dx) + t * a.lddx * XT::kBytes;
@@ -330,14 +404,14 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(const float *partial
 }
 
 template <typename XT, typename YT, int LANES, int NV>
-hipError_t launch(const NormArgs &a, bool backward, float *partials, int64_t blocks, hipStream_t s)
+hipError_t launch(const NormArgs &a, bool backward, float *partials, int64_t blocks, const ColumnSums &to, hipStream_t s)
 {
     constexpr int kThreads = LANES > 256 ? LANES : 256;
-    const dim3 grid((unsigned)blocks), block(kThreads);
+    const dim3 grid((unsigned)(blocks + to.blocks)), block(kThreads);
     if (backward) {
         const size_t lds = LANES < 256 && partials ? (size_t)8 * ((a.H + 3) / 4 * 4) : 0;
-        if (a.center) norm_bwd_kernel<XT, YT, LANES, NV, true><<<grid, block, lds, s>>>(a, partials);
-        else norm_bwd_kernel<XT, YT, LANES, NV, false><<<grid, block, lds, s>>>(a, partials);
+        if (a.center) norm_bwd_kernel<XT, YT, LANES, NV, true><<<grid, block, lds, s>>>(a, partials, to);
+        else norm_bwd_kernel<XT, YT, LANES, NV, false><<<grid, block, lds, s>>>(a, partials, to);
     } else if constexpr (XT::kBytes == 4 || LANES > 64 || NV < 4) {  // (the plan gives the forward pass no four of bf16)
         if (a.center) norm_fwd_kernel<XT, YT, LANES, NV, true><<<grid, block, 0, s>>>(a);
         else norm_fwd_kernel<XT, YT, LANES, NV, false><<<grid, block, 0, s>>>(a);
@@ -346,12 +420,12 @@ hipError_t launch(const NormArgs &a, bool backward, float *partials, int64_t blo
 }
 
 template <typename XT, typename YT>
-hipError_t launch_of(const NormArgs &a, bool backward, float *partials, int64_t blocks, hipStream_t s)
+hipError_t launch_of(const NormArgs &a, bool backward, float *partials, int64_t blocks, const ColumnSums &to, hipStream_t s)
 {
     const NormPlan p = norm_plan(a.T, a.H, XT::kBytes, backward);
     // (norm_plan gives no other pair)
 #define A3PO_NORM_CASE(L, N) \
-    if (p.lanes == L && p.vectors == N) return launch<XT, YT, L, N>(a, backward, partials, blocks, s)
+    if (p.lanes == L && p.vectors == N) return launch<XT, YT, L, N>(a, backward, partials, blocks, to, s)
     A3PO_NORM_CASE(64, 1);
     A3PO_NORM_CASE(64, 2);
     A3PO_NORM_CASE(64, 3);
@@ -369,13 +443,13 @@ hipError_t launch_of(const NormArgs &a, bool backward, float *partials, int64_t 
     return hipErrorInvalidValue;
 }
 
-hipError_t launch_any(const NormArgs &a, bool backward, float *partials, int64_t blocks, hipStream_t s)
+hipError_t launch_any(const NormArgs &a, bool backward, float *partials, int64_t blocks, const ColumnSums &to, hipStream_t s)
 {
     if (a.x_dt == A3PO_F32)
-        return a.y_dt == A3PO_F32 ? launch_of<F32, F32>(a, backward, partials, blocks, s)
-                                  : launch_of<F32, Bf16>(a, backward, partials, blocks, s);
-    return a.y_dt == A3PO_F32 ? launch_of<Bf16, F32>(a, backward, partials, blocks, s)
-                              : launch_of<Bf16, Bf16>(a, backward, partials, blocks, s);
+        return a.y_dt == A3PO_F32 ? launch_of<F32, F32>(a, backward, partials, blocks, to, s)
+                                  : launch_of<F32, Bf16>(a, backward, partials, blocks, to, s);
+    return a.y_dt == A3PO_F32 ? launch_of<Bf16, F32>(a, backward, partials, blocks, to, s)
+                              : launch_of<Bf16, Bf16>(a, backward, partials, blocks, to, s);
 }
 
 }  // namespace
@@ -385,18 +459,24 @@ hipError_t launch_norm_fwd(const NormArgs &a, hipStream_t s)
     const NormPlan p = norm_plan(a.T, a.H, a.x_dt == A3PO_F32 ? 4 : 2, false);
     const int rows = p.lanes >= 256 ? 1 : 256 / p.lanes;
     const int64_t want = (a.T + rows - 1) / rows, most = 4096;
-    return launch_any(a, false, nullptr, want < most ? want : most, s);
+    return launch_any(a, false, nullptr, want < most ? want : most, ColumnSums{}, s);
 }
 
 hipError_t launch_norm_bwd(const NormArgs &a, float *dweight, float *dbias, int accumulate, void *workspace, hipStream_t s)
 {
-    const int64_t blocks = norm_bwd_blocks(a.T, a.H, a.x_dt == A3PO_F32 ? 4 : 2);
+    const int x_bytes = a.x_dt == A3PO_F32 ? 4 : 2;
+    const int64_t blocks = norm_bwd_blocks(a.T, a.H, x_bytes);
     NormArgs b = a;
     b.partial_rows = dbias ? 2 : 1;
-    float *partials = dweight || dbias ? static_cast<float *>(workspace) : nullptr;
+    const bool sums = dweight || dbias;
+    if (sums && norm_bwd_in_one(a.T, a.H, a.x, a.dy, a.dx)) {
+        const int columns = kColumnLanes * 16 / x_bytes;
+        return launch_any(b, true, nullptr, blocks, ColumnSums{dweight, dbias, accumulate, (a.H + columns - 1) / columns}, s);
+    }
+    float *partials = sums ? static_cast<float *>(workspace) : nullptr;
     if (a.T > 0)
-        if (const hipError_t e = launch_any(b, true, partials, blocks, s)) return e;
-    if (!dweight && !dbias) return hipSuccess;
+        if (const hipError_t e = launch_any(b, true, partials, blocks, ColumnSums{}, s)) return e;
+    if (!sums) return hipSuccess;
     const int64_t width = b.partial_rows * a.H;
     norm_bwd_sum_kernel<<<dim3((unsigned)((width + 31) / 32)), dim3(1024), 0, s>>>(
         partials, a.T > 0 ? (int)blocks : 0, width, a.H, dweight, dbias, accumulate);

@@ -259,3 +259,43 @@ def test_on_another_stream(a3po):
         got = a3po.norm_fwd(xg, wg, bg)[0]
     s.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("H", WIDTHS)
+@pytest.mark.parametrize("xt,yt", [("bf16", "bf16"), ("f32", "bf16")])
+def test_backward_in_place_takes_the_sums_from_partial_ones(a3po, H, xt, yt):
+    """dx over x: the sums cannot be taken from x and dy a second time."""
+    x, w, _, g = _inputs(7, H, DT[xt], DT[xt], seed=H + 2)
+    dy = torch.randn(7, H, generator=g).to(DT[yt])
+    xg = x.cuda()
+    out = _check_backward(a3po, x, w, dy, True, dx=xg, dev=(xg, dy.cuda()))
+    assert out["workspace"] is not None
+
+
+@pytest.mark.parametrize("T", [1, 2, 63, 64, 65, 192, 193, 255, 256, 257, 511, 1023, 1024, 1025])
+@pytest.mark.parametrize("H,xt", [(96, "f32"), (97, "bf16"), (3, "bf16"), (1001, "f32"), (1536, "bf16")])
+@pytest.mark.parametrize("layer", [True, False], ids=["layer", "rms"])
+def test_sums_over_few_rows_in_one_launch(a3po, T, H, xt, layer):
+    x, w, _, g = _inputs(T, H, DT[xt], DT[xt], seed=T + H)
+    dy = torch.randn(T, H, generator=g).to(DT[xt])
+    out = _check_backward(a3po, x, w, dy, layer)
+    assert (out["workspace"] is None) == (T <= a3po.A3PO_NORM_ONE_LAUNCH_ROWS)
+    again = _check_backward(a3po, x, w, dy, layer)
+    assert torch.equal(out["dweight"], again["dweight"])
+
+
+def test_where_the_sums_need_a_workspace(a3po):
+    x = torch.randn(1024, 3074, device="cuda")       # (beyond A3PO_NORM_ONE_LAUNCH_ELEMENTS)
+    rstd = torch.ones(1024, device="cuda")
+    assert x.numel() > a3po.A3PO_NORM_ONE_LAUNCH_ELEMENTS
+    many = a3po.norm_bwd(x, x, None, rstd, kind=a3po.A3PO_NORM_RMS)
+    few = a3po.norm_bwd(x[:512], x[:512], None, rstd[:512], kind=a3po.A3PO_NORM_RMS)
+    assert many["workspace"] is not None and few["workspace"] is None
+    rest = a3po.norm_bwd(x[512:], x[512:], None, rstd[512:], kind=a3po.A3PO_NORM_RMS, dweight=few["dweight"], accumulate=True)
+    bar = 128 * U * (x.double() ** 2).sum(0)
+    assert ((rest["dweight"].double() - (x.double() ** 2).sum(0)).abs() <= bar).all()
+    assert ((many["dweight"].double() - (x.double() ** 2).sum(0)).abs() <= bar).all()
+    y = x[:8].clone()                                # dx over x: refused before anything runs
+    rc = a3po.lib().a3po_norm_bwd(x.data_ptr(), 0, 3074, y.data_ptr(), 0, 8, 3074, 3074, None, 0, None, rstd.data_ptr(), 1,
+                                  y.data_ptr(), 3074, many["dweight"].data_ptr(), None, 0, None, 0, None)
+    assert rc < 0 and "workspace" in a3po.binding.strerror(rc)
