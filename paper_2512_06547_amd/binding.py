@@ -476,31 +476,38 @@ def fused_lmhead_loss_fwd_bwd(hidden, weight, chosen, logp_behav, versions, curr
 # ---- operators around the log-probs ----------------------------------------------------------------------------------
 
 
+_DTYPE_CODES: dict = {}
+
+
 def _dtype_code(t, name):
-    torch = _torch()
-    if t.dtype == torch.bfloat16:
-        return A3PO_BF16
-    if t.dtype == torch.float32:
-        return A3PO_F32
-    raise TypeError(f"{name} must be float32 or bfloat16")
+    if not _DTYPE_CODES:
+        torch = _torch()
+        _DTYPE_CODES.update({torch.float32: A3PO_F32, torch.bfloat16: A3PO_BF16})
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    return code
 
 
 def _rows(t, name, shape=None):
     """(dtype code, row stride) of a row-major matrix on the GPU."""
-    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), f"{name} must be a row-major CUDA matrix"
-    assert shape is None or tuple(t.shape) == shape, f"{name}: need shape {shape}"
-    return _dtype_code(t, name), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    size = t.shape
+    assert t.is_cuda and len(size) == 2, f"{name} must be a row-major CUDA matrix"
+    ld, step = t.stride()
+    assert step == 1 or size[1] == 1, f"{name} must be a row-major CUDA matrix"
+    assert shape is None or size == shape, f"{name}: need shape {shape}"
+    return _dtype_code(t, name), ld if size[0] > 1 else max(ld, size[1])
 
 
 def _params(weight, bias, H):
     """The dtype code that weight and bias share."""
-    code = None
-    for name, t in (("weight", weight), ("bias", bias)):
-        if t is not None:
-            _vec(t, t.dtype, H, name)
-            assert code is None or code == _dtype_code(t, name), "weight and bias must have one dtype"
-            code = _dtype_code(t, name)
-    return A3PO_F32 if code is None else code
+    if bias is not None:
+        _vec(bias, bias.dtype, H, "bias")
+        assert weight is None or weight.dtype == bias.dtype, "weight and bias must have one dtype"
+    if weight is not None:
+        _vec(weight, weight.dtype, H, "weight")
+        return _dtype_code(weight, "weight")
+    return A3PO_F32 if bias is None else _dtype_code(bias, "bias")
 
 
 def norm_fwd(x, weight=None, bias=None, eps: float = 1e-6, kind: int = A3PO_NORM_LAYER, out=None, out_dtype=None,
