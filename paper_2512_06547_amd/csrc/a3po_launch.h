@@ -446,8 +446,9 @@ inline int64_t norm_bwd_blocks(int64_t T, int64_t H, int x_bytes)
     return want < kNormMaxBlocks ? want : kNormMaxBlocks;
 }
 // Few rows: the sums over rows are taken by workgroups of the same launch that read x and dy a second time, which dx must
-// therefore leave alone.  Against two kernels, us: fp32 300 x 1,536 4.3 / 9.2, 1,000 x 1,536 8.4 / 10.7, 1,000 x 4,096 17.4 / 15.9;
-// bf16 16 x 4,096 3.7 / 7.0, 300 x 8,192 7.7 / 14.6, 1,000 x 1,536 9.5 / 10.2, 1,000 x 4,096 19.0 / 14.1; a launch less for the host.
+// therefore leave alone.  Against two kernels, us, inputs from memory: fp32 16 x 4,096 3.8 / 7.2, 300 x 1,536 5.4 / 9.8, 1,000 x
+// 1,536 11.8 / 10.7, 1,000 x 3,000 14.8 / 15.5; bf16 300 x 8,192 9.2 / 15.6, 1,000 x 1,536 12.7 / 10.3, 1,000 x 3,000 14.0 / 14.1,
+// beside the gap between two and the 4 us that a launch takes the host; 1,000 x 4,096 17.4 / 15.9 and 19.0 / 14.1.
 inline bool norm_bwd_in_one(int64_t T, int64_t H, const void *x, const void *dy, const void *dx)
 {
     return T > 0 && T <= A3PO_NORM_ONE_LAUNCH_ROWS && T * H <= A3PO_NORM_ONE_LAUNCH_ELEMENTS && dx != x && dx != dy;

@@ -10,7 +10,9 @@
 // difference of two sums loses all digits of rows whose mean is large against their spread.
 // The kernels are bound by memory where there are rows enough: the gradient of 65,536 x 4,096 bfloat16 moves 1.61 GB in 280 us
 // (5.8 TB/s), the forward pass of 10,240 x 2,049 fp32 to bfloat16 126 MB in 25.  Fewer rows are a chain of latencies, a load, two
-// reductions and a store: 64 x 1,536 forward 3.5 us, 1,000 x 1,536 backward 8.4.
+// reductions and a store: 64 x 1,536 forward 3.5 us, 1,000 x 1,536 fp32 backward 11.8.
+#include <type_traits>
+
 #include "a3po_common.h"
 #include "a3po_launch.h"
 
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(Nor
 // Each workgroup takes rows in turn and leaves its share of dw and db in partials [workgroup][dw | db][H]; a second
 // kernel adds the shares in one order, so that identical inputs give identical sums.
 // The sums over rows of 4 vectors of columns, straight from x and dy (mean and rstd are known): four lanes read a row's 64 bytes,
-// so that a workgroup takes 64 rows at a time (32 rows of 128 bytes: 1,000 x 1,536 10.3 us, 64: 8.4), three or four rows each in
+// so that a workgroup takes 64 rows at a time (32 rows of 128 bytes: a fifth more time), three or four rows each in
 // flight; lanes and wavefronts add theirs in a fixed order.  A vector at the end moves down to end with
 // the row, its first columns are another lane's.
 struct ColumnSums {
@@ -207,35 +209,41 @@ __device__ __forceinline__ void column_sums(const NormArgs &a, const ColumnSums 
     float dw[EPV], db[EPV];
 #pragma unroll
     for (int k = 0; k < EPV; ++k) dw[k] = db[k] = 0.0f;
-    for (int64_t t0 = group; t0 < a.T; t0 += kGroups * kInFlight) {
-        float x[kInFlight][EPV], g[kInFlight][EPV], rstd[kInFlight], mean[kInFlight];
+    // (rows shorter than a vector are read by elements; which, is asked once: loads on either side of a branch are waited for there)
+    auto sum_rows = [&](auto whole) {
+        for (int64_t t0 = group; t0 < a.T; t0 += kGroups * kInFlight) {
+            float x[kInFlight][EPV], g[kInFlight][EPV], rstd[kInFlight], mean[kInFlight];
 #pragma unroll
-        for (int j = 0; j < kInFlight; ++j) {
-            const int64_t t = min(t0 + j * kGroups, a.T - 1);
-            const char *row = static_cast<const char *>(a.x) + t * a.ldx * XT::kBytes;
-            const char *grow = static_cast<const char *>(a.dy) + t * a.ldy * YT::kBytes;
-            rstd[j] = a.rstd[t];
-            mean[j] = CENTER ? a.mean[t] : 0.0f;
-            if (a.H >= EPV) {
-                load_vec<XT, EPV>(row + at * XT::kBytes, x[j]);
-                load_vec<YT, EPV>(grow + at * YT::kBytes, g[j]);
-            } else {
+            for (int j = 0; j < kInFlight; ++j) {
+                const int64_t t = min(t0 + j * kGroups, a.T - 1);
+                const char *row = static_cast<const char *>(a.x) + t * a.ldx * XT::kBytes;
+                const char *grow = static_cast<const char *>(a.dy) + t * a.ldy * YT::kBytes;
+                rstd[j] = a.rstd[t];
+                mean[j] = CENTER ? a.mean[t] : 0.0f;
+                if constexpr (whole) {
+                    load_vec<XT, EPV>(row + at * XT::kBytes, x[j]);
+                    load_vec<YT, EPV>(grow + at * YT::kBytes, g[j]);
+                } else {
 #pragma unroll
-                for (int k = 0; k < EPV; ++k) {
-                    x[j][k] = load_elem<XT>(row, min(k, a.H - 1));
-                    g[j][k] = load_elem<YT>(grow, min(k, a.H - 1));
+                    for (int k = 0; k < EPV; ++k) {
+                        x[j][k] = load_elem<XT>(row, min(k, a.H - 1));
+                        g[j][k] = load_elem<YT>(grow, min(k, a.H - 1));
+                    }
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < kInFlight; ++j)
+#pragma unroll
+                for (int k = 0; k < EPV; ++k) {
+                    const float v = t0 + j * kGroups < a.T ? g[j][k] : 0.0f;
+                    dw[k] = fmaf(v, (CENTER ? x[j][k] - mean[j] : x[j][k]) * rstd[j], dw[k]);
+                    if constexpr (CENTER) db[k] += v;
+                }
         }
-#pragma unroll
-        for (int j = 0; j < kInFlight; ++j)
-#pragma unroll
-            for (int k = 0; k < EPV; ++k) {
-                const float v = t0 + j * kGroups < a.T ? g[j][k] : 0.0f;
-                dw[k] = fmaf(v, (CENTER ? x[j][k] - mean[j] : x[j][k]) * rstd[j], dw[k]);
-                if constexpr (CENTER) db[k] += v;
-            }
-    }
+    };
+    if (a.H >= EPV) sum_rows(std::true_type{});
+    else sum_rows(std::false_type{});
 #pragma unroll
     for (int k = 0; k < EPV; ++k)
 #pragma unroll
