@@ -13,12 +13,12 @@
 // order of additions), and the entries join the sum and the output.  A test per entry with the penalties behind it costs more
 // than the exponential, and the work on the history, the reductions and the row's parameters cost what some forty entries a
 // thread do, so that rows are not cut further than it takes to fill the chip (scoring of 8,192 x 50,001 bfloat16: a test per
-// entry, four parts a row 1,055 us; a penalty per entry in LDS 553; bits, four parts 735; bits, whole rows 306; now 280).
-// What bounds it: scoring, 819 MB in 280 us, the vector instructions (212 us without a history, 31 for the bits, 16 for the
-// counts, 36 for the entries); decoding, 64 x 151,936 to fp32 with 16,384 tokens of history, 33 us, the passes over the history
+// entry, four parts a row 1,055 us; a penalty per entry in LDS 553; bits, four parts 735; bits, whole rows 306; now 227).
+// What bounds it: scoring, 819 MB in 227 us (3.6 TB/s), the vector instructions and the history's latencies (with workgroups of
+// 512, 280 us: 212 without a history, 31 for the bits, 16 for the counts, 36 for the entries); decoding, 64 x 151,936 to fp32 with 16,384 tokens of history, 33 us, the passes over the history
 // (18 us without one); the gradient, two streams and little else, memory: 8,192 x 151,936 4.98 GB in 1,050 us (4.7 TB/s, what a large copy reaches).
-// Rows are read and written through the caches: the entries of the history are fetched a second time (non-temporal: scoring
-// 301 us, decoding 38), and the next kernel reads what is written here.
+// Rows are read and written through the caches: the entries of the history are fetched a second time (non-temporal: 301 for
+// 281 us, decoding 42 for 38), and the next kernel reads what is written here.
 // Maximum and sum of exp are taken before the temperature, which then is part of the exponent's scale.  All arithmetic is
 // fp32; what is stored in bfloat16 is rounded once, and lse and logp are those of the fp32 values.
 #include "a3po_common.h"
@@ -27,7 +27,6 @@
 namespace a3po {
 namespace {
 
-constexpr int kThreads = kAdjustThreads;
 constexpr float kInf = __builtin_huge_valf(), kLowest = -3.402823466e38f;
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -86,11 +85,11 @@ struct Part {
 
 // f(places, valid, output) for the tokens of the row's history, four at a time: places[k] is the k-th one's entry in the part
 // if bit k of `valid` says that it is one of the part's; bit k of `output`: it is behind the prompt
-template <typename F>
+template <int THREADS, typename F>
 __device__ __forceinline__ void each_tokens(const AdjustArgs &a, const RowPolicy &p, const Part &part, F f)
 {
     const int32_t *h = a.history + p.start;
-    constexpr uint32_t kLoads = 4, kRound = kThreads * 4 * kLoads;
+    constexpr uint32_t kLoads = 4, kRound = THREADS * 4 * kLoads;
     const uint32_t len = (uint32_t)p.len, prompt = (uint32_t)max(p.prompt, 0), lane = threadIdx.x;
     auto one = [&](int32_t id, uint32_t at_history, int k, uint32_t(&at)[4], uint32_t &valid, uint32_t &output) {
         valid |= (part.has(id, a.V, at[k]) ? 1u : 0u) << k;
@@ -100,30 +99,31 @@ __device__ __forceinline__ void each_tokens(const AdjustArgs &a, const RowPolicy
     for (; len - i >= kRound; i += kRound) {
         i32x4_any v[kLoads];
 #pragma unroll
-        for (uint32_t j = 0; j < kLoads; ++j) v[j] = *reinterpret_cast<const i32x4_any *>(h + i + (j * kThreads + lane) * 4);
+        for (uint32_t j = 0; j < kLoads; ++j) v[j] = *reinterpret_cast<const i32x4_any *>(h + i + (j * THREADS + lane) * 4);
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j) {
             uint32_t at[4], valid = 0, output = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) one(v[j][k], i + (j * kThreads + lane) * 4 + k, k, at, valid, output);
+            for (int k = 0; k < 4; ++k) one(v[j][k], i + (j * THREADS + lane) * 4 + k, k, at, valid, output);
             f(at, valid, output);
         }
     }
-    for (; i < len; i += kThreads * kLoads) {
+    for (; i < len; i += THREADS * kLoads) {
         int32_t v[kLoads];
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j) {
-            const uint32_t at = i + j * kThreads + lane;
+            const uint32_t at = i + j * THREADS + lane;
             v[j] = at < len ? h[at] : -1;
         }
         uint32_t at[4], valid = 0, output = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) one(v[k], i + k * kThreads + lane, k, at, valid, output);
+        for (int k = 0; k < 4; ++k) one(v[k], i + k * THREADS + lane, k, at, valid, output);
         f(at, valid, output);
     }
 }
 
 // The part's entries that are in the row's history: a bit each, and the numbers of those entries.
+template <int THREADS>
 struct Seen {
     static constexpr int kBlock = 16;  // words whose numbers share a base
     uint32_t *words;                   // [part / 32]
@@ -144,9 +144,9 @@ struct Seen {
     {
         int listed = 0;
         __syncthreads();  // (the part before this one is done with the bits)
-        for (int w = threadIdx.x; w < nwords / 4; w += kThreads) reinterpret_cast<uint4 *>(words)[w] = make_uint4(0, 0, 0, 0);
+        for (int w = threadIdx.x; w < nwords / 4; w += THREADS) reinterpret_cast<uint4 *>(words)[w] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        each_tokens(a, p, part, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
+        each_tokens<THREADS>(a, p, part, [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
             // (most of a text's tokens are there already: looking first spares the atomics that all would aim at a few words)
             uint32_t have[4];
 #pragma unroll
@@ -191,7 +191,7 @@ struct Seen {
         __syncthreads();
         int base = 0, total = 0;
 #pragma unroll
-        for (int w = 0; w < kThreads / kWave; ++w) {
+        for (int w = 0; w < THREADS / kWave; ++w) {
             base += w < wave ? waves[w] : 0;
             total += waves[w];
         }
@@ -337,10 +337,10 @@ __device__ __host__ constexpr int numbers_of(int part) { return part <= (1 << 16
 __device__ __host__ constexpr int seen_bytes(int part, bool numbers) { return part / 8 + (numbers ? part / 128 + part / 16 : 0); }
 // Tokens that a wavefront notes while it marks them, 4 bytes each, so that they are counted from there: what four workgroups
 // a compute unit leave of the LDS.
-__device__ __host__ constexpr int listed_of(int part)
+__device__ __host__ constexpr int listed_of(int part, int threads)
 {
     const int left = 160 * 1024 / 4 - 512 - seen_bytes(part, true) - 8 * numbers_of(part);
-    return left > 4096 ? left / (4 * kThreads / kWave) & ~1 : 128;
+    return (left > 4096 ? left / 4 : 1024) / (threads / kWave) & ~1;
 }
 
 // what is told of a row: of its (max, sum), and of the chosen token's adjusted logit before the temperature
@@ -354,20 +354,20 @@ __device__ __forceinline__ void finish_row(const AdjustArgs &a, int64_t t, MaxSu
     }
 }
 
-template <typename ZT, typename UT, int NV>
-__global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
+template <typename ZT, typename UT, int NV, int THREADS>
+__global__ __launch_bounds__(THREADS, 4) void adjust_kernel(AdjustArgs a)
 {
-    constexpr int EPV = ZT::kPerVec, kWaves = kThreads / kWave, kStep = kThreads * EPV * NV;
+    constexpr int EPV = ZT::kPerVec, kWaves = THREADS / kWave, kStep = THREADS * EPV * NV;
     constexpr uint32_t kAll = (1u << EPV) - 1;
     extern __shared__ __align__(16) char lds[];
     __shared__ float red[2 * kWaves];
     __shared__ int waves[kWaves];
     __shared__ float u_chosen;
-    Seen seen(lds, a.part);
+    Seen<THREADS> seen(lds, a.part);
     const int room = numbers_of(a.part);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane_e = (threadIdx.x & (kWave - 1)) * EPV;
     uint32_t *counts = reinterpret_cast<uint32_t *>(lds + seen_bytes(a.part, true)), *places = counts + room;
-    const int list_room = listed_of(a.part);
+    const int list_room = listed_of(a.part, THREADS);
     uint32_t *list = places + room + wave * list_room;
     const int64_t items = a.T << a.parts_shift;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
         const int y = a.logp && part.has(a.chosen[t], a.V, y_at) ? (int)y_at : -1;
         const float scale = p.inv_temperature * kLog2e;
         const bool hist = p.len > 0 && (p.repetition != 1.0f || p.frequency != 0.0f || p.presence != 0.0f);
-        const int listed = hist ? __builtin_amdgcn_readfirstlane(seen.mark<true>(a, p, part, list, list_room)) : 0;
+        const int listed = hist ? __builtin_amdgcn_readfirstlane(seen.template mark<true>(a, p, part, list, list_room)) : 0;
 
         MaxSum acc = {kLowest, 0.0f};
         for (int at = 0; at < whole; at += kStep) {
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
                     continue;
                 }
                 raw[i].widen(f + i * EPV);
-                const uint32_t later = hist ? seen.bits<EPV>(e) : 0u;
+                const uint32_t later = hist ? seen.template bits<EPV>(e) : 0u;
                 if (bias) {
                     float b[EPV];
                     load_bias<EPV>(bias + id + lane_e, b);
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
         for (int base = 0; base < numbers; base += room) {
             const int many = min(numbers - base, room);
             __syncthreads();  // (the numbers are there, the row is written, the counts before these are done with)
-            for (int i = threadIdx.x; i < many; i += kThreads) counts[i] = 0;
+            for (int i = threadIdx.x; i < many; i += THREADS) counts[i] = 0;
             __syncthreads();
             // (a token that is there more than once notes the same place)
             auto count_tokens = [&](const uint32_t(&at)[4], uint32_t valid, uint32_t output) {
@@ -509,17 +509,17 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
                     count_tokens(at, valid, output);
                 }
             } else {
-                each_tokens(a, p, part, count_tokens);
+                each_tokens<THREADS>(a, p, part, count_tokens);
             }
             __syncthreads();
             constexpr int kBatch = 4;  // (a thread's loads in flight)
-            for (int i = threadIdx.x; i < many; i += kThreads * kBatch) {
+            for (int i = threadIdx.x; i < many; i += THREADS * kBatch) {
                 int at[kBatch];
                 float v[kBatch], b[kBatch], m = acc.m;
                 bool ok[kBatch];
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
-                    at[k] = (int)places[min(i + k * kThreads, many - 1)];
+                    at[k] = (int)places[min(i + k * THREADS, many - 1)];
                     const uint32_t id = part.id(at[k]);
                     v[k] = load_elem<ZT>(row, id);
                     b[k] = bias_of(id);
@@ -527,8 +527,8 @@ __global__ __launch_bounds__(kThreads, 4) void adjust_kernel(AdjustArgs a)
                 }
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
-                    const bool there = i + k * kThreads < many;
-                    const uint32_t n = there ? counts[i + k * kThreads] : 0;
+                    const bool there = i + k * THREADS < many;
+                    const uint32_t n = there ? counts[i + k * THREADS] : 0;
                     v[k] *= v[k] > 0.0f ? down : p.repetition;
                     if (n) v[k] -= fmaf(p.frequency, (float)n, p.presence);
                     v[k] = there && ok[k] ? v[k] + b[k] : -kInf;
@@ -576,12 +576,12 @@ __global__ __launch_bounds__(256) void adjust_finish_kernel(AdjustArgs a)
 }
 
 template <typename ZT, typename UT, int NV>
-__global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
+__global__ __launch_bounds__(kAdjustThreads) void adjust_bwd_kernel(AdjustArgs a)
 {
-    constexpr int EPV = ZT::kPerVec, kWaves = kThreads / kWave, kStep = kThreads * EPV * NV;
+    constexpr int EPV = ZT::kPerVec, kWaves = kAdjustThreads / kWave, kStep = kAdjustThreads * EPV * NV;
     constexpr uint32_t kAll = (1u << EPV) - 1;
     extern __shared__ __align__(16) char lds[];
-    Seen seen(lds, a.part);
+    Seen<kAdjustThreads> seen(lds, a.part);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane_e = (threadIdx.x & (kWave - 1)) * EPV;
     const int64_t items = a.T << a.parts_shift;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -659,13 +659,14 @@ __global__ __launch_bounds__(kThreads) void adjust_bwd_kernel(AdjustArgs a)
 }
 
 template <typename ZT, typename UT>
-hipError_t launch(const AdjustArgs &a, hipStream_t s)
+hipError_t launch(const AdjustArgs &a, int threads, hipStream_t s)
 {
     const int64_t items = a.T << a.parts_shift, most = 1 << 20;
-    const dim3 grid((unsigned)(items < most ? items : most)), block(kThreads);
-    const size_t lds = a.history ? seen_bytes(a.part, !a.dz) + (a.dz ? 0 : 8 * numbers_of(a.part) + 4 * listed_of(a.part) * (kThreads / kWave)) : 0;
+    const dim3 grid((unsigned)(items < most ? items : most)), block(threads);
+    const size_t lds = a.history ? seen_bytes(a.part, !a.dz) + (a.dz ? 0 : 8 * numbers_of(a.part) + 4 * listed_of(a.part, threads) * (threads / kWave)) : 0;
     if (a.dz) adjust_bwd_kernel<ZT, UT, 2><<<grid, block, lds, s>>>(a);
-    else adjust_kernel<ZT, UT, 2><<<grid, block, lds, s>>>(a);
+    else if (threads == kAdjustThreads) adjust_kernel<ZT, UT, 2, kAdjustThreads><<<grid, block, lds, s>>>(a);
+    else adjust_kernel<ZT, UT, 2, kAdjustThreads / 2><<<grid, block, lds, s>>>(a);
     return hipGetLastError();
 }
 
@@ -674,11 +675,12 @@ hipError_t launch(const AdjustArgs &a, hipStream_t s)
 hipError_t launch_adjust(AdjustArgs a, hipStream_t s)
 {
     const AdjustPlan p = adjust_plan(a.T, a.V, a.z_dt == A3PO_F32 ? 4 : 2, a.dz != nullptr);
+    const int threads = a.dz ? kAdjustThreads : adjust_threads(a.T, p, a.u != nullptr);
     a.parts_shift = p.shift;
     a.part = p.part;
     hipError_t e;
-    if (a.z_dt == A3PO_F32) e = a.u_dt == A3PO_F32 ? launch<F32, F32>(a, s) : launch<F32, Bf16>(a, s);
-    else e = a.u_dt == A3PO_F32 ? launch<Bf16, F32>(a, s) : launch<Bf16, Bf16>(a, s);
+    if (a.z_dt == A3PO_F32) e = a.u_dt == A3PO_F32 ? launch<F32, F32>(a, threads, s) : launch<F32, Bf16>(a, threads, s);
+    else e = a.u_dt == A3PO_F32 ? launch<Bf16, F32>(a, threads, s) : launch<Bf16, Bf16>(a, threads, s);
     if (e != hipSuccess || a.dz || !a.ws_partials || a.parts_shift == 0) return e;
     const int64_t want = (a.T + 3) / 4, most = 1 << 20;
     adjust_finish_kernel<<<dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s>>>(a);

@@ -510,6 +510,17 @@ inline AdjustPlan adjust_plan(int64_t T, int64_t V, int z_bytes, bool backward =
     p.part = (int)((blocks + (1 << p.shift) - 1) >> p.shift) * 512;
     return p;
 }
+// Threads of a forward workgroup.  A compute unit's registers hold two of 512 or four of 256, which have half of the work that each
+// wavefront has besides the entries, and more rows whose latencies cover one another's; a few long parts, which LDS holds two of,
+// keep 512, and so do rows that are written, memory's more than the units', where 512 end in fewer rounds.  512 / 256, us: scoring
+// 8,192 x 50,001 315 / 248, 3,000 x 32,000 83 / 65, 1,036 x 87,709 65 / 66, 500 x 65,000 in halves 28 / 22, 2,500 x 151,936 183 / 193
+// (halves); written 300 x 50,001 in halves 32 / 28, 256 x 151,936 in quarters 94 / 90, 150 x 151,936 in eighths 50 / 57, 1,300 x 87,709
+// 177 / 187; 64 x 151,936 in eighths, 16,384 tokens of history 33 / 42.
+inline int adjust_threads(int64_t T, const AdjustPlan &p, bool written)
+{
+    const int64_t items = T << p.shift, rounds = (items + 511) / 512, rounds256 = (items + 1023) / 1024 * 2;
+    return items > 512 && p.part <= 1 << 17 && (!written || rounds256 <= rounds) ? kAdjustThreads / 2 : kAdjustThreads;
+}
 // workspace: the chosen tokens' adjusted logits, then a (max, sum) per part
 inline size_t adjust_partials_offset(int64_t T) { return ((size_t)T * 4 + 255) / 256 * 256; }
 inline size_t adjust_workspace_bytes(int64_t T, int64_t V)

@@ -380,3 +380,19 @@ def test_more_rows_than_workgroups(a3po):
     ref = torch.log_softmax(u, 1).gather(1, y.clamp(min=0).long()[:, None])[:, 0].masked_fill(y < 0, 0.0)
     for got, ref in ((r["logp"], ref), (r["lse"], torch.logsumexp(u, 1))):
         assert ((got.double() - ref).abs() <= 1e-5 * (1 + ref.abs())).all()
+
+
+@pytest.mark.parametrize("T,V,zt,ut,write", [(600, 1000, "bf16", "bf16", True), (700, 517, "f32", "f32", True), (600, 1000, "bf16", "f32", False),
+                                             (1025, 130, "f32", "bf16", True), (1025, 131, "bf16", "bf16", False), (300, 33001, "bf16", "bf16", True),
+                                             (530, 66001, "bf16", "bf16", False)])
+def test_many_rows_some_with_long_histories(a3po, T, V, zt, ut, write):
+    """Rows enough for the smaller workgroups; histories with more tokens, and more distinct ones, than are noted or numbered at
+    a time."""
+    z, p, ok = make(T, V, seed=T + V, most=20)
+    g = torch.Generator().manual_seed(T)
+    longer = (V * torch.rand(14000, generator=g)).int()
+    p["hist_start"][1], p["hist_len"][1] = p["history"].numel(), 14000
+    p["hist_start"][T - 1], p["hist_len"][T - 1] = p["history"].numel() + 500, 9001
+    p["prompt_len"][1], p["prompt_len"][T - 1] = 6000, 0
+    p["history"] = torch.cat((p["history"], longer))
+    check_forward(a3po, z.to(DT[zt]), p, ok, DT[ut], write=write)
