@@ -8,7 +8,7 @@
 // (16 + zero) * sum x is what the fp32 accumulator of a group starts from, and the group's scale multiplies the sum.
 // Products are exact, sums are fp32, the output is rounded once.
 // With up to 16 tokens the kernel is bound by the weight's bytes, beyond a fixed 6 us for the hidden values and the first codes:
-// one token, 1,536 x 151,936 in groups of 128 28 us, 16 tokens, 4,096 x 151,936 in groups of 128 67 (4.9 TB/s).  With more the
+// one token, 1,536 x 151,936 in groups of 128 27 us (4.4 TB/s), 16 tokens, 4,096 x 151,936 in groups of 128 65 (5.1).  With more the
 // vector instructions (half of the time) and the matrix instructions (a third) share the units' issue: 50 tokens, 4,096 x
 // 151,936, fp32 scales of groups of 32 and zero points, 172 us against 92 for the bytes; a group's scale is a multiply-add for
 // every 32 codes and token, and is the larger half of the vector instructions.
@@ -115,8 +115,8 @@ __device__ __forceinline__ void load_run(const char *p, uint32_t (&w)[(BYTES + 3
 //
 // All hidden values lie in LDS, in the order of the matrix instructions, for as long as the workgroup lives: one workgroup a
 // compute unit, sixteen wavefronts.  A set of 16 x (16 / WK) rows is taken at a time: WK wavefronts share the 16 rows, a run of
-// UPW units each, and add their sums through LDS.  A wavefront's weight is loaded NB sets ahead into registers (eight units or
-// more in flight, 128 KiB a compute unit) and waits for nobody else's.
+// UPW units each, and add their sums through LDS.  A wavefront's weight is loaded NB sets ahead into registers (four units or
+// more in flight, 64 KiB and more a compute unit) and waits for nobody else's.
 
 // a row's codes of UPW units in a row, with their scales and zero points
 template <int UPW, int GROUP, bool ZEROS, bool SCALE_F32>
@@ -178,20 +178,32 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
                 ZEROS ? reinterpret_cast<const char *>(a.zeros) + group + group_lane : nullptr);
         __builtin_amdgcn_sched_barrier(0);  // (in this order: what is waited for first is issued first)
     };
-#pragma unroll
-    for (int b = 0; b < NB; ++b) fetch((int)blockIdx.x + b * (int)gridDim.x, run[b]);
-
-    for (int p = threadIdx.x; p < units * 16 * TP; p += 1024) {
+    // The hidden values first, then the weight: what is asked for later arrives later, and those would be waited for with all of
+    // the weight that is in flight.
+    const int pieces = units * 16 * TP;
+    auto load_x = [&](int p) {
+        p = min(p, pieces - 1);
+        const int64_t token = min((int64_t)(p & (TP - 1)), a.T - 1);
+        return *reinterpret_cast<const u32x4_half *>(static_cast<const char *>(a.x) + (token * a.ldx + p / TP * 8) * 2);
+    };
+    auto keep_x = [&](int p, u32x4_half h) {
         const int token = p & (TP - 1), k8 = p / TP;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (token < a.T) {
-            const u32x4_half h = *reinterpret_cast<const u32x4_half *>(static_cast<const char *>(a.x) + (token * a.ldx + k8 * 8) * 2);
-            v = make_uint4(h.x, h.y, h.z, h.w);
-        }
+        const bool on = token < a.T;
+        const uint4 v = make_uint4(on ? h.x : 0u, on ? h.y : 0u, on ? h.z : 0u, on ? h.w : 0u);
         // groups of a whole unit: the lanes of a block of codes keep it, and the quarter of the unit that they multiply is theirs
         const int at = GROUP == 128 ? (k8 & ~15) | (k8 & 3) << 2 | (k8 >> 2 & 3) : k8;
-        *reinterpret_cast<uint4 *>(xs + ((size_t)at * TP + token) * 16) = order_like_codes(v);
-    }
+        if (p < pieces) *reinterpret_cast<uint4 *>(xs + ((size_t)at * TP + token) * 16) = order_like_codes(v);
+    };
+    constexpr int kFirst = 4;  // (two cost single tokens nothing and gain them 6 %, eight gain 16 x 4,096 3 % and cost 1 x 896 1 us)
+    u32x4_half first[kFirst];
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) first[i] = load_x(threadIdx.x + i * 1024);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) fetch((int)blockIdx.x + b * (int)gridDim.x, run[b]);
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) keep_x(threadIdx.x + i * 1024, first[i]);
+    for (int p = threadIdx.x + kFirst * 1024; p < pieces; p += 1024) keep_x(p, load_x(p));
     meet();
     for (int p = threadIdx.x; p < (int)groups * TP; p += 1024) {
         const int token = p & (TP - 1), g = p / TP;
@@ -738,11 +750,11 @@ hipError_t launch_resident(const W4Args &a, const W4Plan &p, hipStream_t s)
 template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
 hipError_t launch_units(const W4Args &a, const W4Plan &p, hipStream_t s)
 {
-    // registers of a unit in flight; as many units ahead as the 128 registers of sixteen wavefronts hold
-    constexpr int kRegs = 4 + (128 / GROUP * (SCALE_F32 ? 4 : 2) + 3) / 4 + (ZEROS ? 1 : 0), kAhead = kRegs >= 8 ? 6 : kRegs == 7 && MT == 2 ? 8 : 9;
-    if (p.units == 2) return launch_resident<MT, 2, kAhead / 2, GROUP, ZEROS, SCALE_F32>(a, p, s);
-    if (p.units == 3) return launch_resident<MT, 3, kAhead / 3, GROUP, ZEROS, SCALE_F32>(a, p, s);
-    if constexpr (kAhead >= 8) return launch_resident<MT, 4, kAhead / 4, GROUP, ZEROS, SCALE_F32>(a, p, s);
+    // Two sets ahead are enough, and a third costs the registers that keep addresses: 1 x 1,536 x 151,936, us, three / two: groups of
+    // 32 bf16 with zero points 48 (spilled) / 38, of 64 31 / 28, of 128 31 / 29.
+    if (p.units == 2) return launch_resident<MT, 2, 2, GROUP, ZEROS, SCALE_F32>(a, p, s);
+    if (p.units == 3) return launch_resident<MT, 3, 2, GROUP, ZEROS, SCALE_F32>(a, p, s);
+    if constexpr (GROUP > 32 || !SCALE_F32) return launch_resident<MT, 4, 2, GROUP, ZEROS, SCALE_F32>(a, p, s);
     return hipErrorInvalidValue;  // (w4_plan gives no such call four units)
 }
 
