@@ -476,7 +476,8 @@ typedef struct {
  * logp 0.  lse_out, logp_out [T] float, nullable; at least one output is required.  Everything is computed in fp32, and lse
  * and logp are those of the fp32 values: out in float32 holds exactly these, out in bfloat16 rounds them once.
  * A row with nothing allowed (or all -inf) has lse -inf; a chosen token with u = -inf has logp -inf.
- * Masked entries are -inf whatever the logit holds, NaN included; an unmasked NaN or +inf makes the row's lse and logp NaN.
+ * Masked entries are -inf whatever the logit holds, NaN included; an unmasked NaN or +inf makes the row's lse and logp NaN,
+ * also where the chosen token's u is -inf.
  * V <= 2^31 - 1.  workspace: a3po_workspace_bytes(A3PO_WS_ADJUST_LOGITS, T, V, 0) bytes, 256-byte aligned (not needed, and
  * NULL, when out alone is asked for).
  */

@@ -350,7 +350,9 @@ __device__ __forceinline__ void finish_row(const AdjustArgs &a, int64_t t, MaxSu
     if (a.lse) a.lse[t] = fmaf(v.m, inv_temperature, log_s);
     if (a.logp) {
         const int64_t y = a.chosen[t];
-        a.logp[t] = y < 0 || y >= a.V ? 0.0f : u == -kInf ? -kInf : (u - v.m) * inv_temperature - log_s;
+        // (a row of which nothing is left has -inf - -inf; a sum that is NaN stays one whatever the token's logit)
+        const bool never = u == -kInf && v.s >= 0.0f;
+        a.logp[t] = y < 0 || y >= a.V ? 0.0f : never ? -kInf : (u - v.m) * inv_temperature - log_s;
     }
 }
 

@@ -396,3 +396,23 @@ def test_many_rows_some_with_long_histories(a3po, T, V, zt, ut, write):
     p["prompt_len"][1], p["prompt_len"][T - 1] = 6000, 0
     p["history"] = torch.cat((p["history"], longer))
     check_forward(a3po, z.to(DT[zt]), p, ok, DT[ut], write=write)
+
+
+@pytest.mark.parametrize("V", [700, 40001])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_row_s_nan_shows_in_the_log_prob_of_a_token_that_is_masked(a3po, V, bad):
+    """NaN or +inf in an unmasked place: the row's log-sum-exp is NaN, and no log-prob of the row is a number, that of a masked
+    token, or of one with -inf for a logit, among them.  Rows in one part and in many."""
+    T = 6
+    z, p, _ = make(T, V, seed=31, bias=None, mask=False)
+    ok = torch.ones(T, V, dtype=torch.bool)
+    ok[:, 3] = False
+    z[:, 5] = -math.inf
+    z[1::2, V - 2] = bad
+    p["allowed"] = pack_bits(ok)
+    for token in (3, 5):
+        y = torch.full((T,), token, dtype=torch.int32, device="cuda")
+        r = a3po.adjust_logits(z.cuda(), chosen=y, write=False, **dev(p))
+        lse, logp = r["lse"].cpu(), r["logp"].cpu()
+        assert lse[1::2].isnan().all() and logp[1::2].isnan().all(), token
+        assert lse[::2].isfinite().all() and (logp[::2] == -math.inf).all(), token
