@@ -499,6 +499,11 @@ def _rows(t, name, shape=None):
     return _dtype_code(t, name), ld if size[0] > 1 else max(ld, size[1])
 
 
+def _matrix(t, dtype, shape, name):
+    """Arrays with a row for each of the weight's: by their number of elements a transposed one would pass too."""
+    assert t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous(), f"{name}: need contiguous {dtype}{list(shape)} on GPU"
+
+
 def _params(weight, bias, H):
     """The dtype code that weight and bias share."""
     if bias is not None:
@@ -667,10 +672,10 @@ def w4_linear(x, codes, scales, zeros=None, group: int = 128, out=None, out_dtyp
     T, H = x.shape
     N = codes.shape[0]
     assert group in (32, 64, 128) and H % group == 0, "group must be 32, 64 or 128 and divide H"
-    _vec(codes, torch.uint8, N * (H // 2), "codes")
-    _vec(scales, scales.dtype, N * (H // group), "scales")
+    _matrix(codes, torch.uint8, (N, H // 2), "codes")
+    _matrix(scales, scales.dtype, (N, H // group), "scales")
     if zeros is not None:
-        _vec(zeros, torch.uint8, N * (H // group), "zeros")
+        _matrix(zeros, torch.uint8, (N, H // group), "zeros")
     if out is None:
         out = torch.empty((T, N), dtype=torch.bfloat16 if out_dtype is None else out_dtype, device=x.device)
     od, ld_out = _rows(out, "out", (T, N))

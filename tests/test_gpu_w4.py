@@ -149,3 +149,23 @@ def test_more_sets_than_compute_units(a3po, zeros):
     """Workgroups take several sets of rows each, the last of them not all."""
     for T, N, H in ((2, 33333, 256), (16, 20011, 512), (30, 9001, 768), (5, 12345, 384)):
         _check(a3po, T, N, H, 128, zeros, seed=N)
+
+
+def test_refuses_arrays_that_are_not_the_weight_s_shape(a3po):
+    """As many elements as it takes, in another shape: a transposed array would scale every group by another one's value."""
+    T, N, H, group = 3, 96, 256, 64
+    g = torch.Generator().manual_seed(8)
+    codes, scales, z, _, _ = _weight(N, H, group, True, torch.float32, g)
+    good = dict(x=torch.zeros(T, H, dtype=torch.bfloat16), codes=codes, scales=scales, zeros=z)
+    call = lambda **kw: a3po.w4_linear(**{k: v.cuda() for k, v in {**good, **kw}.items()}, group=group)
+    assert call().shape == (T, N)
+    for name in ("codes", "scales", "zeros"):
+        t = good[name]
+        wrong = [t.t().contiguous(), t.flatten(), t[:-1], t[:, :-1].contiguous(), t.t().contiguous().cuda().t(), t.short()]
+        if name == "codes":    # (its first length is the number of rows: the others' then do not fit)
+            wrong = [t.flatten(), t[:, :-1].contiguous(), t.t().contiguous().cuda().t(), t.short()]
+            with pytest.raises(AssertionError, match="codes: need"):
+                call(codes=t.t().contiguous())
+        for w in wrong:
+            with pytest.raises((AssertionError, TypeError), match=name):
+                call(**{name: w})
