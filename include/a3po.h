@@ -508,7 +508,9 @@ int a3po_adjust_logits_bwd(const void *dout, a3po_dtype out_dt, int64_t ld_out, 
  * T <= 64 * 65,535; the weight is read once per 64 tokens: the kernels are made for single tokens and small batches.
  * workspace: a3po_workspace_bytes(A3PO_WS_W4_LINEAR, T, 0, H) bytes, 256-byte aligned; 0 (and NULL) for up to 16 tokens
  * with H a multiple of 128 from 256 to 4,096, whose hidden values stay on chip.
- * Products are exact and summed in fp32, out is rounded once.  x is expected to be finite (an infinity gives NaN).
+ * Products are exact and summed in fp32, out is rounded once.  (Hidden values enter as float16 times a power of two of their
+ * token's.  Those smaller than 2^-33 of the token's largest lose up to 2^-40 of that; sums are up to 2^46 in magnitude before a
+ * scale multiplies them, so scales from 2^82 on may overflow.)  Infinities and NaN in x reach their token's outputs only.
  */
 int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8_t *codes, const void *scales,
                    a3po_dtype scale_dt, const uint8_t *zeros, int32_t group, int64_t N, void *out, a3po_dtype out_dt,

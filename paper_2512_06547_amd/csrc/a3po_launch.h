@@ -531,7 +531,7 @@ inline size_t adjust_workspace_bytes(int64_t T, int64_t V)
 }
 hipError_t launch_adjust(AdjustArgs a, hipStream_t s);
 
-constexpr int kW4UnitBytes = 4096 + 256;  // of 16 tokens' hidden values of a unit (128) and of their sums
+constexpr int kW4UnitBytes = 4096;            // of 16 tokens' hidden values of a unit (128)
 constexpr int64_t kW4MaxTokens = 65535 * 64;  // (blocks of 64 tokens are the grid's second dimension)
 struct W4Args {
     const void *x;
@@ -553,16 +553,25 @@ struct W4Plan {
     int lds;
 };
 constexpr int kW4MaxLds = 160 * 1024;
+// hidden values, sums of 16 wavefronts on their way to one another, a power of two for each token
+inline int w4_tokens_shift(int64_t T) { return T <= 4 ? 2 : T <= 8 ? 3 : T <= 16 ? 4 : 5; }
+inline int64_t w4_resident_lds(int64_t T, int64_t H)
+{
+    const int64_t tp = (int64_t)1 << w4_tokens_shift(T);
+    return tp * H * 2 + 16 * 1024 * (T <= 16 ? 1 : 2) + tp * 4;
+}
 inline W4Plan w4_plan(int64_t T, int64_t H, int64_t N, int group, bool scale_f32, int64_t cus)
 {
     W4Plan p = {};
-    if (T > 32 || H % 128 != 0 || H < 256 || H > 8192) return p;
+    // (rows beyond 4,096 are shared by all sixteen wavefronts, whose last ones have little or nothing of them: 16 tokens of H 4,224 /
+    // 4,352 / 4,480 x 151,936, groups of 128, take 100 / 109 / 103 us here and 94 / 82 / 95 in chunks, 9 of 4,352 in groups of 64 120
+    // and 87)
+    if (T > 32 || H % 128 != 0 || H < 256 || H > (T > 8 ? 4096 : 8192)) return p;
     p.blocks16 = T <= 16 ? 1 : 2;
-    p.tp_shift = T <= 4 ? 2 : T <= 8 ? 3 : T <= 16 ? 4 : 5;
-    const int64_t tp = (int64_t)1 << p.tp_shift, units = H / 128;
-    const int64_t lds = tp * H * 2 + H / group * tp * 4 + 16 * 1024 * p.blocks16;
-    if (lds > kW4MaxLds) return p;
-    p.lds = (int)lds;
+    p.tp_shift = w4_tokens_shift(T);
+    const int64_t units = H / 128;
+    p.lds = (int)w4_resident_lds(T, H);
+    if (p.lds > kW4MaxLds) return p;
     // the split of rows over wavefronts that leaves the busiest compute unit the fewest units in turn (a set's joining counts
     // for one)
     int64_t best = 0;
@@ -602,7 +611,7 @@ inline size_t w4_workspace_bytes(int64_t T, int64_t H)
 {
     if (T <= 0 || H <= 0 || (T <= 16 && H % 128 == 0 && H >= 256 && H <= 4096)) return 0;
     const int64_t tokens = T <= 16 ? 16 : T <= 32 ? 32 : (T + 63) / 64 * 64;
-    return (size_t)(tokens / 16) * (size_t)((H + 511) / 512 * 4) * kW4UnitBytes + 2 * kW4ShortBytes;
+    return (size_t)(tokens / 16) * (size_t)((H + 511) / 512 * 4) * kW4UnitBytes + ((size_t)tokens * 4 + 255) / 256 * 256 + 2 * kW4ShortBytes;
 }
 hipError_t launch_w4_linear(const W4Args &a, void *workspace, hipStream_t s);
 

@@ -3,15 +3,19 @@
 //   out[t, n] = sum over groups g of scale[n, g] * sum over k in g of (code[n, k] - zero[n, g]) x[t, k]
 //
 // The weight is read once, straight into registers: 16 bytes a lane are 32 codes of one row, a wavefront holds 16 rows of
-// 128 codes (a unit).  A code n becomes the bfloat16 16 + n by putting its bits into the mantissa of 16 (one shift and one
-// and-or for two codes), so that matrix-core products of 16 tokens x 16 rows x 32 codes take it exactly; the excess
-// (16 + zero) * sum x is what the fp32 accumulator of a group starts from, and the group's scale multiplies the sum.
-// Products are exact, sums are fp32, the output is rounded once.
+// 128 codes (a unit).  Matrix-core products of 16 tokens x 16 rows x 32 codes take float16, in which code - zero is exact: a
+// code's bits go into the mantissa of 1,024, and one addition for two codes takes 1,024 + zero off (1,024 + 16 n, for
+// the codes that lie four bits higher, leave with a factor of 1/16 in the same instruction).  Hidden values become float16 times
+// a power of two of the token's, which brings its largest to between 2^15 and 2^16: bfloat16's eight digits are kept by all that
+// are not below 2^-33 of that, and those lose no more than 2^-40 of it.  So products are exact, a group's sum in fp32 is of
+// the size of its terms, its scale multiplies it in fp32, and the token's power of two leaves from the output, which is rounded
+// once.  (Codes as bfloat16 16 + n with the excess (16 + zero) sum x taken off the sum cost an instruction less for eight, and
+// digits: where hidden values are of one sign the sum is many times what is left of it, and errors of 4e-6 came of that, 2e-7 here.)
 // With up to 16 tokens the kernel is bound by the weight's bytes, beyond a fixed 6 us for the hidden values and the first codes:
-// one token, 1,536 x 151,936 in groups of 128 27 us (4.4 TB/s), 16 tokens, 4,096 x 151,936 in groups of 128 65 (5.1).  With more the
-// vector instructions (half of the time) and the matrix instructions (a third) share the units' issue: 50 tokens, 4,096 x
-// 151,936, fp32 scales of groups of 32 and zero points, 172 us against 92 for the bytes; a group's scale is a multiply-add for
-// every 32 codes and token, and is the larger half of the vector instructions.
+// one token, 1,536 x 151,936 in groups of 128 27 us (4.4 TB/s), 16 tokens, 4,096 x 151,936 in groups of 128 66 (5.1).  With more it is
+// the vector instructions, and that they and the matrix instructions take turns rather than overlap: 50 tokens, 4,096 x 151,936, fp32
+// scales of groups of 32 and zero points, 156 us against 92 for the bytes; a group's scale is a multiply-add for every 32 codes
+// and token, and is the larger half of the vector instructions.
 #include "a3po_common.h"
 #include "a3po_direct.h"
 #include "a3po_launch.h"
@@ -21,33 +25,73 @@ namespace {
 
 typedef uint32_t u32x4_half __attribute__((ext_vector_type(4), aligned(2)));
 
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+
 // Constants in registers that the compiler knows nothing of: it would fold them into an instruction each, of which an and-or
 // holds one at most.
+template <uint32_t VALUE>
 __device__ __forceinline__ uint32_t opaque_scalar()
 {
     uint32_t v;
-    asm("s_mov_b32 %0, %1" : "=s"(v) : "i"(0x00780078));
+    asm("s_mov_b32 %0, %1" : "=s"(v) : "i"(VALUE));
     return v;
 }
+template <uint32_t VALUE>
 __device__ __forceinline__ uint32_t opaque_vector()
 {
     uint32_t v;
-    asm("v_mov_b32 %0, %1" : "=v"(v) : "i"(0x41804180));
+    asm("v_mov_b32 %0, %1" : "=v"(v) : "i"(VALUE));
     return v;
 }
 
-// codes of dword d, as bfloat16 16 + n, in the order 0 4 1 5 2 6 3 7 (mask, sixteen: the two constants)
-__device__ __forceinline__ bf16x8_t widen(uint32_t d, uint32_t mask, uint32_t sixteen)
-{
-    const u32x4_t w = {((d << 3) & mask) | sixteen, ((d >> 1) & mask) | sixteen, ((d >> 5) & mask) | sixteen,
-                       ((d >> 9) & mask) | sixteen};
-    return __builtin_bit_cast(bf16x8_t, w);
-}
+// what a code's zero point takes off two codes: -(1,024 + zero), and -(64 + zero) of those that come as 64 + n
+struct Zero {
+    f16x2_t low, high;
+    __device__ __forceinline__ explicit Zero(uint32_t zero)
+    {
+        low = __builtin_bit_cast(f16x2_t, (zero | zero << 16) | 0xE400E400u);
+        high = low + f16x2_t{(_Float16)960.0f, (_Float16)960.0f};
+    }
+};
+// Codes of a dword, as float16 code - zero, in the order 0 4 1 5 2 6 3 7.
+struct Widen {
+    uint32_t first = opaque_scalar<0x000F000F>(), second = opaque_scalar<0x00F000F0>(), kilo = opaque_vector<0x64006400>();
+    __device__ __forceinline__ f16x8_t operator()(uint32_t d, const Zero &z) const
+    {
+        const f16x2_t sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
+        auto at = [&](uint32_t v, uint32_t mask) { return __builtin_bit_cast(f16x2_t, (v & mask) | kilo); };
+        const f16x2_t a = at(d, first) + z.low, b = __builtin_elementwise_fma(at(d, second), sixteenth, z.high);
+        const f16x2_t c = at(d >> 8, first) + z.low, e = __builtin_elementwise_fma(at(d >> 8, second), sixteenth, z.high);
+        return f16x8_t{a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
+    }
+};
 // eight hidden values in the same order
 __device__ __forceinline__ uint4 order_like_codes(const uint4 &v)
 {
     return make_uint4(__builtin_amdgcn_perm(v.z, v.x, 0x05040100u), __builtin_amdgcn_perm(v.z, v.x, 0x07060302u),
                       __builtin_amdgcn_perm(v.w, v.y, 0x05040100u), __builtin_amdgcn_perm(v.w, v.y, 0x07060302u));
+}
+// the larger magnitude at each place of a pair, as bits
+__device__ __forceinline__ uint32_t larger(uint32_t most, const uint4 &v)
+{
+    u16x2_t m = __builtin_bit_cast(u16x2_t, most);
+#pragma unroll
+    for (uint32_t w : {v.x, v.y, v.z, v.w}) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, w & 0x7FFF7FFFu));
+    return __builtin_bit_cast(uint32_t, m);
+}
+// the power of two that brings a token whose largest magnitude has these bits to between 2^15 and 2^16
+__device__ __forceinline__ int token_shift(uint32_t most) { return most ? 142 - max((int)(most >> 7), 1) : 0; }
+__device__ __forceinline__ uint4 to_halves(const uint4 &v, int shift)
+{
+    auto two = [&](uint32_t w) {
+        typedef float f32x2_t __attribute__((ext_vector_type(2)));
+        const f32x2_t f = {__builtin_amdgcn_ldexpf(__uint_as_float(w << 16), shift),
+                           __builtin_amdgcn_ldexpf(__uint_as_float(w & 0xFFFF0000u), shift)};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2_t));
+    };
+    return make_uint4(two(v.x), two(v.y), two(v.z), two(v.w));
 }
 
 // Lanes l, l + 16, l + 32, l + 48 hold four blocks of 32 codes of one row, a block each; afterwards d[b] of the four lanes
@@ -141,7 +185,7 @@ struct Run {
         if constexpr (SCALE_F32) return __uint_as_float(scales[g]);
         else return __uint_as_float(g & 1 ? scales[g / 2] & 0xFFFF0000u : scales[g / 2] << 16);
     }
-    __device__ __forceinline__ float zero(int g) const { return (float)(zeros[g / 4] >> (8 * (g % 4)) & 0xFFu); }
+    __device__ __forceinline__ Zero zero(int g) const { return Zero(ZEROS ? zeros[g / 4] >> (8 * (g % 4)) & 0xFFu : 8u); }
 };
 
 template <int MT, int UPW, int NB, int GROUP, bool ZEROS, bool SCALE_F32>
@@ -156,9 +200,9 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
     // (the last wavefronts' runs move down to end with the row; units that another one has as well count for nothing here)
     const int units = a.H >> 7, u0 = min(wk * UPW, units - UPW), skip = wk * UPW - u0;
     const int64_t groups = a.H / GROUP, row_bytes = a.H / 2;
-    char *xs = lds;                                                             // [units][4][4][TP] 16 bytes
-    float *sums = reinterpret_cast<float *>(lds + (size_t)a.H * TP * 2);        // [groups][TP]
-    char *red = reinterpret_cast<char *>(sums + groups * TP);                   // [16 wavefronts][MT][64] 16 bytes
+    char *xs = lds;                                          // [units][4][4][TP] 16 bytes
+    char *red = lds + (size_t)a.H * TP * 2;                  // [16 wavefronts][MT][64] 16 bytes
+    int *shifts = reinterpret_cast<int *>(red + 16 * 1024 * MT);  // [TP]
 
     // lane offsets from a set's first row (fewer than 16 rows in all: the last one again)
     const uint32_t row_lane = (uint32_t)min((int64_t)n16, a.V - 1);
@@ -180,19 +224,21 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
     };
     // The hidden values first, then the weight: what is asked for later arrives later, and those would be waited for with all of
     // the weight that is in flight.
-    const int pieces = units * 16 * TP;
+    const int pieces = units * 16 * TP, token = (int)threadIdx.x & (TP - 1);  // (a thread's pieces are all one token's)
     auto load_x = [&](int p) {
         p = min(p, pieces - 1);
-        const int64_t token = min((int64_t)(p & (TP - 1)), a.T - 1);
-        return *reinterpret_cast<const u32x4_half *>(static_cast<const char *>(a.x) + (token * a.ldx + p / TP * 8) * 2);
+        const int64_t from = min((int64_t)(p & (TP - 1)), a.T - 1);
+        return *reinterpret_cast<const u32x4_half *>(static_cast<const char *>(a.x) + (from * a.ldx + p / TP * 8) * 2);
     };
-    auto keep_x = [&](int p, u32x4_half h) {
-        const int token = p & (TP - 1), k8 = p / TP;
+    auto ordered = [&](u32x4_half h) {
         const bool on = token < a.T;
-        const uint4 v = make_uint4(on ? h.x : 0u, on ? h.y : 0u, on ? h.z : 0u, on ? h.w : 0u);
+        return order_like_codes(make_uint4(on ? h.x : 0u, on ? h.y : 0u, on ? h.z : 0u, on ? h.w : 0u));
+    };
+    auto place_x = [&](int p) {
+        const int k8 = p / TP;
         // groups of a whole unit: the lanes of a block of codes keep it, and the quarter of the unit that they multiply is theirs
         const int at = GROUP == 128 ? (k8 & ~15) | (k8 & 3) << 2 | (k8 >> 2 & 3) : k8;
-        if (p < pieces) *reinterpret_cast<uint4 *>(xs + ((size_t)at * TP + token) * 16) = order_like_codes(v);
+        return reinterpret_cast<uint4 *>(xs + ((size_t)at * TP + token) * 16);
     };
     constexpr int kFirst = 4;  // (two cost single tokens nothing and gain them 6 %, eight gain 16 x 4,096 3 % and cost 1 x 896 1 us)
     u32x4_half first[kFirst];
@@ -201,27 +247,38 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int b = 0; b < NB; ++b) fetch((int)blockIdx.x + b * (int)gridDim.x, run[b]);
+    // the token's largest value: of this thread's, the wavefront's, all sixteen's
+    uint4 mine[kFirst];
+    uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < kFirst; ++i) keep_x(threadIdx.x + i * 1024, first[i]);
-    for (int p = threadIdx.x + kFirst * 1024; p < pieces; p += 1024) keep_x(p, load_x(p));
-    meet();
-    for (int p = threadIdx.x; p < (int)groups * TP; p += 1024) {
-        const int token = p & (TP - 1), g = p / TP;
-        float total = 0.0f;
-#pragma unroll
-        for (int k = 0; k < GROUP / 8; ++k) {
-            float f[8];
-            unpack<Bf16>(*reinterpret_cast<const uint4 *>(xs + ((size_t)(g * (GROUP / 8) + k) * TP + token) * 16), f);
-            total += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-        }
-        sums[p] = ZEROS ? -total : -24.0f * total;  // (the codes' excess: 16 + 8 without zero points)
+    for (int i = 0; i < kFirst; ++i) {
+        mine[i] = ordered(first[i]);
+        if ((int)threadIdx.x + i * 1024 < pieces) most = larger(most, mine[i]);
     }
+    for (int p = threadIdx.x + kFirst * 1024; p < pieces; p += 1024) {
+        const uint4 v = ordered(load_x(p));
+        most = larger(most, v);
+        *place_x(p) = v;
+    }
+    most = max(most & 0xFFFFu, most >> 16);
+    for (int off = TP; off < kWave; off <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, off, kWave));
+    if (lane < TP) reinterpret_cast<uint32_t *>(red)[wave * TP + lane] = most;
+    meet();
+#pragma unroll
+    for (int w = 0; w < kAll; ++w) most = max(most, reinterpret_cast<const uint32_t *>(red)[w * TP + token]);
+    const int shift = token_shift(most);
+    if ((int)threadIdx.x < TP) shifts[threadIdx.x] = shift;
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) {
+        const int p = threadIdx.x + i * 1024;
+        if (p < pieces) *place_x(p) = to_halves(mine[i], shift);
+    }
+    for (int p = threadIdx.x + kFirst * 1024; p < pieces; p += 1024) *place_x(p) = to_halves(*place_x(p), shift);
     meet();
 
-    const uint32_t mask = opaque_scalar(), sixteen = opaque_vector();
+    const Widen widen;
     // (with fewer than 16 tokens the lanes of the others read these again; their products are not stored)
     const char *x_lane = xs + (q * TP + (n16 & (TP - 1))) * 16;
-    const float *sum_lane = sums + ((q * 4) & (TP - 1));
 
     auto multiply = [&](const Run<UPW, GROUP, ZEROS, SCALE_F32> &from, f32x4_t (&acc)[MT]) {
 #pragma unroll
@@ -238,22 +295,16 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
             uint32_t(&d)[4] = codes[u];
             if constexpr (GROUP < 128) transpose_blocks(d);
             const char *x = x_lane + (size_t)(u0 + u) * 16 * TP * 16;
-            const float *sum = sum_lane + (u0 + u) * S * TP;
             f32x4_t part[MT];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int gi = g / BLOCKS;
-                if (g % BLOCKS == 0)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        part[m] = *reinterpret_cast<const f32x4_t *>(sum + gi * TP + m * 16);
-                        if (ZEROS) part[m] *= 16.0f + from.zero(u * S + gi);
-                    }
-                const bf16x8_t wide = widen(d[g], mask, sixteen);
+                const f16x8_t wide = widen(d[g], from.zero(u * S + gi));
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
-                    part[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        *reinterpret_cast<const bf16x8_t *>(x + ((size_t)g * 4 * TP + m * 16) * 16), wide, part[m], 0, 0, 0);
+                    part[m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                        *reinterpret_cast<const f16x8_t *>(x + ((size_t)g * 4 * TP + m * 16) * 16), wide,
+                        g % BLOCKS == 0 ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : part[m], 0, 0, 0);
                 if (g % BLOCKS == BLOCKS - 1) {
                     const float scale = u < skip ? 0.0f : from.scale(u * S + gi);
 #pragma unroll
@@ -285,7 +336,7 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
                 for (int j = 0; j < 4; ++j) total += k + j < WK ? v[j] : 0.0f;
             }
             const int64_t want = ((int64_t)set * WR + block) * 16, row = min(want, max(a.V - 16, (int64_t)0)) + n;
-            if (row >= want && row < a.V) put_out(token, row, total);
+            if (row >= want && row < a.V) put_out(token, row, __builtin_amdgcn_ldexpf(total, -shifts[token]));
         }
     };
 
@@ -310,46 +361,55 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
 
 // ---- more tokens, long or odd rows: hidden values stream through LDS ----------------------------------------------------
 //
-// A first kernel writes the hidden values in the order of the matrix instructions, with the sums of each group, so that the
-// second copies them to LDS as they are: [pass of 16 MT tokens][unit][4 blocks of codes][MT][64 lanes] 16 bytes, then
-// [4 groups][16 MT] sums.  Units are a multiple of four, those beyond the row hold zeros (a branch around them would cost the wait
-// that loads are kept out of branches for).
+// A first kernel writes the hidden values as float16 in the order of the matrix instructions, so that the second copies them to
+// LDS as they are: [pass of 16 MT tokens][unit][4 blocks of codes][MT][64 lanes] 16 bytes, then the tokens' powers of
+// two.  Units are a multiple of four, those beyond the row hold zeros (a branch around them would cost the wait that loads
+// are kept out of branches for).
 
 constexpr int unit_bytes(int mt) { return kW4UnitBytes * mt; }
 
+// a workgroup takes a token (those beyond the last are zeros); what it has no registers for it reads again
 template <int MT>
-__global__ __launch_bounds__(256) void w4_order_kernel(W4Args a, char *to, int units, bool zeros)
+__global__ __launch_bounds__(256) void w4_order_kernel(W4Args a, char *to, int units, int *shifts)
 {
-    const int unit = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t pass = blockIdx.y;
-    char *out = to + (pass * units + unit) * unit_bytes(MT);
-    float *sums = reinterpret_cast<float *>(out + 4096 * MT);
-    const int q = lane >> 4, n16 = lane & 15, S = 128 / a.group, per = 4 / S;
-    for (int m = wave; m < MT; m += 4) {
-        const int64_t token = pass * (16 * MT) + m * 16 + n16;
-        const char *row = static_cast<const char *>(a.x) + token * a.ldx * 2;
-        float total = 0.0f;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int k = unit * 128 + g * 32 + q * 8;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (token < a.T && k < a.H) {
-                const u32x4_half h = *reinterpret_cast<const u32x4_half *>(row + (int64_t)k * 2);
-                v = make_uint4(h.x, h.y, h.z, h.w);
-            }
-            *reinterpret_cast<uint4 *>(out + ((g * MT + m) * kWave + lane) * 16) = order_like_codes(v);
-            float f[8], s;
-            unpack<Bf16>(v, f);
-            s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-            s += __shfl_xor(s, 16, kWave);
-            s += __shfl_xor(s, 32, kWave);
-            total = g % per == 0 ? s : total + s;
-            // (the codes' excess: 16 + 8 without zero points)
-            if (g % per == per - 1 && q == 0) sums[(g / per) * (16 * MT) + m * 16 + n16] = zeros ? -total : -24.0f * total;
+    constexpr int kFirst = 2;
+    __shared__ uint32_t red[256 / kWave];
+    const int64_t token = blockIdx.x, pass = token / (16 * MT);
+    const int in_pass = (int)(token % (16 * MT)), pieces = units * 16;
+    const char *row = static_cast<const char *>(a.x) + token * a.ldx * 2;
+    auto load = [&](int p) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (token < a.T && p * 8 < a.H) {
+            const u32x4_half h = *reinterpret_cast<const u32x4_half *>(row + (int64_t)p * 16);
+            v = make_uint4(h.x, h.y, h.z, h.w);
         }
-        if (q == 0)
-            for (int g = S; g < 4; ++g) sums[g * (16 * MT) + m * 16 + n16] = 0.0f;
-    }
+        return v;
+    };
+    uint4 first[kFirst];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) first[i] = load(threadIdx.x + i * 256);
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) most = larger(most, first[i]);
+    for (int p = threadIdx.x + kFirst * 256; p < pieces; p += 256) most = larger(most, load(p));
+    most = max(most & 0xFFFFu, most >> 16);
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, off, kWave));
+    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = most;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t m : red) most = max(most, m);
+    const int shift = token_shift(most);
+    if (threadIdx.x == 0) shifts[token] = shift;
+    auto keep = [&](int p, const uint4 &v) {
+        if (p < pieces)
+            *reinterpret_cast<uint4 *>(to + (pass * units + (p >> 4)) * unit_bytes(MT) +
+                                       (((p >> 2 & 3) * MT + in_pass / 16) * kWave + (p & 3) * 16 + in_pass % 16) * 16) =
+                to_halves(order_like_codes(v), shift);
+    };
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) keep(threadIdx.x + i * 256, first[i]);
+    for (int p = threadIdx.x + kFirst * 256; p < pieces; p += 256) keep(p, load(p));
 }
 
 // arrays of scales or zero points too short for the loads of the second kernel, with zeros behind them
@@ -469,30 +529,22 @@ struct GroupBlocks {
             for (int g = 0; g < S; ++g) out[g] = __uint_as_float(g & 1 ? w[g / 2] & 0xFFFF0000u : w[g / 2] << 16);
         }
     }
-    // scale (16 + zero) of the unit's group g, which differs from lane to lane; 0 beyond its groups
-    __device__ __forceinline__ static float excess(const char *lds, int r, int u, int g)
+    __device__ __forceinline__ static Zero zero(const char *lds, int r, int u, int g)
     {
-        const int at = u * S + min(g, S - 1);
-        const char *p = lds + r * kStride + at * kBytes;
-        float s;
-        if constexpr (SCALE_F32) s = lds_get<float>(p);
-        else s = bf16_bits_to_float(lds_get<uint16_t>(p));
-        const float z = (float)lds_get<uint8_t>(lds + 32 * kStride + r * kZeroStride + at);
-        return S == 4 || g < S ? s * (16.0f + z) : 0.0f;
+        return Zero(ZEROS ? lds_get<uint8_t>(lds + 32 * kStride + r * kZeroStride + u * S + g) : 8u);
     }
 };
 
 // Eight wavefronts of 16 R rows each, tile after tile.  Two units a chunk: chunk c is multiplied from LDS while chunks c + 1 and
 // c + 2 of the hidden values arrive in LDS (direct loads) and of the codes in registers, the next tile's among them.  What is
 // waited for before a barrier is counted by hand: everything but the operations issued behind the next chunk's direct loads.
-// With zero points the excess leaves by a matrix instruction of its own (fp32 operands: a group's sum times scale (16 + zero)):
-// as a start value of each group's accumulators it took as many instructions as the scales themselves.
 template <int MT, int R, int GROUP, bool ZEROS, bool SCALE_F32>
 __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int units, int64_t first_row, int tiles, int64_t t0, char *xs,
-                                             char *own)
+                                             char *own, const int *shifts)
 {
     constexpr int UC = 2, S = 128 / GROUP, BLOCKS = GROUP / 32, kChunk = UC * unit_bytes(MT), kRows = 8 * 16 * R;
-    constexpr int kCopies = (kChunk + 8191) / 8192;                 // direct loads of 1 KiB a wavefront and chunk
+    constexpr int kCopies = kChunk / 8192;                          // direct loads of 1 KiB a wavefront and chunk
+    static_assert(kChunk % 8192 == 0, "whole loads");
     constexpr int kBehind = UC * R + kCopies + UC * R;              // operations behind the next chunk's
     using Groups = GroupBlocks<R, GROUP, ZEROS, SCALE_F32>;
     constexpr int kPerBlock = Groups::kUnits / UC;  // chunks of a block of scales
@@ -541,7 +593,7 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
     auto fetch_x = [&](int to) {
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
-            const int at = min(i * 8192 + wave * 1024, kChunk - 1024);  // (the last piece overlaps: the same bytes again)
+            const int at = i * 8192 + wave * 1024;
             dma16(x_buffer, lane * 16, (uint32_t)(xc * kChunk + at), xs + to * kChunk + at);
         }
         xc = xc + 1 == chunks ? 0 : xc + 1;
@@ -559,7 +611,7 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
         gi = gb == 0 ? min(gi + 1, mine - 1) : gi;
     };
 
-    const uint32_t mask = opaque_scalar(), sixteen = opaque_vector();
+    const Widen widen;
     f32x4_t acc[R][MT];
     auto clear = [&]() {
 #pragma unroll
@@ -584,38 +636,25 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
 #pragma unroll
         for (int i = 0; i < UC; ++i) {
             const char *unit = xs + which * kChunk + i * unit_bytes(MT);
-            const float *sums = reinterpret_cast<const float *>(unit + 4096 * MT);
             float scale[R][S];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 transpose_blocks(d[r][i]);
                 Groups::scales(own, r * 16 + n16, in_block * UC + i, scale[r]);
             }
-            if constexpr (ZEROS) {
-                float excess[R];
-#pragma unroll
-                for (int r = 0; r < R; ++r) excess[r] = Groups::excess(own, r * 16 + n16, in_block * UC + i, q);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const float e = lds_get<float>(sums + q * (16 * MT) + m * 16 + n16);
-#pragma unroll
-                    for (int r = 0; r < R; ++r) acc[r][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(e, excess[r], acc[r][m], 0, 0, 0);
-                }
-            }
             f32x4_t part[R][MT];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                bf16x8_t wide[R];
+                f16x8_t wide[R];
 #pragma unroll
-                for (int r = 0; r < R; ++r) wide[r] = widen(d[r][i][g], mask, sixteen);
+                for (int r = 0; r < R; ++r) wide[r] = widen(d[r][i][g], Groups::zero(own, r * 16 + n16, in_block * UC + i, g / BLOCKS));
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    const bf16x8_t xv = lds_get<bf16x8_t>(unit + ((g * MT + m) * kWave + lane) * 16);
-                    f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if (!ZEROS && g % BLOCKS == 0) start = lds_get<f32x4_t>(sums + (g / BLOCKS) * (16 * MT) + m * 16 + q * 4);
+                    const f16x8_t xv = lds_get<f16x8_t>(unit + ((g * MT + m) * kWave + lane) * 16);
 #pragma unroll
                     for (int r = 0; r < R; ++r)
-                        part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wide[r], g % BLOCKS == 0 ? start : part[r][m], 0, 0, 0);
+                        part[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                            xv, wide[r], g % BLOCKS == 0 ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : part[r][m], 0, 0, 0);
                 }
                 // (behind the products of all tokens: a sum that is read at once holds the wavefront up for its whole length)
                 if (g % BLOCKS == BLOCKS - 1)
@@ -628,6 +667,15 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
     };
     auto put_out = [&](int i) {
         const int64_t want = wanted(i), at = row_of(i);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            typedef int i32x4_t __attribute__((ext_vector_type(4)));
+            const i32x4_t shift = lds_get<i32x4_t>(shifts + m * 16 + q * 4);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[r][m][k] = __builtin_amdgcn_ldexpf(acc[r][m][k], -shift[k]);
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t n = at + r * 16 + n16;
@@ -696,15 +744,18 @@ __device__ __forceinline__ void stream_tiles(const W4Args &a, const char *x, int
 // Tiles of 256 rows first, then a last round of 128 rows where no more are left for it: a compute unit is done with those in
 // half the time.
 template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
-__global__ __launch_bounds__(512) void w4_stream_kernel(W4Args a, const char *ordered, int units, int wide_tiles, int narrow_tiles)
+__global__ __launch_bounds__(512) void w4_stream_kernel(W4Args a, const char *ordered, const int *token_shifts, int units, int wide_tiles,
+                                                        int narrow_tiles)
 {
     constexpr int kOwn = GroupBlocks<2, GROUP, ZEROS, SCALE_F32>::kLds;
     extern __shared__ __align__(16) char lds[];
-    char *own = lds + 6 * unit_bytes(MT) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kOwn;
+    int *shifts = reinterpret_cast<int *>(lds + 6 * unit_bytes(MT));  // of this pass' tokens
+    char *own = lds + 6 * unit_bytes(MT) + 64 * MT + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kOwn;
+    if (threadIdx.x < 16 * MT) shifts[threadIdx.x] = token_shifts[blockIdx.y * (16 * MT) + threadIdx.x];  // (read behind barriers)
     const char *x = ordered + (int64_t)blockIdx.y * units * unit_bytes(MT);
     const int64_t t0 = (int64_t)blockIdx.y * (16 * MT);
-    stream_tiles<MT, 2, GROUP, ZEROS, SCALE_F32>(a, x, units, 0, wide_tiles, t0, lds, own);
-    stream_tiles<MT, 1, GROUP, ZEROS, SCALE_F32>(a, x, units, (int64_t)wide_tiles * 256, narrow_tiles, t0, lds, own);
+    stream_tiles<MT, 2, GROUP, ZEROS, SCALE_F32>(a, x, units, 0, wide_tiles, t0, lds, own, shifts);
+    stream_tiles<MT, 1, GROUP, ZEROS, SCALE_F32>(a, x, units, (int64_t)wide_tiles * 256, narrow_tiles, t0, lds, own, shifts);
 }
 
 template <int MT, int GROUP, bool ZEROS, bool SCALE_F32>
@@ -716,10 +767,11 @@ hipError_t launch_stream(W4Args a, void *workspace, int cus, hipStream_t s)
     const int units = (a.H + 511) / 512 * 4;
     const unsigned passes = (unsigned)((a.T + 16 * MT - 1) / (16 * MT));
     char *ordered = static_cast<char *>(workspace);
-    w4_order_kernel<MT><<<dim3(units, passes), dim3(256), 0, s>>>(a, ordered, units, ZEROS);
+    int *shifts = reinterpret_cast<int *>(ordered + (size_t)passes * units * unit_bytes(MT));
+    w4_order_kernel<MT><<<dim3(passes * (16 * MT)), dim3(256), 0, s>>>(a, ordered, units, shifts);
     if (const hipError_t e = hipGetLastError()) return e;
     // scales and zero points are loaded 16 bytes at a time: short arrays from a copy behind the hidden values
-    uint8_t *spare = static_cast<uint8_t *>(workspace) + (size_t)passes * units * unit_bytes(MT);
+    uint8_t *spare = reinterpret_cast<uint8_t *>(shifts + passes * (16 * MT));
     const int64_t groups = a.V * (a.H / GROUP), bytes = groups * (SCALE_F32 ? 4 : 2);
     if (bytes < 16) {
         w4_short_kernel<<<1, kW4ShortBytes, 0, s>>>(static_cast<const uint8_t *>(a.scales), (int)bytes, spare);
@@ -732,8 +784,8 @@ hipError_t launch_stream(W4Args a, void *workspace, int cus, hipStream_t s)
         a.zeros = spare + kW4ShortBytes;
     }
     const W4Tiles p = w4_tiles(a.V, cus);
-    const int lds = 6 * unit_bytes(MT) + 8 * GroupBlocks<2, GROUP, ZEROS, SCALE_F32>::kLds;
-    kernel<<<dim3((unsigned)p.blocks, passes), dim3(512), lds, s>>>(a, ordered, units, p.wide, p.narrow);
+    const int lds = 6 * unit_bytes(MT) + 64 * MT + 8 * GroupBlocks<2, GROUP, ZEROS, SCALE_F32>::kLds;
+    kernel<<<dim3((unsigned)p.blocks, passes), dim3(512), lds, s>>>(a, ordered, shifts, units, p.wide, p.narrow);
     return hipGetLastError();
 }
 

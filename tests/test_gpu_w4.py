@@ -169,3 +169,85 @@ def test_refuses_arrays_that_are_not_the_weight_s_shape(a3po):
         for w in wrong:
             with pytest.raises((AssertionError, TypeError), match=name):
                 call(**{name: w})
+
+
+# ---- digits: hidden values of one sign, of all sizes --------------------------------------------------------------------
+
+
+def _relative_error(a3po, x, codes, scales, zeros, group):
+    half = codes[:, 0::2] | (codes[:, 1::2] << 4)
+    got = a3po.w4_linear(x.cuda(), half.cuda(), scales.cuda(), zeros=None if zeros is None else zeros.cuda(), group=group,
+                         out_dtype=torch.float32).cpu().double()
+    zero = 8.0 if zeros is None else zeros.double().repeat_interleave(group, 1)
+    w = (codes.double() - zero) * scales.double().repeat_interleave(group, 1)
+    ref = x.double() @ w.t()
+    return float((got - ref).norm() / ref.norm())
+
+
+@pytest.mark.parametrize("T", [1, 16, 24, 50])
+@pytest.mark.parametrize("group,zeros", [(128, False), (128, True), (64, True), (32, True), (32, False)])
+@pytest.mark.parametrize("kind", ["zero mean", "around 1", "positive", "outliers"])
+def test_errors_are_those_of_a_product_in_fp32_whatever_the_hidden_values_signs(a3po, T, group, zeros, kind):
+    """Weights around zero against hidden values that are not: the sums of codes times hidden values are many times what the
+    weights' differing signs leave.  With exact operands the errors are roundings of partial sums, each 2^-24 / sqrt(3) of one:
+    the sum over groups grows to the result in H / group steps, sqrt(H / (2 group)) times that, up to 2.7e-7 here; a
+    group's own sum, 1 / sqrt(H / group) of the result, is rounded up to 32 times in each of them, 2e-7: 3.4e-7
+    together, and held to three times that."""
+    H, N = 4096, 300
+    g = torch.Generator().manual_seed(T + group)
+    codes = (2.5 * torch.randn(N, H, generator=g) + 8.5).clamp(0, 15.99).to(torch.uint8)
+    scales = 0.01 * (0.5 + torch.rand(N, H // group, generator=g))
+    z = torch.randint(7, 10, (N, H // group), generator=g, dtype=torch.uint8) if zeros else None
+    x = torch.randn(T, H, generator=g)
+    if kind == "around 1":
+        x = 1.0 + 0.5 * x
+    elif kind == "positive":
+        x = x.abs()
+    elif kind == "outliers":
+        x[:, ::97] *= 300.0
+    assert _relative_error(a3po, x.bfloat16(), codes, scales, z, group) <= 1e-6
+
+
+@pytest.mark.parametrize("T,H", [(3, 512), (16, 1024), (20, 1024), (40, 1056)])
+def test_powers_of_two_pass_through_exactly(a3po, T, H):
+    """Tokens times powers of two, each its own, from the least to the largest that bfloat16 holds: the same products."""
+    g = torch.Generator().manual_seed(T)
+    codes, scales, z, _, _ = _weight(70, H, 32, True, torch.float32, g)
+    call = lambda x: a3po.w4_linear(x.cuda(), codes.cuda(), scales.cuda(), zeros=z.cuda(), group=32, out_dtype=torch.float32)
+    x = torch.randn(T, H, generator=g).clamp(-3, 3).bfloat16()
+    x[x.abs() < 2.0 ** -6] = 0.25             # (nothing falls below the least normal value on the way down)
+    want = call(x).cpu().double()
+    up = torch.linspace(-118, 120, T).round()
+    got = call((x.double() * 2.0 ** up[:, None].double()).bfloat16()).cpu().double()
+    scaled = want * 2.0 ** up[:, None].double()
+    fine = (scaled.abs() < 3e38) & (scaled.abs() > 2e-38)
+    assert fine.float().mean() > 0.8 and torch.equal(got[fine], scaled[fine])
+
+
+@pytest.mark.parametrize("T,H", [(2, 512), (16, 1024), (30, 1024), (50, 1056)])
+@pytest.mark.parametrize("below", [10, 20, 32])
+def test_small_hidden_values_beside_a_large_one_keep_their_digits(a3po, T, H, below):
+    """A hidden value 2^below times the others that every row multiplies with nothing (its code is the zero point): what is
+    left is the others' product, of values with all of bfloat16's digits."""
+    g = torch.Generator().manual_seed(below)
+    N, group = 60, 32
+    codes = torch.randint(0, 16, (N, H), generator=g, dtype=torch.uint8)
+    z = torch.randint(0, 16, (N, H // group), generator=g, dtype=torch.uint8)
+    scales = 0.01 * (0.5 + torch.rand(N, H // group, generator=g))
+    at = torch.arange(0, H, group * 3)
+    codes[:, at] = z[:, at // group]
+    x = ((1.0 + torch.rand(T, H, generator=g)) * 2.0 ** -below).bfloat16()
+    x[:, at] = 1.5
+    assert _relative_error(a3po, x, codes, scales, z, group) <= 1e-6
+
+
+@pytest.mark.parametrize("T,H", [(4, 512), (18, 1024), (40, 1056)])
+def test_infinite_and_nan_hidden_values_stay_in_their_tokens(a3po, T, H):
+    g = torch.Generator().manual_seed(9)
+    codes, scales, z, w, _ = _weight(50, H, 32, True, torch.bfloat16, g)
+    x = torch.randn(T, H, generator=g).bfloat16()
+    want = a3po.w4_linear(x.cuda(), (codes).cuda(), scales.cuda(), zeros=z.cuda(), group=32, out_dtype=torch.float32).cpu()
+    x[1, 5], x[3, H - 1] = float("nan"), float("inf")
+    got = a3po.w4_linear(x.cuda(), (codes).cuda(), scales.cuda(), zeros=z.cuda(), group=32, out_dtype=torch.float32).cpu()
+    rest = [t for t in range(T) if t not in (1, 3)]
+    assert torch.equal(got[rest], want[rest]) and got[1].isnan().all() and not got[3].isfinite().any()
