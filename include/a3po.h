@@ -506,8 +506,9 @@ int a3po_adjust_logits_bwd(const void *dout, a3po_dtype out_dt, int64_t ld_out, 
  * contiguous.  zeros [N, H / group] bytes, nullable (8 everywhere: codes are symmetric).  group 32, 64 or 128; H a multiple
  * of it, at most 2^20.  out [T, N] dtype out_dt, row stride ld_out.
  * T <= 64 * 65,535; the weight is read once per 64 tokens: the kernels are made for single tokens and small batches.
- * workspace: a3po_workspace_bytes(A3PO_WS_W4_LINEAR, T, 0, H) bytes, 256-byte aligned; 0 (and NULL) for up to 16 tokens
- * with H a multiple of 128 from 256 to 4,096, whose hidden values stay on chip.
+ * workspace: a3po_workspace_bytes(A3PO_WS_W4_LINEAR, T, 0, H) bytes, 256-byte aligned.  Not needed, and NULL, where the hidden
+ * values stay on chip: H a multiple of 128 from 256 on, up to 8,192 for up to 8 tokens (6,144 with fp32 scales of groups of 32),
+ * up to 4,096 for 9 to 16, up to 1,920 for 17 to 32.  The size is 0 where that holds for every group and type of scales.
  * Products are exact and summed in fp32, out is rounded once.  (Hidden values enter as float16 times a power of two of their
  * token's.  Those smaller than 2^-33 of the token's largest lose up to 2^-40 of that; sums are up to 2^46 in magnitude before a
  * scale multiplies them, so scales from 2^82 on may overflow.)  Infinities and NaN in x reach their token's outputs only.

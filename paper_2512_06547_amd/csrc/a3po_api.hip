@@ -564,8 +564,8 @@ int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8
     if (!x || !codes || !scales || !out) return A3PO_E_NULL;
     if (!aligned(x, 2) || !aligned(codes, 16) || !aligned(scales, elem(scale_dt)) || !aligned(out, elem(out_dt)))
         return A3PO_E_ALIGN;
-    if (const size_t need = w4_workspace_bytes(T, H)) {
-        if (!workspace || workspace_bytes < need) return A3PO_E_WORKSPACE;
+    if (!w4_resident(T, H, group, scale_dt == A3PO_F32)) {
+        if (!workspace || workspace_bytes < w4_workspace_bytes(T, H)) return A3PO_E_WORKSPACE;
         if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
     }
     W4Args a;

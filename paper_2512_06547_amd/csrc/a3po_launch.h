@@ -560,18 +560,22 @@ inline int64_t w4_resident_lds(int64_t T, int64_t H)
     const int64_t tp = (int64_t)1 << w4_tokens_shift(T);
     return tp * H * 2 + 16 * 1024 * (T <= 16 ? 1 : 2) + tp * 4;
 }
+// Rows beyond 4,096 are shared by all sixteen wavefronts, whose last ones have little or nothing of them: 16 tokens of H 4,224 /
+// 4,352 / 4,480 x 151,936, groups of 128, take 100 / 109 / 103 us so and 94 / 82 / 95 in chunks, 9 of 4,352 in groups of 64 120 and 87.
+inline bool w4_resident(int64_t T, int64_t H, int group, bool scale_f32)
+{
+    // (four units of a row are as many as a wavefront has registers for; of fp32 scales of groups of 32, three)
+    const int64_t most = T > 8 ? 4096 : group == 32 && scale_f32 ? 16 * 3 * 128 : 16 * 4 * 128;
+    return T <= 32 && H % 128 == 0 && H >= 256 && H <= most && w4_resident_lds(T, H) <= kW4MaxLds;
+}
 inline W4Plan w4_plan(int64_t T, int64_t H, int64_t N, int group, bool scale_f32, int64_t cus)
 {
     W4Plan p = {};
-    // (rows beyond 4,096 are shared by all sixteen wavefronts, whose last ones have little or nothing of them: 16 tokens of H 4,224 /
-    // 4,352 / 4,480 x 151,936, groups of 128, take 100 / 109 / 103 us here and 94 / 82 / 95 in chunks, 9 of 4,352 in groups of 64 120
-    // and 87)
-    if (T > 32 || H % 128 != 0 || H < 256 || H > (T > 8 ? 4096 : 8192)) return p;
+    if (!w4_resident(T, H, group, scale_f32)) return p;
     p.blocks16 = T <= 16 ? 1 : 2;
     p.tp_shift = w4_tokens_shift(T);
     const int64_t units = H / 128;
     p.lds = (int)w4_resident_lds(T, H);
-    if (p.lds > kW4MaxLds) return p;
     // the split of rows over wavefronts that leaves the busiest compute unit the fewest units in turn (a set's joining counts
     // for one)
     int64_t best = 0;
@@ -606,10 +610,10 @@ inline W4Tiles w4_tiles(int64_t N, int64_t cus)
     return t;
 }
 constexpr int kW4ShortBytes = 128;
-// its workspace (none for a call that never takes it: see w4_plan)
+// its workspace: none where a call's hidden values stay on chip whatever its groups and scales are
 inline size_t w4_workspace_bytes(int64_t T, int64_t H)
 {
-    if (T <= 0 || H <= 0 || (T <= 16 && H % 128 == 0 && H >= 256 && H <= 4096)) return 0;
+    if (T <= 0 || H <= 0 || w4_resident(T, H, 32, true)) return 0;
     const int64_t tokens = T <= 16 ? 16 : T <= 32 ? 32 : (T + 63) / 64 * 64;
     return (size_t)(tokens / 16) * (size_t)((H + 511) / 512 * 4) * kW4UnitBytes + ((size_t)tokens * 4 + 255) / 256 * 256 + 2 * kW4ShortBytes;
 }

@@ -187,3 +187,70 @@ int main()
 }
 ''')
     assert run_on_host(str(source), tmp_path) == "ok\n"
+
+
+def test_w4_linear_asks_for_a_workspace_where_its_kernel_uses_one(lib):
+    # x, T, H, ldx, codes, scales, scale_dt, zeros, group, N, out, out_dtype, ld_out, workspace, bytes, stream
+    call = caller(lib.a3po_w4_linear, [P(), 1, 256, 1 << 20, P(), P(), 1, P(), 32, 100, P(0x1001), 0, 100, None, 0, None])
+    ws = lib.a3po_workspace_bytes
+    no_ws = [(1, 256), (8, 6144), (16, 4096), (17, 1920), (32, 1024), (32, 256), (20, 1664)]
+    for T, H in no_ws:
+        assert ws(5, T, 0, H) == 0, (T, H)
+    for T, H in [(1, 128), (1, 8192), (9, 4224), (17, 2048), (32, 2176), (33, 256), (64, 4096), (5, 160)]:
+        assert ws(5, T, 0, H) > 0, (T, H)
+    # out of place, out is refused before the workspace; in place, only a missing workspace is
+    for T, H in no_ws:
+        assert call(a1=T, a2=H) == -4
+    assert call(a1=17, a2=2048, a10=P(), a8=128) == -5 and call(a1=9, a2=4224, a10=P(), a8=64, a6=0) == -5
+    assert call(a1=4, a2=8192, a10=P(), a8=32, a6=0) == -5
+
+
+def test_w4_plans_fit_their_kernels(tmp_path):
+    """A call has a resident plan exactly where it needs no workspace; the plan's units, rows and LDS are what its kernels are
+    there for; tiles of the streaming kernel hold every row once; the workspace holds what its first kernels write."""
+    source = tmp_path / "w4.cpp"
+    source.write_text('''#include <cstdio>
+#include "a3po_common.h"
+#include "a3po_launch.h"
+using namespace a3po;
+int main()
+{
+    for (int cus : {256, 304, 80})
+        for (int64_t N : {1, 15, 16, 17, 530, 4096, 65535, 65536, 131073, 151936, 1 << 22}) {
+            const W4Tiles t = w4_tiles(N, cus);
+            const int64_t rows = t.wide * 256ll + t.narrow * 128ll;
+            const bool tight = t.narrow ? rows - 128 < N : rows - 256 < N;
+            if (rows < N || !tight || t.blocks < 1 || t.blocks > cus || (t.narrow > t.blocks && t.blocks < cus))
+                return std::printf("tiles of %lld rows\\n", (long long)N), 1;
+            for (int64_t T = 1; T <= 40; ++T)
+                for (int64_t H = 32; H <= 9000; H += 32)
+                    for (int group : {32, 64, 128})
+                        for (bool f32 : {false, true}) {
+                            if (H % group) continue;
+                            const W4Plan p = w4_plan(T, H, N, group, f32, cus);
+                            const bool resident = w4_resident(T, H, group, f32);
+                            bool ok = (p.units != 0) == resident && (w4_workspace_bytes(T, H) != 0 || resident);
+                            if (p.units) {
+                                const int64_t a_row = 1 << p.wk_shift, rows_a_set = 16 * (16 >> p.wk_shift);
+                                ok = ok && p.units >= 2 && p.units <= (group == 32 && f32 ? 3 : 4) && p.units <= H / 128 &&
+                                     p.units * a_row >= H / 128 && p.lds <= kW4MaxLds && (1 << p.tp_shift) >= T &&
+                                     p.blocks16 * 16 >= (1 << p.tp_shift) && p.sets * rows_a_set >= N &&
+                                     (p.sets - 1) * rows_a_set < N && p.blocks >= 1 && p.blocks <= p.sets && p.blocks <= cus &&
+                                     (p.blocks == cus || p.blocks == p.sets);
+                            }
+                            if (!ok) return std::printf("T %lld H %lld N %lld\\n", (long long)T, (long long)H, (long long)N), 1;
+                        }
+        }
+    for (int64_t T = 1; T < 5000; ++T)
+        for (int64_t H : {32, 160, 4096, 4128, 1 << 20}) {
+            const size_t have = w4_workspace_bytes(T, H);
+            if (!have) continue;
+            const int64_t readings = (T + 63) / 64, even = (T + readings - 1) / readings;
+            const int64_t a_pass = even <= 16 ? 16 : even <= 32 ? 32 : even <= 48 ? 48 : 64, tokens = (T + a_pass - 1) / a_pass * a_pass;
+            const size_t need = (size_t)tokens / 16 * ((H + 511) / 512 * 4) * kW4UnitBytes + tokens * 4 + 2 * kW4ShortBytes;
+            if (have < need || have % 256) return std::printf("T %lld H %lld\\n", (long long)T, (long long)H), 1;
+        }
+    std::printf("ok\\n");
+}
+''')
+    assert run_on_host(str(source), tmp_path) == "ok\n"
