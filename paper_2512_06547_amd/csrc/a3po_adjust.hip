@@ -330,19 +330,6 @@ __device__ __forceinline__ void fold_values(MaxSum &acc, const float (&f)[N], fl
     acc.m = m;
 }
 
-// Entries of the history that are counted at a time, each with 8 bytes of LDS: all that a text has in a part, where the part's
-// bits leave room for them beside three other workgroups' (further rounds go over the tokens again).
-__device__ __host__ constexpr int numbers_of(int part) { return part <= (1 << 16) ? 2048 : 1024; }
-// LDS of a part's bits, and with their numbers
-__device__ __host__ constexpr int seen_bytes(int part, bool numbers) { return part / 8 + (numbers ? part / 128 + part / 16 : 0); }
-// Tokens that a wavefront notes while it marks them, 4 bytes each, so that they are counted from there: what four workgroups
-// a compute unit leave of the LDS.
-__device__ __host__ constexpr int listed_of(int part, int threads)
-{
-    const int left = 160 * 1024 / 4 - 512 - seen_bytes(part, true) - 8 * numbers_of(part);
-    return (left > 4096 ? left / 4 : 1024) / (threads / kWave) & ~1;
-}
-
 // what is told of a row: of its (max, sum), and of the chosen token's adjusted logit before the temperature
 __device__ __forceinline__ void finish_row(const AdjustArgs &a, int64_t t, MaxSum v, float inv_temperature, float u)
 {
@@ -366,10 +353,10 @@ __global__ __launch_bounds__(THREADS, 4) void adjust_kernel(AdjustArgs a)
     __shared__ int waves[kWaves];
     __shared__ float u_chosen;
     Seen<THREADS> seen(lds, a.part);
-    const int room = numbers_of(a.part);
+    const int room = adjust_numbers(a.part);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane_e = (threadIdx.x & (kWave - 1)) * EPV;
-    uint32_t *counts = reinterpret_cast<uint32_t *>(lds + seen_bytes(a.part, true)), *places = counts + room;
-    const int list_room = listed_of(a.part, THREADS);
+    uint32_t *counts = reinterpret_cast<uint32_t *>(lds + adjust_seen_bytes(a.part, true)), *places = counts + room;
+    const int list_room = adjust_listed(a.part, THREADS);
     uint32_t *list = places + room + wave * list_room;
     const int64_t items = a.T << a.parts_shift;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -665,7 +652,7 @@ hipError_t launch(const AdjustArgs &a, int threads, hipStream_t s)
 {
     const int64_t items = a.T << a.parts_shift, most = 1 << 20;
     const dim3 grid((unsigned)(items < most ? items : most)), block(threads);
-    const size_t lds = a.history ? seen_bytes(a.part, !a.dz) + (a.dz ? 0 : 8 * numbers_of(a.part) + 4 * listed_of(a.part, threads) * (threads / kWave)) : 0;
+    const size_t lds = a.history ? adjust_lds(a.part, threads, a.dz) : 0;
     if (a.dz) adjust_bwd_kernel<ZT, UT, 2><<<grid, block, lds, s>>>(a);
     else if (threads == kAdjustThreads) adjust_kernel<ZT, UT, 2, kAdjustThreads><<<grid, block, lds, s>>>(a);
     else adjust_kernel<ZT, UT, 2, kAdjustThreads / 2><<<grid, block, lds, s>>>(a);

@@ -521,6 +521,23 @@ inline int adjust_threads(int64_t T, const AdjustPlan &p, bool written)
     const int64_t items = T << p.shift, rounds = (items + 511) / 512, rounds256 = (items + 1023) / 1024 * 2;
     return items > 512 && p.part <= 1 << 17 && (!written || rounds256 <= rounds) ? kAdjustThreads / 2 : kAdjustThreads;
 }
+// LDS of a part's bits, and with their numbers
+__device__ __host__ constexpr int adjust_seen_bytes(int part, bool numbers) { return part / 8 + (numbers ? part / 128 + part / 16 : 0); }
+// Entries of the history that are counted at a time, each with 8 bytes of LDS: all that a text has in a part, where the part's
+// bits leave room for them beside three other workgroups' (further rounds go over the tokens again).
+__device__ __host__ constexpr int adjust_numbers(int part) { return part <= (1 << 16) ? 2048 : 1024; }
+// Tokens that a wavefront notes while it marks them, 4 bytes each, so that they are counted from there: what four workgroups
+// a compute unit leave of the LDS.
+__device__ __host__ constexpr int adjust_listed(int part, int threads)
+{
+    const int left = 160 * 1024 / 4 - 512 - adjust_seen_bytes(part, true) - 8 * adjust_numbers(part);
+    return (left > 4096 ? left / 4 : 1024) / (threads / kWave) & ~1;
+}
+inline int adjust_lds(int part, int threads, bool backward)
+{
+    if (backward) return adjust_seen_bytes(part, false);
+    return adjust_seen_bytes(part, true) + 8 * adjust_numbers(part) + 4 * adjust_listed(part, threads) * (threads / kWave);
+}
 // workspace: the chosen tokens' adjusted logits, then a (max, sum) per part
 inline size_t adjust_partials_offset(int64_t T) { return ((size_t)T * 4 + 255) / 256 * 256; }
 inline size_t adjust_workspace_bytes(int64_t T, int64_t V)

@@ -416,3 +416,64 @@ def test_a_row_s_nan_shows_in_the_log_prob_of_a_token_that_is_masked(a3po, V, ba
         lse, logp = r["lse"].cpu(), r["logp"].cpu()
         assert lse[1::2].isnan().all() and logp[1::2].isnan().all(), token
         assert lse[::2].isfinite().all() and (logp[::2] == -math.inf).all(), token
+
+
+# ---- rows whole at full vocabularies --------------------------------------------------------------------------------------
+
+
+def _wide(T, V, zt, seed, tokens):
+    """Logits and adjustments on the GPU, every row with `tokens` of history from one array, some with far more."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda lo, hi: lo + (hi - lo) * torch.rand(T, device="cuda", generator=g)
+    z = 4.0 * torch.randn(T, V, device="cuda", generator=g, dtype=DT[zt])
+    n = torch.randint(0, tokens + 1, (T,), device="cuda", generator=g, dtype=torch.int32)
+    n[1], n[T // 2], n[T - 1] = 30000, 9001, 0      # (more than the lists and numbers of a workgroup hold, and nothing)
+    ids = torch.cat(((V * torch.rand(20000, device="cuda", generator=g) ** 3).int(),
+                     torch.randint(0, V, (20000,), device="cuda", generator=g, dtype=torch.int32)))
+    start = torch.randint(0, 10000, (T,), device="cuda", generator=g)
+    p = dict(history=ids, hist_start=start, hist_len=n, prompt_len=(n * rand(0, 1)).int(), repetition=rand(0.8, 1.5),
+             frequency=rand(-0.2, 0.6), presence=rand(-0.2, 0.8), temperature=rand(0.5, 2.0),
+             bias=3.0 * torch.randn(V, device="cuda", generator=g),
+             allowed=torch.randint(-2 ** 31, 2 ** 31, (T, (V + 31) // 32), device="cuda", generator=g).int())
+    y = torch.randint(0, V, (T,), device="cuda", generator=g, dtype=torch.int32)
+    y[3] = ids[start[1] + 12000]
+    rows = torch.unique(torch.cat((torch.tensor([0, 1, 2, 3, T // 2, T - 2, T - 1]), torch.randint(0, T, (8,)))))
+    return z, p, y, rows.cuda()
+
+
+def _rows_of(z, p, rows):
+    """The rows' share of the arguments on the CPU, for `reference`."""
+    ok = (p["allowed"][rows][:, :, None] >> torch.arange(32, device="cuda", dtype=torch.int32)) & 1
+    own = {k: v if k in ("history", "bias") else v[rows] for k, v in p.items()}
+    return z[rows].cpu(), {k: v.cpu() for k, v in own.items()}, ok.view(len(rows), -1)[:, :z.shape[1]].bool().cpu()
+
+
+@pytest.mark.parametrize("T,V", [(1030, 70001), (1030, 131073), (1024, 151936), (1025, 262144), (1030, 262145)])
+@pytest.mark.parametrize("zt,ut,write", [("bf16", "bf16", True), ("bf16", "f32", True), ("f32", "f32", True), ("bf16", "bf16", False)])
+def test_rows_taken_whole_at_full_vocabularies(a3po, T, V, zt, ut, write):
+    '''From 1,024 rows on they are one part each, up to 262,144 entries: the longest bits, half as many numbers, the shortest
+    lists, and workgroups of 512 threads beyond 131,072.'''
+    z, p, y, rows = _wide(T, V, zt, V, 600)
+    r = a3po.adjust_logits(z, chosen=y, write=write, out_dtype=DT[ut], **p)
+    zs, ps, ok = _rows_of(z, p, rows)
+    u, bar, _ = reference(zs, ps, ok)
+    if write:
+        got = r["out"][rows].cpu()
+        fine = u.isfinite()
+        assert torch.equal(got[~fine].double(), u[~fine]) and within(got[fine], u[fine], bar[fine]).all()
+    lse = torch.logsumexp(u, 1)
+    logp = u[torch.arange(len(rows)), y[rows].long().cpu()] - lse
+    for name, ref in (("lse", lse), ("logp", logp)):
+        got, fine = r[name][rows].cpu().double(), ref.isfinite()
+        assert torch.equal(got[~fine], ref[~fine]) and ((got - ref).abs()[fine] <= 1e-5 * (1 + ref.abs()[fine])).all(), name
+
+
+@pytest.mark.parametrize("T,V,zt,ut", [(4100, 65535, "bf16", "bf16"), (2050, 131072, "bf16", "f32"), (1030, 151936, "f32", "f32"),
+                                       (4100, 65537, "bf16", "f32")])
+def test_gradients_of_the_widest_parts(a3po, T, V, zt, ut):
+    z, p, _, rows = _wide(T, V, zt, V, 600)
+    du = torch.randn(T, V, device="cuda", dtype=DT[ut], generator=torch.Generator(device="cuda").manual_seed(5))
+    got = a3po.adjust_logits_bwd(du, z, **p)[rows].cpu()
+    zs, ps, ok = _rows_of(z, p, rows)
+    ref = du[rows].cpu().double() * reference(zs, ps, ok)[2]
+    assert within(got, ref, 4 * U * ref.abs()).all()

@@ -254,3 +254,35 @@ int main()
 }
 ''')
     assert run_on_host(str(source), tmp_path) == "ok\n"
+
+
+def test_adjusted_rows_numbers_and_lists_fit_lds(tmp_path):
+    '''What a part keeps in LDS beside the kernel's own 100 bytes, and the threads that number its blocks of 512 entries.  Every
+    plan that a call can get: parts of the forward pass end at 262,144 entries, those of the backward pass at 65,536.'''
+    source = tmp_path / "lds.cpp"
+    source.write_text('''#include <cstdio>
+#include "a3po_common.h"
+#include "a3po_launch.h"
+using namespace a3po;
+int main()
+{
+    int widest[2] = {0, 0}, small_list = 0, half_numbers = 0, few_threads = 0;
+    for (int bytes : {2, 4})
+        for (bool backward : {false, true})
+            for (int64_t T : {1, 2, 64, 300, 600, 1023, 1024, 1030, 5000, 1 << 22})
+                for (int64_t V = 1; V < 0x7FFFFFFF; V += V < 600000 ? 1 + V / 4096 : 1 + V / 9)
+                    for (bool written : {false, true}) {
+                        const AdjustPlan p = adjust_plan(T, V, bytes, backward);
+                        const int threads = backward ? kAdjustThreads : adjust_threads(T, p, written);
+                        const bool known = threads == kAdjustThreads || (!backward && threads == kAdjustThreads / 2);
+                        if (!known || adjust_lds(p.part, threads, backward) > 64 * 1024 - 128 || (!backward && p.part / 512 > threads))
+                            return std::printf("T %lld V %lld part %d\\n", (long long)T, (long long)V, p.part), 1;
+                        if (p.part > widest[backward]) widest[backward] = p.part;
+                        small_list += !backward && adjust_listed(p.part, threads) * (threads / kWave) == 1024;
+                        half_numbers += !backward && adjust_numbers(p.part) == 1024;
+                        few_threads += threads < kAdjustThreads;
+                    }
+    std::printf("%d %d %d %d %d\\n", widest[0], widest[1], small_list > 0, half_numbers > 0, few_threads > 0);
+}
+''')
+    assert run_on_host(str(source), tmp_path) == f"{1 << 18} {1 << 16} 1 1 1\n"
