@@ -477,3 +477,21 @@ def test_gradients_of_the_widest_parts(a3po, T, V, zt, ut):
     zs, ps, ok = _rows_of(z, p, rows)
     ref = du[rows].cpu().double() * reference(zs, ps, ok)[2]
     assert within(got, ref, 4 * U * ref.abs()).all()
+
+
+@pytest.mark.parametrize("zt,ut", PAIRS)
+@pytest.mark.parametrize("T,V", [(3, 9001), (300, 1025), (1100, 500)])
+def test_what_is_not_finite_has_its_sign(a3po, zt, ut, T, V):
+    '''A masked entry is -inf and nothing else, in the history or not, whatever stood there; an unmasked infinity keeps its sign.'''
+    z, p, ok = make(T, V, seed=21, most=80)
+    z = z.to(DT[zt])
+    z[0, ~ok[0]] = math.inf
+    z[1, ~ok[1]] = math.nan
+    z[2, ::5] = -math.inf
+    z[2, 2::5] = math.inf
+    p["repetition"].clamp_(min=1.0)
+    u, _, _ = reference(z, p, ok)
+    got = a3po.adjust_logits(z.cuda(), out_dtype=DT[ut], **dev(p))["out"].cpu().double()
+    assert torch.equal(got[~ok], torch.full_like(got[~ok], -math.inf))
+    assert torch.equal(got.isposinf(), u.isposinf()) and torch.equal(got.isneginf(), u.isneginf())
+    assert u.isposinf().any() and not got.isnan().any()
