@@ -251,3 +251,37 @@ def test_infinite_and_nan_hidden_values_stay_in_their_tokens(a3po, T, H):
     got = a3po.w4_linear(x.cuda(), (codes).cuda(), scales.cuda(), zeros=z.cuda(), group=32, out_dtype=torch.float32).cpu()
     rest = [t for t in range(T) if t not in (1, 3)]
     assert torch.equal(got[rest], want[rest]) and got[1].isnan().all() and not got[3].isfinite().any()
+
+
+# ---- several sets, several tiles a workgroup ----------------------------------------------------------------------------
+
+# T, N, H, group, zeros, fp32 scales.  With 256 compute units: more than two sets of rows a workgroup, an odd number for some and
+# an even one for others; two, three and four units a wavefront; one and two blocks of tokens.
+MANY_SETS = [(2, 200003, 256, 128, False, False), (16, 140003, 256, 32, True, False), (1, 200003, 384, 64, True, True),
+             (16, 140003, 384, 32, False, True), (2, 200003, 512, 128, False, False), (16, 140003, 512, 64, True, False),
+             (20, 200003, 256, 64, False, True), (32, 140003, 384, 32, True, False), (17, 200003, 512, 128, True, True),
+             (5, 90001, 1536, 128, False, False), (12, 66001, 896, 32, True, False)]
+# streamed: more than two rounds of 256 rows a workgroup and a ragged end; scales of one block of 64 bytes a row and of many
+MANY_TILES = [(3, 140003, 160, 32, True, False), (20, 140003, 160, 32, True, True), (40, 200003, 160, 32, False, False),
+              (50, 140003, 160, 32, True, False), (64, 140003, 384, 128, True, False), (50, 140003, 1056, 32, True, True),
+              (40, 140003, 1088, 64, False, True), (130, 140003, 288, 32, True, False), (9, 140003, 4352, 128, False, False),
+              (20, 140003, 2176, 128, True, True)]
+
+
+@pytest.mark.parametrize("T,N,H,group,zeros,f32", MANY_SETS + MANY_TILES)
+def test_more_rows_than_one_round_of_compute_units(a3po, T, N, H, group, zeros, f32):
+    """Products are exact; what is rounded are the sums, no more often than a group has terms and a row groups, and the scaling."""
+    g = torch.Generator(device="cuda").manual_seed(T + H)
+    q = torch.randint(0, 16, (N, H), device="cuda", generator=g, dtype=torch.uint8)
+    scales = 0.01 * (0.2 + torch.rand(N, H // group, device="cuda", generator=g))
+    scales = scales if f32 else scales.bfloat16()
+    z = torch.randint(0, 16, (N, H // group), device="cuda", generator=g, dtype=torch.uint8) if zeros else None
+    x = (0.5 + torch.randn(T, H, device="cuda", generator=g)).bfloat16()
+    got = a3po.w4_linear(x, q[:, 0::2] | (q[:, 1::2] << 4), scales, zeros=z, group=group, out_dtype=torch.float32)
+    w = q.double()
+    w -= z.double().repeat_interleave(group, 1) if zeros else 8.0
+    w *= scales.double().repeat_interleave(group, 1)
+    ref = x.double() @ w.t().contiguous()
+    err = (got.double() - ref).abs()
+    bar = U * (group + H // group + 4) * (x.double().abs() @ w.abs_().t().contiguous())
+    assert (err <= bar).all() and float(err.norm()) <= 1e-6 * float(ref.norm())

@@ -286,3 +286,33 @@ int main()
 }
 ''')
     assert run_on_host(str(source), tmp_path) == f"{1 << 18} {1 << 16} 1 1 1\n"
+
+
+def test_the_cases_of_many_rows_take_several_sets_and_tiles_a_workgroup(tmp_path):
+    """What the GPU tests' sizes are there for, with the compute units of an MI355X."""
+    pytest.importorskip("torch")
+    from test_gpu_w4 import MANY_SETS, MANY_TILES
+    source = tmp_path / "many.cpp"
+    rows = lambda cases: ", ".join(f"{{{T}, {N}, {H}, {group}, {int(f32)}}}" for T, N, H, group, _, f32 in cases)
+    source.write_text(f'''#include <cstdio>
+#include "a3po_common.h"
+#include "a3po_launch.h"
+using namespace a3po;
+int main()
+{{
+    const int sets[][5] = {{{rows(MANY_SETS)}}}, tiles[][5] = {{{rows(MANY_TILES)}}};
+    for (auto &c : sets) {{
+        const W4Plan p = w4_plan(c[0], c[2], c[1], c[3], c[4], 256);
+        if (p.sets <= 2 * p.blocks || p.sets % p.blocks == 0) return std::printf("T %d N %d H %d\\n", c[0], c[1], c[2]), 1;
+        std::printf("%d%d ", p.units, p.blocks16);
+    }}
+    for (auto &c : tiles) {{
+        const W4Tiles t = w4_tiles(c[1], 256);
+        if (w4_plan(c[0], c[2], c[1], c[3], c[4], 256).units || t.wide < 2 * t.blocks || t.narrow == 0)
+            return std::printf("T %d N %d H %d\\n", c[0], c[1], c[2]), 1;
+    }}
+    std::printf("ok\\n");
+}}
+''')
+    kinds = run_on_host(str(source), tmp_path).split()
+    assert kinds.pop() == "ok" and {"21", "31", "41", "22", "32", "42"} <= set(kinds), kinds
