@@ -495,3 +495,26 @@ def test_what_is_not_finite_has_its_sign(a3po, zt, ut, T, V):
     assert torch.equal(got[~ok], torch.full_like(got[~ok], -math.inf))
     assert torch.equal(got.isposinf(), u.isposinf()) and torch.equal(got.isneginf(), u.isneginf())
     assert u.isposinf().any() and not got.isnan().any()
+
+
+def test_gradient_on_another_stream_and_in_a_graph(a3po):
+    z, p, _ = make(8, 10000, seed=22)
+    d, zg = dev(p), z.to(torch.bfloat16).cuda()
+    du, out = torch.randn(8, 10000, device="cuda"), torch.empty(8, 10000, dtype=torch.bfloat16, device="cuda")
+    want = a3po.adjust_logits_bwd(du, zg, **d)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        a3po.adjust_logits_bwd(du, zg, dlogits=out, **d)
+    s.synchronize()
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a3po.adjust_logits_bwd(du, zg, dlogits=out, **d)
+    for i in range(3):
+        du.copy_(torch.randn(8, 10000, generator=torch.Generator().manual_seed(i)))
+        want = a3po.adjust_logits_bwd(du, zg, **d)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i

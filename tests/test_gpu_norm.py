@@ -299,3 +299,42 @@ def test_where_the_sums_need_a_workspace(a3po):
     rc = a3po.lib().a3po_norm_bwd(x.data_ptr(), 0, 3074, y.data_ptr(), 0, 8, 3074, 3074, None, 0, None, rstd.data_ptr(), 1,
                                   y.data_ptr(), 3074, many["dweight"].data_ptr(), None, 0, None, 0, None)
     assert rc < 0 and "workspace" in a3po.binding.strerror(rc)
+
+
+@pytest.mark.parametrize("T,in_place", [(64, False), (64, True), (3000, False)])
+def test_both_passes_on_another_stream_and_in_a_graph(a3po, T, in_place):
+    """One launch and two (dx over dy, many rows)."""
+    H = 520
+    x, w, b, g = _inputs(T, H, torch.bfloat16, torch.float32, seed=23)
+    x, w, b, dy = x.cuda(), w.cuda(), b.cuda(), torch.randn(T, H, generator=g).to(torch.bfloat16).cuda()
+    ws = torch.empty(a3po.workspace_bytes(T, 0, H, which=a3po.A3PO_WS_NORM_BWD), dtype=torch.uint8, device="cuda")
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    dw, db = torch.empty(H, device="cuda"), torch.empty(H, device="cuda")
+
+    def step(y, dx, dw, db, ws=None):
+        _, mean, rstd = a3po.norm_fwd(x, w, b, out=y)
+        if in_place:
+            dx.copy_(dy)
+        a3po.norm_bwd(dx if in_place else dy, x, w, rstd, mean=mean, want_dbias=True, dx=dx, dweight=dw, dbias=db, workspace=ws)
+        return y, dx, dw, db
+
+    fresh = lambda: step(torch.empty_like(x), torch.empty_like(x), torch.empty_like(dw), torch.empty_like(db))
+    got, want = (y, dx, dw, db), fresh()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(*got, ws)
+    s.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*got, ws)
+    for i in range(3):
+        x.copy_(torch.randn(T, H, generator=g))
+        dy.copy_(torch.randn(T, H, generator=g))
+        want = fresh()
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(got, want)), i
