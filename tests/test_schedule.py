@@ -117,3 +117,13 @@ def test_few_token_kernel_with_one_row_block_waits_for_its_own_count(assembly, b
     wait = [6 + 2 * (blocks // 4), "barrier"]
     first = events.index(wait[0])
     assert events[first:first + 4 * (2 + len(direct) + 2)] == (wait + direct + load * 2) * 4, events[first:]
+
+
+@pytest.mark.parametrize("name,least", [("a3po_norm.hip", 150), ("a3po_adjust.hip", 13), ("a3po_w4.hip", 90)])
+def test_kernels_around_the_head_spill_nothing(assembly, name, least):
+    """Rows of the norm, parts of adjusted logits and codes in flight stay in registers, in every form: a spilled offset or
+    vector makes the loads of a row, which are to be in flight together, wait for one another, and its accesses count among
+    those that the 4-bit products' kernel waits for by number."""
+    spills = vector_spills(assembly(name))
+    assert len(spills) >= least
+    assert not [(kernel, n) for kernel, n in spills if n > 0]
