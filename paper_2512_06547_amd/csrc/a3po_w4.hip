@@ -14,7 +14,7 @@
 // With up to 16 tokens the kernel is bound by the weight's bytes, beyond a fixed 6 us for the hidden values and the first codes:
 // one token, 1,536 x 151,936 in groups of 128 27 us (4.4 TB/s), 16 tokens, 4,096 x 151,936 in groups of 128 66 (5.1).  With more it is
 // the vector instructions, and that they and the matrix instructions take turns rather than overlap: 50 tokens, 4,096 x 151,936, fp32
-// scales of groups of 32 and zero points, 156 us against 92 for the bytes; a group's scale is a multiply-add for every 32 codes
+// scales of groups of 32 and zero points, 153 us against 92 for the bytes; a group's scale is a multiply-add for every 32 codes
 // and token, and is the larger half of the vector instructions.
 #include "a3po_common.h"
 #include "a3po_direct.h"
@@ -751,9 +751,10 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4Args a, const char *or
     extern __shared__ __align__(16) char lds[];
     int *shifts = reinterpret_cast<int *>(lds + 6 * unit_bytes(MT));  // of this pass' tokens
     char *own = lds + 6 * unit_bytes(MT) + 64 * MT + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kOwn;
-    if (threadIdx.x < 16 * MT) shifts[threadIdx.x] = token_shifts[blockIdx.y * (16 * MT) + threadIdx.x];  // (read behind barriers)
-    const char *x = ordered + (int64_t)blockIdx.y * units * unit_bytes(MT);
-    const int64_t t0 = (int64_t)blockIdx.y * (16 * MT);
+    const uint32_t pass = __builtin_amdgcn_readfirstlane(blockIdx.y);  // (or the loads' descriptor ends up in vector registers)
+    if (threadIdx.x < 16 * MT) shifts[threadIdx.x] = token_shifts[pass * (16 * MT) + threadIdx.x];  // (read behind barriers)
+    const char *x = ordered + (int64_t)pass * units * unit_bytes(MT);
+    const int64_t t0 = (int64_t)pass * (16 * MT);
     stream_tiles<MT, 2, GROUP, ZEROS, SCALE_F32>(a, x, units, 0, wide_tiles, t0, lds, own, shifts);
     stream_tiles<MT, 1, GROUP, ZEROS, SCALE_F32>(a, x, units, (int64_t)wide_tiles * 256, narrow_tiles, t0, lds, own, shifts);
 }

@@ -127,3 +127,27 @@ def test_kernels_around_the_head_spill_nothing(assembly, name, least):
     spills = vector_spills(assembly(name))
     assert len(spills) >= least
     assert not [(kernel, n) for kernel, n in spills if n > 0]
+
+
+@pytest.mark.parametrize("blocks", [1, 2, 3, 4])
+@pytest.mark.parametrize("form", [f"Li{group}ELb{zeros}ELb{f32}" for group in (32, 64, 128) for zeros in (0, 1) for f32 in (0, 1)])
+def test_streamed_codes_are_waited_for_by_their_count(assembly, blocks, form):
+    """w4_stream_kernel waits for a chunk of hidden values by the number of operations that may still be in flight, which holds
+    for one order of issue: a chunk's direct loads, then its codes'.  Before the loop there are two chunks, behind each counted
+    wait in it one (scales and zero points come ahead of the first, outputs behind the second, which makes the
+    waits stricter).  A direct load whose descriptor were in vector registers would come in a loop of its own."""
+    body, = kernels(assembly("a3po_w4.hip"), f"w4_stream_kernelILi{blocks}E{form}E").values()
+    assert "v_cmp_eq_u64" not in body
+    events = memory_events(body)
+    assert not [e for e in events if str(e).startswith("scratch")]
+    end = [i for i, e in enumerate(events) if e == 0 and not isinstance(e, str) and i > events.index("direct")]
+    assert len(end) == 2                        # (the wide tiles' loop, the narrow ones')
+    for rows, part in ((2, events[:end[0]]), (1, events[end[0]:end[1]])):
+        chunk, wait = ["direct"] * blocks + ["global_load_dwordx4"] * (2 * rows), 4 * rows + blocks
+        at = [i for i in range(len(part) - 1) if part[i] == wait and part[i + 1] == "barrier"]
+        assert len(at) == 3                     # before the loop, and in it behind its second chunk, then its first
+        loads = lambda lo, hi: [e for e in part[lo:hi] if isinstance(e, str) and e != "barrier"]
+        assert loads(0, at[0])[-2 * len(chunk):] == chunk * 2 and not loads(at[0], at[1])
+        first, second = loads(at[1], at[2]), loads(at[2], len(part))
+        assert first[first.index("direct"):] == chunk and "direct" not in second[len(chunk):]
+        assert second[:len(chunk)] == chunk and not [e for e in second[len(chunk):] if "store" not in e]
