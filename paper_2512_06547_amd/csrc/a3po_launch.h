@@ -581,7 +581,8 @@ inline int64_t w4_resident_lds(int64_t T, int64_t H)
 // 4,352 / 4,480 x 151,936, groups of 128, take 100 / 109 / 103 us so and 94 / 82 / 95 in chunks, 9 of 4,352 in groups of 64 120 and 87.
 inline bool w4_resident(int64_t T, int64_t H, int group, bool scale_f32)
 {
-    // (four units of a row are as many as a wavefront has registers for; of fp32 scales of groups of 32, three)
+    // (four units of a row are as many as a wavefront has registers for; of fp32 scales of groups of 32, three.  With these limits a
+    // thread has no more than eight pieces of 16 bytes of the hidden values.)
     const int64_t most = T > 8 ? 4096 : group == 32 && scale_f32 ? 16 * 3 * 128 : 16 * 4 * 128;
     return T <= 32 && H % 128 == 0 && H >= 256 && H <= most && w4_resident_lds(T, H) <= kW4MaxLds;
 }

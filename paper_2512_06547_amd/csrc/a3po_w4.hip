@@ -67,12 +67,6 @@ struct Widen {
         return f16x8_t{a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
     }
 };
-// eight hidden values in the same order
-__device__ __forceinline__ uint4 order_like_codes(const uint4 &v)
-{
-    return make_uint4(__builtin_amdgcn_perm(v.z, v.x, 0x05040100u), __builtin_amdgcn_perm(v.z, v.x, 0x07060302u),
-                      __builtin_amdgcn_perm(v.w, v.y, 0x05040100u), __builtin_amdgcn_perm(v.w, v.y, 0x07060302u));
-}
 // the larger magnitude at each place of a pair, as bits
 __device__ __forceinline__ uint32_t larger(uint32_t most, const uint4 &v)
 {
@@ -83,15 +77,16 @@ __device__ __forceinline__ uint32_t larger(uint32_t most, const uint4 &v)
 }
 // the power of two that brings a token whose largest magnitude has these bits to between 2^15 and 2^16
 __device__ __forceinline__ int token_shift(uint32_t most) { return most ? 142 - max((int)(most >> 7), 1) : 0; }
+// eight hidden values as float16 times that, in the order of the codes
 __device__ __forceinline__ uint4 to_halves(const uint4 &v, int shift)
 {
-    auto two = [&](uint32_t w) {
+    auto low = [&](uint32_t w) { return __builtin_amdgcn_ldexpf(__uint_as_float(w << 16), shift); };
+    auto high = [&](uint32_t w) { return __builtin_amdgcn_ldexpf(__uint_as_float(w & 0xFFFF0000u), shift); };
+    auto two = [](float a, float b) {
         typedef float f32x2_t __attribute__((ext_vector_type(2)));
-        const f32x2_t f = {__builtin_amdgcn_ldexpf(__uint_as_float(w << 16), shift),
-                           __builtin_amdgcn_ldexpf(__uint_as_float(w & 0xFFFF0000u), shift)};
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2_t));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t));
     };
-    return make_uint4(two(v.x), two(v.y), two(v.z), two(v.w));
+    return make_uint4(two(low(v.x), low(v.z)), two(high(v.x), high(v.z)), two(low(v.y), low(v.w)), two(high(v.y), high(v.w)));
 }
 
 // Lanes l, l + 16, l + 32, l + 48 hold four blocks of 32 codes of one row, a block each; afterwards d[b] of the four lanes
@@ -196,7 +191,8 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int n16 = lane & 15, q = lane >> 4;
     const int WK = 1 << wk_shift, WR = kAll >> wk_shift, wk = wave & (WK - 1), wr = wave >> wk_shift;
-    const int TP = MT > 1 ? 16 * MT : 1 << tp_shift;
+    static_assert(MT <= 2, "tokens are a power of two");
+    const int tps = MT > 1 ? 5 : tp_shift, TP = 1 << tps;
     // (the last wavefronts' runs move down to end with the row; units that another one has as well count for nothing here)
     const int units = a.H >> 7, u0 = min(wk * UPW, units - UPW), skip = wk * UPW - u0;
     const int64_t groups = a.H / GROUP, row_bytes = a.H / 2;
@@ -223,43 +219,38 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
         __builtin_amdgcn_sched_barrier(0);  // (in this order: what is waited for first is issued first)
     };
     // The hidden values first, then the weight: what is asked for later arrives later, and those would be waited for with all of
-    // the weight that is in flight.
-    const int pieces = units * 16 * TP, token = (int)threadIdx.x & (TP - 1);  // (a thread's pieces are all one token's)
-    auto load_x = [&](int p) {
-        p = min(p, pieces - 1);
-        const int64_t from = min((int64_t)(p & (TP - 1)), a.T - 1);
-        return *reinterpret_cast<const u32x4_half *>(static_cast<const char *>(a.x) + (from * a.ldx + p / TP * 8) * 2);
+    // the weight that is in flight.  A thread's pieces, eight values each, are all one token's: piece i is the row's k8_of(i)-th.
+    // (Threads beyond the last token have that one again; their products are not stored.)
+    const int eights = units * 16, token = (int)threadIdx.x & (TP - 1), most_pieces = (eights + (1024 >> tps) - 1) >> (10 - tps);
+    auto k8_of = [&](int i) { return ((int)threadIdx.x >> tps) + (i << (10 - tps)); };
+    const char *x_row = static_cast<const char *>(a.x) + min((int64_t)token, a.T - 1) * a.ldx * 2;
+    auto load_x = [&](int i) {
+        const u32x4_half h = *reinterpret_cast<const u32x4_half *>(x_row + min(k8_of(i), eights - 1) * 16);
+        return make_uint4(h.x, h.y, h.z, h.w);
     };
-    auto ordered = [&](u32x4_half h) {
-        const bool on = token < a.T;
-        return order_like_codes(make_uint4(on ? h.x : 0u, on ? h.y : 0u, on ? h.z : 0u, on ? h.w : 0u));
-    };
-    auto place_x = [&](int p) {
-        const int k8 = p / TP;
+    auto place_x = [&](int i) {
+        const int k8 = k8_of(i);
         // groups of a whole unit: the lanes of a block of codes keep it, and the quarter of the unit that they multiply is theirs
         const int at = GROUP == 128 ? (k8 & ~15) | (k8 & 3) << 2 | (k8 >> 2 & 3) : k8;
-        return reinterpret_cast<uint4 *>(xs + ((size_t)at * TP + token) * 16);
+        return reinterpret_cast<uint4 *>(xs + ((at << tps) + token) * 16);
     };
-    constexpr int kFirst = 4;  // (two cost single tokens nothing and gain them 6 %, eight gain 16 x 4,096 3 % and cost 1 x 896 1 us)
-    u32x4_half first[kFirst];
+    // Four a thread, and four more, two at a time, where rows are long (eight always: 1 x 896 0.5 us more, 16 x 2,048 1.2; the longer
+    // rows' behind the weight: 16 x 4,096 2.5 more).
+    constexpr int kPieces = 8;  // (w4_resident lets no more in)
+    uint4 mine[kPieces];
 #pragma unroll
-    for (int i = 0; i < kFirst; ++i) first[i] = load_x(threadIdx.x + i * 1024);
+    for (int i = 0; i < 4; ++i) mine[i] = load_x(i);
+    if (most_pieces > 4) mine[4] = load_x(4), mine[5] = load_x(5);
+    if (most_pieces > 6) mine[6] = load_x(6), mine[7] = load_x(7);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int b = 0; b < NB; ++b) fetch((int)blockIdx.x + b * (int)gridDim.x, run[b]);
-    // the token's largest value: of this thread's, the wavefront's, all sixteen's
-    uint4 mine[kFirst];
+    // the token's largest value: of this thread's, the wavefront's, all sixteen's (pieces beyond the row are its last again)
     uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < kFirst; ++i) {
-        mine[i] = ordered(first[i]);
-        if ((int)threadIdx.x + i * 1024 < pieces) most = larger(most, mine[i]);
-    }
-    for (int p = threadIdx.x + kFirst * 1024; p < pieces; p += 1024) {
-        const uint4 v = ordered(load_x(p));
-        most = larger(most, v);
-        *place_x(p) = v;
-    }
+    for (int i = 0; i < 4; ++i) most = larger(most, mine[i]);
+    if (most_pieces > 4) most = larger(larger(most, mine[4]), mine[5]);
+    if (most_pieces > 6) most = larger(larger(most, mine[6]), mine[7]);
     most = max(most & 0xFFFFu, most >> 16);
     for (int off = TP; off < kWave; off <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, off, kWave));
     if (lane < TP) reinterpret_cast<uint32_t *>(red)[wave * TP + lane] = most;
@@ -269,11 +260,8 @@ __global__ __launch_bounds__(1024) void w4_resident_kernel(W4Args a, int wk_shif
     const int shift = token_shift(most);
     if ((int)threadIdx.x < TP) shifts[threadIdx.x] = shift;
 #pragma unroll
-    for (int i = 0; i < kFirst; ++i) {
-        const int p = threadIdx.x + i * 1024;
-        if (p < pieces) *place_x(p) = to_halves(mine[i], shift);
-    }
-    for (int p = threadIdx.x + kFirst * 1024; p < pieces; p += 1024) *place_x(p) = to_halves(*place_x(p), shift);
+    for (int i = 0; i < kPieces; ++i)
+        if (k8_of(i) < eights) *place_x(i) = to_halves(mine[i], shift);
     meet();
 
     const Widen widen;
@@ -405,7 +393,7 @@ __global__ __launch_bounds__(256) void w4_order_kernel(W4Args a, char *to, int u
         if (p < pieces)
             *reinterpret_cast<uint4 *>(to + (pass * units + (p >> 4)) * unit_bytes(MT) +
                                        (((p >> 2 & 3) * MT + in_pass / 16) * kWave + (p & 3) * 16 + in_pass % 16) * 16) =
-                to_halves(order_like_codes(v), shift);
+                to_halves(v, shift);
     };
 #pragma unroll
     for (int i = 0; i < kFirst; ++i) keep(threadIdx.x + i * 256, first[i]);

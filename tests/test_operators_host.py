@@ -233,7 +233,7 @@ int main()
                             if (p.units) {
                                 const int64_t a_row = 1 << p.wk_shift, rows_a_set = 16 * (16 >> p.wk_shift);
                                 ok = ok && p.units >= 2 && p.units <= (group == 32 && f32 ? 3 : 4) && p.units <= H / 128 &&
-                                     p.units * a_row >= H / 128 && p.lds <= kW4MaxLds && (1 << p.tp_shift) >= T &&
+                                     p.units * a_row >= H / 128 && p.lds <= kW4MaxLds && (H << p.tp_shift) <= 8 * 8 * 1024 && (1 << p.tp_shift) >= T &&
                                      p.blocks16 * 16 >= (1 << p.tp_shift) && p.sets * rows_a_set >= N &&
                                      (p.sets - 1) * rows_a_set < N && p.blocks >= 1 && p.blocks <= p.sets && p.blocks <= cus &&
                                      (p.blocks == cus || p.blocks == p.sets);
