@@ -473,7 +473,8 @@ typedef struct {
  *   lse_out[t] = log sum_v exp u[t,v],  logp_out[t] = u[t, chosen[t]] - lse_out[t].
  * logits [T, V] dtype dt, row stride ld.  out [T, V] dtype out_dt, row stride ld_out, nullable (log-probs only); it may
  * alias logits exactly when dtype and stride agree.  chosen [T] int32, required with logp_out; an id outside [0,V) gives
- * logp 0.  lse_out, logp_out [T] float, nullable; at least one output is required.  Everything is computed in fp32, and lse
+ * logp 0.  lse_out, logp_out [T] float, nullable; at least one output is required.  Everything is computed in fp32 (divisions by
+ * temperature and repetition are products with their fp32 reciprocals, which have to be finite), and lse
  * and logp are those of the fp32 values: out in float32 holds exactly these, out in bfloat16 rounds them once.
  * A row with nothing allowed (or all -inf) has lse -inf; a chosen token with u = -inf has logp -inf.
  * Masked entries are -inf whatever the logit holds, NaN included; an unmasked NaN or +inf makes the row's lse and logp NaN,
@@ -510,7 +511,7 @@ int a3po_adjust_logits_bwd(const void *dout, a3po_dtype out_dt, int64_t ld_out, 
  * values stay on chip: H a multiple of 128 from 256 on, up to 8,192 for up to 8 tokens (6,144 with fp32 scales of groups of 32),
  * up to 4,096 for 9 to 16, up to 1,920 for 17 to 32.  The size is 0 where that holds for every group and type of scales.
  * Products are exact and summed in fp32, out is rounded once.  (Hidden values enter as float16 times a power of two of their
- * token's.  Those smaller than 2^-33 of the token's largest lose up to 2^-40 of that; sums are up to 2^46 in magnitude before a
+ * token's.  Those smaller than 2^-32 of the token's largest lose up to 2^-40 of that; sums are up to 2^46 in magnitude before a
  * scale multiplies them, so scales from 2^82 on may overflow.)  Infinities and NaN in x reach their token's outputs only.
  */
 int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8_t *codes, const void *scales,

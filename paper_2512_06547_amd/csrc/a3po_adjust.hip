@@ -14,9 +14,12 @@
 // than the exponential, and the work on the history, the reductions and the row's parameters cost what some forty entries a
 // thread do, so that rows are not cut further than it takes to fill the chip (scoring of 8,192 x 50,001 bfloat16: a test per
 // entry, four parts a row 1,055 us; a penalty per entry in LDS 553; bits, four parts 735; bits, whole rows 306; now 227).
-// What bounds it: scoring, 819 MB in 227 us (3.6 TB/s), the vector instructions and the history's latencies (with workgroups of
-// 512, 280 us: 212 without a history, 31 for the bits, 16 for the counts, 36 for the entries); decoding, 64 x 151,936 to fp32 with 16,384 tokens of history, 33 us, the passes over the history
-// (18 us without one); the gradient, two streams and little else, memory: 8,192 x 151,936 4.98 GB in 1,050 us (4.7 TB/s, what a large copy reaches).
+// What bounds it: scoring, 819 MB in 228 us (3.6 TB/s), the vector instructions, active in 91 % of a compute unit's cycles, 17 an entry
+// with the history's (with workgroups of 512, 280 us: 212 without a history, 31 for the bits, 16 for the counts, 36 for the
+// entries; 4,096 x 151,936 without one 237 us, 5.3 TB/s); decoding, 64 x 151,936 to fp32 with 16,384 tokens of history, 34 us, the passes over
+// the history (18 us without one); written rows, 4,096 x 151,936 bfloat16 to fp32, memory where there is no history (805 us, 4.6 TB/s),
+// and the work on one of up to 2,047 tokens, in series with its row, 235 us more; the gradient, two streams and little else, memory:
+// 8,192 x 151,936 4.98 GB in 1,050 us (4.7 TB/s, what a large copy reaches).
 // Rows are read and written through the caches: the entries of the history are fetched a second time (non-temporal: 301 for
 // 281 us, decoding 42 for 38), and the next kernel reads what is written here.
 // Maximum and sum of exp are taken before the temperature, which then is part of the exponent's scale.  All arithmetic is

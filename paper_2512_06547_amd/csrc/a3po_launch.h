@@ -447,8 +447,10 @@ inline int64_t norm_bwd_blocks(int64_t T, int64_t H, int x_bytes)
 }
 // Few rows: the sums over rows are taken by workgroups of the same launch that read x and dy a second time, which dx must
 // therefore leave alone.  Against two kernels, us, inputs from memory: fp32 16 x 4,096 3.8 / 7.2, 300 x 1,536 5.4 / 9.8, 1,000 x
-// 1,536 11.8 / 10.7, 1,000 x 3,000 14.8 / 15.5; bf16 300 x 8,192 9.2 / 15.6, 1,000 x 1,536 12.7 / 10.3, 1,000 x 3,000 14.0 / 14.1,
-// beside the gap between two and the 4 us that a launch takes the host; 1,000 x 4,096 17.4 / 15.9 and 19.0 / 14.1.
+// 1,536 11.8 / 10.7, 1,000 x 3,000 14.8 / 15.5; bf16 300 x 8,192 9.2 / 15.6, 1,000 x 1,536 12.7 / 10.3, 1,000 x 3,000 14.0 / 14.1;
+// 1,000 x 4,096 17.4 / 15.9 and 19.0 / 14.1.  Calls, with the gap between two and the 4 us that a launch takes the host, and replays of a
+// graph, inputs alternating: fp32 300 x 1,536 10.2 / 14.1 and 4.3 / 8.5, 1,000 x 896 10.1 / 14.0 and 7.5 / 8.2, 1,000 x 1,536 10.5 / 13.5 and
+// 10.5 / 9.8, 700 x 4,096 12.7 / 14.8 and 13.0 / 14.7; bf16 1,000 x 1,536 10.1 / 13.7 and 8.1 / 9.2, 1,000 x 3,000 12.5 / 14.2 and 12.5 / 13.6.
 inline bool norm_bwd_in_one(int64_t T, int64_t H, const void *x, const void *dy, const void *dx)
 {
     return T > 0 && T <= A3PO_NORM_ONE_LAUNCH_ROWS && T * H <= A3PO_NORM_ONE_LAUNCH_ELEMENTS && dx != x && dx != dy;
@@ -512,10 +514,10 @@ inline AdjustPlan adjust_plan(int64_t T, int64_t V, int z_bytes, bool backward =
 }
 // Threads of a forward workgroup.  A compute unit's registers hold two of 512 or four of 256, which have half of the work that each
 // wavefront has besides the entries, and more rows whose latencies cover one another's; a few long parts, which LDS holds two of,
-// keep 512, and so do rows that are written, memory's more than the units', where 512 end in fewer rounds.  512 / 256, us: scoring
-// 8,192 x 50,001 315 / 248, 3,000 x 32,000 83 / 65, 1,036 x 87,709 65 / 66, 500 x 65,000 in halves 28 / 22, 2,500 x 151,936 183 / 193
-// (halves); written 300 x 50,001 in halves 32 / 28, 256 x 151,936 in quarters 94 / 90, 150 x 151,936 in eighths 50 / 57, 1,300 x 87,709
-// 177 / 187; 64 x 151,936 in eighths, 16,384 tokens of history 33 / 42.
+// keep 512, and so do rows that are written, memory's more than the units', where 512 end in fewer rounds.  512 / 256, us, bf16 logits,
+// up to 2,048 tokens of history: scoring 8,192 x 50,001 277 / 232, 3,000 x 32,000 80 / 64, 1,036 x 87,709 64 / 67, 500 x 65,000 in halves
+// 31 / 25; written as bf16 and as fp32, 300 x 50,001 in halves 29 / 25 and 32 / 29, 256 x 151,936 in quarters 44 / 38 and 68 / 68, 150 x
+// 151,936 in eighths 35 / 31 and 45 / 46, 1,300 x 87,709 141 / 150 and 213 / 224; 64 x 151,936 in eighths, 16,384 tokens 33 / 40 and 34 / 41.
 inline int adjust_threads(int64_t T, const AdjustPlan &p, bool written)
 {
     const int64_t items = T << p.shift, rounds = (items + 511) / 512, rounds256 = (items + 1023) / 1024 * 2;

@@ -5,12 +5,13 @@
 //   dx = rstd (g - mean(g) - xhat mean(g xhat)),  g = dy w   (without mean(g) in the root-mean-square form)
 //   dw = sum over rows of dy xhat,  db = sum over rows of dy
 //
-// Both passes read each row once and keep it in registers; statistics, products and sums are fp32, and every output is
-// rounded once.  The variance is the mean of (x - mean)^2, taken from the registers after the mean is known: the
-// difference of two sums loses all digits of rows whose mean is large against their spread.
+// Both passes keep each row in registers and read it once (the gradient of few rows a second time, for the sums over rows);
+// statistics, products and sums are fp32, and every output is rounded once.  The variance is the mean of (x - mean)^2, taken from
+// the registers after the mean is known: the difference of two sums loses all digits of rows whose mean is large against their
+// spread.
 // The kernels are bound by memory where there are rows enough: the gradient of 65,536 x 4,096 bfloat16 moves 1.61 GB in 280 us
 // (5.8 TB/s), the forward pass of 10,240 x 2,049 fp32 to bfloat16 126 MB in 25.  Fewer rows are a chain of latencies, a load, two
-// reductions and a store: 64 x 1,536 forward 3.5 us, 1,000 x 1,536 fp32 backward 11.8.
+// reductions and a store: 64 x 1,536 forward 3.5 us, 1,000 x 1,536 fp32 backward 10.5.
 #include <type_traits>
 
 #include "a3po_common.h"
@@ -187,8 +188,6 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(Nor
     }
 }
 
-// Each workgroup takes rows in turn and leaves its share of dw and db in partials [workgroup][dw | db][H]; a second
-// kernel adds the shares in one order, so that identical inputs give identical sums.
 // The sums over rows of 4 vectors of columns, straight from x and dy (mean and rstd are known): four lanes read a row's 64 bytes,
 // so that a workgroup takes 64 rows at a time (32 rows of 128 bytes: a fifth more time), three or four rows each in
 // flight; lanes and wavefronts add theirs in a fixed order.  A vector at the end moves down to end with
@@ -267,6 +266,8 @@ __device__ __forceinline__ void column_sums(const NormArgs &a, const ColumnSums 
     out[column] = to.accumulate ? out[column] + total : total;
 }
 
+// Each workgroup takes rows in turn and leaves its share of dw and db in partials [workgroup][dw | db][H]; a second
+// kernel adds the shares in one order, so that identical inputs give identical sums.
 // With to.blocks, that many workgroups come first that take the sums over rows, and no partial sums are left.
 template <typename XT, typename YT, int LANES, int NV, bool CENTER>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(NormArgs a, float *partials, ColumnSums to)

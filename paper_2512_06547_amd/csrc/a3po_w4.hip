@@ -7,15 +7,15 @@
 // code's bits go into the mantissa of 1,024, and one addition for two codes takes 1,024 + zero off (1,024 + 16 n, for
 // the codes that lie four bits higher, leave with a factor of 1/16 in the same instruction).  Hidden values become float16 times
 // a power of two of the token's, which brings its largest to between 2^15 and 2^16: bfloat16's eight digits are kept by all that
-// are not below 2^-33 of that, and those lose no more than 2^-40 of it.  So products are exact, a group's sum in fp32 is of
+// are not below 2^-32 of that, and those lose no more than 2^-40 of it.  So products are exact, a group's sum in fp32 is of
 // the size of its terms, its scale multiplies it in fp32, and the token's power of two leaves from the output, which is rounded
 // once.  (Codes as bfloat16 16 + n with the excess (16 + zero) sum x taken off the sum cost an instruction less for eight, and
 // digits: where hidden values are of one sign the sum is many times what is left of it, and errors of 4e-6 came of that, 2e-7 here.)
 // With up to 16 tokens the kernel is bound by the weight's bytes, beyond a fixed 6 us for the hidden values and the first codes:
-// one token, 1,536 x 151,936 in groups of 128 27 us (4.4 TB/s), 16 tokens, 4,096 x 151,936 in groups of 128 66 (5.1).  With more it is
-// the vector instructions, and that they and the matrix instructions take turns rather than overlap: 50 tokens, 4,096 x 151,936, fp32
-// scales of groups of 32 and zero points, 153 us against 92 for the bytes; a group's scale is a multiply-add for every 32 codes
-// and token, and is the larger half of the vector instructions.
+// one token, 1,536 x 151,936 in groups of 128 28 us (4.3 TB/s), 16 tokens, 4,096 x 151,936 in groups of 128 67 (4.9).  With more it is
+// the vector instructions, and that they and the matrix instructions take turns rather than overlap, two wavefronts a SIMD that meet
+// every two units: 50 tokens, 4,096 x 151,936, fp32 scales of groups of 32 and zero points, 153 us against 92 for the bytes, of
+// its cycles vector instructions 61 %, matrix instructions 25 %; a group's scale is a multiply-add for every 32 codes and token.
 #include "a3po_common.h"
 #include "a3po_direct.h"
 #include "a3po_launch.h"
