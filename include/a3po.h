@@ -115,7 +115,9 @@ enum {
     A3PO_WS_FUSED_LMHEAD_LOSS = 2,
     A3PO_WS_NORM_BWD = 3,     /* T and H */
     A3PO_WS_ADJUST_LOGITS = 4, /* T and V */
-    A3PO_WS_W4_LINEAR = 5      /* T and H */
+    A3PO_WS_W4_LINEAR = 5,     /* T and H */
+    A3PO_WS_SAMPLE = 6,        /* T and V */
+    A3PO_WS_GRAD_NORM = 7      /* T: the number of tensors */
 };
 
 /* Bytes of device workspace the given entry point needs (256-byte aligned base). */
@@ -517,6 +519,107 @@ int a3po_adjust_logits_bwd(const void *dout, a3po_dtype out_dt, int64_t ld_out, 
 int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8_t *codes, const void *scales,
                    a3po_dtype scale_dt, const uint8_t *zeros, int32_t group, int64_t N, void *out, a3po_dtype out_dt,
                    int64_t ld_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- operators that close the loop ------------------------------------------------------------------
+ *
+ * A rollout draws tokens from the policy's logits, training updates the weights with the gradients that the loss leaves, and
+ * the updated head is laid out in 4 bits for the next rollouts.
+ */
+
+/* The policy that a token is drawn from.  Host struct of device pointers [T], read during the call only; every array but
+ * `uniform` may be NULL (no such cut; temperature 1). */
+typedef struct {
+    const float *uniform;     /* the random numbers, in [0, 1): below 0 counts as 0, from 1 on as just below 1           */
+    const float *temperature; /* x = (z - max z) / temperature, >= 0; 0 is greedy: temperature 1 with top_k 1            */
+    const int32_t *top_k;     /* the k largest entries stay; <= 0: all                                                  */
+    const float *top_p;       /* of those, the fewest largest whose mass reaches top_p of theirs; >= 1: all, <= 0: one  */
+    const float *min_p;       /* of those, the ones whose probability is at least min_p of the largest's; <= 0: all,    */
+                              /* >= 1: the entries that equal the largest                                               */
+} a3po_sampling;
+
+/*
+ * Draws a token of every row.  With x as above and w = exp(x), entries are ordered by logit, the lower index first among equal
+ * ones; the cuts each leave the beginning of that order, the largest entry always among it, entries at -inf never.  Then, over
+ * the entries kept, in the order of their indices,
+ *   token_out[t] = the first v with sum_{j <= v} w_j > uniform[t] sum_j w_j,
+ *   logp_out[t] = x_token - log sum_{kept} w,   logp_full_out[t] = x_token - log sum_{all} w,
+ *   kept_out[t] = how many entries are kept,  allowed_out: bit v % 32 of word allowed_out[t * allowed_ld + v / 32] says that v is.
+ * The words are what a3po_adjust_logits takes as `allowed` (bits past V are 0): training then sees the policy that was cut.
+ * logits [T, V] dtype dt, row stride ld.  token_out [T] is required; the other outputs are nullable; allowed_ld >= ceil(V / 32).
+ * Weights and their sums are computed in 64 bits, so the token is the definition's unless a border of two tokens lies within
+ * about 2^-36 of the sum of the drawn number; identical calls give identical results.
+ * A row without an entry above -inf has token -1, kept 0, no allowed bit and log-probs of -inf.  A NaN or +inf in the row, a
+ * negative temperature or a NaN among the row's parameters give token -1, kept 0, no bit and log-probs NaN.  (The loss treats
+ * a token of -1 as masked.)
+ * workspace: a3po_workspace_bytes(A3PO_WS_SAMPLE, T, V, 0) bytes, 256-byte aligned; not needed, and NULL, where that is 0.
+ */
+int a3po_sample(const void *logits, a3po_dtype dt, int64_t T, int64_t V, int64_t ld, const a3po_sampling *policy,
+                int32_t *token_out, float *logp_out, float *logp_full_out, int32_t *kept_out, int32_t *allowed_out,
+                int64_t allowed_ld, void *workspace, size_t workspace_bytes, void *stream);
+
+typedef enum {
+    A3PO_STATE_F32 = 0, /* exp_avg and exp_avg_sq are float [n] */
+    A3PO_STATE_8BIT = 1 /* 8 bits an element and 8 an exponent of 32 elements */
+} a3po_state_format;
+
+/* One tensor of an optimizer step: n elements, contiguous, all pointers on the device.
+ * A3PO_STATE_8BIT: element i of a state is value(i) * 2^(scale[i / 32] - 127), where value is a byte: exp_avg in e4m3 (OCP
+ * float8, 3 bits of mantissa), exp_avg_sq in e5m2; the scales are bytes [ceil(n / 32)].  All bytes zero is a state of zeros. */
+typedef struct {
+    void *param;               /* dtype param_dt; updated in place                                  */
+    const void *grad;          /* dtype grad_dt                                                     */
+    void *exp_avg;             /* the running mean of gradients, updated in place                   */
+    void *exp_avg_sq;          /* the running mean of their squares, updated in place               */
+    uint8_t *exp_avg_scale;    /* A3PO_STATE_8BIT only                                              */
+    uint8_t *exp_avg_sq_scale; /* A3PO_STATE_8BIT only                                              */
+    void *copy;                /* bfloat16 [n], nullable: receives the updated parameters, rounded  */
+    int64_t n;
+} a3po_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;            /* the number of this step, from 1 on                                                          */
+    const float *lr_dev;     /* device [1], nullable: used in place of lr (a captured step whose rate changes)              */
+    const int64_t *step_dev; /* device [1], nullable: used in place of step                                                 */
+    const float *norm;       /* device [1], nullable: the gradients' norm, as a3po_grad_norm leaves it.  Gradients enter     */
+                             /* times min(1, max_norm / (norm + 1e-6)); where the norm is not finite nothing is changed.    */
+    double max_norm;         /* > 0 with norm                                                                               */
+    uint32_t seed;           /* of the stochastic roundings: a new one each step                                            */
+} a3po_adamw_options;
+
+/*
+ * sqrt(sum over all tensors and elements of (scale g)^2) -> norm_out [1] float.  Host arrays: grads [count] device pointers of
+ * contiguous tensors, dtype dt, sizes [count] elements.  Squares are summed in 64 bits in a fixed order.  No tensors: 0.
+ * workspace: a3po_workspace_bytes(A3PO_WS_GRAD_NORM, count, 0, 0) bytes, 256-byte aligned.
+ */
+int a3po_grad_norm(const void *const *grads, const int64_t *sizes, int64_t count, a3po_dtype dt, float scale, float *norm_out,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One step of AdamW for every tensor (host array [count], read during the call only):
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps).
+ * All arithmetic is fp32 on the states' unrounded new values.  Roundings: float parameters none, their copy to nearest;
+ * bfloat16 parameters stochastically (the share of an update below the last bit that is not lost is its mean); 8-bit exp_avg to
+ * nearest; 8-bit exp_avg_sq stochastically (to nearest it would never fall: one step takes away less than half a bit) and never
+ * from above zero to zero, so that no update is divided by eps alone.  The random bits of element i of tensor k are a function
+ * of seed, k and i alone.  A block of 32 that holds an infinity or NaN reads as NaN afterwards; with `norm` such a step is left out.
+ * Tensors must not overlap.  0 <= beta < 1, eps >= 0, lr >= 0, weight_decay >= 0, step >= 1, else A3PO_E_VALUE.
+ */
+int a3po_adamw_step(const a3po_adamw_tensor *tensors, int64_t count, a3po_dtype param_dt, a3po_dtype grad_dt, int32_t state_format,
+                    const a3po_adamw_options *options, void *stream);
+
+/*
+ * Lays a weight out for a3po_w4_linear: per group of `group` consecutive elements of a row of weight [N, H] (dtype dt, row
+ * stride ld), with hi and lo its extremes,
+ *   zeros given: scale = (max(hi, 0) - min(lo, 0)) / 15 and zero = round(-min(lo, 0) / scale);  else scale = max(hi / 7, -lo / 8)
+ *   and zero = 8;  code = round(w / scale) + zero within [0, 15].
+ * (The scale is rounded to scale_dt first, divisions are products with fp32 reciprocals, and rounding is to the nearest even.)
+ * A group of zeros, or of values so small that the scale falls below 2^-126, stands for zeros.  Weights must be finite.
+ * codes, scales, zeros (nullable) as in a3po_w4_linear; group 32, 64 or 128, H a multiple of it, at most 2^20.
+ */
+int a3po_w4_quantize(const void *weight, a3po_dtype dt, int64_t N, int64_t H, int64_t ld, int32_t group, uint8_t *codes,
+                     void *scales, a3po_dtype scale_dt, uint8_t *zeros, void *stream);
 
 #ifdef __cplusplus
 }

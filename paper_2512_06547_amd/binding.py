@@ -22,6 +22,9 @@ A3PO_WS_FUSED_LMHEAD_LOSS = 2
 A3PO_WS_NORM_BWD = 3
 A3PO_WS_ADJUST_LOGITS = 4
 A3PO_WS_W4_LINEAR = 5
+A3PO_WS_SAMPLE = 6
+A3PO_WS_GRAD_NORM = 7
+A3PO_STATE_F32, A3PO_STATE_8BIT = 0, 1
 A3PO_NORM_LAYER, A3PO_NORM_RMS = 0, 1
 A3PO_NORM_ONE_LAUNCH_ROWS, A3PO_NORM_ONE_LAUNCH_ELEMENTS = 1024, 3 << 20
 
@@ -49,6 +52,27 @@ class LogitAdjustments(ctypes.Structure):
                 ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
                 ("bias", ctypes.c_void_p), ("bias_ld", ctypes.c_int64), ("allowed", ctypes.c_void_p),
                 ("allowed_ld", ctypes.c_int64)]
+
+
+class Sampling(ctypes.Structure):
+    """a3po_sampling (include/a3po.h)."""
+    _fields_ = [("uniform", ctypes.c_void_p), ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
+
+
+class AdamwTensor(ctypes.Structure):
+    """a3po_adamw_tensor (include/a3po.h)."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p),
+                ("exp_avg_sq", ctypes.c_void_p), ("exp_avg_scale", ctypes.c_void_p), ("exp_avg_sq_scale", ctypes.c_void_p),
+                ("copy", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class AdamwOptions(ctypes.Structure):
+    """a3po_adamw_options (include/a3po.h)."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("lr_dev", ctypes.c_void_p),
+                ("step_dev", ctypes.c_void_p), ("norm", ctypes.c_void_p), ("max_norm", ctypes.c_double),
+                ("seed", ctypes.c_uint32)]
 
 
 _SIGNATURES = {
@@ -85,6 +109,11 @@ _SIGNATURES = {
                                               ctypes.POINTER(LogitAdjustments), _P, _I64, _P]),
     "a3po_w4_linear": (ctypes.c_int, [_P, _I64, _I64, _I64, _P, _P, ctypes.c_int, _P, _I32, _I64, _P, ctypes.c_int, _I64,
                                       _P, _SZ, _P]),
+    "a3po_sample": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I64, _I64, ctypes.POINTER(Sampling), _P, _P, _P, _P, _P, _I64, _P,
+                                   _SZ, _P]),
+    "a3po_grad_norm": (ctypes.c_int, [_P, _P, _I64, ctypes.c_int, _F32, _P, _P, _SZ, _P]),
+    "a3po_adamw_step": (ctypes.c_int, [_P, _I64, ctypes.c_int, ctypes.c_int, _I32, ctypes.POINTER(AdamwOptions), _P]),
+    "a3po_w4_quantize": (ctypes.c_int, [_P, ctypes.c_int, _I64, _I64, _I64, _I32, _P, _P, ctypes.c_int, _P, _P]),
 }
 
 _lib = None
@@ -686,6 +715,178 @@ def w4_linear(x, codes, scales, zeros=None, group: int = 128, out=None, out_dtyp
                                 int(group), N, _ptr(out), od, ld_out, _ptr(workspace), 0 if workspace is None else workspace.numel(),
                                 _stream()), "a3po_w4_linear")
     return out
+
+
+# ---- operators that close the loop -----------------------------------------------------------------------------------
+
+
+def _here(*tensors):
+    """Calls go to the current device's current stream: tensors of another device are refused."""
+    now = None
+    for t in tensors:
+        if t is None:
+            continue
+        at = t.get_device()  # (-1: none)
+        if now is None and at >= 0:
+            now = _torch()._C._cuda_getDevice()
+        if at != now:
+            raise ValueError(f"a tensor on {t.device}, but calls go to the current device" + ("" if now is None else f", cuda:{now}"))
+
+
+def sample(logits, uniform, V=None, *, temperature=None, top_k=None, top_p=None, min_p=None, want_logp=True,
+           want_logp_full=False, want_kept=False, want_allowed=False, workspace=None):
+    """a3po_sample -> dict(token int32[T], logp, logp_full float32[T] | None, kept int32[T] | None, allowed int32[T, ceil(V/32)]
+    | None, workspace | None).
+
+    A token of each row, drawn by the row's number of ``uniform`` float32 [T] from what temperature, top_k, top_p and min_p
+    ([T], float32 but for top_k, int32) leave of it; logp is the log-prob under that cut policy, logp_full under the uncut one.
+    ``allowed`` holds the kept entries as adjust_logits takes them: training on the tokens then sees the policy they came from."""
+    torch = _torch()
+    dt, T, V, ld = _logits_meta(logits, V)
+    dev = logits.device
+    assert logits.shape[1] >= V, f"logits: need [{T}, {V}]"
+    policy = Sampling()
+    policy.uniform = _ptr(_vec(uniform, torch.float32, T, "uniform"))
+    if temperature is not None:
+        policy.temperature = _ptr(_vec(temperature, torch.float32, T, "temperature"))
+    if top_k is not None:
+        policy.top_k = _ptr(_vec(top_k, torch.int32, T, "top_k"))
+    if top_p is not None:
+        policy.top_p = _ptr(_vec(top_p, torch.float32, T, "top_p"))
+    if min_p is not None:
+        policy.min_p = _ptr(_vec(min_p, torch.float32, T, "min_p"))
+    _here(logits, uniform, temperature, top_k, top_p, min_p, workspace)
+    token = torch.empty(T, dtype=torch.int32, device=dev)
+    logp = torch.empty(T, dtype=torch.float32, device=dev) if want_logp else None
+    full = torch.empty(T, dtype=torch.float32, device=dev) if want_logp_full else None
+    kept = torch.empty(T, dtype=torch.int32, device=dev) if want_kept else None
+    words = (V + 31) // 32
+    allowed = torch.empty((T, words), dtype=torch.int32, device=dev) if want_allowed else None
+    if workspace is None:
+        need = workspace_bytes(T, V, which=A3PO_WS_SAMPLE)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _check(lib().a3po_sample(_ptr(logits), dt, T, V, ld, ctypes.byref(policy), _ptr(token), _ptr(logp), _ptr(full), _ptr(kept),
+                             _ptr(allowed), words, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()),
+           "a3po_sample")
+    return dict(token=token, logp=logp, logp_full=full, kept=kept, allowed=allowed, workspace=workspace)
+
+
+def _tensors(tensors, name):
+    """The dtype code that all of them share; each is contiguous on the current GPU."""
+    tensors = list(tensors)
+    _here(*tensors)
+    dtype = tensors[0].dtype if tensors else None
+    for t in tensors:
+        assert t.is_cuda and t.dtype == dtype and t.is_contiguous(), f"{name}: need contiguous tensors of one dtype on GPU"
+    return tensors, _dtype_code(tensors[0], name) if tensors else A3PO_F32
+
+
+def grad_norm(grads, scale: float = 1.0, out=None, workspace=None):
+    """a3po_grad_norm -> norm float32 [1] (``out``, or a new tensor): the 2-norm of all gradients times ``scale`` together."""
+    torch = _torch()
+    grads, dt = _tensors(grads, "grads")
+    count = len(grads)
+    if out is None:
+        out = torch.empty(1, dtype=torch.float32, device=grads[0].device if grads else "cuda")
+    _vec(out, torch.float32, 1, "out")
+    _here(out, workspace)
+    if workspace is None and count:
+        workspace = torch.empty(workspace_bytes(count, which=A3PO_WS_GRAD_NORM), dtype=torch.uint8, device=out.device)
+    pointers = (ctypes.c_void_p * count)(*[t.data_ptr() or None for t in grads])
+    sizes = (ctypes.c_int64 * count)(*[t.numel() for t in grads])
+    _check(lib().a3po_grad_norm(pointers, sizes, count, dt, float(scale), _ptr(out), _ptr(workspace),
+                                0 if workspace is None else workspace.numel(), _stream()), "a3po_grad_norm")
+    return out
+
+
+def adamw_state(param, bits: int = 32):
+    """(exp_avg, exp_avg_sq, scales) of zeros for a parameter: float32 of its size and None, or with ``bits`` 8 float8_e4m3fn,
+    float8_e5m2 and the pair of uint8 exponents that blocks of 32 elements share."""
+    torch = _torch()
+    if bits == 32:
+        return torch.zeros_like(param, dtype=torch.float32), torch.zeros_like(param, dtype=torch.float32), None
+    if bits != 8:
+        raise ValueError("states have 32 bits or 8")
+    zero = lambda n: torch.zeros(n, dtype=torch.uint8, device=param.device)
+    return (zero(param.shape).view(torch.float8_e4m3fn), zero(param.shape).view(torch.float8_e5m2),
+            (zero((param.numel() + 31) // 32), zero((param.numel() + 31) // 32)))
+
+
+def adamw_state_values(state, scale):
+    """The float32 values that an 8-bit state stands for (for checkpoints and inspection; elementary torch operations)."""
+    torch = _torch()
+    unit = (scale.to(torch.int32) << 23).view(torch.float32).repeat_interleave(32)[:state.numel()]
+    return (state.float().view(-1) * unit).view(state.shape)
+
+
+def adamw_step(params, grads, exp_avgs, exp_avg_sqs, *, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+               weight_decay: float = 0.0, scales=None, copies=None, norm=None, max_norm: float = 1.0, seed: int = 0):
+    """a3po_adamw_step: one step for every tensor of the list ``params``, in place, with the states that adamw_state made
+    (``scales``: their pairs, with 8-bit states) and, where ``copies`` are given, the updated parameters rounded to bfloat16.
+
+    ``step`` (from 1 on) and ``lr`` are numbers, or CUDA tensors of one int64 and one float32 where a captured graph is to see
+    them change.  ``norm``: what grad_norm left; gradients are scaled to ``max_norm`` at most, and a step whose norm is not
+    finite changes nothing.  ``seed``: of the roundings by chance (bfloat16 parameters, 8-bit exp_avg_sq), another each step."""
+    torch = _torch()
+    params, pd = _tensors(params, "params")
+    grads, gd = _tensors(grads, "grads")
+    count = len(params)
+    exp_avgs, exp_avg_sqs = list(exp_avgs), list(exp_avg_sqs)
+    assert len(grads) == len(exp_avgs) == len(exp_avg_sqs) == count, "need a gradient and two states for each parameter"
+    bytes_ = scales is not None
+    first, second = (torch.float8_e4m3fn, torch.float8_e5m2) if bytes_ else (torch.float32, torch.float32)
+    scales = list(scales) if bytes_ else None
+    copies = list(copies) if copies is not None else None
+    assert scales is None or len(scales) == count, "need a pair of scales for each parameter"
+    assert copies is None or len(copies) == count, "need a copy for each parameter"
+    table = (AdamwTensor * count)()
+    u8 = torch.uint8
+    for i in range(count):
+        p, g, m, v, t = params[i], grads[i], exp_avgs[i], exp_avg_sqs[i], table[i]
+        n = p.numel()
+        assert g.numel() == n, f"grads[{i}]: need {n} elements"
+        _vec(m, first, n, "exp_avgs")
+        _vec(v, second, n, "exp_avg_sqs")
+        t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.n = p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), n
+        if bytes_:
+            a, b = scales[i]
+            t.exp_avg_scale = _vec(a, u8, (n + 31) // 32, "scales").data_ptr()
+            t.exp_avg_sq_scale = _vec(b, u8, (n + 31) // 32, "scales").data_ptr()
+        if copies is not None:
+            t.copy = _vec(copies[i], torch.bfloat16, n, "copies").data_ptr()
+    opt = AdamwOptions(beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay, max_norm=max_norm, seed=int(seed) & 0xFFFFFFFF)
+    if isinstance(step, torch.Tensor):
+        opt.step_dev = _ptr(_vec(step, torch.int64, 1, "step"))
+        _here(step)
+    else:
+        opt.step = int(step)
+    if isinstance(lr, torch.Tensor):
+        opt.lr_dev = _ptr(_vec(lr, torch.float32, 1, "lr"))
+        _here(lr)
+    else:
+        opt.lr = float(lr)
+    if norm is not None:
+        opt.norm = _ptr(_vec(norm, torch.float32, 1, "norm"))
+        _here(norm)
+    _check(lib().a3po_adamw_step(table, count, pd, gd, A3PO_STATE_8BIT if bytes_ else A3PO_STATE_F32, ctypes.byref(opt), _stream()),
+           "a3po_adamw_step")
+
+
+def w4_quantize(weight, group: int = 128, scale_dtype=None, zeros: bool = False):
+    """a3po_w4_quantize -> (codes uint8 [N, H/2], scales [N, H/group] of ``scale_dtype`` (float32 by default), zeros uint8
+    [N, H/group] or None), as w4_linear takes them: the 4-bit layout of weight [N, H]."""
+    torch = _torch()
+    dt, ld = _rows(weight, "weight")
+    N, H = weight.shape
+    assert group in (32, 64, 128) and H % group == 0, "group must be 32, 64 or 128 and divide H"
+    _here(weight)
+    dev = weight.device
+    codes = torch.empty((N, H // 2), dtype=torch.uint8, device=dev)
+    scales = torch.empty((N, H // group), dtype=torch.float32 if scale_dtype is None else scale_dtype, device=dev)
+    zero = torch.empty((N, H // group), dtype=torch.uint8, device=dev) if zeros else None
+    _check(lib().a3po_w4_quantize(_ptr(weight), dt, N, H, ld, int(group), _ptr(codes), _ptr(scales),
+                                  _dtype_code(scales, "scales"), _ptr(zero), _stream()), "a3po_w4_quantize")
+    return codes, scales, zero
 
 
 

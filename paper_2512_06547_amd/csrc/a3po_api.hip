@@ -19,6 +19,7 @@ namespace {
 using WsLayout = LossWsLayout;
 
 constexpr int64_t kMaxRows = (int64_t)1 << 40, kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxTensors = (int64_t)1 << 24, kMaxElements = (int64_t)1 << 40;
 
 inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -113,6 +114,8 @@ size_t a3po_workspace_bytes(int which, int64_t T, int64_t V, int64_t H)
     if (which == A3PO_WS_FUSED_LMHEAD_LOSS) return lmhead_bwd_workspace_bytes(T, V, H);
     if (which == A3PO_WS_NORM_BWD) return norm_bwd_workspace_bytes(T, H);
     if (which == A3PO_WS_ADJUST_LOGITS) return adjust_workspace_bytes(T, V);
+    if (which == A3PO_WS_SAMPLE) return T > 0 && V > 0 && T <= kMaxRows && V <= (int64_t)0x7FFFFFFF ? sample_workspace_bytes(T, V) : 0;
+    if (which == A3PO_WS_GRAD_NORM) return T <= kMaxTensors ? grad_norm_workspace_bytes(T) : 0;
     if (which == A3PO_WS_W4_LINEAR) return T > kW4MaxTokens || H > (1 << 20) ? 0 : w4_workspace_bytes(T, H);
     return 0;
 }
@@ -583,6 +586,117 @@ int a3po_w4_linear(const void *x, int64_t T, int64_t H, int64_t ldx, const uint8
     a.ldo = ld_out;
     a.H = (int)H;
     return launch_w4_linear(a, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+}
+
+int a3po_sample(const void *logits, a3po_dtype dt, int64_t T, int64_t V, int64_t ld, const a3po_sampling *policy,
+                int32_t *token_out, float *logp_out, float *logp_full_out, int32_t *kept_out, int32_t *allowed_out,
+                int64_t allowed_ld, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_logits(logits, (int)dt, T, V, ld)) return rc;
+    if (allowed_out && (allowed_ld < (V + 31) / 32 || allowed_ld > kMaxStride)) return A3PO_E_SIZE;
+    if (T == 0) return A3PO_OK;
+    if (!policy || !policy->uniform || !token_out) return A3PO_E_NULL;
+    const void *words[] = {policy->uniform, policy->temperature, policy->top_k, policy->top_p, policy->min_p, token_out,
+                           logp_out, logp_full_out, kept_out, allowed_out};
+    for (const void *p : words)
+        if (!aligned(p, 4)) return A3PO_E_ALIGN;
+    if (const size_t need = sample_workspace_bytes(T, V)) {
+        if (!workspace || workspace_bytes < need) return A3PO_E_WORKSPACE;
+        if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
+    }
+    SampleArgs a = {};
+    a.z = logits;
+    a.dt = (int)dt;
+    a.T = T;
+    a.V = V;
+    a.ld = ld;
+    a.allowed_ld = allowed_ld;
+    a.uniform = policy->uniform;
+    a.temperature = policy->temperature;
+    a.top_k = policy->top_k;
+    a.top_p = policy->top_p;
+    a.min_p = policy->min_p;
+    a.token = token_out;
+    a.logp = logp_out;
+    a.logp_full = logp_full_out;
+    a.kept = kept_out;
+    a.allowed = allowed_out;
+    a.shift = sample_shift(V);
+    sample_blocks(a);
+    return launch_sample(a, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+}
+
+int a3po_grad_norm(const void *const *grads, const int64_t *sizes, int64_t count, a3po_dtype dt, float scale, float *norm_out,
+                   void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (dt != A3PO_F32 && dt != A3PO_BF16) return A3PO_E_DTYPE;
+    if (count < 0 || count > kMaxTensors) return A3PO_E_SIZE;
+    if (scale != scale) return A3PO_E_VALUE;
+    if (!norm_out || (count > 0 && (!grads || !sizes))) return A3PO_E_NULL;
+    if (!aligned(norm_out, 4)) return A3PO_E_ALIGN;
+    for (int64_t i = 0; i < count; ++i) {
+        if (sizes[i] < 0 || sizes[i] > kMaxElements) return A3PO_E_SIZE;
+        if (sizes[i] > 0 && !grads[i]) return A3PO_E_NULL;
+        if (!aligned(grads[i], elem(dt))) return A3PO_E_ALIGN;
+    }
+    if (count > 0) {
+        if (!workspace || workspace_bytes < grad_norm_workspace_bytes(count)) return A3PO_E_WORKSPACE;
+        if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
+    }
+    const hipError_t e = launch_grad_norm(grads, sizes, count, (int)dt, scale, norm_out, workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+}
+
+int a3po_adamw_step(const a3po_adamw_tensor *tensors, int64_t count, a3po_dtype param_dt, a3po_dtype grad_dt, int32_t state_format,
+                    const a3po_adamw_options *options, void *stream)
+{
+    for (int dt : {(int)param_dt, (int)grad_dt})
+        if (dt != A3PO_F32 && dt != A3PO_BF16) return A3PO_E_DTYPE;
+    if (state_format != A3PO_STATE_F32 && state_format != A3PO_STATE_8BIT) return A3PO_E_VALUE;
+    if (count < 0 || count > kMaxTensors) return A3PO_E_SIZE;
+    if (!options || (count > 0 && !tensors)) return A3PO_E_NULL;
+    const a3po_adamw_options &o = *options;
+    if (!(o.beta1 >= 0.0 && o.beta1 < 1.0 && o.beta2 >= 0.0 && o.beta2 < 1.0) || !(o.eps >= 0.0) || !(o.weight_decay >= 0.0) ||
+        (!o.lr_dev && !(o.lr >= 0.0)) || (!o.step_dev && o.step < 1) || (o.norm && !(o.max_norm > 0.0)))
+        return A3PO_E_VALUE;
+    if (!aligned(o.lr_dev, 4) || !aligned(o.step_dev, 8) || !aligned(o.norm, 4)) return A3PO_E_ALIGN;
+    const uintptr_t state = state_format == A3PO_STATE_F32 ? 4 : 1;
+    for (int64_t i = 0; i < count; ++i) {
+        const a3po_adamw_tensor &t = tensors[i];
+        if (t.n < 0 || t.n > kMaxElements) return A3PO_E_SIZE;
+        if (t.n == 0) continue;
+        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq) return A3PO_E_NULL;
+        if (state_format == A3PO_STATE_8BIT && (!t.exp_avg_scale || !t.exp_avg_sq_scale)) return A3PO_E_NULL;
+        if (!aligned(t.param, elem(param_dt)) || !aligned(t.grad, elem(grad_dt)) || !aligned(t.exp_avg, state) ||
+            !aligned(t.exp_avg_sq, state) || !aligned(t.copy, 2))
+            return A3PO_E_ALIGN;
+    }
+    const hipError_t e = launch_adamw(tensors, count, (int)param_dt, (int)grad_dt, state_format, o, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
+}
+
+int a3po_w4_quantize(const void *weight, a3po_dtype dt, int64_t N, int64_t H, int64_t ld, int32_t group, uint8_t *codes,
+                     void *scales, a3po_dtype scale_dt, uint8_t *zeros, void *stream)
+{
+    for (int t : {(int)dt, (int)scale_dt})
+        if (t != A3PO_F32 && t != A3PO_BF16) return A3PO_E_DTYPE;
+    if (group != 32 && group != 64 && group != 128) return A3PO_E_SIZE;
+    if (N < 0 || N > (int64_t)0x7FFFFFFF || H <= 0 || H % group != 0 || H > (1 << 20) || ld < H || ld > kMaxStride) return A3PO_E_SIZE;
+    if (N == 0) return A3PO_OK;
+    if (!weight || !codes || !scales) return A3PO_E_NULL;
+    if (!aligned(weight, elem(dt)) || !aligned(codes, 16) || !aligned(scales, elem(scale_dt))) return A3PO_E_ALIGN;
+    W4QuantizeArgs a;
+    a.w = weight;
+    a.dt = (int)dt;
+    a.scale_dt = (int)scale_dt;
+    a.group = group;
+    a.N = N;
+    a.H = H;
+    a.ld = ld;
+    a.codes = codes;
+    a.zeros = zeros;
+    a.scales = scales;
+    return launch_w4_quantize(a, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
 }
 
 }  // extern "C"

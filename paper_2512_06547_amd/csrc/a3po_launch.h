@@ -639,4 +639,55 @@ inline size_t w4_workspace_bytes(int64_t T, int64_t H)
 }
 hipError_t launch_w4_linear(const W4Args &a, void *workspace, hipStream_t s);
 
+// ---- operators that close the loop: drawn tokens, optimizer step, 4-bit layout --------------------------------------------
+
+struct SampleArgs {
+    const void *z;
+    int dt;  // a3po_dtype
+    int64_t T, V, ld, allowed_ld;
+    const float *uniform, *temperature, *top_p, *min_p;  // [T], all but the first nullable
+    const int32_t *top_k;
+    int32_t *token, *kept, *allowed;  // all but the first nullable
+    float *logp, *logp_full;
+    int shift;          // weights are whole numbers of 2^-shift of the largest
+    int blocks, steps;  // a row is `blocks` blocks of `steps` times 64 vectors of 16 bytes
+};
+constexpr int kSampleBlocks = 1024;  // at most
+inline int sample_shift(int64_t V)
+{
+    int bits = 0;
+    while (((int64_t)1 << bits) < V) ++bits;
+    return bits < 12 ? 50 : 62 - bits;
+}
+inline void sample_blocks(SampleArgs &a)
+{
+    const int64_t wave = 64 * (a.dt == A3PO_F32 ? 4 : 8);
+    const int64_t vectors = (a.V + wave - 1) / wave;
+    a.steps = (int)((vectors + kSampleBlocks - 1) / kSampleBlocks);
+    a.blocks = (int)((vectors + a.steps - 1) / a.steps);
+}
+inline size_t sample_workspace_bytes(int64_t, int64_t) { return 0; }
+hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
+
+// Tensors reach the kernels as launch arguments, so many a launch (4 KiB of arguments at most).
+constexpr int kAdamTensors = 40, kNormTensors = 200, kNormBlocks = 1024;
+inline size_t grad_norm_workspace_bytes(int64_t count)
+{
+    const int64_t launches = count > 0 ? (count + kNormTensors - 1) / kNormTensors : 0;
+    return (size_t)launches * kNormBlocks * sizeof(double);
+}
+hipError_t launch_grad_norm(const void *const *grads, const int64_t *sizes, int64_t count, int dt, float scale, float *norm,
+                            void *workspace, hipStream_t s);
+hipError_t launch_adamw(const a3po_adamw_tensor *tensors, int64_t count, int param_dt, int grad_dt, int state_format,
+                        const a3po_adamw_options &o, hipStream_t s);
+
+struct W4QuantizeArgs {
+    const void *w;
+    int dt, scale_dt, group;  // a3po_dtype
+    int64_t N, H, ld;
+    uint8_t *codes, *zeros;   // zeros nullable
+    void *scales;
+};
+hipError_t launch_w4_quantize(const W4QuantizeArgs &a, hipStream_t s);
+
 }  // namespace a3po
