@@ -551,7 +551,7 @@ typedef struct {
  * A row without an entry above -inf has token -1, kept 0, no allowed bit and log-probs of -inf.  A NaN or +inf in the row, a
  * negative temperature or a NaN among the row's parameters give token -1, kept 0, no bit and log-probs NaN.  (The loss treats
  * a token of -1 as masked.)
- * workspace: a3po_workspace_bytes(A3PO_WS_SAMPLE, T, V, 0) bytes, 256-byte aligned; not needed, and NULL, where that is 0.
+ * workspace: a3po_workspace_bytes(A3PO_WS_SAMPLE, T, V, 0) bytes, 256-byte aligned.
  */
 int a3po_sample(const void *logits, a3po_dtype dt, int64_t T, int64_t V, int64_t ld, const a3po_sampling *policy,
                 int32_t *token_out, float *logp_out, float *logp_full_out, int32_t *kept_out, int32_t *allowed_out,

@@ -600,10 +600,8 @@ int a3po_sample(const void *logits, a3po_dtype dt, int64_t T, int64_t V, int64_t
                            logp_out, logp_full_out, kept_out, allowed_out};
     for (const void *p : words)
         if (!aligned(p, 4)) return A3PO_E_ALIGN;
-    if (const size_t need = sample_workspace_bytes(T, V)) {
-        if (!workspace || workspace_bytes < need) return A3PO_E_WORKSPACE;
-        if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
-    }
+    if (!workspace || workspace_bytes < sample_workspace_bytes(T, V)) return A3PO_E_WORKSPACE;
+    if (!aligned(workspace, 256)) return A3PO_E_ALIGN;
     SampleArgs a = {};
     a.z = logits;
     a.dt = (int)dt;
@@ -623,6 +621,8 @@ int a3po_sample(const void *logits, a3po_dtype dt, int64_t T, int64_t V, int64_t
     a.allowed = allowed_out;
     a.shift = sample_shift(V);
     sample_blocks(a);
+    a.parts = (int)sample_parts(V);
+    sample_workspace(a, workspace);
     return launch_sample(a, static_cast<hipStream_t>(stream)) == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;
 }
 

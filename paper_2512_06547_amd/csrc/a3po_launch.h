@@ -641,6 +641,33 @@ hipError_t launch_w4_linear(const W4Args &a, void *workspace, hipStream_t s);
 
 // ---- operators that close the loop: drawn tokens, optimizer step, 4-bit layout --------------------------------------------
 
+constexpr int kSamplePart = 8192;      // entries of a part
+constexpr int kSampleBins = 512;       // of a part, 1/16 power of two each
+constexpr int kSampleListed = 4864;    // entries of a row that may be gathered
+constexpr int64_t kSampleRows = 1024;  // rows at a time, which bounds the workspace
+constexpr int kSampleAll = 0x7FFFFFFF, kSampleFar = -0x7FFFFFFF;
+
+struct SamplePart {
+    double mass;     // uncut: sum of exp((z - max) / temperature); cut: the same over what lies behind the bins, by their first
+    float max;       // NaN: one of the part's entries is, or is +inf
+    int place;       // of the maximum on the grid; kSampleFar: too far out for it
+    uint32_t bins;   // that there are
+    uint32_t count;  // entries above -inf (uncut: where asked for)
+};
+enum { kSampleDone, kSampleFew, kSampleBin, kSamplePasses };
+struct SampleRow {
+    double full, above, share;  // sums over all, over the bins before the border's, up to the border; in units of 2^-36 of bin 0
+    int64_t rank;               // of the border in its bin, where it is one of a count
+    float top;
+    bool by_k;                  // top_k leaves entries out
+    int mode, place, bin;       // place of bin 0; the border's bin (kSampleAll: behind all)
+    uint32_t count, cursor;     // entries before the border's bin; room taken in the list
+};
+struct SampleSegment {
+    double above;            // the part's share of SampleRow::above
+    uint32_t start, listed;  // its entries in the list
+};
+
 struct SampleArgs {
     const void *z;
     int dt;  // a3po_dtype
@@ -651,6 +678,12 @@ struct SampleArgs {
     float *logp, *logp_full;
     int shift;          // weights are whole numbers of 2^-shift of the largest
     int blocks, steps;  // a row is `blocks` blocks of `steps` times 64 vectors of 16 bytes
+    int parts;
+    SamplePart *part;        // [rows at a time, parts]
+    SampleSegment *segment;  // [rows at a time, parts]
+    SampleRow *row;          // [rows at a time]
+    uint64_t *bins;          // [rows at a time, parts, kSampleBins]
+    uint2 *list;             // [rows at a time, kSampleListed]: an entry's bits and index
 };
 constexpr int kSampleBlocks = 1024;  // at most
 inline int sample_shift(int64_t V)
@@ -666,7 +699,31 @@ inline void sample_blocks(SampleArgs &a)
     a.steps = (int)((vectors + kSampleBlocks - 1) / kSampleBlocks);
     a.blocks = (int)((vectors + a.steps - 1) / a.steps);
 }
-inline size_t sample_workspace_bytes(int64_t, int64_t) { return 0; }
+inline int64_t sample_parts(int64_t V) { return (V + kSamplePart - 1) / kSamplePart; }
+// sets the workspace's arrays in `a` and returns its size
+inline size_t sample_workspace(SampleArgs &a, void *workspace)
+{
+    const int64_t rows = a.T < kSampleRows ? a.T : kSampleRows, parts = rows * sample_parts(a.V);
+    char *p = static_cast<char *>(workspace);
+    size_t at = 0;
+    auto take = [&](int64_t n, size_t bytes) {
+        const size_t begin = at;
+        at += ((size_t)n * bytes + 255) / 256 * 256;
+        return p ? p + begin : nullptr;
+    };
+    a.part = reinterpret_cast<SamplePart *>(take(parts, sizeof(SamplePart)));
+    a.segment = reinterpret_cast<SampleSegment *>(take(parts, sizeof(SampleSegment)));
+    a.row = reinterpret_cast<SampleRow *>(take(rows, sizeof(SampleRow)));
+    a.bins = reinterpret_cast<uint64_t *>(take(parts, kSampleBins * 8));
+    a.list = reinterpret_cast<uint2 *>(take(rows, kSampleListed * 8));
+    return at;
+}
+inline size_t sample_workspace_bytes(int64_t T, int64_t V)
+{
+    SampleArgs a = {};
+    a.T = T, a.V = V;
+    return sample_workspace(a, nullptr);
+}
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
 
 // Tensors reach the kernels as launch arguments, so many a launch (4 KiB of arguments at most).
