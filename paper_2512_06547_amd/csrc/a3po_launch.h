@@ -643,25 +643,27 @@ hipError_t launch_w4_linear(const W4Args &a, void *workspace, hipStream_t s);
 
 constexpr int kSamplePart = 8192;      // entries of a part
 constexpr int kSampleBins = 512;       // of a part, 1/16 power of two each
-constexpr int kSampleListed = 4864;    // entries of a row that may be gathered
+constexpr int kSampleListed = 9728, kSampleFewest = kSampleListed / 2;  // entries of a row that may be gathered, of a bin or of all down to it
 constexpr int64_t kSampleRows = 1024;  // rows at a time, which bounds the workspace
 constexpr int kSampleAll = 0x7FFFFFFF, kSampleFar = -0x7FFFFFFF;
 
-struct SamplePart {
-    double mass;     // uncut: sum of exp((z - max) / temperature); cut: the same over what lies behind the bins, by their first
+struct alignas(64) SamplePart {
+    double mass[4];  // of a quarter each.  Uncut: weights relative to the maximum's; cut: to the middle of bin 0, in any order
     float max;       // NaN: one of the part's entries is, or is +inf
     int place;       // of the maximum on the grid; kSampleFar: too far out for it
     uint32_t bins;   // that there are
     uint32_t count;  // entries above -inf (uncut: where asked for)
 };
 enum { kSampleDone, kSampleFew, kSampleBin, kSamplePasses };
-struct SampleRow {
+struct alignas(128) SampleRow {
     double full, above, share;  // sums over all, over the bins before the border's, up to the border; in units of 2^-36 of bin 0
     int64_t rank;               // of the border in its bin, where it is one of a count
     float top;
-    bool by_k;                  // top_k leaves entries out
+    int by_k;                   // top_k leaves entries out
     int mode, place, bin;       // place of bin 0; the border's bin (kSampleAll: behind all)
     uint32_t count, cursor;     // entries before the border's bin; room taken in the list
+    uint32_t key;               // the last entry kept, for the bits of many
+    int32_t last;
 };
 struct SampleSegment {
     double above;            // the part's share of SampleRow::above
@@ -685,7 +687,7 @@ struct SampleArgs {
     uint64_t *bins;          // [rows at a time, parts, kSampleBins]
     uint2 *list;             // [rows at a time, kSampleListed]: an entry's bits and index
 };
-constexpr int kSampleBlocks = 1024;  // at most
+constexpr int kSampleBlocks = 512;  // at most
 inline int sample_shift(int64_t V)
 {
     int bits = 0;

@@ -25,12 +25,15 @@
 namespace a3po {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / kWave;
+constexpr int kThreads = 512, kWaves = kThreads / kWave;
 constexpr int kBins = 4096;
 constexpr uint32_t kKeyOfNegInf = 0x007FFFFFu;
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / kWave;
+constexpr int kDirect = 128;  // gathered entries that are each compared with all others
 
 constexpr float kInf = __builtin_huge_valf();
+constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: added to a number it leaves the whole number next to it in the low word
+constexpr double kUnit = 46.166241308446828384;  // 32 log2(e)
 
 // 2^(i / 32)
 __device__ const double kTable[32] = {
@@ -43,14 +46,6 @@ __device__ const double kTable[32] = {
     0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
     0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
 
-// a b + c, the constant c from scalar registers (left to itself the compiler copies it to the sum's registers every time)
-__device__ __forceinline__ double fma_const(double a, double b, double c)
-{
-    double d;
-    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "s"(c));
-    return d;
-}
-
 // e^x: 2^(i / 32) from a table (one entry a pair of LDS banks: lanes never wait for one another), the rest of the exponent by a
 // series whose first term left out, (ln 2 / 64)^6 / 720, is 2^-48
 struct Weigh {
@@ -59,23 +54,25 @@ struct Weigh {
     __device__ __forceinline__ double operator()(float z) const
     {
         constexpr double a1 = 0.69314718055994530942 / 32, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
-        constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: the sum's low word is the whole number
         const double y = fmax(((double)z - max) * unit, -32000.0);
         const double t = y + kRound;
         const int n = __double2loint(t);
         const double r = y - (t - kRound);
         const double b = table[n & 31];
         const double scale = __hiloint2double(__double2hiint(b) + ((n >> 5) << 20), __double2loint(b));
-        double q = r * a5 + a4;
-        q = fma_const(q, r, a3), q = fma_const(q, r, a2), q = fma_const(q, r, a1);
-        return fma(scale, r * q, scale);
+        return scale * (1.0 + r * (a1 + r * (a2 + r * (a3 + r * (a4 + r * a5)))));
     }
     __device__ __forceinline__ uint64_t whole(float z) const
     {
         return (uint64_t)__double_as_longlong((*this)(z) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
     }
 };
-constexpr double kUnit = 46.166241308446828384;  // 32 log2(e)
+// 2^(-b / 16)
+__device__ __forceinline__ double down_by(int b)
+{
+    const int whole = (b + 15) >> 4;
+    return ldexp(kTable[2 * (whole * 16 - b)], -whole);
+}
 
 // orders floats as whole numbers; -0 and 0 are one
 __device__ __forceinline__ uint32_t key_of(float z)
@@ -84,29 +81,62 @@ __device__ __forceinline__ uint32_t key_of(float z)
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
+// Sums over the lanes before and up to each: within rows of 16 lanes, then rows 1 and 3 take what ends row 0 and 2, then the upper
+// half what ends the lower.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lanes(uint32_t v)  // 0 where there is no such lane
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T from_lanes(T v)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, lanes<CTRL, ROWS>(__builtin_bit_cast(uint32_t, v)));
+    } else {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        return __builtin_bit_cast(T, (uint64_t)lanes<CTRL, ROWS>((uint32_t)(u >> 32)) << 32 | lanes<CTRL, ROWS>((uint32_t)u));
+    }
+}
 template <typename T>
 __device__ __forceinline__ T wave_scan(T v)  // inclusive
 {
-    const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const T up = __shfl_up(v, off, kWave);
-        if (lane >= off) v += up;
-    }
-    return v;
+    v += from_lanes<0x111, 0xF>(v);
+    v += from_lanes<0x112, 0xF>(v);
+    v += from_lanes<0x114, 0xF>(v);
+    v += from_lanes<0x118, 0xF>(v);
+    v += from_lanes<0x142, 0xA>(v);
+    return v + from_lanes<0x143, 0xC>(v);
 }
-__device__ __forceinline__ float wave_max(float v)
+template <typename T>
+__device__ __forceinline__ T last_lane(T v)
 {
-#pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, kWave));
-    return v;
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1));
+    } else {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        return __builtin_bit_cast(T, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), kWave - 1) << 32 |
+                                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, kWave - 1));
+    }
 }
 template <typename T>
 __device__ __forceinline__ T wave_sum(T v)
 {
-#pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
-    return v;
+    return last_lane(wave_scan(v));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_with(float v)
+{
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, ROWS, 0xF, false)));
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = max_with<0x111, 0xF>(v);
+    v = max_with<0x112, 0xF>(v);
+    v = max_with<0x114, 0xF>(v);
+    v = max_with<0x118, 0xF>(v);
+    v = max_with<0x142, 0xA>(v);
+    return last_lane(max_with<0x143, 0xC>(v));
 }
 
 // the last entry of the order that is kept
@@ -126,22 +156,23 @@ __device__ __forceinline__ Border tighter(Border a, Border b)
     return Border{a.key, min(a.last, b.last)};
 }
 
-// What the row's arrays say, absent ones being neutral.
+// What the row's arrays say, absent ones being neutral; a temperature of NaN where they say nothing that can be followed.
 struct Policy {
     float tau, p, min_p, u;
     int64_t k;
-    bool bad, by_k, by_p, by_min;
     __device__ __forceinline__ Policy(const SampleArgs &a, int64_t t)
         : tau(a.temperature ? a.temperature[t] : 1.0f), p(a.top_p ? a.top_p[t] : 1.0f), min_p(a.min_p ? a.min_p[t] : 0.0f),
           u(a.uniform[t]), k(a.top_k ? a.top_k[t] : 0)
     {
-        bad = !(tau >= 0.0f) || p != p || min_p != min_p || u != u;
         if (tau == 0.0f) tau = 1.0f, k = 1;
-        by_k = k > 0 && k < a.V;
-        by_p = p < 1.0f;
-        by_min = min_p > 0.0f;
+        if (!(tau >= 0.0f) || p != p || min_p != min_p || u != u) tau = __builtin_nanf("");
+        if (k >= a.V) k = 0;
     }
-    __device__ __forceinline__ bool cut() const { return by_k || by_p || by_min; }
+    __device__ __forceinline__ bool bad() const { return tau != tau; }
+    __device__ __forceinline__ bool by_k() const { return k > 0; }
+    __device__ __forceinline__ bool by_p() const { return p < 1.0f; }
+    __device__ __forceinline__ bool by_min() const { return min_p > 0.0f; }
+    __device__ __forceinline__ bool cut() const { return by_k() || by_p() || by_min(); }
 };
 
 // ---- parts -------------------------------------------------------------------------------------------------------------
@@ -184,13 +215,20 @@ struct PartEntries {
     }
 };
 
-// Places on the grid: the whole number next to z times 16 log2(e) / temperature, in 64 bits so that larger logits never have
-// smaller places; what is further below zero than kFar counts as there.
-constexpr double kGrid = kUnit / 2, kFar = -1.5e9, kNear = 1.0e9, kRound = 6755399441055744.0;
-__device__ __forceinline__ int place_of(float z, double grid) { return __double2loint(fmax((double)z * grid, kFar) + kRound); }
-// in a bin's sum: the count in the upper 14 bits, weights times 2^36 below (8,192 of them, each below 1.03, are below 2^50; the bin's middle is 1)
+// Places on the grid: the whole number next to z times 16 log2(e) / temperature, by one rounding, so that larger logits never have
+// smaller places.  `lowest` stands for everything that is further below than whole numbers of 32 bits reach.
+constexpr double kNear = 1.0e9;
+__device__ __forceinline__ float lowest_of(double unit) { return (float)(-1.5e9 / unit); }
+__device__ __forceinline__ int place_of(float z, double grid, float lowest) { return __double2loint(fma((double)fmaxf(z, lowest), grid, kRound)); }
+// in a bin's sum: the count in the upper 14 bits, weights times 2^36 below (8,192 of them, each below 1.03, are below 2^50; the
+// bin's middle is 1)
 constexpr int kWeightBits = 50;
 constexpr uint64_t kWeightMask = (1ull << kWeightBits) - 1;
+
+// The weights of an uncut part are relative to 2^(R / 32), R being the whole number next to max * unit: z * unit - R then comes from
+// one rounding, and R from none.  Where R leaves 32 bits, or no float is far below the maximum (temperatures from 1e28 on), they
+// are relative to the maximum.
+__device__ __forceinline__ bool is_far(float top, double unit) { return !(fabs((double)top * unit) < kNear && unit > 1e-27); }
 
 template <typename DT>
 __global__ __launch_bounds__(kPartThreads, 4) void sample_parts_kernel(SampleArgs a, int64_t row0, int64_t rows)
@@ -199,96 +237,133 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_parts_kernel(SampleArg
     __shared__ double table[32];
     __shared__ uint64_t bins[kSampleBins];
     __shared__ float wave_top[kPartWaves];
-    __shared__ double wave_mass[kPartWaves];
     __shared__ uint32_t wave_count[kPartWaves], wave_last[kPartWaves];
+    __shared__ union {
+        SamplePart part;
+        uint32_t words[sizeof(SamplePart) / 4];
+    } record;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    if (tid < 32) table[tid] = kTable[tid];
+    // (with the exponent's share of 15 bits taken out, so that adding n << 15 puts the whole exponent in)
+    if (tid < 32) table[tid] = __hiloint2double(__double2hiint(kTable[tid]) - (tid << 15), __double2loint(kTable[tid]));
     for (int64_t i = blockIdx.x; i < rows * a.parts; i += gridDim.x) {
         const int64_t r = i / a.parts, t = row0 + r;
         const int64_t begin = (i - r * a.parts) * kSamplePart;
         Entries z;
         z.load(reinterpret_cast<const char *>(a.z) + (t * a.ld + begin) * DT::kBytes, (int)min(a.V - begin, (int64_t)kSamplePart));
         const Policy policy(a, t);
-        float top = -kInf;
+        const bool cut = policy.cut();
+        const double unit = kUnit / (double)policy.tau;
+        float top = -kInf, last_one = 0.0f;
         bool bad = false;
-        z.each([&](float x, int) { top = fmaxf(top, x), bad |= !(x < kInf); });
+        z.each([&](float x, int k) {
+            top = fmaxf(top, x);
+            if (k & 1) bad |= __builtin_isunordered(x, last_one);  // (two at a time)
+            last_one = x;
+        });
         top = wave_max(top);
-        if (__any(bad)) top = __builtin_nanf("");
+        if (__any(bad) || top == kInf) top = __builtin_nanf("");
         __syncthreads();  // (the part before this one is done with the shared arrays)
         if (lane == 0) wave_top[wave] = top;
+        if (cut)
 #pragma unroll
-        for (int b = tid; b < kSampleBins; b += kPartThreads) bins[b] = 0;
+            for (int b = tid; b < kSampleBins; b += kPartThreads) bins[b] = 0;
         __syncthreads();
-        top = wave_top[0], bad = top != top;
+        bad = false, top = -kInf;
 #pragma unroll
-        for (int w = 1; w < kPartWaves; ++w) bad |= wave_top[w] != wave_top[w], top = fmaxf(top, wave_top[w]);
-        SamplePart out = {};
-        out.max = bad ? __builtin_nanf("") : top;
-        if (bad || policy.bad || top == -kInf) {  // (nothing to sum)
-            if (tid == 0) a.part[i] = out;
+        for (int w = 0; w < kPartWaves; ++w) bad |= wave_top[w] != wave_top[w], top = fmaxf(top, wave_top[w]);
+        if (bad || policy.bad() || top == -kInf) {  // (nothing to sum)
+            if (tid == 0) {
+                SamplePart out = {};
+                out.max = bad ? __builtin_nanf("") : top;
+                a.part[i] = out;
+            }
             continue;
         }
         double mass = 0.0;
-        uint32_t count = 0;
-        if (!policy.cut()) {
-            const Weigh weigh{(double)top, kUnit / (double)policy.tau, table};
-            z.each([&](float x, int) {
-                mass += weigh(x);  // (-inf: 2^-1000)
-                asm volatile("" : "+v"(mass));  // (here, not where it is used)
-            });
-            if (a.kept) z.each([&](float x, int) { count += x > -kInf ? 1u : 0u; });
-        } else {
-            const double grid = kGrid / (double)policy.tau;
-            const bool near = fabs((double)top * grid) < kNear;  // (beyond it the row is gone over)
-            const int place = near ? place_of(top, grid) : 0;
-            out.place = near ? place : kSampleFar;
-            float tail = 0.0f;
-            if (near) {
-                uint32_t furthest = 0;
-                z.each([&](float x, int) {
-                    constexpr double a1 = 0.69314718055994530942 / 16, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
-                    constexpr double kOne = 68719476736.0, kWhole = 4503599627370496.0;  // 2^36, 2^52
-                    const double y = fmax((double)x * grid, kFar), n = y + kRound, q = y - (n - kRound);
-                    const uint32_t bin = (uint32_t)(place - __double2loint(n));
-                    double w = q * (a5 * kOne) + a4 * kOne;
-                    w = fma_const(w, q, a3 * kOne), w = fma_const(w, q, a2 * kOne), w = fma_const(w, q, a1 * kOne), w = fma_const(w, q, kOne + kWhole);
-                    furthest = max(furthest, bin);
-                    if (bin < kSampleBins) {
-                        const uint64_t add = (uint64_t)(((uint32_t)__double2hiint(w) & 0xFFFFFu) | 1u << (kWeightBits - 32)) << 32 | (uint32_t)__double2loint(w);
-                        atomicAdd(reinterpret_cast<unsigned long long *>(&bins[bin]), (unsigned long long)add);
-                    }
+        uint32_t count = 0, bins_used = 0;
+        int place = kSampleFar;
+        const bool far = is_far(top, unit);
+        if (!cut) {
+            if (!far) {
+                constexpr double a1 = 0.69314718055994530942 / 32, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
+                // (a5 r^5 is replaced by the cubic next to it on [-1/2, 1/2]: off by a5 / 512 at most, 2^-43)
+                constexpr double b3 = a3 + a5 * (5.0 / 16), b1 = a1 - a5 * (5.0 / 256);
+                const double R = __double2loint((double)top * unit + kRound), K = kRound - R;
+                const float lowest = (float)(((R - 32000.0) / unit));
+                z.each([&](float x, int k) {
+                    const double d = (double)fmaxf(x, lowest), n = fma(d, unit, K), q = fma(d, unit, -(n - K));
+                    const int low = __double2loint(n);
+                    const double e = table[low & 31];
+                    const double p = fma(fma(fma(fma(q, a4, b3), q, a2), q, b1), q, 1.0);
+                    mass = fma(__hiloint2double(__double2hiint(e) + (low << 15), __double2loint(e)), p, mass);
+                    if (k % 4 == 3) asm volatile("" : "+v"(mass));  // (here, not where it is used)
                 });
-                // what lies behind the bins is below 2^-32 of the largest, all of it below 2^-19: what fp32 loses of that is below 2^-38
-                if (__any(furthest >= kSampleBins))
-                    z.each([&](float x, int) {
-                        const double y = fmax((double)x * grid, kFar), n = y + kRound, q = y - (n - kRound);
-                        const uint32_t bin = (uint32_t)(place - __double2loint(n));
-                        const bool behind = bin >= kSampleBins && x > -kInf;
-                        tail += behind ? exp2_hw(((float)q - (float)bin) * 0.0625f) : 0.0f;
-                        count += behind ? 1u : 0u;
-                        asm volatile("" : "+v"(tail), "+v"(count));
-                    });
+            } else {
+                const Weigh weigh{(double)top, unit, kTable};
+                z.each([&](float x, int) {
+                    mass += weigh(x);
+                    asm volatile("" : "+v"(mass));
+                });
             }
-            mass = (double)tail;
-        }
-        mass = wave_sum(mass);
-        __syncthreads();  // (the bins are whole)
-        uint32_t last = 0;
-        if (out.place != kSampleFar)
+            if (a.kept) z.each([&](float x, int) { count += x > -kInf ? 1u : 0u; });
+        } else if (!far) {
+            constexpr double a1 = 0.69314718055994530942 / 16, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
+            constexpr double kOne = 68719476736.0, kWhole = 4503599627370496.0;  // 2^36, 2^52
+            const double grid = unit * 0.5;
+            const float lowest = lowest_of(unit);
+            place = place_of(top, grid, lowest);
+            uint32_t furthest = 0;
+            z.each([&](float x, int k) {
+                const double d = (double)fmaxf(x, lowest), n = fma(d, grid, kRound), q = fma(d, grid, -(n - kRound));
+                const uint32_t bin = (uint32_t)(place - __double2loint(n));
+                const double w = fma(fma(fma(fma(fma(q, a5 * kOne, a4 * kOne), q, a3 * kOne), q, a2 * kOne), q, a1 * kOne), q, kOne + kWhole);
+                furthest = max(furthest, bin);
+                if (bin < kSampleBins) {
+                    const uint64_t add = (uint64_t)(((uint32_t)__double2hiint(w) & 0xFFFFFu) | 1u << (kWeightBits - 32)) << 32 | (uint32_t)__double2loint(w);
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&bins[bin]), (unsigned long long)add);
+                }
+            });
+            // what lies behind the bins is below 2^-32 of the largest, all of it below 2^-19: what fp32 loses of that is below 2^-38
+            if (__any(furthest >= kSampleBins)) {
+                float tail = 0.0f;
+                z.each([&](float x, int) {
+                    const double d = (double)fmaxf(x, lowest), n = fma(d, grid, kRound), q = fma(d, grid, -(n - kRound));
+                    const uint32_t bin = (uint32_t)(place - __double2loint(n));
+                    const bool behind = bin >= kSampleBins && x > -kInf;
+                    tail += behind ? exp2_hw(((float)q - (float)bin) * 0.0625f) : 0.0f;
+                    count += behind ? 1u : 0u;
+                    asm volatile("" : "+v"(tail), "+v"(count));
+                });
+                mass = (double)tail;
+            }
+            __syncthreads();  // (the bins are whole)
 #pragma unroll
             for (int b = tid; b < kSampleBins; b += kPartThreads) {
                 const uint64_t sum = bins[b];
-                if (sum) last = b + 1, count += (uint32_t)(sum >> kWeightBits);
+                if (sum) bins_used = b + 1, count += (uint32_t)(sum >> kWeightBits);
+                const double middle = table[-2 * b & 31];  // 2^(-b / 16)
+                mass = fma((double)(sum & kWeightMask) * (1.0 / kOne), __hiloint2double(__double2hiint(middle) - (b << 16), __double2loint(middle)), mass);
             }
+        } else {
+            z.each([&](float x, int) { count += x > -kInf ? 1u : 0u; });
+        }
+        mass = wave_sum(mass);
         count = wave_sum(count);
-#pragma unroll
-        for (int off = kWave / 2; off > 0; off >>= 1) last = max(last, (uint32_t)__shfl_xor((int)last, off, kWave));
-        if (lane == 0) wave_mass[wave] = mass, wave_count[wave] = count, wave_last[wave] = last;
+        bins_used = (uint32_t)wave_max((float)bins_used);
+        if (lane == 0) record.part.mass[wave] = mass, wave_count[wave] = count, wave_last[wave] = bins_used;
         __syncthreads();
+        count = bins_used = 0;
 #pragma unroll
-        for (int w = 0; w < kPartWaves; ++w) out.mass += wave_mass[w], out.count += wave_count[w], out.bins = max(out.bins, wave_last[w]);
-        for (int b = tid; b < (int)out.bins; b += kPartThreads) a.bins[i * kSampleBins + b] = bins[b];
-        if (tid == 0) a.part[i] = out;
+        for (int w = 0; w < kPartWaves; ++w) count += wave_count[w], bins_used = max(bins_used, wave_last[w]);
+        if (cut)
+            // (through to memory at once: what lies in the L2s when the kernel ends, the next one waits for, 14 us for 20 MB)
+            for (int b = tid; b < (int)bins_used; b += kPartThreads)
+                __hip_atomic_store(a.bins + i * kSampleBins + b, bins[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (wave == 0) {
+            if (tid == 0) record.part.max = top, record.part.place = place, record.part.bins = bins_used, record.part.count = count;
+            // (in one store: memory takes half a line's writing in two turns, and the next kernel waits for it)
+            if (lane < (int)(sizeof(SamplePart) / 4)) reinterpret_cast<uint32_t *>(a.part + i)[lane] = record.words[lane];
+        }
     }
 }
 
@@ -305,9 +380,15 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_gather_kernel(SampleAr
     for (int64_t i = blockIdx.x; i < rows * a.parts; i += gridDim.x) {
         const int64_t r = i / a.parts, t = row0 + r;
         SampleRow &row = a.row[r];
-        if (row.mode != kSampleFew && row.mode != kSampleBin) continue;
-        SampleSegment out = {};
         const SamplePart part = a.part[i];
+        // (asked for before it is known whether they are needed, or there)
+        constexpr int kEach = kSampleBins / kPartThreads;
+        uint64_t bins[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) bins[j] = a.bins[i * kSampleBins + j * kPartThreads + tid];
+        if (row.mode != kSampleFew && row.mode != kSampleBin) continue;
+        SampleSegment out;
+        out.above = 0.0, out.start = out.listed = 0;
         // the part's own bins that are looked for: up to `last`, of many only that one
         const int shift = part.max > -kInf ? row.place - part.place : 0;  // part's bin 0 is the row's bin `shift`
         const bool few = row.mode == kSampleFew, all = row.bin == kSampleAll;
@@ -315,10 +396,13 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_gather_kernel(SampleAr
         if (part.max > -kInf && last >= 0) {
             uint32_t n = 0;
             double above = 0.0;
-            for (int b = tid; b < (int)part.bins; b += kPartThreads) {
-                const uint64_t v = a.bins[i * kSampleBins + b];
-                if (few ? b <= last : b == last) n += (uint32_t)(v >> kWeightBits);
-                if (!few && b < last) above += (double)(v & kWeightMask) * exp2(-0.0625 * (b + shift));
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                const int b = j * kPartThreads + tid;
+                if (b < (int)part.bins) {
+                    if (few ? b <= last : b == last) n += (uint32_t)(bins[j] >> kWeightBits);
+                    if (!few && b < last) above += (double)(bins[j] & kWeightMask) * down_by(b + shift);
+                }
             }
             if (all) n = tid == 0 ? part.count : 0;
             n = wave_sum(n);
@@ -331,15 +415,17 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_gather_kernel(SampleAr
             for (int w = 0; w < kPartWaves; ++w) n += wave_count[w], out.above += wave_mass[w];
             out.listed = n;
             if (n > 0) {
+                if (tid == 0) start = atomicAdd(&row.cursor, n);  // (while the entries are on their way)
                 Policy policy(a, t);
-                const double grid = kGrid / (double)policy.tau;
+                const double unit = kUnit / (double)policy.tau, grid = unit * 0.5;
+                const float lowest_logit = lowest_of(unit);
                 const int64_t begin = (i - r * a.parts) * kSamplePart;
                 Entries z;
                 z.load(reinterpret_cast<const char *>(a.z) + (t * a.ld + begin) * DT::kBytes, (int)min(a.V - begin, (int64_t)kSamplePart));
                 const int lowest = all ? -0x7FFFFFFF : row.place - row.bin, highest = few ? 0x7FFFFFFF : lowest;
                 uint32_t taken = 0;  // a bit an entry
                 z.each([&](float x, int k) {
-                    const int p = place_of(x, grid);
+                    const int p = place_of(x, grid, lowest_logit);
                     taken |= (x > -kInf && p >= lowest && p <= highest ? 1u : 0u) << k;
                 });
                 // how many of each 64 vectors are before a lane's, 16 bits each
@@ -351,12 +437,11 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_gather_kernel(SampleAr
                     for (int h = 0; h < 2; ++h) own |= (uint32_t)__popc(taken >> ((2 * w + h) * EPV) & ((1u << EPV) - 1)) << (16 * h);
                     const uint32_t scan = wave_scan(own);
                     pos[w] = scan - own;
-                    sum[w] = __shfl(scan, kWave - 1, kWave);
+                    sum[w] = last_lane(scan);
                     in_wave += (sum[w] & 0xFFFFu) + (sum[w] >> 16);
                 }
                 __syncthreads();  // (wave_count has been read)
                 if (lane == 0) wave_count[wave] = in_wave;
-                if (tid == 0) start = atomicAdd(&row.cursor, n);
                 __syncthreads();
                 out.start = start;
                 uint32_t base = start;
@@ -379,21 +464,32 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_gather_kernel(SampleAr
                 }
             }
         }
-        if (tid == 0) a.segment[i] = out;
+        if (tid == 0) {
+            SampleSegment &to = a.segment[i];
+            to.above = out.above, to.start = out.start, to.listed = out.listed;
+        }
     }
 }
 
 // ---- rows and finish -------------------------------------------------------------------------------------------------
 
+// What the waves of a workgroup tell one another.  Two sets of places in turn: between a wave's writes to one and the reads of
+// it two turns before lies the barrier of the turn between.
+struct Turn {
+    uint64_t whole[kWaves];
+    double sum[kWaves], other[kWaves];
+    uint32_t count[kWaves], more[kWaves];
+    float top[kWaves], low[kWaves];
+};
 struct Scans {
-    double table[32];
-    uint64_t wave_mass[kWaves];
-    double wave_sum[kWaves];
-    uint32_t wave_count[kWaves];
-    float wave_top[kWaves];
+    Turn turn[2];
+    double table[32], told[2];
+    float told_top;
     uint64_t found_mass;
     uint32_t found_digit, found_count, gathered;
     Border found;
+    int64_t token;
+    float token_logit, entries[16];
 };
 struct Shared : Scans {
     union {
@@ -402,8 +498,13 @@ struct Shared : Scans {
             uint32_t count[kBins];
         } key;
         struct {
-            float value[kSampleListed];
-            int32_t index[kSampleListed];
+            union {
+                float value[kSampleListed];
+                struct {
+                    float few_values[kSampleFewest];
+                    int32_t index[kSampleFewest];  // (only where they are few)
+                };
+            };
             uint64_t bin_mass[kThreads];
             uint32_t bin_count[kThreads];
         } list;
@@ -411,57 +512,104 @@ struct Shared : Scans {
     uint64_t block_mass[kSampleBlocks];
     uint32_t block_count[kSampleBlocks];
 };
+static_assert(kSampleListed == 2 * kSampleFewest, "few values leave room for their indices");
+static_assert(kSampleBlocks == kThreads && kSampleBins == kThreads, "a block and a bin a thread");
 
-// inclusive over the workgroup, with the totals
+// Sum over the waves before a thread's own, and over all: of N / 64 waves' totals, which the lanes of each wave add up.
+template <int N, typename T>
+__device__ __forceinline__ T before_wave(const T *totals, T &total)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const T v = lane < N / kWave ? totals[lane] : T(0), upto = wave_scan(v);
+    total = last_lane(upto);
+    // (scan less own would round sums of floats)
+    const T before = from_lanes<0x138, 0xF>(upto);  // of the lane before
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, before), wave));
+    } else {
+        const uint64_t u = __builtin_bit_cast(uint64_t, before);
+        return __builtin_bit_cast(T, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), wave) << 32 |
+                                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, wave));
+    }
+}
+
+// Sums over the threads before and up to each, and over all; N threads, TURN 0 and 1 in turn.
+template <int N, int TURN>
 __device__ __forceinline__ void block_scan(Scans &sh, uint64_t &mass, uint32_t &count, uint64_t &mass_total, uint32_t &count_total)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    mass = wave_scan((unsigned long long)mass);
+    mass = wave_scan(mass);
     count = wave_scan(count);
+    if (lane == kWave - 1) sh.turn[TURN].whole[wave] = mass, sh.turn[TURN].count[wave] = count;
     __syncthreads();
-    if (lane == kWave - 1) sh.wave_mass[wave] = mass, sh.wave_count[wave] = count;
-    __syncthreads();
-    uint64_t m = 0;
-    uint32_t c = 0;
-    mass_total = 0, count_total = 0;
-#pragma unroll 4
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) m += sh.wave_mass[w], c += sh.wave_count[w];
-        mass_total += sh.wave_mass[w], count_total += sh.wave_count[w];
-    }
-    mass += m, count += c;
+    mass += before_wave<N>(sh.turn[TURN].whole, mass_total);
+    count += before_wave<N>(sh.turn[TURN].count, count_total);
 }
-__device__ __forceinline__ void block_scan(Scans &sh, double &mass, double &total)
+template <int N, int TURN>
+__device__ __forceinline__ void block_scan(Scans &sh, uint32_t &count, uint32_t &count_total)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    mass = wave_scan(mass);
+    count = wave_scan(count);
+    if (lane == kWave - 1) sh.turn[TURN].count[wave] = count;
     __syncthreads();
-    if (lane == kWave - 1) sh.wave_sum[wave] = mass;
+    count += before_wave<N>(sh.turn[TURN].count, count_total);
+}
+// `other` and `more` are only summed
+template <int N, int TURN>
+__device__ __forceinline__ void block_scan(Scans &sh, double &sum, double &total, double &other, uint32_t &count, uint32_t &count_total, uint32_t &more)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    sum = wave_scan(sum);
+    count = wave_scan(count);
+    other = wave_sum(other);
+    more = wave_sum(more);
+    Turn &t = sh.turn[TURN];
+    if (lane == kWave - 1) t.sum[wave] = sum, t.count[wave] = count, t.other[wave] = other, t.more[wave] = more;
     __syncthreads();
-    double before = 0.0;
-    total = 0.0;
-#pragma unroll 4
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) before = total;
-        total += sh.wave_sum[w];
-    }
-    mass += before;
+    double all_other;
+    uint32_t all_more;
+    sum += before_wave<N>(t.sum, total);
+    count += before_wave<N>(t.count, count_total);
+    (void)before_wave<N>(t.other, all_other);
+    (void)before_wave<N>(t.more, all_more);
+    other = all_other, more = all_more;
+}
+template <int N, int TURN>
+__device__ __forceinline__ void block_scan(Scans &sh, double &sum, double &total)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    sum = wave_scan(sum);
+    if (lane == kWave - 1) sh.turn[TURN].sum[wave] = sum;
+    __syncthreads();
+    sum += before_wave<N>(sh.turn[TURN].sum, total);
 }
 // the first thread for which `here` holds, or else the last for which `other` does (-1: none)
+template <int N, int TURN>
 __device__ __forceinline__ int block_first(Scans &sh, bool here, bool other)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const uint64_t a = __ballot(here), b = __ballot(other);
-    __syncthreads();
-    if (lane == 0) sh.wave_mass[wave] = a, sh.wave_sum[wave] = __longlong_as_double((long long)b);
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w)
-        if (sh.wave_mass[w]) return w * kWave + __builtin_ctzll(sh.wave_mass[w]);
-    for (int w = kWaves - 1; w >= 0; --w) {
-        const uint64_t bits = (uint64_t)__double_as_longlong(sh.wave_sum[w]);
-        if (bits) return w * kWave + 63 - __builtin_clzll(bits);
+    // (a wave's first and last thread, 0 for none)
+    if (lane == 0) {
+        sh.turn[TURN].count[wave] = a ? wave * kWave + __builtin_ctzll(a) + 1 : 0;
+        sh.turn[TURN].more[wave] = b ? wave * kWave + 64 - __builtin_clzll(b) : 0;
     }
-    return -1;
+    __syncthreads();
+    const uint32_t first = lane < N / kWave ? sh.turn[TURN].count[lane] : 0, last = lane < N / kWave ? sh.turn[TURN].more[lane] : 0;
+    const uint64_t firsts = __ballot(first != 0), lasts = __ballot(last != 0);
+    if (firsts) return __builtin_amdgcn_readlane((int)first, __builtin_ctzll(firsts)) - 1;
+    return lasts ? __builtin_amdgcn_readlane((int)last, 63 - __builtin_clzll(lasts)) - 1 : -1;
+}
+// the largest and the smallest over the workgroup
+template <int N, int TURN>
+__device__ __forceinline__ void block_range(Scans &sh, float &high, float &low)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    high = wave_max(high), low = wave_max(-low);
+    if (lane == 0) sh.turn[TURN].top[wave] = high, sh.turn[TURN].low[wave] = low;
+    __syncthreads();
+    high = wave_max(lane < N / kWave ? sh.turn[TURN].top[lane] : -kInf);
+    low = -wave_max(lane < N / kWave ? sh.turn[TURN].low[lane] : -kInf);
 }
 
 template <typename DT>
@@ -475,39 +623,55 @@ struct Row {
     {
         return ((int64_t)b * steps + s) * (kWave * kEpv) + (int)(threadIdx.x & (kWave - 1)) * kEpv;
     }
-    __device__ __forceinline__ void load(int64_t e, float *f) const  // -inf behind the row's end
+    __device__ __forceinline__ uint4 load_raw(int64_t e) const  // -inf behind the row's end
     {
-        if (e + kEpv <= V) {
-            unpack<DT>(row_load<true, true>(p + e * DT::kBytes), f);
-        } else {
+        if (e + kEpv <= V) return row_load<true, true>(p + e * DT::kBytes);
+        uint4 v = neg_inf_vec<DT>();
+        if (e < V) {
+            float f[kEpv];
 #pragma unroll
             for (int k = 0; k < kEpv; ++k) f[k] = e + k < V ? load_elem<DT>(p, e + k) : -kInf;
+            v = pack<DT>(f);
         }
+        return v;
     }
-    // f(values, first entry, block) of every 64 vectors of the row, a wavefront each
+    __device__ __forceinline__ void load(int64_t e, float *f) const { unpack<DT>(load_raw(e), f); }
+    // f(values, first entry, block) of every 64 vectors of the row, a wavefront each, its loads kAhead together
     template <typename F>
     __device__ __forceinline__ void each(F f) const
     {
+        constexpr int kAhead = 4;
+        for (int s = 0; s < steps; ++s)
 #pragma unroll 1
-        for (int b = threadIdx.x / kWave; b < blocks; b += kWaves)
+            for (int b = threadIdx.x / kWave; b < blocks; b += kWaves * kAhead) {
+                uint4 raw[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) raw[i] = load_raw(first(b + i * kWaves, s));
 #pragma unroll 1
-            for (int s = 0; s < steps; ++s) {
-                float v[kEpv];
-                const int64_t e = first(b, s);
-                load(e, v);
-                f(v, e, b);
+                for (int i = 0; i < kAhead; ++i) {
+                    float v[kEpv];
+                    unpack<DT>(raw[0], v);
+#pragma unroll
+                    for (int j = 1; j < kAhead; ++j) raw[j - 1] = raw[j];
+                    if (b + i * kWaves < blocks) f(v, first(b + i * kWaves, s), b + i * kWaves);
+                }
             }
     }
 };
 
-// what is written for the token v, x being its logit less the maximum over the temperature; sums are in units of 2^-shift
-__device__ __forceinline__ void tell(const SampleArgs &a, int64_t t, int64_t v, double x, double kept_mass, double full_mass, uint32_t kept)
+// What is written for the drawn token, which its thread has left in sh; sums are in units of 2^-shift of the largest weight.
+__device__ __forceinline__ void tell(const SampleArgs &a, Scans &sh, int64_t t, float top, float tau, double kept_mass, double full_mass, uint32_t kept)
 {
-    const double unit = a.shift * 0.69314718055994530942;
-    a.token[t] = (int32_t)v;
-    if (a.logp) a.logp[t] = (float)(x - (log(kept_mass) - unit));
-    if (a.logp_full) a.logp_full[t] = (float)(x - (log(full_mass) - unit));
-    if (a.kept) a.kept[t] = (int32_t)kept;
+    __syncthreads();
+    if (threadIdx.x >= 2) return;
+    const double x = ((double)sh.token_logit - (double)top) / (double)tau, unit = a.shift * 0.69314718055994530942;
+    // (a thread each: the logarithm is there once)
+    float *to = threadIdx.x ? a.logp_full : a.logp;
+    if (to) to[t] = (float)(x - (log(threadIdx.x ? full_mass : kept_mass) - unit));
+    if (threadIdx.x == 0) {
+        a.token[t] = (int32_t)sh.token;
+        if (a.kept) a.kept[t] = (int32_t)kept;
+    }
 }
 
 // All passes over a row that its lists do not settle.
@@ -523,6 +687,7 @@ struct Passes {
     __device__ void histogram(uint32_t prefix, int shift, int bits)
     {
         __syncthreads();
+#pragma unroll 1
         for (int i = threadIdx.x; i < kBins; i += kThreads) sh.key.mass[i] = 0, sh.key.count[i] = 0;
         __syncthreads();
         const uint32_t mask = (1u << bits) - 1;
@@ -551,7 +716,8 @@ struct Passes {
         for (int i = 0; i < kEach; ++i) ms += sh.key.mass[top - i], cs += sh.key.count[top - i];
         uint64_t mi = ms;
         uint32_t ci = cs;
-        block_scan(sh, mi, ci, mass_total, count_total);
+        __syncthreads();
+        block_scan<kThreads, 0>(sh, mi, ci, mass_total, count_total);
         uint64_t ma = mass + mi - ms;
         uint32_t ca = count + ci - cs;
 #pragma unroll
@@ -581,9 +747,8 @@ struct Passes {
         });
         __syncthreads();
         const uint32_t own = sh.block_count[tid];
-        uint64_t m = 0, mt;
-        uint32_t upto = own, ct;
-        block_scan(sh, m, upto, mt, ct);
+        uint32_t upto = own, all_equal;
+        block_scan<kThreads, 1>(sh, upto, all_equal);
         if (upto >= n && upto - own < n) sh.found_digit = tid, sh.found_count = n - (upto - own);
         __syncthreads();
         if (tid < kWave) {
@@ -603,7 +768,7 @@ struct Passes {
                     for (int k = 0; k < EPV; ++k)
                         if (key_of(v[k]) == key && ++at == left) sh.found.last = (int32_t)(e + k);
                 }
-                const uint32_t all = __shfl(scan, kWave - 1, kWave);
+                const uint32_t all = last_lane(scan);
                 if (all >= left) break;
                 left -= all;
             }
@@ -640,16 +805,16 @@ struct Passes {
     __device__ Border cut(const Policy &policy)
     {
         Border border{kKeyOfNegInf, -1};
-        if (!policy.by_k && !policy.by_p) return border;
+        if (!policy.by_k() && !policy.by_p()) return border;
         histogram(0, 20, 12);
         uint64_t mass = 0, total;
         uint32_t count = 0, finite;
         find<true>(1, mass, count, total, finite);
-        if (policy.by_k && policy.k < finite) {
+        if (policy.by_k() && policy.k < finite) {
             border = select<false>((uint64_t)policy.k, total);
-            if (policy.by_p) histogram(0, 20, 12);
+            if (policy.by_p()) histogram(0, 20, 12);
         }
-        if (policy.by_p) {
+        if (policy.by_p()) {
             const double need = ceil((double)fmaxf(policy.p, 0.0f) * (double)total);
             uint64_t target = need < 1.0 ? 1 : (uint64_t)need;
             if (target > total) target = total;
@@ -691,108 +856,53 @@ struct Passes {
                     if ((e & 31) == 0 && e < a.V) a.allowed[t * a.allowed_ld + (e >> 5)] = (int32_t)word;
                 }
             }
-            const uint64_t sum = wave_sum((unsigned long long)in_block);
+            const uint64_t sum = wave_sum((uint64_t)in_block);
             if (lane == 0) sh.block_mass[b] = sum;
         }
         uint64_t full_total, total;
         uint32_t kept, none, zero = 0;
-        block_scan(sh, full, mine, full_total, kept);
-        __syncthreads();
-        const uint64_t own = sh.block_mass[tid];
+        block_scan<kThreads, 0>(sh, full, mine, full_total, kept);
+        const uint64_t own = sh.block_mass[tid];  // (written before the scan's barrier)
         uint64_t mass = own;
-        block_scan(sh, mass, zero, total, none);
+        block_scan<kThreads, 1>(sh, mass, zero, total, none);
         // the block, then the entry, in whose part of the sum the number falls
         const uint64_t target = (uint64_t)((double)policy.u * (double)total);
         if (mass > target && mass - own <= target) sh.found_digit = tid, sh.found_mass = target - (mass - own);
         __syncthreads();
-        if (wave != 0) return;
-        const int b = (int)sh.found_digit;
-        uint64_t left = sh.found_mass;
+        if (wave == 0) {
+            const int b = (int)sh.found_digit;
+            uint64_t left = sh.found_mass;
 #pragma unroll 1
-        for (int s = 0; s < row.steps; ++s) {
-            float v[EPV];
-            const int64_t e = row.first(b, s);
-            row.load(e, v);
-            uint64_t sum = 0;
+            for (int s = 0; s < row.steps; ++s) {
+                float v[EPV];
+                const int64_t e = row.first(b, s);
+                row.load(e, v);
+                uint64_t sum = 0;
 #pragma unroll
-            for (int i = 0; i < EPV; ++i) sum += border.keeps(v[i], (int32_t)(e + i)) ? weigh.whole(v[i]) : 0;
-            const uint64_t upto = wave_scan((unsigned long long)sum);
-            if (upto > left && upto - sum <= left) {
-                uint64_t at = upto - sum;
-                bool done = false;
+                for (int i = 0; i < EPV; ++i) sum += border.keeps(v[i], (int32_t)(e + i)) ? weigh.whole(v[i]) : 0;
+                const uint64_t upto = wave_scan(sum);
+                if (upto > left && upto - sum <= left) {
+                    uint64_t at = upto - sum;
+                    bool done = false;
 #pragma unroll
-                for (int i = 0; i < EPV; ++i) {
-                    at += border.keeps(v[i], (int32_t)(e + i)) ? weigh.whole(v[i]) : 0;
-                    if (!done && at > left) {
-                        done = true;
-                        tell(a, t, e + i, ((double)v[i] - (double)top) / (double)policy.tau, (double)total, (double)full_total, kept);
+                    for (int i = 0; i < EPV; ++i) {
+                        at += border.keeps(v[i], (int32_t)(e + i)) ? weigh.whole(v[i]) : 0;
+                        if (!done && at > left) sh.token = e + i, sh.token_logit = v[i], done = true;
                     }
                 }
+                if (__any(upto > left)) break;
+                left -= last_lane(upto);
             }
-            if (__any(upto > left)) break;
-            left -= __shfl((unsigned long long)upto, kWave - 1, kWave);
         }
+        tell(a, sh, t, top, policy.tau, (double)total, (double)full_total, kept);
     }
 };
 
-// The gathered entries.  Positions are in the order of the indices.
-struct Lists {
-    Shared &sh;
-    const Weigh &weigh;
-    uint32_t n;
-
-    __device__ __forceinline__ int bin_of(float v, float top, float scale) const
-    {
-        return (int)fminf(fmaxf((top - v) * scale, 0.0f), (float)(kThreads - 1));
-    }
-    // the last entry that is kept: in bin found_digit, before which there are found_mass and found_count; false: too many there
-    template <bool MASS>
-    __device__ bool resolve(uint64_t target, float top, float scale, Border &border, uint64_t &mass) const
-    {
-        const int tid = threadIdx.x;
-        const int bin = (int)sh.found_digit;
-        const uint64_t mass_before = sh.found_mass;
-        const uint32_t count_before = sh.found_count;
-        if (sh.list.bin_count[bin] > kThreads) return false;  // (the same for all)
-        uint32_t *at = sh.block_count;
-        uint64_t *weight = sh.block_mass;
-        if (tid == 0) sh.gathered = 0;
-        __syncthreads();
-        for (uint32_t i = tid; i < n; i += kThreads) {
-            const float v = sh.list.value[i];
-            if (bin_of(v, top, scale) == bin) {
-                const uint32_t to = atomicAdd(&sh.gathered, 1u);
-                at[to] = i;
-                weight[to] = weigh.whole(v);
-            }
-        }
-        __syncthreads();
-        const uint32_t m = sh.gathered;
-        if ((uint32_t)tid < m) {
-            const uint32_t mine = at[tid];
-            const float v = sh.list.value[mine];
-            uint64_t ahead = mass_before;
-            uint32_t before = count_before;
-            for (uint32_t q = 0; q < m; ++q) {
-                const float o = sh.list.value[at[q]];
-                const bool first = o > v || (o == v && at[q] < mine);
-                ahead += first ? weight[q] : 0;
-                before += first ? 1u : 0u;
-            }
-            if (MASS ? ahead < target && ahead + weight[tid] >= target : before + 1 == target)
-                sh.found = Border{key_of(v), sh.list.index[mine]}, sh.found_mass = ahead + weight[tid];
-        }
-        __syncthreads();
-        border = sh.found;
-        mass = sh.found_mass;
-        return true;
-    }
-};
-
+template <int N>
 __device__ __forceinline__ void tell_none(const SampleArgs &a, int64_t t, bool bad)
 {
     if (a.allowed)
-        for (int64_t w = threadIdx.x; w < (a.V + 31) / 32; w += kThreads) a.allowed[t * a.allowed_ld + w] = 0;
+        for (int64_t w = threadIdx.x; w < (a.V + 31) / 32; w += N) a.allowed[t * a.allowed_ld + w] = 0;
     if (threadIdx.x == 0) {
         const float none = bad ? __builtin_nanf("") : -kInf;
         a.token[t] = -1;
@@ -810,364 +920,554 @@ __device__ __forceinline__ float least_of(const Policy &policy, float top)
     return (double)zt < least ? nextafterf(zt, kInf) : zt;
 }
 
-// The entry of a part in whose part of the kept sum the number falls; `within`: what of it lies in the part, in units of 2^-shift of
-// the weight of weigh's maximum.
-template <typename DT>
-__device__ __forceinline__ void draw_in_part(const SampleArgs &a, Scans &sh, const Row<DT> &row, const Weigh &weigh, int part, double within,
-                                             Border border, int64_t t, float top, float tau, double kept_mass, double full, uint32_t kept)
+// Of so many entries from `begin` on, kEach a thread, the one in whose part of the kept sum the number falls; `within`: what of it lies there, in
+// units of the weight of weigh's maximum times what its table is scaled by.  Turns 0 and 1, in this order.
+template <int N, int kEach, typename DT>
+__device__ __forceinline__ void draw(Scans &sh, const Row<DT> &row, const Weigh &weigh, int64_t begin, int entries, double within, Border border)
 {
-    constexpr int kEach = kSamplePart / kThreads;
+    constexpr int EPV = DT::kPerVec;
     const int tid = threadIdx.x;
-    const int64_t e = (int64_t)part * kSamplePart + tid * kEach;
-    float v[kEach];
-    double w[kEach], sum = 0.0;
+    const int64_t e = begin + tid * kEach;
+    const bool active = tid * kEach < entries;
+    uint4 raw[kEach / EPV];
 #pragma unroll
-    for (int k = 0; k < kEach; k += Row<DT>::kEpv) row.load(e + k, v + k);
+    for (int k = 0; k < kEach / EPV; ++k) raw[k] = active ? row.load_raw(e + k * EPV) : neg_inf_vec<DT>();
+    double sum = 0.0;
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) w[k] = border.keeps(v[k], (int32_t)(e + k)) ? weigh(v[k]) : 0.0, sum += w[k];
+    for (int k = 0; k < kEach / EPV; ++k) {
+        float v[EPV];
+        unpack<DT>(raw[k], v);
+#pragma unroll
+        for (int j = 0; j < EPV; ++j) sum += border.keeps(v[j], (int32_t)(e + k * EPV + j)) ? weigh(v[j]) : 0.0;
+        asm volatile("" : "+v"(sum));
+    }
     double scan = sum, all;
-    block_scan(sh, scan, all);
-    const int thread = block_first(sh, scan > within && sum > 0.0, sum > 0.0);
+    block_scan<N, 0>(sh, scan, all);
+    const int thread = block_first<N, 1>(sh, scan > within && sum > 0.0, sum > 0.0);
     if (tid == thread) {
-        double at = scan - sum;
-        int64_t token = -1;
-        double x = 0.0;
-        bool done = false;
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            at += w[k];
-            if (!done && w[k] > 0.0) token = e + k, x = (double)v[k], done = at > within;
+        for (int k = 0; k < kEach / EPV; ++k) {
+            float v[EPV];
+            unpack<DT>(raw[k], v);
+#pragma unroll
+            for (int j = 0; j < EPV; ++j) sh.entries[k * EPV + j] = v[j];
         }
-        tell(a, t, token, (x - (double)top) / (double)tau, kept_mass, full, kept);
+        sh.told[1] = scan - sum;
+    }
+    __syncthreads();
+    if (tid < kWave) {
+        // its entries, a lane each
+        const float v = tid < kEach ? sh.entries[tid] : -kInf;
+        const int64_t at = begin + (int64_t)thread * kEach + tid;
+        const double w = tid < kEach && border.keeps(v, (int32_t)at) ? weigh(v) : 0.0, upto = sh.told[1] + wave_scan(w);
+        const uint64_t here = __ballot(w > 0.0 && upto > within), some = __ballot(w > 0.0);
+        if (tid == (here ? __builtin_ctzll(here) : 63 - __builtin_clzll(some | 1))) sh.token = at, sh.token_logit = v;
     }
 }
 
+// What all parts say together: the maximum, NaN where there is no policy, and whether one is off the grid.  The thread's own part is
+// left in `mine`.  Turn 0.
+template <int N>
+__device__ __forceinline__ float top_of(const SampleArgs &a, Scans &sh, const SamplePart *part, SamplePart &mine, bool &far)
+{
+    float top = -kInf;
+    bool bad = false, off = false;
+    mine = {};
+    mine.max = -kInf;
+    for (int q = threadIdx.x; q < a.parts; q += N) {
+        mine = part[q];
+        top = fmaxf(top, mine.max), bad |= mine.max != mine.max, off |= mine.max > -kInf && mine.place == kSampleFar;
+    }
+    float worst = bad ? 0.0f : off ? 1.0f : 2.0f;
+    block_range<N, 0>(sh, top, worst);
+    far = worst == 1.0f;
+    return worst == 0.0f ? __builtin_nanf("") : top;
+}
+
+// An uncut row: the part, a quarter of it, the entry, in whose part of the sum the number falls.  Turns 1, 0, ...
+template <int N, typename DT>
+__device__ __forceinline__ void draw_uncut(const SampleArgs &a, Scans &sh, const Policy &policy, const SamplePart &mine, int64_t t, float top)
+{
+    const int tid = threadIdx.x;
+    const double unit = kUnit / (double)policy.tau;
+    const Weigh weigh{(double)top, unit, sh.table};
+    // what the part's weights are relative to, in units of 2^-shift of the row's largest, and of its own
+    const double scale = ldexp(1.0, a.shift);
+    const bool some = mine.max > -kInf, far = is_far(mine.max, unit);
+    const double R = some && !far ? (double)__double2loint((double)mine.max * unit + kRound) : 0.0;
+    const double factor = !some ? 0.0 : far ? weigh(mine.max) : scale * exp2(fma(-(double)top, unit, R) * 0.03125);
+    const double own = (mine.mass[0] + mine.mass[1] + mine.mass[2] + mine.mass[3]) * factor;
+    double upto = own, full, none = 0.0;
+    uint32_t finite = mine.count, kept, more = 0;
+    block_scan<N, 1>(sh, upto, full, none, finite, kept, more);
+    const double target = (double)number_of(policy) * full;
+    const int chosen = block_first<N, 0>(sh, upto > target && own > 0.0, own > 0.0);
+    if (tid == chosen) {
+        double within = fmax(target - (upto - own), 0.0) / factor;
+        const double m0 = mine.mass[0], m1 = mine.mass[1], m2 = mine.mass[2], m3 = mine.mass[3];
+        const int last = m3 > 0.0 ? 3 : m2 > 0.0 ? 2 : m1 > 0.0 ? 1 : 0;
+        int quarter = 0;
+        if (last > 0 && !(m0 > within)) within -= m0, quarter = 1;
+        if (quarter == 1 && last > 1 && !(m1 > within)) within -= m1, quarter = 2;
+        if (quarter == 2 && last > 2 && !(m2 > within)) within -= m2, quarter = 3;
+        sh.told[0] = within * (far ? 1.0 : exp2(fma(-(double)mine.max, unit, R) * 0.03125)) * scale;
+        sh.told_top = mine.max;
+        sh.found_digit = chosen * kPartWaves + quarter;
+    }
+    __syncthreads();
+    const Weigh here{(double)sh.told_top, unit, sh.table};
+    const Row<DT> row{reinterpret_cast<const char *>(a.z) + t * a.ld * DT::kBytes, a.V, a.steps, a.blocks};
+    constexpr int kQuarter = kSamplePart / kPartWaves;
+    draw<N, 8>(sh, row, here, (int64_t)sh.found_digit * kQuarter, kQuarter, sh.told[0], Border{kKeyOfNegInf, -1});
+    tell(a, sh, t, top, policy.tau, full, full, kept);
+}
+
+// Rows that the host knows to be uncut.
 template <typename DT>
-__global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a, int64_t row0, int64_t rows)
+__global__ __launch_bounds__(kPartThreads, 4) void sample_uncut_kernel(SampleArgs a, int64_t row0, int64_t rows)
+{
+    __shared__ Scans sh;
+    if (threadIdx.x < 32) sh.table[threadIdx.x] = ldexp(kTable[threadIdx.x], a.shift);
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        SamplePart mine;
+        bool far;
+        __syncthreads();  // (the row before this one is done with everything)
+        const float top = top_of<kPartThreads>(a, sh, a.part + r * a.parts, mine, far);
+        const Policy policy(a, row0 + r);
+        if (policy.bad() || !(top > -kInf)) tell_none<kPartThreads>(a, row0 + r, policy.bad() || top != top);
+        else draw_uncut<kPartThreads, DT>(a, sh, policy, mine, row0 + r, top);
+    }
+}
+
+// ---- rows --------------------------------------------------------------------------------------------------------------
+
+template <typename DT>
+__global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
     __shared__ Scans sh;
     __shared__ int part_place[kThreads];
     __shared__ uint32_t part_bins[kThreads];
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int tid = threadIdx.x;
     if (tid < 32) sh.table[tid] = ldexp(kTable[tid], a.shift);
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const int64_t t = row0 + r;
-        const SamplePart *part = a.part + r * a.parts;
-        // ---- what the parts say together; a thread's own part where there is one for each
-        float top = -kInf;
-        SamplePart mine = {};
-        mine.max = -kInf;
-        bool bad = false;
-        int far = 0;
-        for (int q = tid; q < a.parts; q += kThreads) {
-            mine = part[q];
-            top = fmaxf(top, mine.max), bad |= mine.max != mine.max;
-            far |= mine.max > -kInf && mine.place == kSampleFar;
-        }
-        top = wave_max(top);
-        if (__any(bad)) top = __builtin_nanf("");
+        SamplePart mine;
+        bool far;
         __syncthreads();  // (the row before this one is done with everything)
-        if (lane == 0) sh.wave_top[wave] = top;
-        const bool any_far = __syncthreads_or(far);
-        bad = false;
-#pragma unroll 4
-        for (int w = 0; w < kWaves; ++w) bad |= sh.wave_top[w] != sh.wave_top[w], top = fmaxf(top, sh.wave_top[w]);
+        const float top = top_of<kThreads>(a, sh, a.part + r * a.parts, mine, far);
         const Policy policy(a, t);
-        bad |= policy.bad;
-        SampleRow out = {};
-        out.top = top;
-        out.mode = kSampleDone;
-        if (bad || top == -kInf) {
-            tell_none(a, t, bad);
-            if (tid == 0) a.row[r] = out;
-            continue;
-        }
         const bool each_part = a.parts <= kThreads;
-        if (!policy.cut() && each_part && !a.allowed) {
-            // ---- uncut: the part, then the entry, in whose part of the sum the number falls
-            const double unit = kUnit / (double)policy.tau;
-            const Weigh weigh{(double)top, unit, sh.table};
-            double upto = mine.mass * weigh(mine.max), full;
-            const double own = upto;
-            block_scan(sh, upto, full);
-            const double target = (double)number_of(policy) * full;
-            const int chosen = block_first(sh, upto > target && own > 0.0, own > 0.0);
-            __syncthreads();
-            if (tid == chosen) sh.wave_sum[0] = fmax(target - (upto - own), 0.0) / weigh(mine.max), sh.wave_top[0] = mine.max;
-            __syncthreads();
-            const double within = sh.wave_sum[0] * ldexp(1.0, a.shift);
-            const Weigh here{(double)sh.wave_top[0], unit, sh.table};
-            uint64_t none = 0, none_total;
-            uint32_t finite = mine.count, kept = 0;
-            if (a.kept) block_scan(sh, none, finite, none_total, kept);
-            const Row<DT> row{reinterpret_cast<const char *>(a.z) + t * a.ld * DT::kBytes, a.V, a.steps, a.blocks};
-            draw_in_part(a, sh, row, here, chosen, within, Border{kKeyOfNegInf, -1}, t, top, policy.tau, full, full, kept);
-            if (tid == 0) a.row[r] = out;
-            continue;
-        }
-        out.mode = kSamplePasses;
-        if (policy.cut() && each_part && !any_far) {
-            // ---- cut: all parts' bins on the row's grid, a bin a thread
-            const double grid = kGrid / (double)policy.tau;
-            out.place = place_of(top, grid);
-            if (tid < a.parts) part_place[tid] = mine.max > -kInf ? mine.place : kSampleFar, part_bins[tid] = mine.max > -kInf ? mine.bins : 0;
+        const double unit = kUnit / (double)policy.tau;
+        SampleRow out;
+        out.full = out.above = out.share = 0.0, out.rank = 0, out.top = top;
+        out.mode = kSamplePasses, out.by_k = out.place = out.bin = 0, out.count = 0;
+        if (policy.bad() || !(top > -kInf)) {
+            tell_none<kThreads>(a, t, policy.bad() || top != top);
+            out.mode = kSampleDone;
+        } else if (!policy.cut() && each_part && !a.allowed) {
+            draw_uncut<kThreads, DT>(a, sh, policy, mine, t, top);
+            out.mode = kSampleDone;
+        } else if (policy.cut() && each_part && !far) {
+            // ---- all parts' bins on the row's grid, a bin a thread
+            const double grid = unit * 0.5;
+            const float lowest = lowest_of(unit);
+            out.place = place_of(top, grid, lowest);
+            const bool some = mine.max > -kInf;
+            part_place[tid] = some ? mine.place : 0, part_bins[tid] = some ? mine.bins : 0;
+            const int64_t apart = some ? (int64_t)out.place - mine.place : 0;
+            double mass = some && apart < 16000 ? (mine.mass[0] + mine.mass[1] + mine.mass[2] + mine.mass[3]) * down_by((int)apart) * 68719476736.0 : 0.0;
             __syncthreads();
             uint64_t sum = 0;
             uint32_t own_count = 0;
-#pragma unroll 8
-            for (int q = 0; q < a.parts; ++q) {
-                const uint32_t b = (uint32_t)tid - ((uint32_t)out.place - (uint32_t)part_place[q]);
-                if (b < part_bins[q]) {
-                    const uint64_t v = a.bins[(r * a.parts + q) * kSampleBins + b];
-                    sum += v & kWeightMask, own_count += (uint32_t)(v >> kWeightBits);
+            const uint64_t *bins = a.bins + r * a.parts * kSampleBins;
+            constexpr int kTogether = 8;
+#pragma unroll 1
+            for (int first = 0; first < a.parts; first += kTogether) {
+                uint64_t v[kTogether];
+#pragma unroll
+                for (int j = 0; j < kTogether; ++j) {
+                    // (what is not there is read all the same, from within the array, and left out below)
+                    const int q = min(first + j, a.parts - 1);
+                    const uint32_t b = (uint32_t)tid - ((uint32_t)out.place - (uint32_t)part_place[q]);
+                    v[j] = bins[q * kSampleBins + min(b, (uint32_t)kSampleBins - 1)];
+                }
+#pragma unroll
+                for (int j = 0; j < kTogether; ++j) {
+                    const int q = min(first + j, a.parts - 1);
+                    const uint32_t b = (uint32_t)tid - ((uint32_t)out.place - (uint32_t)part_place[q]);
+                    const bool there = first + j < a.parts && b < part_bins[q];
+                    sum += there ? v[j] & kWeightMask : 0, own_count += there ? (uint32_t)(v[j] >> kWeightBits) : 0;
                 }
             }
-            // in units of the weight in the middle of bin 0, times 2^36: bins of 16 a power of two (even places of the table)
-            const int down = (tid + 15) >> 4;
-            const double own = (double)sum * ldexp(kTable[2 * (down * 16 - tid)], -down);
-            double upto = own, all, tails = 0.0;
-            block_scan(sh, upto, all);
-            if (tid < a.parts && mine.max > -kInf) tails = mine.mass * exp2(-0.0625 * (double)(out.place - mine.place)) * 68719476736.0;
-            double none = tails, tail;
-            block_scan(sh, none, tail);
-            uint64_t unused = 0, unused_total;
-            uint32_t count = own_count, binned, finite = tid < a.parts ? mine.count : 0, all_finite;
-            block_scan(sh, unused, count, unused_total, binned);
-            unused = 0;
-            block_scan(sh, unused, finite, unused_total, all_finite);
-            out.full = all + tail;
-            // ---- the bin of the tightest border; several may share it.  (The first kSampleBins hold all entries of every part.)
-            const bool whole = tid < kSampleBins;
-            const bool by_k = policy.by_k && policy.k < (int64_t)all_finite;
+            // in units of the weight in the middle of bin 0, times 2^36
+            const double own = (double)sum * down_by(tid);
+            double upto = own, all;
+            uint32_t count = own_count, binned, finite = mine.count;
+            block_scan<kThreads, 1>(sh, upto, all, mass, count, binned, finite);
+            out.full = mass;
+            // ---- the bin of the tightest border; several may share it
+            const bool by_k = policy.by_k() && policy.k < (int64_t)finite;
             const double need = (double)fmaxf(policy.p, 0.0f) * out.full;
-            int bin_k = -1, bin_p = -1, bin_min = -1;
             bool lost = false;
-            if (by_k) bin_k = block_first(sh, whole && (int64_t)count >= policy.k, false), lost |= bin_k < 0;
-            if (policy.by_p && !by_k) bin_p = block_first(sh, whole && own_count > 0 && upto >= need, false), lost |= bin_p < 0;
-            if (policy.by_min) {
-                const float zt = least_of(policy, top);
-                const int64_t b = (int64_t)out.place - place_of(zt, grid);
-                bin_min = b < kSampleBins ? (int)b : kSampleBins;
+            int bin = kSampleAll, bin_p = -1;
+            if (by_k || policy.by_p()) {
+                bin = block_first<kThreads, 0>(sh, own_count > 0 && (by_k ? (int64_t)count >= policy.k : upto >= need), false);
+                if (bin < 0) bin = kSampleAll, lost = true;
+                else if (!by_k) bin_p = bin;
             }
-            int bin = kSampleAll;
-            if (bin_k >= 0) bin = bin_k;
-            if (bin_p >= 0) bin = bin_p;
+            const int bin_k = by_k ? bin : -1;
             // (top_p is a share of what top_k leaves, so with both all of that is needed)
-            if (bin_min >= 0 && bin_min < bin && !(by_k && policy.by_p)) bin = bin_min;
-            if (bin == kSampleBins) bin = kSampleAll, lost |= all_finite > kSampleListed;
+            if (policy.by_min() && !(by_k && policy.by_p())) {
+                const int64_t b = (int64_t)out.place - place_of(least_of(policy, top), grid, lowest);
+                if (b < kSampleBins && b < bin) bin = (int)b, lost = false;
+            }
             // how many there are down to it, and in it
-            if (tid == 0) sh.found_count = all_finite, sh.found_digit = 0, sh.wave_sum[0] = 0.0;
+            if (tid == 0) sh.found_count = finite, sh.found_digit = 0, sh.told[0] = 0.0;
             __syncthreads();
-            if (tid == bin) sh.found_count = count, sh.found_digit = own_count, sh.wave_sum[0] = upto - own;
+            if (tid == bin) sh.found_count = count, sh.found_digit = own_count, sh.told[0] = upto - own;
             __syncthreads();
             const uint32_t down_to = sh.found_count, in_bin = sh.found_digit;
             out.bin = bin;
-            out.above = sh.wave_sum[0];
+            out.above = sh.told[0];
             out.count = down_to - in_bin;
-            out.share = policy.by_p && bin_p == bin ? need : -1.0;
-            out.rank = bin_k == bin && bin_k >= 0 ? policy.k - out.count : -1;
+            out.share = bin_p == bin ? need : -1.0;
+            out.rank = bin_k == bin && by_k ? policy.k - out.count : -1;
             out.by_k = by_k;
-            if (!lost) {
-                if (down_to <= kSampleListed) out.mode = kSampleFew;
-                else if (bin != kSampleAll && in_bin <= kSampleListed && !(by_k && policy.by_p)) out.mode = kSampleBin;
+            if (down_to <= kSampleFewest) out.mode = kSampleFew;
+            else if (!lost && bin != kSampleAll && in_bin <= kSampleListed && !(by_k && policy.by_p())) out.mode = kSampleBin;
+        }
+        // (field by field: a whole struct's copy takes its padding along, through a private array that ends up in LDS by a thread
+        // number from the dispatch packet in host memory, 4 to 14 us at the kernel's beginning)
+        if (tid == 0) {
+            SampleRow &to = a.row[r];
+            to.full = out.full, to.above = out.above, to.share = out.share, to.rank = out.rank, to.top = out.top;
+            to.mode = out.mode, to.by_k = out.by_k, to.place = out.place, to.bin = out.bin, to.count = out.count, to.cursor = 0;
+        }
+    }
+}
+
+// ---- finish ------------------------------------------------------------------------------------------------------------
+
+// The gathered entries; positions are in the order of the indices.  The last entry kept, by its logit and its position.
+struct Last {
+    float value;
+    uint32_t position;
+    __device__ __forceinline__ bool keeps(float v, uint32_t q) const { return v > value || (v == value && q <= position); }
+};
+__device__ __forceinline__ Last tighter(Last a, Last b)
+{
+    if (a.value != b.value) return a.value > b.value ? a : b;
+    return Last{a.value, min(a.position, b.position)};
+}
+
+// Of n entries between low and high, the last of those that make `target`, whole numbers: a count, or a mass.  mass: up to it.
+// Bins, then the bins of one bin, until few enough are left to compare each with all others, or all left are equal.
+__device__ __forceinline__ Last last_of(Shared &sh, const Weigh &weigh, uint32_t n, float high, float low, bool by_mass, uint64_t target, uint64_t &mass)
+{
+    const int tid = threadIdx.x;
+    uint32_t m = n, count_before = 0;
+    uint64_t mass_before = 0;
+#pragma unroll 1
+    while (m > kDirect && low < high) {
+        const float scale = (float)(kThreads - 1) / (high - low);
+        auto bin_of = [&](float v) {
+            const int b = (int)fminf(fmaxf((high - v) * scale, 0.0f), (float)(kThreads - 1));
+            return v == low ? kThreads - 1 : v == high ? 0 : b;  // (apart whatever the scale is)
+        };
+        __syncthreads();
+        sh.list.bin_mass[tid] = 0, sh.list.bin_count[tid] = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t i = tid; i < n; i += kThreads) {
+            const float v = sh.list.value[i];
+            if (v >= low && v <= high) {
+                const int b = bin_of(v);
+                atomicAdd(&sh.list.bin_count[b], 1u);
+                atomicAdd(reinterpret_cast<unsigned long long *>(&sh.list.bin_mass[b]), (unsigned long long)weigh.whole(v));
             }
         }
-        if (tid == 0) a.row[r] = out;
+        __syncthreads();
+        const uint64_t own = sh.list.bin_mass[tid];
+        const uint32_t own_count = sh.list.bin_count[tid];
+        uint64_t upto = own, all;
+        uint32_t count = own_count, all_count;
+        block_scan<kThreads, 0>(sh, upto, count, all, all_count);
+        if (by_mass) target = min(target, mass_before + all);  // (rounding may ask for more than there is)
+        upto += mass_before, count += count_before;
+        if (by_mass ? upto >= target && upto - own < target : count >= target && count - own_count < target)
+            sh.found_digit = tid, sh.found_mass = upto - own, sh.found_count = count - own_count;
+        __syncthreads();
+        const int bin = (int)sh.found_digit;
+        mass_before = sh.found_mass, count_before = sh.found_count;
+        m = sh.list.bin_count[bin];
+        float h = -kInf, l = kInf;
+#pragma unroll 1
+        for (uint32_t i = tid; i < n; i += kThreads) {
+            const float v = sh.list.value[i];
+            if (v >= low && v <= high && bin_of(v) == bin) h = fmaxf(h, v), l = fminf(l, v);
+        }
+        block_range<kThreads, 1>(sh, h, l);
+        high = h, low = l;
+    }
+    __syncthreads();
+    if (m <= kDirect) {
+        uint32_t *at = sh.block_count;
+        uint64_t *weight = sh.block_mass;
+        float *value = reinterpret_cast<float *>(sh.list.bin_count);
+        if (tid == 0) sh.gathered = 0;
+        at[tid] = 0, weight[tid] = 0, value[tid] = -kInf;
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t i = tid; i < n; i += kThreads) {
+            const float v = sh.list.value[i];
+            if (v >= low && v <= high) {
+                const uint32_t to = atomicAdd(&sh.gathered, 1u);
+                at[to] = i, value[to] = v;
+                weight[to] = weigh.whole(v);
+            }
+        }
+        __syncthreads();
+        if ((uint32_t)tid < m) {
+            const uint32_t mine = at[tid];
+            const float v = value[tid];
+            uint64_t ahead = mass_before, all = mass_before;
+            uint32_t before = count_before;
+#pragma unroll 1
+            for (uint32_t q = 0; q < m; q += 8)
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) {  // (behind the m-th there is nothing, at -inf)
+                    const float o = value[q + j];
+                    const uint64_t w = weight[q + j];
+                    const uint32_t first = (uint32_t)(o > v) | ((uint32_t)(o == v) & (uint32_t)(at[q + j] < mine));
+                    ahead += w & (0ull - first);
+                    all += w;
+                    before += first;
+                }
+            if (by_mass) target = min(target, all);
+            if (by_mass ? ahead < target && ahead + weight[tid] >= target : before + 1 == target)
+                sh.found = Border{__float_as_uint(v), (int32_t)mine}, sh.found_mass = ahead + weight[tid];
+        }
+    } else {
+        // all the m left are equal: the c-th of them
+        const uint64_t each = weigh.whole(high), left = target - (by_mass ? mass_before : count_before);
+        const uint32_t c = by_mass ? (uint32_t)min((left + each - 1) / (each ? each : 1), (uint64_t)m) : (uint32_t)left;
+        const uint32_t run = (n + kThreads - 1) / kThreads;
+        uint32_t own = 0, all;
+        for (uint32_t i = tid * run; i < min(n, (tid + 1) * run); ++i) own += sh.list.value[i] == high ? 1u : 0u;
+        uint32_t upto = own;
+        block_scan<kThreads, 0>(sh, upto, all);
+        if (upto >= c && upto - own < c) {
+            uint32_t k = upto - own;
+            for (uint32_t i = tid * run; i < min(n, (tid + 1) * run); ++i)
+                if (sh.list.value[i] == high && ++k == c) sh.found = Border{__float_as_uint(high), (int32_t)i}, sh.found_mass = mass_before + c * each;
+        }
+    }
+    __syncthreads();
+    mass = sh.found_mass;
+    return Last{__uint_as_float(sh.found.key), (uint32_t)sh.found.last};
+}
+
+// Rows that the bins do not settle, as often as their cuts ask.
+template <typename DT>
+__global__ __launch_bounds__(kThreads, 4) void sample_passes_kernel(SampleArgs a, int64_t row0, int64_t rows)
+{
+    __shared__ Shared sh;
+    if (threadIdx.x < 32) sh.table[threadIdx.x] = ldexp(kTable[threadIdx.x], a.shift);
+#pragma unroll 1
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const int64_t t = row0 + r;
+        if (a.row[r].mode != kSamplePasses) continue;
+        __syncthreads();  // (the table is there; the row before this one is done with everything)
+        const float top = a.row[r].top;
+        Policy policy(a, t);
+        policy.u = number_of(policy);
+        const Weigh weigh{(double)top, kUnit / (double)policy.tau, sh.table};
+        Passes<DT> passes{a, sh, Row<DT>{reinterpret_cast<const char *>(a.z) + t * a.ld * DT::kBytes, a.V, a.steps, a.blocks}, weigh};
+        Border border{kKeyOfNegInf, -1};
+        if (policy.by_min()) border = Border{key_of(fmaxf(least_of(policy, top), -3.402823466e38f)), kAnyIndex};
+        passes.finish(policy, tighter(border, passes.cut(policy)), t, top);
     }
 }
 
 template <typename DT>
-__global__ __launch_bounds__(kThreads) void sample_finish_kernel(SampleArgs a, int64_t row0, int64_t rows)
+__global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
     __shared__ Shared sh;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int tid = threadIdx.x;
     if (tid < 32) sh.table[tid] = ldexp(kTable[tid], a.shift);
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const int64_t t = row0 + r;
         const SampleRow row = a.row[r];
-        if (row.mode == kSampleDone) continue;
+        if (row.mode != kSampleFew && row.mode != kSampleBin) continue;
         __syncthreads();  // (the table is there; the row before this one is done with everything)
         Policy policy(a, t);
         policy.u = number_of(policy);
         const float top = row.top;
-        const Weigh weigh{(double)top, kUnit / (double)policy.tau, sh.table};
+        const double unit = kUnit / (double)policy.tau;
+        const Weigh weigh{(double)top, unit, sh.table};
         const Row<DT> data{reinterpret_cast<const char *>(a.z) + t * a.ld * DT::kBytes, a.V, a.steps, a.blocks};
-        Border border{kKeyOfNegInf, -1};
-        if (policy.by_min) {
-            const float zt = least_of(policy, top);
-            if (zt > -kInf) border = Border{key_of(zt), kAnyIndex};
-        }
-        bool settled = row.mode != kSamplePasses;
+        const float least = policy.by_min() ? fmaxf(least_of(policy, top), -3.402823466e38f) : -3.402823466e38f;
         // what one unit of the bins' sums (2^-36 of the middle of bin 0) is in units of 2^-shift of the largest weight
-        const double grid = kGrid / (double)policy.tau;
-        const double to_whole = settled ? ldexp(exp2(((double)row.place - (double)top * grid) * 0.0625), a.shift - 36) : 0.0;
+        const double to_whole = ldexp(exp2(fma(-(double)top, unit * 0.5, (double)row.place) * 0.0625), a.shift - 36);
         const double full = row.full * to_whole;
+        const bool few = row.mode == kSampleFew;
+        // ---- the gathered entries, from the order in which the parts found room to the parts' own
         SampleSegment segment = {};
-        uint32_t n = 0, place = 0;  // entries; where this thread's part's begin
-        if (settled) {
-            // ---- the gathered entries, in the order of the parts
-            if (tid < a.parts) segment = a.segment[r * a.parts + tid];
-            uint64_t none = 0, none_total;
-            place = segment.listed;
-            block_scan(sh, none, place, none_total, n);
-            place -= segment.listed;
-            if (tid < a.parts) sh.block_count[tid] = place;
-            __syncthreads();
-            for (int q = wave; q < a.parts; q += kWaves) {
-                const SampleSegment &from = a.segment[r * a.parts + q];
-                const uint32_t to = sh.block_count[q], many = from.listed;
-                const uint2 *list = a.list + r * kSampleListed + from.start;
-                for (uint32_t i = lane; i < many; i += kWave) {
-                    const uint2 v = list[i];
-                    sh.list.value[to + i] = __uint_as_float(v.x), sh.list.index[to + i] = (int32_t)v.y;
-                }
+        if (tid < a.parts) segment = a.segment[r * a.parts + tid];
+        uint32_t place = segment.listed, n;  // where this thread's part's begin; entries
+        block_scan<kThreads, 0>(sh, place, n);
+        place -= segment.listed;
+        sh.block_count[tid] = place - segment.start;
+        __syncthreads();
+        float high = -kInf, low = kInf;
+        const uint2 *list = a.list + r * kSampleListed;
+        constexpr int kTogether = 4;
+#pragma unroll 1
+        for (uint32_t first = tid; first < n; first += kThreads * kTogether) {
+            uint2 v[kTogether];
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) v[j] = list[min(first + j * kThreads, n - 1)];  // (the last one again and again)
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) {
+                const uint32_t to = min(first + j * kThreads, n - 1) + sh.block_count[v[j].y / kSamplePart];
+                const float x = __uint_as_float(v[j].x);
+                sh.list.value[to] = x;
+                if (few) sh.list.index[to] = (int32_t)v[j].y;
+                high = fmaxf(high, x), low = fminf(low, x);
             }
-            const bool few = row.mode == kSampleFew;
-            const bool by_k = few ? row.by_k : row.rank > 0, by_p = few ? policy.by_p : row.share >= 0.0;
-            if (by_k || by_p) {
-                // by logit, in bins between the largest and the smallest of them
-                const Lists lists{sh, weigh, n};
-                __syncthreads();
-                float highest = -kInf, lowest = kInf;
-                for (uint32_t i = tid; i < n; i += kThreads) highest = fmaxf(highest, sh.list.value[i]), lowest = fminf(lowest, sh.list.value[i]);
-                highest = wave_max(highest), lowest = -wave_max(-lowest);
-                if (lane == 0) sh.wave_top[wave] = highest, sh.wave_count[wave] = __float_as_uint(lowest);
-                sh.list.bin_mass[tid] = 0, sh.list.bin_count[tid] = 0;
-                __syncthreads();
-#pragma unroll 4
-                for (int w = 0; w < kWaves; ++w) highest = fmaxf(highest, sh.wave_top[w]), lowest = fminf(lowest, __uint_as_float(sh.wave_count[w]));
-                const float scale = lowest < highest ? (float)(kThreads - 1) / (highest - lowest) : 0.0f;
-                for (uint32_t i = tid; i < n; i += kThreads) {
-                    const float v = sh.list.value[i];
-                    const int b = lists.bin_of(v, highest, scale);
-                    atomicAdd(&sh.list.bin_count[b], 1u);
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.list.bin_mass[b]), (unsigned long long)weigh.whole(v));
-                }
-                __syncthreads();
-                const uint64_t own = sh.list.bin_mass[tid];
-                const uint32_t own_count = sh.list.bin_count[tid];
-                uint64_t mass = own, list_mass;
-                uint32_t count = own_count, list_count;
-                block_scan(sh, mass, count, list_mass, list_count);
-                double total = full;  // of what top_p is a share of
-                const int64_t k = few ? policy.k : row.rank;
-                if (by_k && k <= (int64_t)list_count) {
-                    if ((int64_t)count >= k && (int64_t)(count - own_count) < k)
-                        sh.found_digit = tid, sh.found_mass = mass - own, sh.found_count = count - own_count;
-                    __syncthreads();
-                    Border here;
-                    uint64_t left;
-                    settled = lists.resolve<false>((uint64_t)k, highest, scale, here, left);
-                    if (settled) border = tighter(border, here), total = (double)left;
-                    __syncthreads();
-                }  // (else min_p ends the list before the k-th, and there is no top_p)
-                if (settled && by_p) {
-                    const double need = ceil(few ? (double)fmaxf(policy.p, 0.0f) * total : (row.share - row.above) * to_whole);
-                    uint64_t target = need < 1.0 ? 1 : (uint64_t)need;
-                    if (target > list_mass) target = list_mass;
-                    if (mass >= target && mass - own < target)
-                        sh.found_digit = tid, sh.found_mass = mass - own, sh.found_count = count - own_count;
-                    __syncthreads();
-                    Border here;
-                    uint64_t left;
-                    settled = lists.resolve<true>(target, highest, scale, here, left);
-                    if (settled) border = tighter(border, here);
-                }
-            }
-            __syncthreads();
         }
-        if (settled) {
-            // ---- the kept of the gathered: in the order of their indices, so many a thread
-            const int each = (int)((n + kThreads - 1) / kThreads);
+        block_range<kThreads, 1>(sh, high, low);
+        // ---- the border among them
+        Last border{least, 0xFFFFFFFFu};
+        double total = full;  // of what top_p is a share of
+        const int64_t k = few ? policy.k : row.rank;
+        const bool by_k = few ? row.by_k && k <= (int64_t)n : k > 0;  // (min_p may end the list before the k-th; there is no top_p then)
+        const bool by_p = few ? policy.by_p() : row.share >= 0.0;
+#pragma unroll 1
+        for (int which = 0; which < 2; ++which) {
+            if (which == 0 ? !by_k : !by_p) continue;
+            uint64_t target = (uint64_t)k, mass;
+            if (which == 1) {
+                const double need = ceil(few ? (double)fmaxf(policy.p, 0.0f) * total : (row.share - row.above) * to_whole);
+                target = need < 1.0 ? 1 : (uint64_t)need;
+            }
+            border = tighter(border, last_of(sh, weigh, n, high, low, which == 1, target, mass));
+            if (which == 0) total = (double)mass;
+        }
+        __syncthreads();
+        if (few) {
+            // ---- the kept in the order of their indices, so many a thread
+            const uint32_t run = (n + kThreads - 1) / kThreads;
             uint64_t sum = 0;
             uint32_t kept = 0;
-            for (int i = 0; i < each; ++i) {
-                const uint32_t q = tid * each + i;
-                if (q < n && border.keeps(sh.list.value[q], sh.list.index[q])) sum += weigh.whole(sh.list.value[q]), ++kept;
-            }
-            uint64_t scan = sum, total;
+#pragma unroll 1
+            for (uint32_t q = tid * run; q < min(n, (tid + 1) * run); ++q)
+                if (border.keeps(sh.list.value[q], q)) sum += weigh.whole(sh.list.value[q]), ++kept;
+            uint64_t scan = sum, all;
             uint32_t kept_total;
-            block_scan(sh, scan, kept, total, kept_total);
-            if (row.mode == kSampleBin) {
-                // ---- each part's kept: what is above the bin, and of the bin what is in its segment
-                if (tid < a.parts) sh.block_count[tid] = place;
-                __syncthreads();
-                for (int q = wave; q < a.parts; q += kWaves) {
-                    const uint32_t to = sh.block_count[q], many = a.segment[r * a.parts + q].listed;
-                    uint64_t in_part = 0;
-                    for (uint32_t i = lane; i < many; i += kWave)
-                        if (border.keeps(sh.list.value[to + i], sh.list.index[to + i])) in_part += weigh.whole(sh.list.value[to + i]);
-                    in_part = wave_sum((unsigned long long)in_part);
-                    if (lane == 0) sh.block_mass[q] = in_part;
-                }
-                __syncthreads();
-                const double own = tid < a.parts ? segment.above * to_whole + (double)sh.block_mass[tid] : 0.0;
-                double upto = own, mass;
-                block_scan(sh, upto, mass);
-                const double target = (double)policy.u * mass;
-                const int chosen = block_first(sh, upto > target && own > 0.0, own > 0.0);
-                __syncthreads();
-                if (tid == chosen) sh.wave_sum[0] = fmax(target - (upto - own), 0.0);
-                __syncthreads();
-                const double within = sh.wave_sum[0];
-                draw_in_part(a, sh, data, weigh, chosen, within, border, t, top, policy.tau, mass, full, row.count + kept_total);
-                if (a.allowed) {
-                    // (entries above the bin, and the border's part of it: what the border says of every entry)
-                    constexpr int EPV = DT::kPerVec;
-                    data.each([&](const float *v, int64_t e, int) {
-                        uint32_t word = 0;
-#pragma unroll
-                        for (int k = 0; k < EPV; ++k) word |= (border.keeps(v[k], (int32_t)(e + k)) ? 1u : 0u) << k;
-                        word <<= e & 31;
-#pragma unroll
-                        for (int off = 1; off < 32 / EPV; off <<= 1) word |= __shfl_xor(word, off, kWave);
-                        if ((e & 31) == 0 && e < a.V) a.allowed[t * a.allowed_ld + (e >> 5)] = (int32_t)word;
-                    });
-                }
-                continue;
-            }
-            // ---- few: the entry in whose part of the sum the number falls
-            const uint64_t target = (uint64_t)((double)policy.u * (double)total);
+            block_scan<kThreads, 1>(sh, scan, kept, all, kept_total);
+            const uint64_t target = (uint64_t)((double)policy.u * (double)all);
             if (scan > target && scan - sum <= target) {
                 uint64_t at = scan - sum;
-                for (int i = 0; i < each; ++i) {
-                    const uint32_t q = tid * each + i;
+#pragma unroll 1
+                for (uint32_t q = tid * run; q < n; ++q) {
                     const float v = sh.list.value[q];
-                    if (border.keeps(v, sh.list.index[q])) at += weigh.whole(v);
+                    if (border.keeps(v, q)) at += weigh.whole(v);
                     if (at > target) {
-                        tell(a, t, sh.list.index[q], ((double)v - (double)top) / (double)policy.tau, (double)total, full, kept_total);
+                        sh.token = sh.list.index[q], sh.token_logit = v;
                         break;
                     }
                 }
             }
+            tell(a, sh, t, top, policy.tau, (double)all, full, kept_total);
             if (a.allowed) {
                 // bits of so many words at a time
                 constexpr int kWords = 2 * kSampleBlocks;
                 uint32_t *words = reinterpret_cast<uint32_t *>(sh.block_mass);
-                const int64_t all = (a.V + 31) / 32;
-                for (int64_t begin = 0; begin < all; begin += kWords) {
+                const int64_t words_all = (a.V + 31) / 32;
+#pragma unroll 1
+                for (int64_t begin = 0; begin < words_all; begin += kWords) {
                     __syncthreads();
                     words[tid] = 0, words[tid + kThreads] = 0;
                     __syncthreads();
+#pragma unroll 1
                     for (uint32_t q = tid; q < n; q += kThreads) {
                         const int32_t e = sh.list.index[q];
                         const int64_t w = (e >> 5) - begin;
-                        if (w >= 0 && w < kWords && border.keeps(sh.list.value[q], e)) atomicOr(&words[w], 1u << (e & 31));
+                        if (w >= 0 && w < kWords && border.keeps(sh.list.value[q], q)) atomicOr(&words[w], 1u << (e & 31));
                     }
                     __syncthreads();
-                    for (int64_t w = tid; w < kWords && begin + w < all; w += kThreads) a.allowed[t * a.allowed_ld + begin + w] = (int32_t)words[w];
+                    for (int64_t w = tid; w < kWords && begin + w < words_all; w += kThreads) a.allowed[t * a.allowed_ld + begin + w] = (int32_t)words[w];
                 }
             }
             continue;
         }
-        // ---- the row, as often as its cuts ask
-        border = Border{kKeyOfNegInf, -1};
-        if (policy.by_min) {
-            const float zt = least_of(policy, top);
-            if (zt > -kInf) border = Border{key_of(zt), kAnyIndex};
+        // ---- each part's kept: what is above the bin, and of the bin what is in its segment
+        sh.block_count[tid] = place - segment.start, sh.block_mass[tid] = 0;
+        // (the part that holds the border's position says its index)
+        if (border.position - place < segment.listed) sh.found.last = (int32_t)list[segment.start + (border.position - place)].y;
+        __syncthreads();
+        const Border last{key_of(border.value), border.position == 0xFFFFFFFFu ? kAnyIndex : sh.found.last};
+        uint32_t kept = 0;
+#pragma unroll 1
+        for (uint32_t first = tid; first < n; first += kThreads * kTogether) {
+            uint2 v[kTogether];
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) v[j] = list[min(first + j * kThreads, n - 1)];
+#pragma unroll 1
+            for (int j = 0; j < kTogether && first + j * kThreads < n; ++j) {
+                const uint2 u = v[0];
+                v[0] = v[1], v[1] = v[2], v[2] = v[3];
+                if (last.keeps(__uint_as_float(u.x), (int32_t)u.y)) {
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.block_mass[u.y / kSamplePart]), (unsigned long long)weigh.whole(__uint_as_float(u.x)));
+                    ++kept;
+                }
+            }
         }
-        Passes<DT> passes{a, sh, data, weigh};
-        passes.finish(policy, tighter(border, passes.cut(policy)), t, top);
+        __syncthreads();
+        const double own = tid < a.parts ? segment.above * to_whole + (double)sh.block_mass[tid] : 0.0;
+        double upto = own, mass, none = 0.0;
+        uint32_t zero = 0, zero_total;
+        block_scan<kThreads, 1>(sh, upto, mass, none, zero, zero_total, kept);
+        const double target = (double)policy.u * mass;
+        const int chosen = block_first<kThreads, 0>(sh, upto > target && own > 0.0, own > 0.0);
+        if (tid == chosen) sh.told[0] = fmax(target - (upto - own), 0.0);
+        __syncthreads();
+        draw<kThreads, kSamplePart / kThreads>(sh, data, weigh, (int64_t)chosen * kSamplePart, kSamplePart, sh.told[0], last);
+        tell(a, sh, t, top, policy.tau, mass, full, row.count + kept);
+        if (tid == 0) a.row[r].key = last.key, a.row[r].last = last.last;
+    }
+}
+
+// ---- bits of rows with many kept, a workgroup a part -----------------------------------------------------------------------
+
+template <typename DT>
+__global__ __launch_bounds__(kPartThreads, 4) void sample_bits_kernel(SampleArgs a, int64_t row0, int64_t rows)
+{
+    using Entries = PartEntries<DT>;
+    constexpr int EPV = Entries::EPV, kVectors = Entries::kVectors;
+    for (int64_t i = blockIdx.x; i < rows * a.parts; i += gridDim.x) {
+        const int64_t r = i / a.parts, t = row0 + r;
+        if (a.row[r].mode != kSampleBin) continue;
+        const int64_t begin = (i - r * a.parts) * kSamplePart;
+        const int left = (int)min(a.V - begin, (int64_t)kSamplePart);
+        Entries z;
+        z.load(reinterpret_cast<const char *>(a.z) + (t * a.ld + begin) * DT::kBytes, left);
+        const Border last{a.row[r].key, a.row[r].last};
+        int32_t *words = a.allowed + t * a.allowed_ld + begin / 32;
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+            const int e = Entries::first() + v * kWave * EPV;
+            float x[EPV];
+            unpack<DT>(z.raw[v], x);
+            uint32_t word = 0;
+#pragma unroll
+            for (int k = 0; k < EPV; ++k) word |= (last.keeps(x[k], (int32_t)(begin + e + k)) ? 1u : 0u) << k;
+            word <<= e & 31;
+#pragma unroll
+            for (int off = 1; off < 32 / EPV; off <<= 1) word |= __shfl_xor(word, off, kWave);
+            if ((e & 31) == 0 && e < left) words[e >> 5] = (int32_t)word;
+        }
     }
 }
 
@@ -1178,11 +1478,16 @@ void launch(const SampleArgs &a, hipStream_t s)
         const int64_t rows = a.T - row0 < kSampleRows ? a.T - row0 : kSampleRows, parts = rows * a.parts;
         const int grid = (int)(parts < (1 << 24) ? parts : 1 << 24);
         sample_parts_kernel<DT><<<grid, kPartThreads, 0, s>>>(a, row0, rows);
+        // (temperatures of 0 cut, and so may what the other arrays hold)
+        if (!a.temperature && !a.top_k && !a.top_p && !a.min_p && !a.allowed && a.parts <= kPartThreads) {
+            sample_uncut_kernel<DT><<<(int)rows, kPartThreads, 0, s>>>(a, row0, rows);
+            continue;
+        }
         sample_rows_kernel<DT><<<(int)rows, kThreads, 0, s>>>(a, row0, rows);
-        // (rows that are all uncut are done; what is not known on the host, temperatures of 0 among it, may cut)
-        if (!a.temperature && !a.top_k && !a.top_p && !a.min_p && !a.allowed && a.parts <= kThreads) continue;
         sample_gather_kernel<DT><<<grid, kPartThreads, 0, s>>>(a, row0, rows);
         sample_finish_kernel<DT><<<(int)rows, kThreads, 0, s>>>(a, row0, rows);
+        sample_passes_kernel<DT><<<(int)(rows < 512 ? rows : 512), kThreads, 0, s>>>(a, row0, rows);
+        if (a.allowed) sample_bits_kernel<DT><<<grid, kPartThreads, 0, s>>>(a, row0, rows);
     }
 }
 
