@@ -664,6 +664,7 @@ struct alignas(128) SampleRow {
     uint32_t count, cursor;     // entries before the border's bin; room taken in the list
     uint32_t key;               // the last entry kept, for the bits of many
     int32_t last;
+    float from, to;             // logits to be gathered
 };
 struct SampleSegment {
     double above;            // the part's share of SampleRow::above

@@ -81,6 +81,26 @@ __device__ __forceinline__ uint32_t key_of(float z)
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
+// (fmaxf makes a quiet NaN of each operand first, an instruction each; NaN is looked for apart)
+__device__ __forceinline__ float max2(float a, float b)
+{
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // Sums over the lanes before and up to each: within rows of 16 lanes, then rows 1 and 3 take what ends row 0 and 2, then the upper
 // half what ends the lower.
 template <int CTRL, int ROWS>
@@ -200,14 +220,13 @@ struct PartEntries {
     }
     // f(value, its number among the lane's) of every entry
     template <typename F>
-    __device__ __forceinline__ void each(F f) const
+    __device__ __forceinline__ void each(F f)
     {
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
             float x[EPV];
-            uint4 r = raw[v];
-            asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w));  // (nothing of one pass is kept for the next)
-            unpack<DT>(r, x);
+            asm volatile("" : "+v"(raw[v].x), "+v"(raw[v].y), "+v"(raw[v].z), "+v"(raw[v].w));  // (nothing of one pass is kept for the next)
+            unpack<DT>(raw[v], x);
 #pragma unroll
             for (int k = 0; k < EPV; ++k) f(x[k], v * EPV + k);
             __builtin_amdgcn_sched_barrier(0);  // (all vectors at once take more registers than they save time)
@@ -219,29 +238,147 @@ struct PartEntries {
 // smaller places.  `lowest` stands for everything that is further below than whole numbers of 32 bits reach.
 constexpr double kNear = 1.0e9;
 __device__ __forceinline__ float lowest_of(double unit) { return (float)(-1.5e9 / unit); }
-__device__ __forceinline__ int place_of(float z, double grid, float lowest) { return __double2loint(fma((double)fmaxf(z, lowest), grid, kRound)); }
+__device__ __forceinline__ int place_of(float z, double grid, float lowest) { return __double2loint(fma((double)max2(z, lowest), grid, kRound)); }
+// the smallest float whose place is at least p
+__device__ __forceinline__ float first_at(int p, double grid, float lowest)
+{
+    float z = (float)(((double)p - 0.5) / grid);
+#pragma unroll 1
+    while (place_of(z, grid, lowest) >= p) z = nextafterf(z, -kInf);
+#pragma unroll 1
+    while (place_of(z, grid, lowest) < p) z = nextafterf(z, kInf);
+    return z;
+}
 // in a bin's sum: the count in the upper 14 bits, weights times 2^36 below (8,192 of them, each below 1.03, are below 2^50; the
 // bin's middle is 1)
 constexpr int kWeightBits = 50;
 constexpr uint64_t kWeightMask = (1ull << kWeightBits) - 1;
+constexpr double kOne = 68719476736.0, kWhole = 4503599627370496.0;  // 2^36, 2^52
 
-// The weights of an uncut part are relative to 2^(R / 32), R being the whole number next to max * unit: z * unit - R then comes from
-// one rounding, and R from none.  Where R leaves 32 bits, or no float is far below the maximum (temperatures from 1e28 on), they
-// are relative to the maximum.
+// The weights of an uncut part are 2^(z unit / 32) as they are: 64 bits hold 900 powers of two either way, and no maximum has to be
+// known before.  Where the part's reaches further, or no float is far below it (temperatures from 1e28 on), they are relative to the
+// maximum.  (The grid reaches further; see kNear.)
+constexpr double kWide = 900.0 * 32;
+__device__ __forceinline__ bool is_wide(float top, double unit) { return !(fabs((double)top * unit) < kWide && unit > 1e-27); }
 __device__ __forceinline__ bool is_far(float top, double unit) { return !(fabs((double)top * unit) < kNear && unit > 1e-27); }
 
+// NaN if either is
+__device__ __forceinline__ float maximum(float a, float b)
+{
+    float r;
+    asm("v_maximum3_f32 %0, %1, %2, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
+// One pass over an uncut part: the sum of the weights (NaN where an entry is NaN or +inf), the largest and the smallest logit.
 template <typename DT>
-__global__ __launch_bounds__(kPartThreads, 4) void sample_parts_kernel(SampleArgs a, int64_t row0, int64_t rows)
+__device__ __forceinline__ double sum_of(PartEntries<DT> &z, double unit, const double *table, float &top, float &low)
+{
+    constexpr double a1 = 0.69314718055994530942 / 32, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
+    // (a5 r^5 is replaced by the cubic next to it on [-1/2, 1/2]: off by a5 / 512 at most, 2^-43)
+    constexpr double b3 = a3 + a5 * (5.0 / 16), b1 = a1 - a5 * (5.0 / 256);
+    const float lowest = fmaxf((float)(-32000.0 / unit), -3.402823466e38f);
+    double mass = 0.0;
+    float last_one = 0.0f;
+    top = -kInf, low = kInf;
+    z.each([&](float x, int k) {
+        if (k & 1) top = max3(top, last_one, x), low = min3(low, last_one, x);
+        last_one = x;
+        const double d = (double)maximum(x, lowest), n = fma(d, unit, kRound), q = fma(d, unit, -(n - kRound));
+        const int whole = __double2loint(n);
+        const double e = table[whole & 31];
+        const double p = fma(fma(fma(fma(q, a4, b3), q, a2), q, b1), q, 1.0);
+        mass = fma(__hiloint2double(__double2hiint(e) + (whole << 15), __double2loint(e)), p, mass);
+        if (k % 4 == 3) asm volatile("" : "+v"(mass));  // (here, not where it is used)
+    });
+    return mass;
+}
+
+// What a part has found, written in one store: memory takes half a line's writing in two turns, and the next kernel waits for it.
+union PartRecord {
+    SamplePart part;
+    uint32_t words[sizeof(SamplePart) / 4];
+};
+__device__ __forceinline__ void write_part(PartRecord &record, SamplePart &to, float top, int place, uint32_t bins, uint32_t count)
+{
+    if (threadIdx.x >= kWave) return;
+    if (threadIdx.x == 0) record.part.max = top, record.part.place = place, record.part.bins = bins, record.part.count = count;
+    if (threadIdx.x < sizeof(SamplePart) / 4) reinterpret_cast<uint32_t *>(&to)[threadIdx.x] = record.words[threadIdx.x];
+}
+
+// An uncut part: four waves that do not wait for one another until they have their sums.
+template <typename DT>
+__device__ __forceinline__ void sum_part(const SampleArgs &a, PartEntries<DT> &z, float tau, const double *table, PartRecord &record, float (&wave_top)[kPartWaves],
+                                         uint32_t (&wave_count)[kPartWaves], SamplePart &to)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const double unit = kUnit / (double)tau;
+    float top, low;
+    double mass = wave_sum(sum_of(z, unit, table, top, low));
+    top = wave_max(top), low = -wave_max(-low);
+    bool bad = mass != mass || top == kInf;
+    if (bad && top < kInf && is_wide(top, unit)) {  // (the sum says nothing)
+        bad = false;
+        z.each([&](float x, int) { bad |= x != x; });
+        bad = __any(bad);
+    }
+    uint32_t count = 0;
+    if (a.kept) {
+        if (low > -kInf) count = kWave * PartEntries<DT>::kEach;  // (the same for all of the wave)
+        else {
+            z.each([&](float x, int) { count += x > -kInf ? 1u : 0u; });
+            count = wave_sum(count);
+        }
+    }
+    if (lane == 0) wave_top[wave] = bad ? __builtin_nanf("") : top, wave_count[wave] = count;
+    __syncthreads();
+    bool any_bad = false;
+    top = -kInf, count = 0;
+#pragma unroll
+    for (int w = 0; w < kPartWaves; ++w) any_bad |= wave_top[w] != wave_top[w], top = fmaxf(top, wave_top[w]), count += wave_count[w];
+    if (!any_bad && top > -kInf && is_wide(top, unit)) {
+        const Weigh weigh{(double)top, unit, kTable};
+        mass = 0.0;
+        z.each([&](float x, int) {
+            mass += weigh(x);
+            asm volatile("" : "+v"(mass));
+        });
+        mass = wave_sum(mass);
+    }
+    if (lane == 0) record.part.mass[wave] = top > -kInf ? mass : 0.0;
+    __syncthreads();
+    write_part(record, to, any_bad ? __builtin_nanf("") : top, kSampleFar, 0, count);
+}
+
+// Rows that the host knows to be uncut.
+template <typename DT>
+__global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_sums_kernel(SampleArgs a, int64_t row0, int64_t rows)
+{
+    __shared__ double table[32];
+    __shared__ float wave_top[kPartWaves];
+    __shared__ uint32_t wave_count[kPartWaves];
+    __shared__ PartRecord record;
+    const int tid = threadIdx.x;
+    if (tid < 32) table[tid] = __hiloint2double(__double2hiint(kTable[tid]) - (tid << 15), __double2loint(kTable[tid]));
+    for (int64_t i = blockIdx.x; i < rows * a.parts; i += gridDim.x) {
+        const int64_t r = i / a.parts, t = row0 + r;
+        const int64_t begin = (i - r * a.parts) * kSamplePart;
+        PartEntries<DT> z;
+        z.load(reinterpret_cast<const char *>(a.z) + (t * a.ld + begin) * DT::kBytes, (int)min(a.V - begin, (int64_t)kSamplePart));
+        __syncthreads();  // (the table is there; the part before this one is done with the shared arrays)
+        sum_part(a, z, 1.0f, table, record, wave_top, wave_count, a.part[i]);
+    }
+}
+
+template <typename DT>
+__global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_parts_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
     using Entries = PartEntries<DT>;
     __shared__ double table[32];
     __shared__ uint64_t bins[kSampleBins];
     __shared__ float wave_top[kPartWaves];
     __shared__ uint32_t wave_count[kPartWaves], wave_last[kPartWaves];
-    __shared__ union {
-        SamplePart part;
-        uint32_t words[sizeof(SamplePart) / 4];
-    } record;
+    __shared__ PartRecord record;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     // (with the exponent's share of 15 bits taken out, so that adding n << 15 puts the whole exponent in)
     if (tid < 32) table[tid] = __hiloint2double(__double2hiint(kTable[tid]) - (tid << 15), __double2loint(kTable[tid]));
@@ -251,22 +388,25 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_parts_kernel(SampleArg
         Entries z;
         z.load(reinterpret_cast<const char *>(a.z) + (t * a.ld + begin) * DT::kBytes, (int)min(a.V - begin, (int64_t)kSamplePart));
         const Policy policy(a, t);
-        const bool cut = policy.cut();
+        if (!policy.cut() && !policy.bad()) {
+            __syncthreads();  // (the part before this one is done with the shared arrays)
+            sum_part(a, z, policy.tau, table, record, wave_top, wave_count, a.part[i]);
+            continue;
+        }
         const double unit = kUnit / (double)policy.tau;
-        float top = -kInf, last_one = 0.0f;
+        float top = -kInf, low = kInf, last_one = 0.0f;
         bool bad = false;
         z.each([&](float x, int k) {
-            top = fmaxf(top, x);
-            if (k & 1) bad |= __builtin_isunordered(x, last_one);  // (two at a time)
+            // (two at a time)
+            if (k & 1) top = max3(top, last_one, x), low = min3(low, last_one, x), bad |= __builtin_isunordered(x, last_one);
             last_one = x;
         });
-        top = wave_max(top);
+        top = wave_max(top), low = -wave_max(-low);
         if (__any(bad) || top == kInf) top = __builtin_nanf("");
         __syncthreads();  // (the part before this one is done with the shared arrays)
         if (lane == 0) wave_top[wave] = top;
-        if (cut)
 #pragma unroll
-            for (int b = tid; b < kSampleBins; b += kPartThreads) bins[b] = 0;
+        for (int b = tid; b < kSampleBins; b += kPartThreads) bins[b] = 0;
         __syncthreads();
         bad = false, top = -kInf;
 #pragma unroll
@@ -283,56 +423,28 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_parts_kernel(SampleArg
         uint32_t count = 0, bins_used = 0;
         int place = kSampleFar;
         const bool far = is_far(top, unit);
-        if (!cut) {
-            if (!far) {
-                constexpr double a1 = 0.69314718055994530942 / 32, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
-                // (a5 r^5 is replaced by the cubic next to it on [-1/2, 1/2]: off by a5 / 512 at most, 2^-43)
-                constexpr double b3 = a3 + a5 * (5.0 / 16), b1 = a1 - a5 * (5.0 / 256);
-                const double R = __double2loint((double)top * unit + kRound), K = kRound - R;
-                const float lowest = (float)(((R - 32000.0) / unit));
-                z.each([&](float x, int k) {
-                    const double d = (double)fmaxf(x, lowest), n = fma(d, unit, K), q = fma(d, unit, -(n - K));
-                    const int low = __double2loint(n);
-                    const double e = table[low & 31];
-                    const double p = fma(fma(fma(fma(q, a4, b3), q, a2), q, b1), q, 1.0);
-                    mass = fma(__hiloint2double(__double2hiint(e) + (low << 15), __double2loint(e)), p, mass);
-                    if (k % 4 == 3) asm volatile("" : "+v"(mass));  // (here, not where it is used)
-                });
-            } else {
-                const Weigh weigh{(double)top, unit, kTable};
-                z.each([&](float x, int) {
-                    mass += weigh(x);
-                    asm volatile("" : "+v"(mass));
-                });
-            }
-            if (a.kept) z.each([&](float x, int) { count += x > -kInf ? 1u : 0u; });
-        } else if (!far) {
+        if (!far) {
             constexpr double a1 = 0.69314718055994530942 / 16, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
-            constexpr double kOne = 68719476736.0, kWhole = 4503599627370496.0;  // 2^36, 2^52
             const double grid = unit * 0.5;
             const float lowest = lowest_of(unit);
             place = place_of(top, grid, lowest);
-            uint32_t furthest = 0;
-            z.each([&](float x, int k) {
-                const double d = (double)fmaxf(x, lowest), n = fma(d, grid, kRound), q = fma(d, grid, -(n - kRound));
-                const uint32_t bin = (uint32_t)(place - __double2loint(n));
+            const float behind = first_at(place - kSampleBins + 1, grid, lowest);  // the bins' smallest logit
+            z.each([&](float x, int) {
+                const double d = (double)x, n = fma(d, grid, kRound), q = fma(d, grid, -(n - kRound));
                 const double w = fma(fma(fma(fma(fma(q, a5 * kOne, a4 * kOne), q, a3 * kOne), q, a2 * kOne), q, a1 * kOne), q, kOne + kWhole);
-                furthest = max(furthest, bin);
-                if (bin < kSampleBins) {
+                if (x >= behind) {
                     const uint64_t add = (uint64_t)(((uint32_t)__double2hiint(w) & 0xFFFFFu) | 1u << (kWeightBits - 32)) << 32 | (uint32_t)__double2loint(w);
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&bins[bin]), (unsigned long long)add);
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&bins[place - __double2loint(n)]), (unsigned long long)add);
                 }
             });
-            // what lies behind the bins is below 2^-32 of the largest, all of it below 2^-19: what fp32 loses of that is below 2^-38
-            if (__any(furthest >= kSampleBins)) {
+            // what lies behind the bins is below 2^-32 of the largest, all of it below 2^-19: what fp32 loses of that, 2^-18 of it, is
+            // below 2^-37
+            if (low < behind) {
+                const float scale = (float)(grid * 0.0625), shift = (float)(fma((double)top, grid, -(double)place) * 0.0625);
                 float tail = 0.0f;
-                z.each([&](float x, int) {
-                    const double d = (double)fmaxf(x, lowest), n = fma(d, grid, kRound), q = fma(d, grid, -(n - kRound));
-                    const uint32_t bin = (uint32_t)(place - __double2loint(n));
-                    const bool behind = bin >= kSampleBins && x > -kInf;
-                    tail += behind ? exp2_hw(((float)q - (float)bin) * 0.0625f) : 0.0f;
-                    count += behind ? 1u : 0u;
-                    asm volatile("" : "+v"(tail), "+v"(count));
+                z.each([&](float x, int k) {
+                    tail += x < behind ? exp2_hw(fmaf(x - top, scale, shift)) : 0.0f;
+                    if (k % 4 == 3) asm volatile("" : "+v"(tail));
                 });
                 mass = (double)tail;
             }
@@ -340,13 +452,13 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_parts_kernel(SampleArg
 #pragma unroll
             for (int b = tid; b < kSampleBins; b += kPartThreads) {
                 const uint64_t sum = bins[b];
-                if (sum) bins_used = b + 1, count += (uint32_t)(sum >> kWeightBits);
+                if (sum) bins_used = b + 1;
                 const double middle = table[-2 * b & 31];  // 2^(-b / 16)
                 mass = fma((double)(sum & kWeightMask) * (1.0 / kOne), __hiloint2double(__double2hiint(middle) - (b << 16), __double2loint(middle)), mass);
             }
-        } else {
-            z.each([&](float x, int) { count += x > -kInf ? 1u : 0u; });
         }
+        if (low > -kInf) count = Entries::kEach;  // (the same for all of the wave)
+        else z.each([&](float x, int) { count += x > -kInf ? 1u : 0u; });
         mass = wave_sum(mass);
         count = wave_sum(count);
         bins_used = (uint32_t)wave_max((float)bins_used);
@@ -355,22 +467,15 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_parts_kernel(SampleArg
         count = bins_used = 0;
 #pragma unroll
         for (int w = 0; w < kPartWaves; ++w) count += wave_count[w], bins_used = max(bins_used, wave_last[w]);
-        if (cut)
-            // (through to memory at once: what lies in the L2s when the kernel ends, the next one waits for, 14 us for 20 MB)
-            for (int b = tid; b < (int)bins_used; b += kPartThreads)
-                __hip_atomic_store(a.bins + i * kSampleBins + b, bins[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (wave == 0) {
-            if (tid == 0) record.part.max = top, record.part.place = place, record.part.bins = bins_used, record.part.count = count;
-            // (in one store: memory takes half a line's writing in two turns, and the next kernel waits for it)
-            if (lane < (int)(sizeof(SamplePart) / 4)) reinterpret_cast<uint32_t *>(a.part + i)[lane] = record.words[lane];
-        }
+        for (int b = tid; b < (int)bins_used; b += kPartThreads) a.bins[i * kSampleBins + b] = bins[b];
+        write_part(record, a.part[i], top, place, bins_used, count);
     }
 }
 
 // ---- gather ------------------------------------------------------------------------------------------------------------
 
 template <typename DT>
-__global__ __launch_bounds__(kPartThreads, 4) void sample_gather_kernel(SampleArgs a, int64_t row0, int64_t rows)
+__global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_gather_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
     using Entries = PartEntries<DT>;
     constexpr int EPV = Entries::EPV, kVectors = Entries::kVectors;
@@ -416,18 +521,12 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_gather_kernel(SampleAr
             out.listed = n;
             if (n > 0) {
                 if (tid == 0) start = atomicAdd(&row.cursor, n);  // (while the entries are on their way)
-                Policy policy(a, t);
-                const double unit = kUnit / (double)policy.tau, grid = unit * 0.5;
-                const float lowest_logit = lowest_of(unit);
                 const int64_t begin = (i - r * a.parts) * kSamplePart;
                 Entries z;
                 z.load(reinterpret_cast<const char *>(a.z) + (t * a.ld + begin) * DT::kBytes, (int)min(a.V - begin, (int64_t)kSamplePart));
-                const int lowest = all ? -0x7FFFFFFF : row.place - row.bin, highest = few ? 0x7FFFFFFF : lowest;
+                const float from = row.from, to = row.to;
                 uint32_t taken = 0;  // a bit an entry
-                z.each([&](float x, int k) {
-                    const int p = place_of(x, grid, lowest_logit);
-                    taken |= (x > -kInf && p >= lowest && p <= highest ? 1u : 0u) << k;
-                });
+                z.each([&](float x, int k) { taken |= (x >= from && x <= to ? 1u : 0u) << k; });
                 // how many of each 64 vectors are before a lane's, 16 bits each
                 uint32_t pos[(kVectors + 1) / 2], sum[(kVectors + 1) / 2], in_wave = 0;
 #pragma unroll
@@ -450,15 +549,15 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_gather_kernel(SampleAr
                 uint2 *list = a.list + r * kSampleListed;
 #pragma unroll
                 for (int v = 0; v < kVectors; ++v) {
-                    uint32_t to = base + (pos[v / 2] >> (16 * (v & 1)) & 0xFFFFu);
+                    uint32_t at = base + (pos[v / 2] >> (16 * (v & 1)) & 0xFFFFu);
                     float x[EPV];
                     unpack<DT>(z.raw[v], x);
 #pragma unroll
                     for (int k = 0; k < EPV; ++k)
                         if (taken >> (v * EPV + k) & 1u) {
-                            if (to < kSampleListed)
-                                list[to] = make_uint2(__float_as_uint(x[k]), (uint32_t)(begin + Entries::first() + v * kWave * EPV + k));
-                            ++to;
+                            if (at < kSampleListed)
+                                list[at] = make_uint2(__float_as_uint(x[k]), (uint32_t)(begin + Entries::first() + v * kWave * EPV + k));
+                            ++at;
                         }
                     base += sum[v / 2] >> (16 * (v & 1)) & 0xFFFFu;
                 }
@@ -993,9 +1092,8 @@ __device__ __forceinline__ void draw_uncut(const SampleArgs &a, Scans &sh, const
     const Weigh weigh{(double)top, unit, sh.table};
     // what the part's weights are relative to, in units of 2^-shift of the row's largest, and of its own
     const double scale = ldexp(1.0, a.shift);
-    const bool some = mine.max > -kInf, far = is_far(mine.max, unit);
-    const double R = some && !far ? (double)__double2loint((double)mine.max * unit + kRound) : 0.0;
-    const double factor = !some ? 0.0 : far ? weigh(mine.max) : scale * exp2(fma(-(double)top, unit, R) * 0.03125);
+    const bool some = mine.max > -kInf, wide = is_wide(mine.max, unit);
+    const double factor = !some ? 0.0 : wide ? weigh(mine.max) : scale * exp2((double)top * unit * -0.03125);
     const double own = (mine.mass[0] + mine.mass[1] + mine.mass[2] + mine.mass[3]) * factor;
     double upto = own, full, none = 0.0;
     uint32_t finite = mine.count, kept, more = 0;
@@ -1010,7 +1108,7 @@ __device__ __forceinline__ void draw_uncut(const SampleArgs &a, Scans &sh, const
         if (last > 0 && !(m0 > within)) within -= m0, quarter = 1;
         if (quarter == 1 && last > 1 && !(m1 > within)) within -= m1, quarter = 2;
         if (quarter == 2 && last > 2 && !(m2 > within)) within -= m2, quarter = 3;
-        sh.told[0] = within * (far ? 1.0 : exp2(fma(-(double)mine.max, unit, R) * 0.03125)) * scale;
+        sh.told[0] = within * (wide ? 1.0 : exp2((double)mine.max * unit * -0.03125)) * scale;
         sh.told_top = mine.max;
         sh.found_digit = chosen * kPartWaves + quarter;
     }
@@ -1054,13 +1152,13 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
         SamplePart mine;
         bool far;
         __syncthreads();  // (the row before this one is done with everything)
-        const float top = top_of<kThreads>(a, sh, a.part + r * a.parts, mine, far);
         const Policy policy(a, t);
+        const float top = top_of<kThreads>(a, sh, a.part + r * a.parts, mine, far);
         const bool each_part = a.parts <= kThreads;
         const double unit = kUnit / (double)policy.tau;
         SampleRow out;
         out.full = out.above = out.share = 0.0, out.rank = 0, out.top = top;
-        out.mode = kSamplePasses, out.by_k = out.place = out.bin = 0, out.count = 0;
+        out.mode = kSamplePasses, out.by_k = out.place = out.bin = 0, out.count = 0, out.from = out.to = 0.0f;
         if (policy.bad() || !(top > -kInf)) {
             tell_none<kThreads>(a, t, policy.bad() || top != top);
             out.mode = kSampleDone;
@@ -1135,6 +1233,10 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
             out.by_k = by_k;
             if (down_to <= kSampleFewest) out.mode = kSampleFew;
             else if (!lost && bin != kSampleAll && in_bin <= kSampleListed && !(by_k && policy.by_p())) out.mode = kSampleBin;
+            if (out.mode != kSamplePasses) {
+                out.from = bin == kSampleAll ? -3.402823466e38f : first_at(out.place - bin, grid, lowest);
+                out.to = out.mode == kSampleFew ? kInf : nextafterf(first_at(out.place - bin + 1, grid, lowest), -kInf);
+            }
         }
         // (field by field: a whole struct's copy takes its padding along, through a private array that ends up in LDS by a thread
         // number from the dispatch packet in host memory, 4 to 14 us at the kernel's beginning)
@@ -1142,6 +1244,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
             SampleRow &to = a.row[r];
             to.full = out.full, to.above = out.above, to.share = out.share, to.rank = out.rank, to.top = out.top;
             to.mode = out.mode, to.by_k = out.by_k, to.place = out.place, to.bin = out.bin, to.count = out.count, to.cursor = 0;
+            to.from = out.from, to.to = out.to;
         }
     }
 }
@@ -1272,11 +1375,12 @@ template <typename DT>
 __global__ __launch_bounds__(kThreads, 4) void sample_passes_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
     __shared__ Shared sh;
-    if (threadIdx.x < 32) sh.table[threadIdx.x] = ldexp(kTable[threadIdx.x], a.shift);
 #pragma unroll 1
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const int64_t t = row0 + r;
         if (a.row[r].mode != kSamplePasses) continue;
+        __syncthreads();
+        if (threadIdx.x < 32) sh.table[threadIdx.x] = ldexp(kTable[threadIdx.x], a.shift);
         __syncthreads();  // (the table is there; the row before this one is done with everything)
         const float top = a.row[r].top;
         Policy policy(a, t);
@@ -1297,10 +1401,12 @@ __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a
     if (tid < 32) sh.table[tid] = ldexp(kTable[tid], a.shift);
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const int64_t t = row0 + r;
-        const SampleRow row = a.row[r];
+        // (asked for before it is known whether they are needed, or there)
+        const SampleRow &row = a.row[r];
+        const SampleSegment segment_read = a.segment[r * a.parts + min(tid, a.parts - 1)];
+        Policy policy(a, t);
         if (row.mode != kSampleFew && row.mode != kSampleBin) continue;
         __syncthreads();  // (the table is there; the row before this one is done with everything)
-        Policy policy(a, t);
         policy.u = number_of(policy);
         const float top = row.top;
         const double unit = kUnit / (double)policy.tau;
@@ -1312,8 +1418,8 @@ __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a
         const double full = row.full * to_whole;
         const bool few = row.mode == kSampleFew;
         // ---- the gathered entries, from the order in which the parts found room to the parts' own
-        SampleSegment segment = {};
-        if (tid < a.parts) segment = a.segment[r * a.parts + tid];
+        SampleSegment segment = segment_read;
+        if (tid >= a.parts) segment.above = 0.0, segment.start = segment.listed = 0;
         uint32_t place = segment.listed, n;  // where this thread's part's begin; entries
         block_scan<kThreads, 0>(sh, place, n);
         place -= segment.listed;
@@ -1477,12 +1583,13 @@ void launch(const SampleArgs &a, hipStream_t s)
     for (int64_t row0 = 0; row0 < a.T; row0 += kSampleRows) {
         const int64_t rows = a.T - row0 < kSampleRows ? a.T - row0 : kSampleRows, parts = rows * a.parts;
         const int grid = (int)(parts < (1 << 24) ? parts : 1 << 24);
-        sample_parts_kernel<DT><<<grid, kPartThreads, 0, s>>>(a, row0, rows);
         // (temperatures of 0 cut, and so may what the other arrays hold)
         if (!a.temperature && !a.top_k && !a.top_p && !a.min_p && !a.allowed && a.parts <= kPartThreads) {
+            sample_sums_kernel<DT><<<grid, kPartThreads, 0, s>>>(a, row0, rows);
             sample_uncut_kernel<DT><<<(int)rows, kPartThreads, 0, s>>>(a, row0, rows);
             continue;
         }
+        sample_parts_kernel<DT><<<grid, kPartThreads, 0, s>>>(a, row0, rows);
         sample_rows_kernel<DT><<<(int)rows, kThreads, 0, s>>>(a, row0, rows);
         sample_gather_kernel<DT><<<grid, kPartThreads, 0, s>>>(a, row0, rows);
         sample_finish_kernel<DT><<<(int)rows, kThreads, 0, s>>>(a, row0, rows);
