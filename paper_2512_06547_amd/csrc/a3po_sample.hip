@@ -371,7 +371,7 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_
 }
 
 template <typename DT>
-__global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_parts_kernel(SampleArgs a, int64_t row0, int64_t rows)
+__global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_parts_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
     using Entries = PartEntries<DT>;
     __shared__ double table[32];
