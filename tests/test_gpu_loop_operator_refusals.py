@@ -27,8 +27,8 @@ def test_sample(a3po, change, message):  # noqa: F811
 
 
 @pytest.mark.parametrize("change,message", [
-    (dict(grads=lambda: [zeros(5), zeros(5).bfloat16()]), "grads: need"), (dict(grads=lambda: [zeros(5).half()]), "grads must be"),
-    (dict(grads=lambda: [zeros(5).cpu()]), "current device"), (dict(grads=lambda: [zeros(10)[::2]]), "grads: need"), (dict(out=lambda: zeros(2)), "out: need")])
+    (dict(grads=lambda: [zeros(5), zeros(5).bfloat16()]), "grads.1.: need"), (dict(grads=lambda: [zeros(5).half()]), "grads must be"),
+    (dict(grads=lambda: [zeros(5).cpu()]), "current device"), (dict(grads=lambda: [zeros(10)[::2]]), "grads.0.: need"), (dict(out=lambda: zeros(2)), "out: need")])
 def test_grad_norm(a3po, change, message):  # noqa: F811
     args = dict(grads=[zeros(5), zeros(3)], out=zeros(1))
     a3po.grad_norm(**args)
@@ -41,12 +41,12 @@ E4, E5 = torch.float8_e4m3fn, torch.float8_e5m2
 
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("change,message", [
-    (dict(params=lambda: [zeros(n).half()]), "params must be"), (dict(params=lambda: [zeros(2 * n)[::2]]), "params: need"), (dict(grads=lambda: [zeros(n + 1)]), "grads.0.: need"),
-    (dict(grads=lambda: []), "need a gradient"), (dict(exp_avgs=lambda: [zeros(n - 1)]), "exp_avgs: need"), (dict(exp_avgs=lambda: [zeros(n).double()]), "exp_avgs: need"),
-    (dict(exp_avg_sqs=lambda: [zeros(n).cpu()]), "exp_avg_sqs: need"), (dict(exp_avg_sqs=lambda: []), "need a gradient"), (dict(copies=lambda: [zeros(n)]), "copies: need"),
+    (dict(params=lambda: [zeros(n).half()]), "params must be"), (dict(params=lambda: [zeros(2 * n)[::2]]), "params.0.: need"), (dict(grads=lambda: [zeros(n + 1)]), "grads.0.: need"),
+    (dict(grads=lambda: []), "need a gradient"), (dict(exp_avgs=lambda: [zeros(n - 1)]), "exp_avgs.0.: need"), (dict(exp_avgs=lambda: [zeros(n).double()]), "exp_avgs.0.: need"),
+    (dict(exp_avg_sqs=lambda: [zeros(n).cpu()]), "current device"), (dict(exp_avg_sqs=lambda: []), "need a gradient"), (dict(copies=lambda: [zeros(n)]), "copies.0.: need"),
     (dict(copies=lambda: []), "need a copy"), (dict(norm=lambda: zeros(2)), "norm: need"), (dict(step=lambda: zeros(1)), "step: need"),
-    (dict(lr=lambda: zeros(1).double()), "lr: need"), (dict(scales=lambda: []), "need a pair|exp_avgs: need"),
-    (dict(scales=lambda: [(zeros(2, **U8), zeros(3, **U8))]), "scales: need|exp_avgs: need"), (dict(scales=lambda: [(zeros(3, **U8), zeros(3))]), "scales: need|exp_avgs: need")])
+    (dict(lr=lambda: zeros(1).double()), "lr: need"), (dict(scales=lambda: []), "need a pair|exp_avgs.0.: need"),
+    (dict(scales=lambda: [(zeros(2, **U8), zeros(3, **U8))]), "scales.0.: need|exp_avgs.0.: need"), (dict(scales=lambda: [(zeros(3, **U8), zeros(3))]), "scales.0.: need|exp_avgs.0.: need")])
 def test_adamw_step(a3po, change, message, bits):  # noqa: F811
     p = zeros(n)
     m, v, scales = a3po.adamw_state(p, bits)
