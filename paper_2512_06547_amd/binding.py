@@ -7,7 +7,6 @@ fallback: if the shared library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
-import operator
 import os
 
 import numpy as np
@@ -772,47 +771,65 @@ def sample(logits, uniform, V=None, *, temperature=None, top_k=None, top_p=None,
     return dict(token=token, logp=logp, logp_full=full, kept=kept, allowed=allowed, workspace=workspace)
 
 
-_get_dtype = operator.attrgetter("dtype")
+_tensor_list_fn = None
 
 
-def _pointers(tensors, dtype, sizes, name):
-    """Addresses of tensors that are all contiguous, of one dtype, of these sizes (None: any) and on the current device.  Whole lists
-    are asked for one property after the other without a line of Python for each tensor: 0.2 us a tensor where checking them one by
-    one takes 0.5."""
-    of = _torch().Tensor
-    if tensors and not (set(map(_get_dtype, tensors)) == {dtype} and set(map(of.get_device, tensors)) == {_torch()._C._cuda_getDevice()}
-                        and all(map(of.is_contiguous, tensors)) and (sizes is None or list(map(of.numel, tensors)) == sizes)):
-        _here(*tensors)
-        for i, t in enumerate(tensors):
-            n = t.numel() if sizes is None else sizes[i]
-            assert t.dtype == dtype and t.is_contiguous() and t.numel() == n, f"{name}[{i}]: need contiguous {dtype}[{n}] on GPU"
-    return list(map(of.data_ptr, tensors))
+def _tensor_list():
+    """a3po_tensor_list (csrc/a3po_tensors.cpp): it holds the interpreter's lock and reads Python's objects."""
+    global _tensor_list_fn
+    if _tensor_list_fn is None:
+        _torch()
+        path = os.path.join(_PKG, "a3po_tensors.so")
+        if not os.path.exists(path):
+            raise FileNotFoundError(f"{path} is missing: build it with `python -m paper_2512_06547_amd.build`")
+        fn = ctypes.PyDLL(path).a3po_tensor_list
+        fn.restype, fn.argtypes = _I64, [ctypes.py_object, _I64, _P, _P, _P]
+        _tensor_list_fn = fn
+    return _tensor_list_fn
 
 
-def _tensors(tensors, name):
-    """(list, dtype, dtype code, sizes, addresses) of tensors that share a dtype."""
-    tensors = list(tensors)
-    if not tensors:
-        return tensors, None, A3PO_F32, [], []
-    first = tensors[0]
-    _here(first)
-    code = _dtype_code(first, name)
-    return tensors, first.dtype, code, list(map(type(first).numel, tensors)), _pointers(tensors, first.dtype, None, name)
+def _device_of(t) -> int:
+    _here(t)
+    return t.get_device()
+
+
+def _pointers(tensors, dtype, count, want, address, size, name, device):
+    """Writes addresses (and sizes) of a list's tensors to int64 arrays, which are given by their own addresses: tensors that are all
+    contiguous, of one dtype and the sizes ``want`` (0: any), on the GPU ``device``."""
+    assert len(tensors) == count, f"{name}: need one for each parameter"
+    right = _tensor_list()(tensors, device, want, address, size)
+    if right == count and (not count or tensors[0].dtype == dtype):
+        return
+    right %= count
+    t = tensors[0] if tensors[0].dtype != dtype else tensors[right]
+    if isinstance(t, _torch().Tensor):
+        _here(t)
+    n = ctypes.c_int64.from_address(want + 8 * right).value if want else "n"
+    raise AssertionError(f"{name}[{right}]: need contiguous {dtype}[{n}] on GPU")
 
 
 def grad_norm(grads, scale: float = 1.0, out=None, workspace=None):
     """a3po_grad_norm -> norm float32 [1] (``out``, or a new tensor): the 2-norm of all gradients times ``scale`` together."""
     torch = _torch()
-    grads, _, dt, sizes, at = _tensors(grads, "grads")
+    grads = list(grads)
     count = len(grads)
+    columns = (ctypes.c_int64 * (2 * count))()  # addresses, sizes
+    at = ctypes.addressof(columns)
+    dt = A3PO_F32
+    if count:
+        dt, device = _dtype_code(grads[0], "grads"), _device_of(grads[0])
+        _pointers(grads, grads[0].dtype, count, 0, at, at + 8 * count, "grads", device)
     if out is None:
-        out = torch.empty(1, dtype=torch.float32, device=grads[0].device if grads else "cuda")
-    _vec(out, torch.float32, 1, "out")
-    _here(out, workspace)
-    if workspace is None and count:
-        workspace = torch.empty(workspace_bytes(count, which=A3PO_WS_GRAD_NORM), dtype=torch.uint8, device=out.device)
-    table = np.array((at, sizes), dtype=np.int64)
-    _check(lib().a3po_grad_norm(table.ctypes.data, table.ctypes.data + 8 * count, count, dt, float(scale), _ptr(out), _ptr(workspace),
+        out = torch.empty(1, dtype=torch.float32, device=grads[0].device if count else "cuda")
+    else:
+        _vec(out, torch.float32, 1, "out")
+        _here(out)
+    if workspace is None:
+        if count:
+            workspace = torch.empty(workspace_bytes(count, which=A3PO_WS_GRAD_NORM), dtype=torch.uint8, device=out.device)
+    else:
+        _here(workspace)
+    _check(lib().a3po_grad_norm(at, at + 8 * count, count, dt, float(scale), _ptr(out), _ptr(workspace),
                                 0 if workspace is None else workspace.numel(), _stream()), "a3po_grad_norm")
     return out
 
@@ -846,27 +863,28 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, *, step, lr, beta1: float =
     them change.  ``norm``: what grad_norm left; gradients are scaled to ``max_norm`` at most, and a step whose norm is not
     finite changes nothing.  ``seed``: of the roundings by chance (bfloat16 parameters, 8-bit exp_avg_sq), another each step."""
     torch = _torch()
-    params, _, pd, sizes, at = _tensors(params, "params")
-    grads, grad_dtype, gd, _, _ = _tensors(grads, "grads")
-    exp_avgs, exp_avg_sqs, count = list(exp_avgs), list(exp_avg_sqs), len(params)
-    assert len(grads) == len(exp_avgs) == len(exp_avg_sqs) == count, "need a gradient and two states for each parameter"
+    params, grads = list(params), list(grads)
+    count = len(params)
+    columns = np.zeros((8, count), dtype=np.int64)  # of the fields of a3po_adamw_tensor
+    at = columns.ctypes.data
+    pd = gd = device = 0
+    if count and grads:
+        pd, gd, device = _dtype_code(params[0], "params"), _dtype_code(grads[0], "grads"), _device_of(params[0])
+    field = lambda i: at + 8 * count * i
+    sizes = field(7)
+    put = lambda i, tensors, dtype, name, want=sizes: _pointers(tensors, dtype, count, want, field(i), 0, name, device)
+    _pointers(params, params[0].dtype if count else None, count, 0, at, sizes, "params", device)
+    put(1, grads, grads[0].dtype if grads else None, "grads")
     bytes_ = scales is not None
-    first, second = (torch.float8_e4m3fn, torch.float8_e5m2) if bytes_ else (torch.float32, torch.float32)
-    table = np.zeros((count, 8), dtype=np.int64)  # a3po_adamw_tensor
-    table[:, 0], table[:, 7] = at, sizes
-    table[:, 1] = _pointers(grads, grad_dtype, sizes, "grads")
-    table[:, 2] = _pointers(exp_avgs, first, sizes, "exp_avgs")
-    table[:, 3] = _pointers(exp_avg_sqs, second, sizes, "exp_avg_sqs")
+    put(2, list(exp_avgs), torch.float8_e4m3fn if bytes_ else torch.float32, "exp_avgs")
+    put(3, list(exp_avg_sqs), torch.float8_e5m2 if bytes_ else torch.float32, "exp_avg_sqs")
     if bytes_:
-        scales = list(scales)
-        assert len(scales) == count, "need a pair of scales for each parameter"
-        blocks = [(n + 31) // 32 for n in sizes]
-        table[:, 4] = _pointers([s[0] for s in scales], torch.uint8, blocks, "scales")
-        table[:, 5] = _pointers([s[1] for s in scales], torch.uint8, blocks, "scales")
+        scales, blocks = list(scales), (columns[7] + 31) // 32
+        for i in (0, 1):
+            put(4 + i, [s[i] for s in scales], torch.uint8, "scales", blocks.ctypes.data)
     if copies is not None:
-        copies = list(copies)
-        assert len(copies) == count, "need a copy for each parameter"
-        table[:, 6] = _pointers(copies, torch.bfloat16, sizes, "copies")
+        put(6, list(copies), torch.bfloat16, "copies")
+    table = np.ascontiguousarray(columns.T)
     opt = AdamwOptions(beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay, max_norm=max_norm, seed=int(seed) & 0xFFFFFFFF)
     if isinstance(step, torch.Tensor):
         opt.step_dev = _ptr(_vec(step, torch.int64, 1, "step"))

@@ -1,4 +1,4 @@
-"""Builds liba3po.so (HIP, gfx950 only) in-tree with hipcc."""
+"""Builds liba3po.so (HIP, gfx950 only) in-tree with hipcc, and the binding's look at lists of tensors with the host compiler."""
 from __future__ import annotations
 
 import os
@@ -10,6 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liba3po.so")
+TENSORS = os.path.join(PKG, "a3po_tensors.so")  # against PyTorch's headers; loaded by the binding alone
 SOURCES = ["a3po_api.hip", "a3po_rows.hip", "a3po_few.hip", "a3po_tokens.hip", "a3po_shard.hip", "a3po_gemm.hip", "a3po_lmhead.hip",
            "a3po_lmhead_bwd.hip", "a3po_norm.hip", "a3po_adjust.hip", "a3po_w4.hip", "a3po_sample.hip", "a3po_adamw.hip", "a3po_w4_quantize.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -27,7 +28,7 @@ def sources():
 
 
 def _newest_input() -> float:
-    paths = sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
+    paths = sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cpp"))]
     paths.append(os.path.join(ROOT, "include", "a3po.h"))
     return max(os.path.getmtime(p) for p in paths)
 
@@ -38,13 +39,27 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _compile_tensors() -> None:
+    import sysconfig
+
+    import torch
+    at = os.path.dirname(torch.__file__)
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+                           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-I", os.path.join(at, "include"),
+                           "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+                           "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "a3po_tensors.cpp"), "-o", TENSORS,
+                           "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
+
+
 def build(force: bool = True, verbose: bool = False) -> str:
     """Compile every kernel file and link liba3po.so.  force=False skips an up-to-date library."""
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_input():
+    if not force and all(os.path.exists(so) and os.path.getmtime(so) >= _newest_input() for so in (LIB, TENSORS)):
         return LIB
     os.makedirs(OBJ, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        tensors = ex.submit(_compile_tensors)
         objs = list(ex.map(_compile, sources()))
+        tensors.result()
     subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
     if verbose:
         print("built", LIB)
