@@ -6,11 +6,16 @@ The policy is an embedding, a norm and a vocabulary head: enough to need every o
 small enough that nothing else is in the way.  A step draws a group of answers to each prompt as a serving process does,
 from a copy of the weights that is some steps old and has its head in 4 bits:
 
-    norm_fwd -> w4_linear -> adjust_logits (penalties, temperature, grammar mask; log-probs of the drawn tokens)
+    norm_fwd -> w4_linear -> adjust_logits (penalties, temperature, grammar mask) -> sample (tokens and their log-probs)
 
-and trains on them, the policy being the adjusted one that the tokens were drawn from:
+trains on them, the policy being the adjusted one that the tokens were drawn from:
 
     norm_fwd -> head -> adjust_logits -> loss_fwd_bwd -> adjust_logits_bwd -> head's gradients -> norm_bwd
+
+and takes a step of AdamW on fp32 weights, whose bfloat16 copies are the model's, and of which w4_quantize makes the next head in
+4 bits:
+
+    grad_norm -> adamw_step -> w4_quantize
 
 The reward is the share of even tokens in an answer, so a rising mean reward says that the whole chain points the right way.
 """
@@ -61,13 +66,7 @@ def new_policy(V, H, dtype, device, seed=0):
 def quantize_w4(weight, group):
     """codes uint8 [N, H/2], scales float32 and zero points uint8 [N, H/group] for w4_linear: the nearest of 16 evenly spaced
     values between each group's extremes, zero among them."""
-    N, H = weight.shape
-    w = weight.float().view(N, H // group, group)
-    low, high = w.amin(2).clamp(max=0), w.amax(2).clamp(min=0)
-    scales = ((high - low) / 15).clamp(min=1e-12)
-    zeros = torch.round(-low / scales).clamp(0, 15)
-    q = (torch.round(w / scales[..., None]) + zeros[..., None]).clamp(0, 15).to(torch.uint8).view(N, H // 2, 2)
-    return (q[..., 0] | q[..., 1] << 4).contiguous(), scales.contiguous(), zeros.to(torch.uint8).contiguous()
+    return a3po.w4_quantize(weight, group, zeros=True)
 
 
 def rollout(policy, sampling, prompts, new_tokens, group=128, generator=None):
@@ -88,9 +87,8 @@ def rollout(policy, sampling, prompts, new_tokens, group=128, generator=None):
         logits = a3po.w4_linear(hidden, codes, scales, zeros, group=group, out_dtype=torch.float32)
         rows = sampling.rows(history.view(-1), start, length, prompt)
         u = a3po.adjust_logits(logits, out=logits, want_lse=False, **rows)["out"]
-        noise = torch.empty_like(u).exponential_(generator=generator).clamp_(min=1e-30).log_()  # (the largest u - noise is a sample)
-        token = (u - noise).argmax(1).int()
-        logp[:, i] = a3po.token_logprobs(u, token, want_lse=False, want_chosen_logit=False)[0]
+        drawn = a3po.sample(u, torch.rand(S, generator=generator, device=dev))  # (u is adjusted: no temperature is left to apply)
+        token, logp[:, i] = drawn["token"], drawn["logp"]
         history[:, P + i] = token
     return history, logp
 
@@ -119,6 +117,27 @@ def gradients(policy, sampling, history, logp_behav, versions, rewards, P, G, cl
                 dhead=dz.t() @ normed)
 
 
+class Trainer:
+    """The fp32 weights behind a policy, and AdamW's states for them."""
+
+    def __init__(self, policy, lr, bits=32, max_norm=1.0, weight_decay=0.0):
+        self.names, self.lr, self.max_norm, self.weight_decay, self.steps = ("embed", "gamma", "head"), lr, max_norm, weight_decay, 0
+        self.master = [getattr(policy, k).float() for k in self.names]
+        states = [a3po.adamw_state(p, bits) for p in self.master]
+        self.exp_avgs, self.exp_avg_sqs = [s[0] for s in states], [s[1] for s in states]
+        self.scales = None if bits == 32 else [s[2] for s in states]
+
+    def step(self, policy, got):
+        """One update from what gradients() gave; policy's weights become bfloat16 copies of the new ones."""
+        embed = torch.zeros_like(self.master[0]).index_add_(0, got["source"], got["dhidden"].float())
+        grads = [embed, got["dgamma"], got["dhead"].float()]
+        self.steps += 1
+        a3po.adamw_step(self.master, grads, self.exp_avgs, self.exp_avg_sqs, scales=self.scales, copies=[getattr(policy, k) for k in self.names],
+                        step=self.steps, lr=self.lr, weight_decay=self.weight_decay, norm=a3po.grad_norm(grads), max_norm=self.max_norm,
+                        seed=self.steps)
+        policy.version += 1
+
+
 def even_share(history, P):
     return (history[:, P:] % 2 == 0).float().mean(1)
 
@@ -132,11 +151,12 @@ def main(argv=None):
     ap.add_argument("--group", type=int, default=8, help="answers a prompt")
     ap.add_argument("--new-tokens", type=int, default=32)
     ap.add_argument("--lag", type=int, default=2, help="steps that the sampling weights are behind by, at most")
-    ap.add_argument("--lr", type=float, default=2.0)
+    ap.add_argument("--lr", type=float, default=0.02)
+    ap.add_argument("--state-bits", type=int, default=32, choices=(32, 8), help="of AdamW's states")
     args = ap.parse_args(argv)
     dev, P = "cuda", 8
     policy = new_policy(args.vocab, args.hidden, torch.bfloat16, dev)
-    master = {k: getattr(policy, k).float() for k in ("embed", "gamma", "head")}
+    trainer = Trainer(policy, args.lr, args.state_bits)
     sampling = Sampling()
     g, gpu = torch.Generator().manual_seed(1), torch.Generator(device=dev).manual_seed(1)
     behaviour, shares = policy, []
@@ -149,12 +169,7 @@ def main(argv=None):
         rewards = even_share(history, P)
         versions = torch.full((logp.numel(),), behaviour.version, dtype=torch.int32, device=dev)
         got = gradients(policy, sampling, history, logp, versions, rewards, P, args.group)
-        master["embed"].index_add_(0, got["source"], got["dhidden"].float(), alpha=-args.lr)
-        master["head"] -= args.lr * got["dhead"].float()
-        master["gamma"] -= args.lr * got["dgamma"]
-        for k, v in master.items():
-            setattr(policy, k, v.to(torch.bfloat16))
-        policy.version += 1
+        trainer.step(policy, got)
         shares.append(float(rewards.mean()))
         print(f"step {step}: version {behaviour.version} of {policy.version - 1}, even tokens {shares[-1]:.3f}, "
               f"loss {float(got['loss']):+.4f}, clipped {a3po.stats_to_dict(got['stats'])['n_clipped']}", flush=True)
