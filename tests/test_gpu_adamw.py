@@ -324,3 +324,32 @@ def test_no_tensors(a3po):
     m, v, s = a3po.adamw_state(p)
     a3po.adamw_step([p], [p], [m], [v], step=1, lr=0.1)
     assert float(a3po.grad_norm([])) == 0.0
+
+
+def test_more_elements_than_32_bits_count(a3po):
+    """A tensor of 2^31 + 1,000 elements: its last ones are updated as they are alone."""
+    n, last = 2 ** 31 + 1000, 5000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    p = torch.randn(n, generator=g, device="cuda")
+    grad = torch.randn(n, generator=g, device="cuda", dtype=torch.bfloat16)
+    m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    tail = [t[-last:].clone() for t in (p, grad, m, v)]
+    a3po.adamw_step([p], [grad], [m], [v], step=2, **HYPER)
+    a3po.adamw_step([tail[0]], [tail[1]], [tail[2]], [tail[3]], step=2, **HYPER)
+    assert torch.equal(p[-last:], tail[0]) and torch.equal(m[-last:], tail[2]) and torch.equal(v[-last:], tail[3])
+    total = float(grad[:n // 2].double().square().sum() + grad[n // 2:].double().square().sum())
+    assert abs(float(a3po.grad_norm([grad])) - math.sqrt(total)) <= (U + 2.0 ** -40) * math.sqrt(total)
+
+
+def test_parameters_and_shapes_of_modules(a3po):
+    """Tensors of any shape, parameters that want gradients among them, states in their shape."""
+    p = torch.nn.Parameter(torch.randn(7, 5, 3, device="cuda"))
+    grad = torch.randn(7, 5, 3, device="cuda")
+    flat = p.detach().clone().view(-1)
+    for bits in (32, 8):
+        m, v, s = a3po.adamw_state(p, bits)
+        assert m.shape == v.shape == p.shape
+        fm, fv, fs = a3po.adamw_state(flat, bits)
+        a3po.adamw_step([p], [grad], [m], [v], scales=None if s is None else [s], step=1, **HYPER)
+        a3po.adamw_step([flat], [grad.view(-1)], [fm], [fv], scales=None if fs is None else [fs], step=1, **HYPER)
+        assert torch.equal(p.detach().view(-1), flat)

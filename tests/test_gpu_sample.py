@@ -310,3 +310,70 @@ def test_empty_calls(a3po):
     z = torch.empty(0, 100, device="cuda")
     out = a3po.sample(z, torch.empty(0, device="cuda"), want_kept=True, want_allowed=True)
     assert out["token"].shape == (0,) and out["allowed"].shape == (0, 4)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_borders_among_many_entries(a3po, dt):
+    """Nuclei and counts of thousands to tens of thousands, borders in bins of up to all entries: rows that are flat, equal but for a
+    few, in two levels, with a border far below the rest, with both cuts at once."""
+    V, T = 70001, 10
+    g = torch.Generator().manual_seed(41)
+    z = torch.randn(T, V, generator=g) * torch.logspace(-4, 1, T)[:, None]
+    z[1, 100:] = 0.25
+    z[2] = torch.where(torch.rand(V, generator=g) < 0.5, 1.0, 0.75)
+    z[3, :3] = 40.0
+    z = z.to(DT[dt]).cuda()
+    u = torch.rand(T, generator=g)
+    many = torch.tensor([4863, 4864, 4865, 9727, 9728, 9729, 30000, 69999, 70000, 70001]).int()
+    check(a3po, z, u, k=many)
+    check(a3po, z, u, k=many, p=torch.linspace(0.05, 0.95, T))
+    check(a3po, z, u, k=many.flip(0), min_p=torch.full((T,), 1e-3))
+    for p in (0.3, 0.9, 0.999, 1 - 2.0 ** -20):
+        check(a3po, z, u, p=torch.full((T,), p))
+        check(a3po, z, u, p=torch.full((T,), p), min_p=torch.full((T,), 0.2), tau=torch.linspace(0.3, 2.0, T))
+
+
+@pytest.mark.parametrize("cut", [False, True])
+def test_more_parts_than_threads(a3po, cut):
+    """A row longer than the kernels that go by parts take."""
+    V = 4300000
+    z, u, _ = make(2, V, 51, "bf16", 1.5)
+    check(a3po, z.cuda(), u, **(dict(p=torch.tensor([0.01, 0.7]), k=torch.tensor([0, 100000]).int()) if cut else {}))
+
+
+def test_offsets_beyond_32_bits(a3po):
+    """The last rows of logits that fill more than 4 GiB are drawn as they are alone."""
+    T, V = 18000, 120001
+    z = torch.randn(T, V, dtype=torch.bfloat16, device="cuda")
+    u = torch.rand(T, device="cuda")
+    p = torch.full((T,), 0.8, device="cuda")
+    names = ("token", "logp", "kept", "allowed")
+    for cuts in ({}, dict(top_p=p)):
+        whole = a3po.sample(z, u, want_kept=True, want_allowed=bool(cuts), **cuts)
+        for a, b in ((0, 3), (T - 5, T)):
+            part = a3po.sample(z[a:b].clone(), u[a:b], want_kept=True, want_allowed=bool(cuts), **{k: v[a:b] for k, v in cuts.items()})
+            assert all(torch.equal(whole[n][a:b], part[n]) for n in names if part[n] is not None)
+
+
+def test_two_streams_at_once(a3po):
+    T, V = 64, 50000
+    z, u, cuts = make(T, V, 61)
+    z, u, p = z.cuda(), u.cuda(), cuts["p"].cuda()
+    want = a3po.sample(z, u, top_p=p, want_allowed=True)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    got = []
+    for s in streams:
+        with torch.cuda.stream(s):
+            got += [a3po.sample(z, u, top_p=p, want_allowed=True) for _ in range(3)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(want[n], o[n]) for o in got for n in ("token", "logp", "allowed"))
+
+
+def test_outputs_that_are_not_asked_for(a3po):
+    z, u, cuts = make(9, 3000, 71)
+    z, u, p = z.cuda(), u.cuda(), cuts["p"].cuda()
+    for more in ({}, dict(top_p=p)):
+        full = a3po.sample(z, u, want_logp_full=True, want_kept=True, want_allowed=True, **more)
+        bare = a3po.sample(z, u, want_logp=False, **more)
+        assert torch.equal(full["token"], bare["token"]) and all(bare[n] is None for n in ("logp", "logp_full", "kept", "allowed"))
