@@ -195,6 +195,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a)
         size = (float)(lr / (1.0 - pow(a.dbeta1, step)));
         root = (float)(1.0 / sqrt(1.0 - pow(a.dbeta2, step)));
     }
+    // (a replayed graph's seed is always the one it was captured with)
+    const uint32_t salt = a.step_dev ? mix((uint32_t)*a.step_dev) : 0u;
     const int64_t chunks = a.first[a.count];
     for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         int k = 0;
@@ -227,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a)
         }
         uint32_t chance[kEach];
         if constexpr (BYTES || PT::kBytes == 2) {
-            const uint32_t key = t.key ^ (uint32_t)(at >> 32) * 0x9E3779B9u;
+            const uint32_t key = t.key ^ salt ^ (uint32_t)(at >> 32) * 0x9E3779B9u;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) chance[i] = mix(((uint32_t)at + i) ^ key);
         }

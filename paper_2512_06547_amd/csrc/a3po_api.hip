@@ -1,6 +1,9 @@
 // extern "C" boundary: argument validation on the host, workspace carve-up, launches.
+#include <algorithm>
 #include <cmath>
+#include <memory>
 #include <mutex>
+#include <new>
 
 #include "a3po.h"
 #include "a3po_common.h"
@@ -670,6 +673,15 @@ int a3po_adamw_step(const a3po_adamw_tensor *tensors, int64_t count, a3po_dtype 
         if (!aligned(t.param, elem(param_dt)) || !aligned(t.grad, elem(grad_dt)) || !aligned(t.exp_avg, state) ||
             !aligned(t.exp_avg_sq, state) || !aligned(t.copy, 2))
             return A3PO_E_ALIGN;
+    }
+    if (count > 1) {  // (tied weights listed twice: two workgroups would update the same elements)
+        const std::unique_ptr<const void *[]> seen(new (std::nothrow) const void *[count]);
+        if (!seen) return A3PO_E_SIZE;
+        int64_t k = 0;
+        for (int64_t i = 0; i < count; ++i)
+            if (tensors[i].n > 0) seen[k++] = tensors[i].param;
+        std::sort(seen.get(), seen.get() + k);
+        if (std::adjacent_find(seen.get(), seen.get() + k) != seen.get() + k) return A3PO_E_VALUE;
     }
     const hipError_t e = launch_adamw(tensors, count, (int)param_dt, (int)grad_dt, state_format, o, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? A3PO_OK : A3PO_E_LAUNCH;

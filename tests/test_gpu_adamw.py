@@ -353,3 +353,29 @@ def test_parameters_and_shapes_of_modules(a3po):
         a3po.adamw_step([p], [grad], [m], [v], scales=None if s is None else [s], step=1, **HYPER)
         a3po.adamw_step([flat], [grad.view(-1)], [fm], [fv], scales=None if fs is None else [fs], step=1, **HYPER)
         assert torch.equal(p.detach().view(-1), flat)
+
+
+def test_a_replayed_graph_draws_new_bits(a3po):
+    """v halfway between two numbers at each replay: about half of the places go up each time, and not the same ones."""
+    n = 4000
+    p, g, m = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.float8_e4m3fn, device="cuda")
+    start = torch.full((n,), 2.0 ** 14 * 1.25, device="cuda").to(torch.float8_e5m2)
+    v, scales = start.clone(), tuple(torch.full((n // 32,), 127, dtype=torch.uint8, device="cuda") for _ in range(2))
+    step = torch.tensor([1], device="cuda")
+    call = lambda: a3po.adamw_step([p], [g], [m], [v], scales=[scales], step=step, lr=0.1, beta2=0.9)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    seen = []
+    for i in range(3):
+        v.copy_(start)
+        step.fill_(i + 1)
+        graph.replay()
+        torch.cuda.synchronize()
+        seen.append(a3po.adamw_state_values(v, scales[1]) > 2.0 ** 14 * 1.1)
+        # 1.125 lies halfway between 1 and 1.25; six deviations of 4,000 coins
+        assert abs(float(seen[-1].float().mean()) - 0.5) <= 6 * 0.5 / math.sqrt(n)
+        for other in seen[:-1]:
+            assert abs(float((seen[-1] == other).float().mean()) - 0.5) <= 6 * 0.5 / math.sqrt(n)

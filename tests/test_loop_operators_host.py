@@ -86,6 +86,18 @@ def test_adamw_step_refuses(lib):
     assert call(a0=table(exp_avg_scale=0), a4=1) == -1 and call(a0=table(exp_avg_sq_scale=0), a4=1) == -1
 
 
+def test_adamw_step_refuses_a_parameter_listed_twice(lib):
+    from paper_2512_06547_amd.binding import AdamwOptions, AdamwTensor
+    options = AdamwOptions(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, step=1)
+    row = lambda at, n=8: AdamwTensor(param=at, grad=0x1000, exp_avg=0x2000 + at, exp_avg_sq=0x3000 + at, n=n)
+    for rows in ([0x1000, 0x1000], [0x5000, 0x1000, 0x3000, 0x1000]):
+        table = (AdamwTensor * len(rows))(*map(row, rows))
+        assert lib.a3po_adamw_step(table, len(rows), 0, 0, 0, ctypes.byref(options), None) == -7
+    # (tensors without elements have no address of their own)
+    empty = (AdamwTensor * 2)(row(0x1000, 0), row(0x1000, 0))
+    assert lib.a3po_adamw_step(empty, 2, 0, 0, 0, ctypes.byref(options), None) == 0
+
+
 def test_w4_quantize_refuses(lib):
     # weight, dt, N, H, ld, group, codes, scales, scale_dt, zeros, stream
     call = caller(lib.a3po_w4_quantize, [P(), 0, 4, 256, 256, 64, P(), P(), 0, P(), None])
