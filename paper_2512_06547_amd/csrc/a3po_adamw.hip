@@ -16,18 +16,24 @@ namespace {
 
 constexpr int kThreads = 256, kEach = 8, kChunk = kThreads * kEach;
 
+// Addresses have 48 bits: the upper 16 of two share a word, and the eighth 16 say how many elements the last chunk has.  (80 tensors a
+// launch, 40 with the fields as they are: 300 odd tensors of 5 * 10^7 bfloat16 elements and 8-bit states take 129 us, and took 177)
 struct AdamTensor {
-    void *param, *m, *v;
-    const void *grad;
-    uint8_t *m_scale, *v_scale;
-    uint16_t *copy;
-    int64_t n;
-    uint32_t key;  // of its random bits
+    enum { kParam, kGrad, kM, kV, kCopy, kMScale, kVScale, kPointers };
+    uint32_t low[kPointers], high[(kPointers + 1) / 2];
+    __device__ __forceinline__ uint32_t upper(int i) const { return high[i / 2] >> (16 * (i & 1)) & 0xFFFFu; }
+    template <typename T = char>
+    __device__ __forceinline__ T *at(int i) const
+    {
+        typedef T __attribute__((address_space(1))) global_t;  // (flat loads would count as LDS's too)
+        return (T *)reinterpret_cast<global_t *>((uint64_t)upper(i) << 32 | low[i]);
+    }
 };
 struct AdamArgs {
     AdamTensor tensor[kAdamTensors];
-    int64_t first[kAdamTensors + 1];  // chunk of each tensor's beginning
+    uint32_t first[kAdamTensors + 1];  // chunk of each tensor's beginning
     int count;
+    uint32_t seed, number;  // number: of the first tensor
     float beta1, rest1, beta2, rest2, eps, decay, size, root;  // rest: 1 - beta; size: lr / (1 - beta1^t); root: 1 / sqrt(1 - beta2^t)
     float max_norm;
     const float *norm, *lr_dev;
@@ -197,26 +203,27 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a)
     }
     // (a replayed graph's seed is always the one it was captured with)
     const uint32_t salt = a.step_dev ? mix((uint32_t)*a.step_dev) : 0u;
-    const int64_t chunks = a.first[a.count];
-    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    const uint32_t chunks = a.first[a.count];
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         int k = 0;
-        for (int step = 32; step; step >>= 1)
+        for (int step = 64; step; step >>= 1)
             if (k + step < a.count && a.first[k + step] <= c) k += step;
-        const AdamTensor &t = a.tensor[k];
-        const int64_t at = (c - a.first[k]) * kChunk + (int)threadIdx.x * kEach;
-        const int left = (int)max((int64_t)0, min(t.n - at, (int64_t)kEach));
+        const AdamTensor t = a.tensor[k];
+        const int64_t at = (int64_t)(c - a.first[k]) * kChunk + (int)threadIdx.x * kEach;
+        const int here = c + 1 == a.first[k + 1] ? (int)t.upper(AdamTensor::kPointers) : kChunk;
+        const int left = max(0, min(here - (int)threadIdx.x * kEach, kEach));
         float p[kEach], g[kEach], m[kEach], v[kEach];
         uint32_t wm[2], wv[2];
-        load8<PT>(t.param, at, left, p);
-        load8<GT>(t.grad, at, left, g);
+        load8<PT>(t.at(AdamTensor::kParam), at, left, p);
+        load8<GT>(t.at(AdamTensor::kGrad), at, left, g);
         if constexpr (BYTES) {
-            load_bytes(t.m, at, left, wm);
-            load_bytes(t.v, at, left, wv);
-            decode_m(wm, left > 0 ? t.m_scale[at / 32] : 0u, m);
-            decode_v(wv, left > 0 ? t.v_scale[at / 32] : 0u, v);
+            load_bytes(t.at(AdamTensor::kM), at, left, wm);
+            load_bytes(t.at(AdamTensor::kV), at, left, wv);
+            decode_m(wm, left > 0 ? t.at<uint8_t>(AdamTensor::kMScale)[at / 32] : 0u, m);
+            decode_v(wv, left > 0 ? t.at<uint8_t>(AdamTensor::kVScale)[at / 32] : 0u, v);
         } else {
-            load8<F32>(t.m, at, left, m);
-            load8<F32>(t.v, at, left, v);
+            load8<F32>(t.at(AdamTensor::kM), at, left, m);
+            load8<F32>(t.at(AdamTensor::kV), at, left, v);
         }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -229,7 +236,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a)
         }
         uint32_t chance[kEach];
         if constexpr (BYTES || PT::kBytes == 2) {
-            const uint32_t key = t.key ^ salt ^ (uint32_t)(at >> 32) * 0x9E3779B9u;
+            const uint32_t key = mix(a.seed + 0x9E3779B9u * (a.number + (uint32_t)k + 1u)) ^ salt ^ (uint32_t)(at >> 32) * 0x9E3779B9u;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) chance[i] = mix(((uint32_t)at + i) ^ key);
         }
@@ -238,16 +245,16 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a)
             for (int i = 0; i < kEach; ++i)
                 if (fabsf(p[i]) < __builtin_huge_valf()) p[i] = __uint_as_float((__float_as_uint(p[i]) + (chance[i] >> 16)) & 0xFFFF0000u);
         }
-        store8<PT>(t.param, at, left, p);
-        if (t.copy) store8<Bf16>(t.copy, at, left, p);
+        store8<PT>(t.at(AdamTensor::kParam), at, left, p);
+        if (char *copy = t.at(AdamTensor::kCopy)) store8<Bf16>(copy, at, left, p);
         if constexpr (BYTES) {
             const uint32_t sm = encode_m(m, wm), sv = encode_v(v, chance, wv);
-            store_bytes(t.m, at, left, wm);
-            store_bytes(t.v, at, left, wv);
-            if (left > 0 && (threadIdx.x & 3) == 0) t.m_scale[at / 32] = (uint8_t)sm, t.v_scale[at / 32] = (uint8_t)sv;
+            store_bytes(t.at(AdamTensor::kM), at, left, wm);
+            store_bytes(t.at(AdamTensor::kV), at, left, wv);
+            if (left > 0 && (threadIdx.x & 3) == 0) t.at<uint8_t>(AdamTensor::kMScale)[at / 32] = (uint8_t)sm, t.at<uint8_t>(AdamTensor::kVScale)[at / 32] = (uint8_t)sv;
         } else {
-            store8<F32>(t.m, at, left, m);
-            store8<F32>(t.v, at, left, v);
+            store8<F32>(t.at(AdamTensor::kM), at, left, m);
+            store8<F32>(t.at(AdamTensor::kV), at, left, v);
         }
     }
 }
@@ -333,19 +340,28 @@ hipError_t launch_adamw(const a3po_adamw_tensor *tensors, int64_t count, int par
     a.size = (float)(o.lr / (1.0 - std::pow(o.beta1, (double)o.step)));
     a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(o.beta2, (double)o.step)));
     const bool bytes = state_format == A3PO_STATE_8BIT;
+    a.seed = o.seed;
     for (int64_t i = 0; i < count;) {
         int k = 0;
-        for (; i < count && k < kAdamTensors; ++i) {
+        a.number = (uint32_t)i;
+        for (; i < count && k < kAdamTensors; ++i, ++k) {  // (an empty tensor has no chunks)
             const a3po_adamw_tensor &t = tensors[i];
-            if (t.n == 0) continue;
-            a.tensor[k] = AdamTensor{t.param, t.exp_avg, t.exp_avg_sq, t.grad, t.exp_avg_scale, t.exp_avg_sq_scale,
-                                     static_cast<uint16_t *>(t.copy), t.n, mix(o.seed + 0x9E3779B9u * (uint32_t)(i + 1))};
-            a.first[k + 1] = a.first[k] + (t.n + kChunk - 1) / kChunk;
-            ++k;
+            const int64_t chunks = (t.n + kChunk - 1) / kChunk;
+            if (a.first[k] + chunks > 0x7FFFFFFF) break;
+            const void *const fields[] = {t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.copy, t.exp_avg_scale, t.exp_avg_sq_scale};
+            AdamTensor &to = a.tensor[k];
+            to = {};
+            for (int f = 0; f < AdamTensor::kPointers; ++f) {
+                const uint64_t at = reinterpret_cast<uint64_t>(fields[f]);
+                if (at >> 48) return hipErrorInvalidValue;
+                to.low[f] = (uint32_t)at, to.high[f / 2] |= (uint32_t)(at >> 32) << (16 * (f & 1));
+            }
+            to.high[AdamTensor::kPointers / 2] |= (uint32_t)(t.n - (chunks - 1) * kChunk) << (16 * (AdamTensor::kPointers & 1));
+            a.first[k + 1] = a.first[k] + (uint32_t)chunks;
         }
-        if (k == 0) break;
         a.count = k;
-        const int grid = (int)(a.first[k] < (1 << 22) ? a.first[k] : 1 << 22);
+        if (a.first[k] == 0) continue;
+        const int grid = (int)(a.first[k] < (1u << 22) ? a.first[k] : 1u << 22);
         if (param_dt == A3PO_F32) grad_dt == A3PO_F32 ? launch_step<F32, F32>(a, grid, bytes, s) : launch_step<F32, Bf16>(a, grid, bytes, s);
         else grad_dt == A3PO_F32 ? launch_step<Bf16, F32>(a, grid, bytes, s) : launch_step<Bf16, Bf16>(a, grid, bytes, s);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;

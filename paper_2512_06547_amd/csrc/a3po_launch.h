@@ -730,7 +730,7 @@ inline size_t sample_workspace_bytes(int64_t T, int64_t V)
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
 
 // Tensors reach the kernels as launch arguments, so many a launch (4 KiB of arguments at most).
-constexpr int kAdamTensors = 40, kNormTensors = 200, kNormBlocks = 1024;
+constexpr int kAdamTensors = 80, kNormTensors = 200, kNormBlocks = 1024;
 inline size_t grad_norm_workspace_bytes(int64_t count)
 {
     const int64_t launches = count > 0 ? (count + kNormTensors - 1) / kNormTensors : 0;

@@ -379,3 +379,25 @@ def test_a_replayed_graph_draws_new_bits(a3po):
         assert abs(float(seen[-1].float().mean()) - 0.5) <= 6 * 0.5 / math.sqrt(n)
         for other in seen[:-1]:
             assert abs(float((seen[-1] == other).float().mean()) - 0.5) <= 6 * 0.5 / math.sqrt(n)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tables_of_tensors_cut_anywhere(a3po, bits):
+    """More tensors than a launch takes, empty ones among them: each is updated as its place in the list alone says."""
+    sizes = [(37 * i * i) % 5000 if i % 7 else 0 for i in range(250)]
+    g = torch.Generator(device="cuda").manual_seed(8)
+    ps = [torch.randn(n, generator=g, device="cuda") for n in sizes]
+    gs = [torch.randn(n, generator=g, device="cuda") for n in sizes]
+    def run(keep):
+        mine = [p.clone() if i in keep else torch.empty(0, device="cuda") for i, p in enumerate(ps)]
+        st = [a3po.adamw_state(p, bits) for p in mine]
+        a3po.adamw_step(mine, [x if i in keep else x[:0] for i, x in enumerate(gs)], [s[0] for s in st], [s[1] for s in st],
+                        scales=[s[2] for s in st] if bits == 8 else None, step=1, **HYPER)
+        return mine, st
+    raw = lambda t: t.view(torch.uint8)
+    mine, st = run(range(250))
+    for keep in (range(79, 82), range(159, 250), [0, 249], [1]):
+        part, pst = run(keep)
+        for i in keep:
+            assert torch.equal(part[i], mine[i]) and torch.equal(raw(pst[i][0]), raw(st[i][0])) and torch.equal(raw(pst[i][1]), raw(st[i][1]))
+        assert not sizes[keep[0]] or not torch.equal(part[keep[0]], ps[keep[0]])
