@@ -253,7 +253,7 @@ __device__ __forceinline__ float first_at(int p, double grid, float lowest)
 // bin's middle is 1)
 constexpr int kWeightBits = 50;
 constexpr uint64_t kWeightMask = (1ull << kWeightBits) - 1;
-constexpr double kOne = 68719476736.0, kWhole = 4503599627370496.0;  // 2^36, 2^52
+constexpr double kOne = 68719476736.0, kCounted = 5629499534213120.0;  // 2^36, 2^52 + 2^50
 
 // The weights of an uncut part are 2^(z unit / 32) as they are: 64 bits hold 900 powers of two either way, and no maximum has to be
 // known before.  Where the part's reaches further, or no float is far below it (temperatures from 1e28 on), they are relative to the
@@ -261,6 +261,14 @@ constexpr double kOne = 68719476736.0, kWhole = 4503599627370496.0;  // 2^36, 2^
 constexpr double kWide = 900.0 * 32;
 __device__ __forceinline__ bool is_wide(float top, double unit) { return !(fabs((double)top * unit) < kWide && unit > 1e-27); }
 __device__ __forceinline__ bool is_far(float top, double unit) { return !(fabs((double)top * unit) < kNear && unit > 1e-27); }
+
+// a b + c with c in scalar registers.  (The compiler takes v_fmac_f64, whose c is overwritten, and copies c first.)
+__device__ __forceinline__ double fma_scalar(double a, double b, double c)
+{
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+    return r;
+}
 
 // NaN if either is
 __device__ __forceinline__ float maximum(float a, float b)
@@ -375,7 +383,7 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_
 {
     using Entries = PartEntries<DT>;
     __shared__ double table[32];
-    __shared__ uint64_t bins[kSampleBins];
+    __shared__ uint64_t bins[kSampleBins + kWave];
     __shared__ float wave_top[kPartWaves];
     __shared__ uint32_t wave_count[kPartWaves], wave_last[kPartWaves];
     __shared__ PartRecord record;
@@ -424,18 +432,22 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_
         int place = kSampleFar;
         const bool far = is_far(top, unit);
         if (!far) {
+            // (a5 q^5 is replaced by the cubic next to it on [-1/2, 1/2]: off by a5 / 512 at most, 2^-38)
             constexpr double a1 = 0.69314718055994530942 / 16, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
+            constexpr double b3 = a3 + a5 * (5.0 / 16), b1 = a1 - a5 * (5.0 / 256);
             const double grid = unit * 0.5;
             const float lowest = lowest_of(unit);
             place = place_of(top, grid, lowest);
             const float behind = first_at(place - kSampleBins + 1, grid, lowest);  // the bins' smallest logit
+            // Entry x's bin, the last ones first, or a place of the lane's own: without branches the entries' arithmetic overlaps.
+            // w as it is in memory holds 4301 = 4 * 1075 + 1 where a bin's sum has its count, so N of them hold 4301 N modulo 2^14.
+            const uint32_t base = 8u * (uint32_t)(kSampleBins - 1 - place), beside = 8u * (uint32_t)(kSampleBins + lane);
             z.each([&](float x, int) {
                 const double d = (double)x, n = fma(d, grid, kRound), q = fma(d, grid, -(n - kRound));
-                const double w = fma(fma(fma(fma(fma(q, a5 * kOne, a4 * kOne), q, a3 * kOne), q, a2 * kOne), q, a1 * kOne), q, kOne + kWhole);
-                if (x >= behind) {
-                    const uint64_t add = (uint64_t)(((uint32_t)__double2hiint(w) & 0xFFFFFu) | 1u << (kWeightBits - 32)) << 32 | (uint32_t)__double2loint(w);
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&bins[place - __double2loint(n)]), (unsigned long long)add);
-                }
+                const double w = fma_scalar(fma_scalar(fma_scalar(fma_scalar(q, a4 * kOne, b3 * kOne), q, a2 * kOne), q, b1 * kOne), q, kOne + kCounted);
+                const uint32_t at = ((uint32_t)__double2loint(n) << 3) + base;
+                atomicAdd(reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(bins) + (x >= behind ? at : beside)),
+                          (unsigned long long)__double_as_longlong(w));
             });
             // what lies behind the bins is below 2^-32 of the largest, all of it below 2^-19: what fp32 loses of that, 2^-18 of it, is
             // below 2^-37
@@ -451,7 +463,9 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_
             __syncthreads();  // (the bins are whole)
 #pragma unroll
             for (int b = tid; b < kSampleBins; b += kPartThreads) {
-                const uint64_t sum = bins[b];
+                uint64_t sum = bins[kSampleBins - 1 - b];
+                sum = (sum & kWeightMask) | (uint64_t)((uint32_t)(sum >> kWeightBits) * 7173u & 0x3FFFu) << kWeightBits;  // 1 / 4301 modulo 2^14
+                bins[kSampleBins - 1 - b] = sum;
                 if (sum) bins_used = b + 1;
                 const double middle = table[-2 * b & 31];  // 2^(-b / 16)
                 mass = fma((double)(sum & kWeightMask) * (1.0 / kOne), __hiloint2double(__double2hiint(middle) - (b << 16), __double2loint(middle)), mass);
@@ -467,7 +481,7 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_
         count = bins_used = 0;
 #pragma unroll
         for (int w = 0; w < kPartWaves; ++w) count += wave_count[w], bins_used = max(bins_used, wave_last[w]);
-        for (int b = tid; b < (int)bins_used; b += kPartThreads) a.bins[i * kSampleBins + b] = bins[b];
+        for (int b = tid; b < (int)bins_used; b += kPartThreads) a.bins[i * kSampleBins + b] = bins[kSampleBins - 1 - b];
         write_part(record, a.part[i], top, place, bins_used, count);
     }
 }
