@@ -46,6 +46,14 @@ __device__ const double kTable[32] = {
     0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
     0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
 
+// a b + c with c in scalar registers.  (The compiler takes v_fmac_f64, whose c is overwritten, and copies c first.)
+__device__ __forceinline__ double fma_scalar(double a, double b, double c)
+{
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+    return r;
+}
+
 // e^x: 2^(i / 32) from a table (one entry a pair of LDS banks: lanes never wait for one another), the rest of the exponent by a
 // series whose first term left out, (ln 2 / 64)^6 / 720, is 2^-48
 struct Weigh {
@@ -60,7 +68,7 @@ struct Weigh {
         const double r = y - (t - kRound);
         const double b = table[n & 31];
         const double scale = __hiloint2double(__double2hiint(b) + ((n >> 5) << 20), __double2loint(b));
-        return scale * (1.0 + r * (a1 + r * (a2 + r * (a3 + r * (a4 + r * a5)))));
+        return scale * fma(fma_scalar(fma_scalar(fma_scalar(fma_scalar(r, a5, a4), r, a3), r, a2), r, a1), r, 1.0);
     }
     __device__ __forceinline__ uint64_t whole(float z) const
     {
@@ -261,14 +269,6 @@ constexpr double kOne = 68719476736.0, kCounted = 5629499534213120.0;  // 2^36, 
 constexpr double kWide = 900.0 * 32;
 __device__ __forceinline__ bool is_wide(float top, double unit) { return !(fabs((double)top * unit) < kWide && unit > 1e-27); }
 __device__ __forceinline__ bool is_far(float top, double unit) { return !(fabs((double)top * unit) < kNear && unit > 1e-27); }
-
-// a b + c with c in scalar registers.  (The compiler takes v_fmac_f64, whose c is overwritten, and copies c first.)
-__device__ __forceinline__ double fma_scalar(double a, double b, double c)
-{
-    double r;
-    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
-    return r;
-}
 
 // NaN if either is
 __device__ __forceinline__ float maximum(float a, float b)
