@@ -245,12 +245,13 @@ struct PartEntries {
 // Places on the grid: the whole number next to z times 16 log2(e) / temperature, by one rounding, so that larger logits never have
 // smaller places.  `lowest` stands for everything that is further below than whole numbers of 32 bits reach.
 constexpr double kNear = 1.0e9;
-__device__ __forceinline__ float lowest_of(double unit) { return (float)(-1.5e9 / unit); }
+constexpr double kPlace = 2.0 / kUnit;  // what a place is of a temperature
+__device__ __forceinline__ float lowest_of(float tau) { return (float)(-0.75e9 * kPlace * (double)tau); }
 __device__ __forceinline__ int place_of(float z, double grid, float lowest) { return __double2loint(fma((double)max2(z, lowest), grid, kRound)); }
 // the smallest float whose place is at least p
-__device__ __forceinline__ float first_at(int p, double grid, float lowest)
+__device__ __forceinline__ float first_at(int p, double grid, float tau, float lowest)
 {
-    float z = (float)(((double)p - 0.5) / grid);
+    float z = (float)(((double)p - 0.5) * (kPlace * (double)tau));
 #pragma unroll 1
     while (place_of(z, grid, lowest) >= p) z = nextafterf(z, -kInf);
 #pragma unroll 1
@@ -436,9 +437,9 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_
             constexpr double a1 = 0.69314718055994530942 / 16, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
             constexpr double b3 = a3 + a5 * (5.0 / 16), b1 = a1 - a5 * (5.0 / 256);
             const double grid = unit * 0.5;
-            const float lowest = lowest_of(unit);
+            const float lowest = lowest_of(policy.tau);
             place = place_of(top, grid, lowest);
-            const float behind = first_at(place - kSampleBins + 1, grid, lowest);  // the bins' smallest logit
+            const float behind = first_at(place - kSampleBins + 1, grid, policy.tau, lowest);  // the bins' smallest logit
             // Entry x's bin, the last ones first, or a place of the lane's own: without branches the entries' arithmetic overlaps.
             // w as it is in memory holds 4301 = 4 * 1075 + 1 where a bin's sum has its count, so N of them hold 4301 N modulo 2^14.
             const uint32_t base = 8u * (uint32_t)(kSampleBins - 1 - place), beside = 8u * (uint32_t)(kSampleBins + lane);
@@ -1182,7 +1183,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
         } else if (policy.cut() && each_part && !far) {
             // ---- all parts' bins on the row's grid, a bin a thread
             const double grid = unit * 0.5;
-            const float lowest = lowest_of(unit);
+            const float lowest = lowest_of(policy.tau);
             out.place = place_of(top, grid, lowest);
             const bool some = mine.max > -kInf;
             part_place[tid] = some ? mine.place : 0, part_bins[tid] = some ? mine.bins : 0;
@@ -1248,8 +1249,8 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
             if (down_to <= kSampleFewest) out.mode = kSampleFew;
             else if (!lost && bin != kSampleAll && in_bin <= kSampleListed && !(by_k && policy.by_p())) out.mode = kSampleBin;
             if (out.mode != kSamplePasses) {
-                out.from = bin == kSampleAll ? -3.402823466e38f : first_at(out.place - bin, grid, lowest);
-                out.to = out.mode == kSampleFew ? kInf : nextafterf(first_at(out.place - bin + 1, grid, lowest), -kInf);
+                out.from = bin == kSampleAll ? -3.402823466e38f : first_at(out.place - bin, grid, policy.tau, lowest);
+                out.to = out.mode == kSampleFew ? kInf : nextafterf(first_at(out.place - bin + 1, grid, policy.tau, lowest), -kInf);
             }
         }
         // (field by field: a whole struct's copy takes its padding along, through a private array that ends up in LDS by a thread
