@@ -603,8 +603,10 @@ int a3po_grad_norm(const void *const *grads, const int64_t *sizes, int64_t count
  * bfloat16 parameters stochastically (the share of an update below the last bit that is not lost is its mean); 8-bit exp_avg to
  * nearest; 8-bit exp_avg_sq stochastically (to nearest it would never fall: one step takes away less than half a bit) and never
  * from above zero to zero, so that no update is divided by eps alone.  The random bits of element i of tensor k are a function
- * of seed, k and i, and of step_dev's number where it is given (a replayed graph draws new ones as that goes up).  A block of 32 that holds an infinity or NaN reads as NaN afterwards; with `norm` such a step is left out.
- * Tensors must not overlap; a param listed twice is refused.  0 <= beta < 1, eps >= 0, lr >= 0, weight_decay >= 0, step >= 1, else A3PO_E_VALUE.
+ * of seed, k and i, and of step_dev's number where it is given (a replayed graph draws new ones as that goes up).  A block of 32
+ * that holds an infinity or NaN reads as NaN afterwards; with `norm` such a step is left out.
+ * Tensors must not overlap; a param that is listed twice is refused.  0 <= beta < 1, eps >= 0, lr >= 0, weight_decay >= 0 and
+ * step >= 1, else A3PO_E_VALUE (numbers on the device are not looked at).
  */
 int a3po_adamw_step(const a3po_adamw_tensor *tensors, int64_t count, a3po_dtype param_dt, a3po_dtype grad_dt, int32_t state_format,
                     const a3po_adamw_options *options, void *stream);

@@ -377,3 +377,29 @@ def test_outputs_that_are_not_asked_for(a3po):
         full = a3po.sample(z, u, want_logp_full=True, want_kept=True, want_allowed=True, **more)
         bare = a3po.sample(z, u, want_logp=False, **more)
         assert torch.equal(full["token"], bare["token"]) and all(bare[n] is None for n in ("logp", "logp_full", "kept", "allowed"))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_masks_of_the_lowest_value(a3po, dt):
+    """Entries at the type's lowest value are entries, of no weight beside others: kept where nothing cuts them, never drawn; a row of
+    nothing else is flat."""
+    V, T = 40001, 8
+    g = torch.Generator().manual_seed(81)
+    low = torch.finfo(DT[dt]).min
+    z = (torch.randn(T, V, generator=g) * 3).to(DT[dt])
+    z[0] = low
+    z[1, 1:] = low
+    z[2, :-1] = low
+    z[3, 5:30000] = low
+    z[4] = torch.where(torch.rand(V, generator=g) < 0.999, torch.tensor(low, dtype=DT[dt]), z[4])
+    z[5, ::2] = float("-inf")
+    z[5, 1::2] = low
+    z[6, 7] = -low
+    z[7, 100:] = low
+    z, u = z.cuda(), torch.rand(T, generator=g)
+    check(a3po, z, u)
+    check(a3po, z, u, tau=torch.linspace(0.5, 1.5, T))
+    check(a3po, z, u, k=torch.full((T,), 200).int())
+    check(a3po, z, u, p=torch.full((T,), 0.9))
+    check(a3po, z, u, min_p=torch.full((T,), 0.1), tau=torch.full((T,), 1e-3))
+    check(a3po, z, u, k=torch.full((T,), 20000).int(), p=torch.full((T,), 0.5), min_p=torch.full((T,), 1e-30))
