@@ -826,13 +826,20 @@ struct Passes {
         __syncthreads();
         const uint32_t mask = (1u << bits) - 1;
         row.each([&](const float *v, int64_t, int) {
+            // (64 vectors of one value are added by one lane: additions to one place wait for one another)
+            const float one = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v[0])));
+            bool same = true;
+#pragma unroll
+            for (int k = 0; k < EPV; ++k) same &= v[k] == one;
+            const uint32_t times = __all(same) ? kWave * EPV : 1;
 #pragma unroll
             for (int k = 0; k < EPV; ++k) {
                 const uint32_t key = key_of(v[k]);
+                if (times > 1 && (k > 0 || threadIdx.x % kWave != 0)) continue;
                 if (key > kKeyOfNegInf && (bits + shift == 32 || key >> (shift + bits) == prefix)) {
                     const uint32_t d = key >> shift & mask;
-                    atomicAdd(&sh.key.count[d], 1u);
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.key.mass[d]), (unsigned long long)weigh.whole(v[k]));
+                    atomicAdd(&sh.key.count[d], times);
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.key.mass[d]), (unsigned long long)weigh.whole(v[k]) * times);
                 }
             }
         });
