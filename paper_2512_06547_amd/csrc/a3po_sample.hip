@@ -393,11 +393,12 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_
     }
 }
 
-// A part: maximum, bins, what lies behind them.  256 threads hold 8,192 entries, 32 (fp32) or 16 (bfloat16) registers a thread; four workgroups a
-// compute unit (three with fp32, whose registers would be spilled otherwise: 64 x 151,936 73 us for 67).  Two sets of bins by even and
-// odd lanes, against lanes that add to one bin, changed nothing (flat rows 47.5 us for 46.9): instructions bound it, not the atomics.
+// A part: maximum, bins, what lies behind them.  256 threads hold 8,192 entries, 32 (fp32) or 16 (bfloat16) registers a thread.  Five
+// workgroups a compute unit (flat rows 131 us for four's 134), three with fp32, where four spill 13 registers (64 x 151,936 70 us for 64).  Two
+// sets of bins by even and odd lanes, against lanes that add to one bin, changed nothing (flat rows' parts 47.5 us for 46.9): instructions
+// bound it, not the atomics.
 template <typename DT>
-__global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 4) void sample_parts_kernel(SampleArgs a, int64_t row0, int64_t rows)
+__global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 5) void sample_parts_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
     using Entries = PartEntries<DT>;
     __shared__ double table[32];
