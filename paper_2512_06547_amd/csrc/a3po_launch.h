@@ -665,6 +665,7 @@ struct alignas(128) SampleRow {
     uint32_t key;               // the last entry kept, for the bits of many
     int32_t last;
     float from, to;             // logits to be gathered
+    int coarse;                 // bins are of 2^coarse / 16 powers of two
 };
 struct SampleSegment {
     double above;            // the part's share of SampleRow::above

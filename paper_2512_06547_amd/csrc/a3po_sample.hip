@@ -8,13 +8,13 @@
 //
 // A row is cut into parts of 8,192 entries, a workgroup each.
 //   parts:   the part's maximum and the sum of its weights; where the row is cut, counts and sums of its entries in bins of 1/16
-//            power of two of their weight, on one grid for all parts, so that parts add up
+//            power of two of their weight (1/4 under top-k), on one grid for all parts, so that parts add up
 //   rows:    uncut, the token: the part, then the entry, in whose part of the sum the drawn number falls.  Cut, the bin that the
 //            border is in
 //   gather:  the entries down to that bin, where they are few, else that bin's alone: parts without any are not read again
 //   finish:  the border among those entries, and the token
-// Rows that this does not settle (borders among very many equal logits, or 2^-32 below the largest weight) are gone over by one
-// workgroup as often as their cuts ask.
+// Rows that this does not settle (borders among very many equal logits, or 2^-32 below the largest weight, 2^-128 under top-k) are gone
+// over by one workgroup as often as their cuts ask.
 //
 // Why parts: one row decodes alone as often as a thousand do together, so the row's passes are spread over as many compute units as it
 // has parts, and a part stays in registers from its maximum to its bins.  Why bins on a grid of absolute places: parts need not know the
@@ -24,10 +24,10 @@
 //     1 x  32,000 fp32, top-p 0.95                         30   (6.6 / 5.7 / 6.3 / 11.2 / 2.9: five launches in a row)
 //    64 x 151,936 fp32, top-p 0.95                         64   (19 / 8 / 16 / 20 / 4)
 //   300 x  50,001 fp32, top-k 50, top-p, min-p, bits       79   (29 / 8 / 20 / 18 / 5 / 4)
-//   256 x 151,936 bf16, top-p 0.9 of flat rows, bits      137   (40 / 9 / 35 / 30 / 6 / 18)
+//   256 x 151,936 bf16, top-p 0.9 of flat rows, bits      135   (37 / 9 / 36 / 30 / 6 / 18)
 //  1024 x 151,936 bf16, uncut                             112   (one pass over the rows 111, tokens 10; under the profiler)
 // What bounds them: vector instructions where there are many parts (uncut 21 an entry, 9 of them in 64 bits: active in 94 % of a
-// compute unit's busy cycles; parts of flat rows 26 an entry, 81 %), latencies in a row where there are few: a part's load, maximum, bins; a row's parts,
+// compute unit's busy cycles; parts of flat rows 26 an entry, 85 %), latencies in a row where there are few: a part's load, maximum, bins; a row's parts,
 // scan, border; list, border, part, token.
 //
 // In a bin, weights are relative to the bin's and added as whole numbers of 2^-36, their count above them in the same 64 bits: one
@@ -214,6 +214,9 @@ struct Policy {
     __device__ __forceinline__ bool by_k() const { return k > 0; }
     __device__ __forceinline__ bool by_p() const { return p < 1.0f; }
     __device__ __forceinline__ bool by_min() const { return min_p > 0.0f; }
+    // Bins of 1/4 power of two instead of 1/16 reach four times as far: the k-th entry may be far below the largest.  (Rows with one entry
+    // 40 ahead, top-k 50, 64 / 300 x 151,936 bf16: 47 / 109 us; with bins of 1/16, in passes, 179 / 282.)
+    __device__ __forceinline__ int coarse() const { return by_k() ? 2 : 0; }
     __device__ __forceinline__ bool cut() const { return by_k() || by_p() || by_min(); }
 };
 
@@ -262,10 +265,10 @@ constexpr double kNear = 1.0e9;
 constexpr double kPlace = 2.0 / kUnit;  // what a place is of a temperature
 __device__ __forceinline__ float lowest_of(float tau) { return (float)(-0.75e9 * kPlace * (double)tau); }
 __device__ __forceinline__ int place_of(float z, double grid, float lowest) { return __double2loint(fma((double)max2(z, lowest), grid, kRound)); }
-// the smallest float whose place is at least p
-__device__ __forceinline__ float first_at(int p, double grid, float tau, float lowest)
+// the smallest float whose place is at least p; step: 1 / grid, nearly
+__device__ __forceinline__ float first_at(int p, double grid, double step, float lowest)
 {
-    float z = (float)(((double)p - 0.5) * (kPlace * (double)tau));
+    float z = (float)(((double)p - 0.5) * step);
 #pragma unroll 1
     while (place_of(z, grid, lowest) >= p) z = nextafterf(z, -kInf);
 #pragma unroll 1
@@ -451,27 +454,43 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 5) void sample_
         int place = kSampleFar;
         const bool far = is_far(top, unit);
         if (!far) {
-            // (a5 q^5 is replaced by the cubic next to it on [-1/2, 1/2]: off by a5 / 512 at most, 2^-38)
-            constexpr double a1 = 0.69314718055994530942 / 16, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
-            constexpr double b3 = a3 + a5 * (5.0 / 16), b1 = a1 - a5 * (5.0 / 256);
-            const double grid = unit * 0.5;
+            const int coarse = policy.coarse();
+            const double grid = unit * (coarse ? 0.125 : 0.5), step = kPlace * (double)policy.tau * (coarse ? 4.0 : 1.0);
             const float lowest = lowest_of(policy.tau);
             place = place_of(top, grid, lowest);
-            const float behind = first_at(place - kSampleBins + 1, grid, policy.tau, lowest);  // the bins' smallest logit
+            const float behind = first_at(place - kSampleBins + 1, grid, step, lowest);  // the bins' smallest logit
             // Entry x's bin, the last ones first, or a place of the lane's own: without branches the entries' arithmetic overlaps.
             // w as it is in memory holds 4301 = 4 * 1075 + 1 where a bin's sum has its count, so N of them hold 4301 N modulo 2^14.
             const uint32_t base = 8u * (uint32_t)(kSampleBins - 1 - place), beside = 8u * (uint32_t)(kSampleBins + lane);
-            z.each([&](float x, int) {
-                const double d = (double)x, n = fma(d, grid, kRound), q = fma(d, grid, -(n - kRound));
-                const double w = fma_scalar(fma_scalar(fma_scalar(fma_scalar(q, a4 * kOne, b3 * kOne), q, a2 * kOne), q, b1 * kOne), q, kOne + kCounted);
-                const uint32_t at = ((uint32_t)__double2loint(n) << 3) + base;
-                atomicAdd(reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(bins) + (x >= behind ? at : beside)),
-                          (unsigned long long)__double_as_longlong(w));
-            });
+            auto put = [&](auto weigh) {
+                z.each([&](float x, int) {
+                    const double d = (double)x, n = fma(d, grid, kRound), q = fma(d, grid, -(n - kRound));
+                    const double w = weigh(q);
+                    const uint32_t at = ((uint32_t)__double2loint(n) << 3) + base;
+                    atomicAdd(reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(bins) + (x >= behind ? at : beside)),
+                              (unsigned long long)__double_as_longlong(w));
+                });
+            };
+            // 2^(q / 16), 2^(q / 4): the series' last term, a5 q^5 or a7 q^7, is replaced by the polynomial next to it on [-1/2, 1/2], off by
+            // a5 / 512 or a7 / 8192 at most, 2^-38 or 2^-43
+            if (!coarse)
+                put([](double q) {
+                    constexpr double a1 = 0.69314718055994530942 / 16, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
+                    constexpr double b3 = a3 + a5 * (5.0 / 16), b1 = a1 - a5 * (5.0 / 256);
+                    return fma_scalar(fma_scalar(fma_scalar(fma_scalar(q, a4 * kOne, b3 * kOne), q, a2 * kOne), q, b1 * kOne), q, kOne + kCounted);
+                });
+            else
+                put([](double q) {
+                    constexpr double a1 = 0.69314718055994530942 / 4, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5, a6 = a5 * a1 / 6,
+                                     a7 = a6 * a1 / 7;
+                    constexpr double b5 = a5 + a7 * (7.0 / 16), b3 = a3 - a7 * (7.0 / 128), b1 = a1 + a7 * (7.0 / 4096);
+                    return fma_scalar(fma_scalar(fma_scalar(fma_scalar(fma_scalar(fma_scalar(q, a6 * kOne, b5 * kOne), q, a4 * kOne), q, b3 * kOne), q, a2 * kOne), q, b1 * kOne),
+                                      q, kOne + kCounted);
+                });
             // what lies behind the bins is below 2^-32 of the largest, all of it below 2^-19: what fp32 loses of that, 2^-18 of it, is
             // below 2^-37
             if (low < behind) {
-                const float scale = (float)(grid * 0.0625), shift = (float)(fma((double)top, grid, -(double)place) * 0.0625);
+                const float scale = (float)(unit * 0.03125), shift = (float)(fma((double)top, grid, -(double)place) * (coarse ? 0.25 : 0.0625));
                 float tail = 0.0f;
                 z.each([&](float x, int k) {
                     tail += x < behind ? exp2_hw(fmaf(x - top, scale, shift)) : 0.0f;
@@ -486,8 +505,9 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 5) void sample_
                 sum = (sum & kWeightMask) | (uint64_t)((uint32_t)(sum >> kWeightBits) * 7173u & 0x3FFFu) << kWeightBits;  // 1 / 4301 modulo 2^14
                 bins[kSampleBins - 1 - b] = sum;
                 if (sum) bins_used = b + 1;
-                const double middle = table[-2 * b & 31];  // 2^(-b / 16)
-                mass = fma((double)(sum & kWeightMask) * (1.0 / kOne), __hiloint2double(__double2hiint(middle) - (b << 16), __double2loint(middle)), mass);
+                const int e = b << policy.coarse();
+                const double middle = table[-2 * e & 31];  // 2^(-e / 16)
+                mass = fma((double)(sum & kWeightMask) * (1.0 / kOne), __hiloint2double(__double2hiint(middle) - (e << 16), __double2loint(middle)), mass);
             }
         }
         if (low > -kInf) count = Entries::kEach;  // (the same for all of the wave)
@@ -542,7 +562,7 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 4 : 5) void sample_
                 const int b = j * kPartThreads + tid;
                 if (b < (int)part.bins) {
                     if (few ? b <= last : b == last) n += (uint32_t)(bins[j] >> kWeightBits);
-                    if (!few && b < last) above += (double)(bins[j] & kWeightMask) * down_by(b + shift);
+                    if (!few && b < last) above += (double)(bins[j] & kWeightMask) * down_by((b + shift) << row.coarse);
                 }
             }
             if (all) n = tid == 0 ? part.count : 0;
@@ -1212,13 +1232,14 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
             out.mode = kSampleDone;
         } else if (policy.cut() && each_part && !far) {
             // ---- all parts' bins on the row's grid, a bin a thread
-            const double grid = unit * 0.5;
+            const int coarse = policy.coarse();
+            const double grid = unit * (coarse ? 0.125 : 0.5), step = kPlace * (double)policy.tau * (coarse ? 4.0 : 1.0);
             const float lowest = lowest_of(policy.tau);
             out.place = place_of(top, grid, lowest);
             const bool some = mine.max > -kInf;
             part_place[tid] = some ? mine.place : 0, part_bins[tid] = some ? mine.bins : 0;
             const int64_t apart = some ? (int64_t)out.place - mine.place : 0;
-            double mass = some && apart < 16000 ? (mine.mass[0] + mine.mass[1] + mine.mass[2] + mine.mass[3]) * down_by((int)apart) * 68719476736.0 : 0.0;
+            double mass = some && apart < 16000 >> coarse ? (mine.mass[0] + mine.mass[1] + mine.mass[2] + mine.mass[3]) * down_by((int)apart << coarse) * 68719476736.0 : 0.0;
             __syncthreads();
             uint64_t sum = 0;
             uint32_t own_count = 0;
@@ -1243,7 +1264,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
                 }
             }
             // in units of the weight in the middle of bin 0, times 2^36
-            const double own = (double)sum * down_by(tid);
+            const double own = (double)sum * down_by(tid << coarse);
             double upto = own, all;
             uint32_t count = own_count, binned, finite = mine.count;
             block_scan<kThreads, 1>(sh, upto, all, mass, count, binned, finite);
@@ -1279,8 +1300,8 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
             if (down_to <= kSampleFewest) out.mode = kSampleFew;
             else if (!lost && bin != kSampleAll && in_bin <= kSampleListed && !(by_k && policy.by_p())) out.mode = kSampleBin;
             if (out.mode != kSamplePasses) {
-                out.from = bin == kSampleAll ? -3.402823466e38f : first_at(out.place - bin, grid, policy.tau, lowest);
-                out.to = out.mode == kSampleFew ? kInf : nextafterf(first_at(out.place - bin + 1, grid, policy.tau, lowest), -kInf);
+                out.from = bin == kSampleAll ? -3.402823466e38f : first_at(out.place - bin, grid, step, lowest);
+                out.to = out.mode == kSampleFew ? kInf : nextafterf(first_at(out.place - bin + 1, grid, step, lowest), -kInf);
             }
         }
         // (field by field: a whole struct's copy takes its padding along, through a private array that ends up in LDS by a thread
@@ -1289,7 +1310,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
             SampleRow &to = a.row[r];
             to.full = out.full, to.above = out.above, to.share = out.share, to.rank = out.rank, to.top = out.top;
             to.mode = out.mode, to.by_k = out.by_k, to.place = out.place, to.bin = out.bin, to.count = out.count, to.cursor = 0;
-            to.from = out.from, to.to = out.to;
+            to.from = out.from, to.to = out.to, to.coarse = policy.coarse();
         }
     }
 }
@@ -1461,7 +1482,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a
         const Row<DT> data{reinterpret_cast<const char *>(a.z) + t * a.ld * DT::kBytes, a.V, a.steps, a.blocks};
         const float least = policy.by_min() ? fmaxf(least_of(policy, top), -3.402823466e38f) : -3.402823466e38f;
         // what one unit of the bins' sums (2^-36 of the middle of bin 0) is in units of 2^-shift of the largest weight
-        const double to_whole = ldexp(exp2(fma(-(double)top, unit * 0.5, (double)row.place) * 0.0625), a.shift - 36);
+        const double to_whole = ldexp(exp2(fma(-(double)top, unit * 0.5, (double)row.place * (double)(1 << row.coarse)) * 0.0625), a.shift - 36);
         const double full = row.full * to_whole;
         const bool few = row.mode == kSampleFew;
         // ---- the gathered entries, from the order in which the parts found room to the parts' own

@@ -403,3 +403,21 @@ def test_masks_of_the_lowest_value(a3po, dt):
     check(a3po, z, u, p=torch.full((T,), 0.9))
     check(a3po, z, u, min_p=torch.full((T,), 0.1), tau=torch.full((T,), 1e-3))
     check(a3po, z, u, k=torch.full((T,), 20000).int(), p=torch.full((T,), 0.5), min_p=torch.full((T,), 1e-30))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("gap", [5.0, 21.0, 23.0, 40.0, 86.0, 90.0, 200.0])
+def test_counts_that_end_far_below_the_largest(a3po, gap, dt):
+    """A few entries lead by `gap`; the k-th is among the many behind them, as it is in rows that are nearly certain of a token."""
+    V, T = 20011, 9
+    g = torch.Generator().manual_seed(91)
+    z = torch.randn(T, V, generator=g)
+    for t in range(T):
+        z[t, torch.randperm(V, generator=g)[:1 + t]] += gap
+    z = z.to(DT[dt]).cuda()
+    u = torch.rand(T, generator=g)
+    k = torch.tensor([1, 2, 3, 5, 40, 50, 1000, 2400, 5000]).int()
+    check(a3po, z, u, k=k)
+    check(a3po, z, u, k=k, p=torch.linspace(0.3, 0.999999, T))
+    check(a3po, z, u, k=k, min_p=torch.full((T,), math.exp(-gap - 1)), tau=torch.full((T,), 1.25))
+    check(a3po, z, u, k=k, p=torch.full((T,), 0.9), min_p=torch.full((T,), 0.02), tau=torch.linspace(0.4, 1.6, T))
