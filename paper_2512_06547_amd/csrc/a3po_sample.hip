@@ -23,7 +23,7 @@
 // Measured, us (all five or six kernels back to back; by kernel: parts / rows / gather / finish / rows with passes / bits):
 //     1 x  32,000 fp32, top-p 0.95                         30   (6.6 / 5.7 / 6.3 / 11.2 / 2.9: five launches in a row)
 //    64 x 151,936 fp32, top-p 0.95                         64   (19 / 8 / 16 / 20 / 4)
-//   300 x  50,001 fp32, top-k 50, top-p, min-p, bits       79   (29 / 8 / 20 / 18 / 5 / 4)
+//   300 x  50,001 fp32, top-k 50, top-p, min-p, bits       80   (29 / 8 / 20 / 18 / 5 / 4)
 //   256 x 151,936 bf16, top-p 0.9 of flat rows, bits      135   (37 / 9 / 36 / 30 / 6 / 18)
 //  1024 x 151,936 bf16, uncut                             112   (one pass over the rows 111, tokens 10; under the profiler)
 // What bounds them: vector instructions where there are many parts (uncut 21 an entry, 9 of them in 64 bits: active in 94 % of a
@@ -484,8 +484,8 @@ __global__ __launch_bounds__(kPartThreads, DT::kBytes == 4 ? 3 : 5) void sample_
                     constexpr double a1 = 0.69314718055994530942 / 4, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5, a6 = a5 * a1 / 6,
                                      a7 = a6 * a1 / 7;
                     constexpr double b5 = a5 + a7 * (7.0 / 16), b3 = a3 - a7 * (7.0 / 128), b1 = a1 + a7 * (7.0 / 4096);
-                    return fma_scalar(fma_scalar(fma_scalar(fma_scalar(fma_scalar(fma_scalar(q, a6 * kOne, b5 * kOne), q, a4 * kOne), q, b3 * kOne), q, a2 * kOne), q, b1 * kOne),
-                                      q, kOne + kCounted);
+                    const double high = fma_scalar(fma_scalar(fma_scalar(q, a6 * kOne, b5 * kOne), q, a4 * kOne), q, b3 * kOne);
+                    return fma_scalar(fma_scalar(fma_scalar(high, q, a2 * kOne), q, b1 * kOne), q, kOne + kCounted);
                 });
             // what lies behind the bins is below 2^-32 of the largest, all of it below 2^-19: what fp32 loses of that, 2^-18 of it, is
             // below 2^-37
@@ -1239,7 +1239,8 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
             const bool some = mine.max > -kInf;
             part_place[tid] = some ? mine.place : 0, part_bins[tid] = some ? mine.bins : 0;
             const int64_t apart = some ? (int64_t)out.place - mine.place : 0;
-            double mass = some && apart < 16000 >> coarse ? (mine.mass[0] + mine.mass[1] + mine.mass[2] + mine.mass[3]) * down_by((int)apart << coarse) * 68719476736.0 : 0.0;
+            double mass = some && apart < 16000 >> coarse ? mine.mass[0] + mine.mass[1] + mine.mass[2] + mine.mass[3] : 0.0;
+            if (mass > 0.0) mass *= down_by((int)apart << coarse) * kOne;
             __syncthreads();
             uint64_t sum = 0;
             uint32_t own_count = 0;
