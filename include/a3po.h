@@ -599,12 +599,12 @@ int a3po_grad_norm(const void *const *grads, const int64_t *sizes, int64_t count
  * One step of AdamW for every tensor (host array [count], read during the call only):
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps).
- * All arithmetic is fp32 on the states' unrounded new values.  Roundings: float parameters none, their copy to nearest;
- * bfloat16 parameters stochastically (the share of an update below the last bit that is not lost is its mean); 8-bit exp_avg to
- * nearest; 8-bit exp_avg_sq stochastically (to nearest it would never fall: one step takes away less than half a bit) and never
- * from above zero to zero, so that no update is divided by eps alone.  The random bits of element i of tensor k are a function
- * of seed, k and i, and of step_dev's number where it is given (a replayed graph draws new ones as that goes up).  A block of 32
- * that holds an infinity or NaN reads as NaN afterwards; with `norm` such a step is left out.
+ * All arithmetic is fp32 on the states' unrounded new values; m and v have every product and sum rounded once.  Roundings: float
+ * parameters none, their copy to nearest; bfloat16 parameters stochastically (the share of an update below the last bit that is
+ * not lost is its mean); 8-bit exp_avg to nearest; 8-bit exp_avg_sq stochastically (to nearest it would never fall: one step takes
+ * away less than half a bit) and never from above zero to zero, so that no update is divided by eps alone.  The random bits of
+ * element i of tensor k are a function of seed, k and i, and of step_dev's number where it is given (a replayed graph draws new
+ * ones as that goes up).  A block of 32 that holds an infinity or NaN reads as NaN afterwards; with `norm` such a step is left out.
  * Tensors must not overlap; a param that is listed twice is refused.  0 <= beta < 1, eps >= 0, lr >= 0, weight_decay >= 0 and
  * step >= 1, else A3PO_E_VALUE (numbers on the device are not looked at).
  */

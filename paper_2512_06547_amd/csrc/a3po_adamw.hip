@@ -233,12 +233,15 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a)
         }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
+            // (each product and sum of the states is rounded, so that they are what the formulas give in fp32 anywhere: with bfloat16 gradients and
+            // beta1 = 0.9 a new mean often is a tie of two bytes, which a product that enters its sum unrounded would decide otherwise)
+#pragma clang fp contract(off)
             const float x = g[i] * factor;
             m[i] = a.beta1 * m[i] + a.rest1 * x;
             v[i] = a.beta2 * v[i] + a.rest2 * x * x;
-            const float below = __builtin_amdgcn_sqrtf(v[i]) * root + a.eps;
+            const float below = fmaf(__builtin_amdgcn_sqrtf(v[i]), root, a.eps);
             // (where there has been no gradient yet and eps is 0, the mean over its root is 0 over 0: no update)
-            p[i] = p[i] * decay - (m[i] == 0.0f ? 0.0f : size * (m[i] * __builtin_amdgcn_rcpf(below)));
+            p[i] = fmaf(p[i], decay, m[i] == 0.0f ? 0.0f : -size * (m[i] * __builtin_amdgcn_rcpf(below)));
         }
         uint32_t chance[kEach];
         if constexpr (BYTES || PT::kBytes == 2) {
