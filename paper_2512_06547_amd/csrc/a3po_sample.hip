@@ -73,7 +73,11 @@ __device__ __forceinline__ double fma_scalar(double a, double b, double c)
 struct Weigh {
     double max, unit;     // unit: 32 log2(e) / temperature
     const double *table;  // 2^(i / 32) times what the result is to be scaled by
-    __device__ __forceinline__ double operator()(float z) const
+    // below 2^-1000 of the largest there is no weight (masked entries: also where the temperature is infinite, as -inf times 0 is NaN)
+    __device__ __forceinline__ double operator()(float z) const { return has(z) ? floored(z) : 0.0; }
+    __device__ __forceinline__ bool has(float z) const { return ((double)z - max) * unit >= -32000.0; }
+    // (2^-1000 for those)
+    __device__ __forceinline__ double floored(float z) const
     {
         constexpr double a1 = 0.69314718055994530942 / 32, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4, a5 = a4 * a1 / 5;
         const double y = fmax(((double)z - max) * unit, -32000.0);
@@ -86,7 +90,7 @@ struct Weigh {
     }
     __device__ __forceinline__ uint64_t whole(float z) const
     {
-        return (uint64_t)__double_as_longlong((*this)(z) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+        return (uint64_t)__double_as_longlong(floored(z) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
     }
 };
 // 2^(-b / 16)
@@ -359,11 +363,12 @@ __device__ __forceinline__ void sum_part(const SampleArgs &a, PartEntries<DT> &z
     if (lane == 0) wave_top[wave] = bad ? __builtin_nanf("") : top, wave_count[wave] = count;
     __syncthreads();
     bool any_bad = false;
+    const float own_top = top;
     top = -kInf, count = 0;
 #pragma unroll
     for (int w = 0; w < kPartWaves; ++w) any_bad |= wave_top[w] != wave_top[w], top = fmaxf(top, wave_top[w]), count += wave_count[w];
+    const Weigh weigh{(double)top, unit, kTable};
     if (!any_bad && top > -kInf && is_wide(top, unit)) {
-        const Weigh weigh{(double)top, unit, kTable};
         mass = 0.0;
         z.each([&](float x, int) {
             mass += weigh(x);
@@ -371,7 +376,9 @@ __device__ __forceinline__ void sum_part(const SampleArgs &a, PartEntries<DT> &z
         });
         mass = wave_sum(mass);
     }
-    if (lane == 0) record.part.mass[wave] = top > -kInf ? mass : 0.0;
+    // (a quarter has mass where one of its entries has a weight beside the part's largest: sum_of counts those without at its `lowest`, and a
+    // drawn number of 0 would fall to them)
+    if (lane == 0) record.part.mass[wave] = top > -kInf && weigh.has(own_top) ? mass : 0.0;
     __syncthreads();
     write_part(record, to, any_bad ? __builtin_nanf("") : top, kSampleFar, 0, count);
 }
@@ -1083,7 +1090,8 @@ __device__ __forceinline__ float least_of(const Policy &policy, float top)
 }
 
 // Of so many entries from `begin` on, kEach a thread, the one in whose part of the kept sum the number falls; `within`: what of it lies there, in
-// units of the weight of weigh's maximum times what its table is scaled by.  Turns 0 and 1, in this order.
+// units of the weight of weigh's maximum times what its table is scaled by.  At least one of them is kept and has a weight beside that
+// maximum (callers choose by masses that are zero elsewhere), so there is such a thread.  Turns 0 and 1, in this order.
 template <int N, int kEach, typename DT>
 __device__ __forceinline__ void draw(Scans &sh, const Row<DT> &row, const Weigh &weigh, int64_t begin, int entries, double within, Border border)
 {
