@@ -855,13 +855,15 @@ def adamw_state_values(state, scale):
 
 
 def adamw_step(params, grads, exp_avgs, exp_avg_sqs, *, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
-               weight_decay: float = 0.0, scales=None, copies=None, norm=None, max_norm: float = 1.0, seed: int = 0):
+               weight_decay: float = 0.0, scales=None, copies=None, norm=None, max_norm: float = 1.0, seed: int | None = None):
     """a3po_adamw_step: one step for every tensor of the list ``params``, in place, with the states that adamw_state made
     (``scales``: their pairs, with 8-bit states) and, where ``copies`` are given, the updated parameters rounded to bfloat16.
 
     ``step`` (from 1 on) and ``lr`` are numbers, or CUDA tensors of one int64 and one float32 where a captured graph is to see
     them change.  ``norm``: what grad_norm left; gradients are scaled to ``max_norm`` at most, and a step whose norm is not
-    finite changes nothing.  ``seed``: of the roundings by chance (bfloat16 parameters, 8-bit exp_avg_sq), another each step."""
+    finite changes nothing.  ``seed``: of the roundings by chance (bfloat16 parameters, 8-bit exp_avg_sq), another each step: with the
+    same one, what a step takes from exp_avg_sq is lost at the same elements every time.  By default it is the step's number (a step
+    on the device enters the random bits by itself)."""
     torch = _torch()
     params, grads = list(params), list(grads)
     count = len(params)
@@ -885,6 +887,8 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, *, step, lr, beta1: float =
     if copies is not None:
         put(6, list(copies), torch.bfloat16, "copies")
     table = np.ascontiguousarray(columns.T)
+    if seed is None:
+        seed = 0 if isinstance(step, torch.Tensor) else int(step)
     opt = AdamwOptions(beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay, max_norm=max_norm, seed=int(seed) & 0xFFFFFFFF)
     if isinstance(step, torch.Tensor):
         opt.step_dev = _ptr(_vec(step, torch.int64, 1, "step"))
