@@ -239,7 +239,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a)
             const float x = g[i] * factor;
             m[i] = a.beta1 * m[i] + a.rest1 * x;
             v[i] = a.beta2 * v[i] + a.rest2 * x * x;
-            const float below = fmaf(__builtin_amdgcn_sqrtf(v[i]), root, a.eps);
+            // (the root's instruction takes numbers below 2^-126 for 0)
+            const bool tiny = v[i] < 0x1p-96f;
+            const float below = fmaf(__builtin_amdgcn_sqrtf(tiny ? v[i] * 0x1p64f : v[i]), tiny ? root * 0x1p-32f : root, a.eps);
             // (where there has been no gradient yet and eps is 0, the mean over its root is 0 over 0: no update)
             p[i] = fmaf(p[i], decay, m[i] == 0.0f ? 0.0f : -size * (m[i] * __builtin_amdgcn_rcpf(below)));
         }
