@@ -31,6 +31,8 @@ __global__ __launch_bounds__(kThreads) void w4_quantize_kernel(W4QuantizeArgs a)
         for (int off = 1; off < LANES; off <<= 1) hi = fmaxf(hi, __shfl_xor(hi, off, kWave)), lo = fminf(lo, __shfl_xor(lo, off, kWave));
         if constexpr (ZEROS) hi = fmaxf(hi, 0.0f), lo = fminf(lo, 0.0f);
         float scale = ZEROS ? (hi - lo) * (1.0f / 15.0f) : fmaxf(hi * (1.0f / 7.0f), lo * -0.125f);
+        if constexpr (ZEROS)  // (a range beyond fp32's largest number)
+            if (scale > 3.402823466e38f) scale = hi * (1.0f / 15.0f) - lo * (1.0f / 15.0f);
         uint32_t scale16 = 0;
         if constexpr (!SCALE_F32) scale16 = pack_bf16x2(scale, 0.0f) & 0xFFFFu, scale = bf16_bits_to_float(scale16);
         const float inverse = scale >= 1.17549435e-38f ? 1.0f / scale : 0.0f;
