@@ -654,7 +654,7 @@ struct alignas(64) SamplePart {
     uint32_t bins;   // that there are
     uint32_t count;  // entries above -inf (uncut: where asked for)
 };
-enum { kSampleDone, kSampleFew, kSampleBin, kSamplePasses };
+enum { kSampleDone, kSampleDrawn, kSampleFew, kSampleBin, kSamplePasses };  // Drawn: but for the bits of the kept
 struct alignas(128) SampleRow {
     double full, above, share;  // sums over all, over the bins before the border's, up to the border; in units of 2^-36 of bin 0
     int64_t rank;               // of the border in its bin, where it is one of a count

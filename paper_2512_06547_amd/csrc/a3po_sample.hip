@@ -1235,9 +1235,9 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
         if (policy.bad() || !(top > -kInf)) {
             tell_none<kThreads>(a, t, policy.bad() || top != top);
             out.mode = kSampleDone;
-        } else if (!policy.cut() && each_part && !a.allowed) {
+        } else if (!policy.cut() && each_part) {
             draw_uncut<kThreads, DT>(a, sh, policy, mine, t, top);
-            out.mode = kSampleDone;
+            out.mode = kSampleDrawn;
         } else if (policy.cut() && each_part && !far) {
             // ---- all parts' bins on the row's grid, a bin a thread
             const int coarse = policy.coarse();
@@ -1320,6 +1320,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a, 
             to.full = out.full, to.above = out.above, to.share = out.share, to.rank = out.rank, to.top = out.top;
             to.mode = out.mode, to.by_k = out.by_k, to.place = out.place, to.bin = out.bin, to.count = out.count, to.cursor = 0;
             to.from = out.from, to.to = out.to, to.coarse = policy.coarse();
+            to.key = kKeyOfNegInf, to.last = -1;  // (all above -inf; of cut rows finish says it)
         }
     }
 }
@@ -1622,7 +1623,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a
     }
 }
 
-// ---- bits of rows with many kept, a workgroup a part -----------------------------------------------------------------------
+// ---- bits of rows with many kept, and of uncut ones, a workgroup a part -----------------------------------------------------------------------
 
 template <typename DT>
 __global__ __launch_bounds__(kPartThreads, 4) void sample_bits_kernel(SampleArgs a, int64_t row0, int64_t rows)
@@ -1631,7 +1632,7 @@ __global__ __launch_bounds__(kPartThreads, 4) void sample_bits_kernel(SampleArgs
     constexpr int EPV = Entries::EPV, kVectors = Entries::kVectors;
     for (int64_t i = blockIdx.x; i < rows * a.parts; i += gridDim.x) {
         const int64_t r = i / a.parts, t = row0 + r;
-        if (a.row[r].mode != kSampleBin) continue;
+        if (a.row[r].mode != kSampleBin && a.row[r].mode != kSampleDrawn) continue;
         const int64_t begin = (i - r * a.parts) * kSamplePart;
         const int left = (int)min(a.V - begin, (int64_t)kSamplePart);
         Entries z;
