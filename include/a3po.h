@@ -547,7 +547,10 @@ typedef struct {
  * The words are what a3po_adjust_logits takes as `allowed` (bits past V are 0): training then sees the policy that was cut.
  * logits [T, V] dtype dt, row stride ld.  token_out [T] is required; the other outputs are nullable; allowed_ld >= ceil(V / 32).
  * Weights and their sums are computed in 64 bits, so the token is the definition's unless a border of two tokens lies within
- * about 2^-36 of the sum of the drawn number; identical calls give identical results.
+ * 2^-35 of the sum of the drawn number (uncut rows of up to 2^22 entries: 2^-36), and so is top_p's last entry.  In cut rows that
+ * more entries lie at the border of than can be listed (4,864 down to it, or 9,728 around it), or that have a border 2^-32 below the largest
+ * weight (2^-128 under top_k), and in rows of more than 2^22 entries, it is V 2^(ceil(log2 V) - 63) of the sum, at 151,936 entries 2^-27.
+ * A token always is kept, with a weight that is not rounded to zero.  Identical calls give identical results.
  * A row without an entry above -inf has token -1, kept 0, no allowed bit and log-probs of -inf.  A NaN or +inf in the row, a
  * negative temperature or a NaN among the row's parameters give token -1, kept 0, no bit and log-probs NaN.  (The loss treats
  * a token of -1 as masked.)

@@ -680,7 +680,7 @@ struct SampleArgs {
     const int32_t *top_k;
     int32_t *token, *kept, *allowed;  // all but the first nullable
     float *logp, *logp_full;
-    int shift;          // weights are whole numbers of 2^-shift of the largest
+    int shift;          // weights are whole numbers of 2^-shift of the largest, those of listed entries of 2^-kSampleListShift at least
     int blocks, steps;  // a row is `blocks` blocks of `steps` times 64 vectors of 16 bytes
     int parts;
     SamplePart *part;        // [rows at a time, parts]
@@ -690,6 +690,7 @@ struct SampleArgs {
     uint2 *list;             // [rows at a time, kSampleListed]: an entry's bits and index
 };
 constexpr int kSampleBlocks = 512;  // at most
+constexpr int kSampleListShift = 48;  // kSampleListed of 2^48 are below 2^62
 inline int sample_shift(int64_t V)
 {
     int bits = 0;

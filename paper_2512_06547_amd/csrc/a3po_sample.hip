@@ -31,8 +31,10 @@
 // scan, border; list, border, part, token.
 //
 // In a bin, weights are relative to the bin's and added as whole numbers of 2^-36, their count above them in the same 64 bits: one
-// atomic an entry.  Everywhere else that entries are counted by atomics weights are multiples of 2^-shift of the row's largest,
-// shift = 62 - log2 V (50 at most), so that V of them fit 64 bits.  Both make additions commute.
+// atomic an entry.  Everywhere else that entries are counted by atomics weights are multiples of 2^-shift of the row's largest, so many that
+// 64 bits hold the sum: shift = 62 - log2 V (50 at most) in passes, 48 at least among listed entries, of which there are fewer than
+// 2^14.  Both make additions commute.  What that rounds: sums of listed entries and bins are within 2^-35 of the kept sum, those of passes
+// within V 2^-(shift + 1) (151,936 entries 2^-27).  Uncut rows are summed in double, in one order.
 #include "a3po_common.h"
 #include "a3po_launch.h"
 
@@ -822,11 +824,11 @@ struct Row {
 };
 
 // What is written for the drawn token, which its thread has left in sh; sums are in units of 2^-shift of the largest weight.
-__device__ __forceinline__ void tell(const SampleArgs &a, Scans &sh, int64_t t, float top, float tau, double kept_mass, double full_mass, uint32_t kept)
+__device__ __forceinline__ void tell(const SampleArgs &a, Scans &sh, int64_t t, float top, float tau, int shift, double kept_mass, double full_mass, uint32_t kept)
 {
     __syncthreads();
     if (threadIdx.x >= 2) return;
-    const double x = ((double)sh.token_logit - (double)top) / (double)tau, unit = a.shift * 0.69314718055994530942;
+    const double x = ((double)sh.token_logit - (double)top) / (double)tau, unit = shift * 0.69314718055994530942;
     // (a thread each: the logarithm is there once)
     float *to = threadIdx.x ? a.logp_full : a.logp;
     if (to) to[t] = (float)(x - (log(threadIdx.x ? full_mass : kept_mass) - unit));
@@ -1063,7 +1065,7 @@ struct Passes {
                 left -= last_lane(upto);
             }
         }
-        tell(a, sh, t, top, policy.tau, (double)total, (double)full_total, kept);
+        tell(a, sh, t, top, policy.tau, a.shift, (double)total, (double)full_total, kept);
     }
 };
 
@@ -1188,7 +1190,7 @@ __device__ __forceinline__ void draw_uncut(const SampleArgs &a, Scans &sh, const
     const Row<DT> row{reinterpret_cast<const char *>(a.z) + t * a.ld * DT::kBytes, a.V, a.steps, a.blocks};
     constexpr int kQuarter = kSamplePart / kPartWaves;
     draw<N, 8>(sh, row, here, (int64_t)sh.found_digit * kQuarter, kQuarter, sh.told[0], Border{kKeyOfNegInf, -1});
-    tell(a, sh, t, top, policy.tau, full, full, kept);
+    tell(a, sh, t, top, policy.tau, a.shift, full, full, kept);
 }
 
 // Rows that the host knows to be uncut.
@@ -1475,8 +1477,8 @@ template <typename DT>
 __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a, int64_t row0, int64_t rows)
 {
     __shared__ Shared sh;
-    const int tid = threadIdx.x;
-    if (tid < 32) sh.table[tid] = ldexp(kTable[tid], a.shift);
+    const int tid = threadIdx.x, shift = max(a.shift, kSampleListShift);
+    if (tid < 32) sh.table[tid] = ldexp(kTable[tid], shift);
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const int64_t t = row0 + r;
         // (asked for before it is known whether they are needed, or there)
@@ -1492,7 +1494,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a
         const Row<DT> data{reinterpret_cast<const char *>(a.z) + t * a.ld * DT::kBytes, a.V, a.steps, a.blocks};
         const float least = policy.by_min() ? fmaxf(least_of(policy, top), -3.402823466e38f) : -3.402823466e38f;
         // what one unit of the bins' sums (2^-36 of the middle of bin 0) is in units of 2^-shift of the largest weight
-        const double to_whole = ldexp(exp2(fma(-(double)top, unit * 0.5, (double)row.place * (double)(1 << row.coarse)) * 0.0625), a.shift - 36);
+        const double to_whole = ldexp(exp2(fma(-(double)top, unit * 0.5, (double)row.place * (double)(1 << row.coarse)) * 0.0625), shift - 36);
         const double full = row.full * to_whole;
         const bool few = row.mode == kSampleFew;
         // ---- the gathered entries, from the order in which the parts found room to the parts' own
@@ -1533,7 +1535,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a
             uint64_t target = (uint64_t)k, mass;
             if (which == 1) {
                 const double need = ceil(few ? (double)fmaxf(policy.p, 0.0f) * total : (row.share - row.above) * to_whole);
-                target = need < 1.0 ? 1 : (uint64_t)need;
+                target = need < 1.0 ? 1 : (uint64_t)fmin(need, 0x1p62);  // (top_p may ask for far more than min_p has left in the list)
             }
             border = tighter(border, last_of(sh, weigh, n, high, low, which == 1, target, mass));
             if (which == 0) total = (double)mass;
@@ -1563,7 +1565,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a
                     }
                 }
             }
-            tell(a, sh, t, top, policy.tau, (double)all, full, kept_total);
+            tell(a, sh, t, top, policy.tau, shift, (double)all, full, kept_total);
             if (a.allowed) {
                 // bits of so many words at a time
                 constexpr int kWords = 2 * kSampleBlocks;
@@ -1618,7 +1620,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_finish_kernel(SampleArgs a
         if (tid == chosen) sh.told[0] = fmax(target - (upto - own), 0.0);
         __syncthreads();
         draw<kThreads, kSamplePart / kThreads>(sh, data, weigh, (int64_t)chosen * kSamplePart, kSamplePart, sh.told[0], last);
-        tell(a, sh, t, top, policy.tau, mass, full, row.count + kept);
+        tell(a, sh, t, top, policy.tau, shift, mass, full, row.count + kept);
         if (tid == 0) a.row[r].key = last.key, a.row[r].last = last.last;
     }
 }
