@@ -335,6 +335,10 @@ __device__ __forceinline__ void write_part(PartRecord &record, SamplePart &to, f
 {
     if (threadIdx.x >= kWave) return;
     if (threadIdx.x == 0) record.part.max = top, record.part.place = place, record.part.bins = bins, record.part.count = count;
+    // (lane 0's words are read by other lanes: this orders them within the wave, where LDS keeps its order by itself, for no instruction)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (threadIdx.x < sizeof(SamplePart) / 4) reinterpret_cast<uint32_t *>(&to)[threadIdx.x] = record.words[threadIdx.x];
 }
 
