@@ -70,7 +70,8 @@ def quantize_w4(weight, group):
 
 
 def rollout(policy, sampling, prompts, new_tokens, group=128, generator=None):
-    """Draws new_tokens behind each prompt [S, P].  -> history int32 [S, P + new_tokens], logp float32 [S, new_tokens]."""
+    """Draws new_tokens behind each prompt [S, P].  -> history int32 [S, P + new_tokens], logp float32 [S, new_tokens].
+    A ValueError where a row leaves no token to draw."""
     S, P = prompts.shape
     dev, total = prompts.device, P + new_tokens
     history = torch.zeros(S, total, dtype=torch.int32, device=dev)
@@ -90,6 +91,8 @@ def rollout(policy, sampling, prompts, new_tokens, group=128, generator=None):
         drawn = a3po.sample(u, torch.rand(S, generator=generator, device=dev))  # (u is adjusted: no temperature is left to apply)
         token, logp[:, i] = drawn["token"], drawn["logp"]
         history[:, P + i] = token
+    if bool((history < 0).any()):  # (rows whose mask or weights leave nothing: as an index, -1 would be a token elsewhere or none)
+        raise ValueError("no token to draw: a row of the adjusted logits is all masked, or holds NaN or +inf")
     return history, logp
 
 
