@@ -835,7 +835,7 @@ __device__ __forceinline__ void tell(const SampleArgs &a, Scans &sh, int64_t t, 
     const double x = ((double)sh.token_logit - (double)top) / (double)tau, unit = shift * 0.69314718055994530942;
     // (a thread each: the logarithm is there once)
     float *to = threadIdx.x ? a.logp_full : a.logp;
-    if (to) to[t] = (float)(x - (log(threadIdx.x ? full_mass : kept_mass) - unit));
+    if (to) to[t] = (float)fmin(x - (log(threadIdx.x ? full_mass : kept_mass) - unit), 0.0);  // (sums' rounding: a few 2^-52 too little)
     if (threadIdx.x == 0) {
         a.token[t] = (int32_t)sh.token;
         if (a.kept) a.kept[t] = (int32_t)kept;
