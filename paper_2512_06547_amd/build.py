@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import os
 import subprocess
+import sys
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -27,10 +28,12 @@ def sources():
     return [os.path.join(CSRC, s) for s in SOURCES]
 
 
-def _newest_input() -> float:
-    paths = sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cpp"))]
-    paths.append(os.path.join(ROOT, "include", "a3po.h"))
+def _newest(paths) -> float:
     return max(os.path.getmtime(p) for p in paths)
+
+
+def _stale(so: str, paths) -> bool:
+    return not os.path.exists(so) or os.path.getmtime(so) < _newest(paths)
 
 
 def _compile(src: str) -> str:
@@ -51,16 +54,28 @@ def _compile_tensors() -> None:
                            "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
 
 
+def _try_tensors() -> None:
+    """The library does not depend on it: without PyTorch's headers or a host compiler only those two calls of the binding are missing."""
+    try:
+        _compile_tensors()
+    except (ImportError, OSError, subprocess.CalledProcessError) as why:
+        if os.path.exists(TENSORS):
+            os.remove(TENSORS)
+        print(f"{os.path.basename(TENSORS)} was not built ({why}): the binding's adamw_step and grad_norm will raise", file=sys.stderr)
+
+
 def build(force: bool = True, verbose: bool = False) -> str:
-    """Compile every kernel file and link liba3po.so.  force=False skips an up-to-date library."""
-    if not force and all(os.path.exists(so) and os.path.getmtime(so) >= _newest_input() for so in (LIB, TENSORS)):
-        return LIB
-    os.makedirs(OBJ, exist_ok=True)
+    """Compile every kernel file and link liba3po.so, and a3po_tensors.so where that can be.  force=False skips what is up to date."""
+    headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")] + [os.path.join(ROOT, "include", "a3po.h")]
+    library = force or _stale(LIB, sources() + headers)
     with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        tensors = ex.submit(_compile_tensors)
-        objs = list(ex.map(_compile, sources()))
-        tensors.result()
-    subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
+        tensors = ex.submit(_try_tensors) if force or _stale(TENSORS, [os.path.join(CSRC, "a3po_tensors.cpp")]) else None
+        if library:
+            os.makedirs(OBJ, exist_ok=True)
+            objs = list(ex.map(_compile, sources()))
+            subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
+        if tensors:
+            tensors.result()
     if verbose:
         print("built", LIB)
     return LIB
