@@ -885,7 +885,8 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, *, step, lr, beta1: float =
         for i in (0, 1):
             put(4 + i, [s[i] for s in scales], torch.uint8, "scales", blocks.ctypes.data)
     if copies is not None:
-        put(6, list(copies), torch.bfloat16, "copies")
+        copies = list(copies)
+        put(6, copies, torch.bfloat16, "copies")
     table = np.ascontiguousarray(columns.T)
     if seed is None:
         seed = 0 if isinstance(step, torch.Tensor) else int(step)
@@ -905,6 +906,7 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, *, step, lr, beta1: float =
         _here(norm)
     _check(lib().a3po_adamw_step(table.ctypes.data, count, pd, gd, A3PO_STATE_8BIT if bytes_ else A3PO_STATE_F32, ctypes.byref(opt), _stream()),
            "a3po_adamw_step")
+    torch._C._increment_version(params if copies is None else params + copies)  # (autograd may have kept what these held)
 
 
 def w4_quantize(weight, group: int = 128, scale_dtype=None, zeros: bool = False):
