@@ -567,7 +567,8 @@ typedef enum {
 
 /* One tensor of an optimizer step: n elements, contiguous, all pointers on the device.
  * A3PO_STATE_8BIT: element i of a state is value(i) * 2^(scale[i / 32] - 127), where value is a byte: exp_avg in e4m3 (OCP
- * float8, 3 bits of mantissa), exp_avg_sq in e5m2; the scales are bytes [ceil(n / 32)].  All bytes zero is a state of zeros. */
+ * float8, 3 bits of mantissa), exp_avg_sq in e5m2; the scales are bytes [ceil(n / 32)], from 1 on: a block whose scale is 0 holds
+ * zeros (so all bytes zero is a state of zeros). */
 typedef struct {
     void *param;               /* dtype param_dt; updated in place                                  */
     const void *grad;          /* dtype grad_dt                                                     */
@@ -587,7 +588,8 @@ typedef struct {
     const float *norm;       /* device [1], nullable: the gradients' norm, as a3po_grad_norm leaves it.  Gradients enter     */
                              /* times min(1, max_norm / (norm + 1e-6)); where the norm is not finite nothing is changed.    */
     double max_norm;         /* > 0 with norm                                                                               */
-    uint32_t seed;           /* of the stochastic roundings: a new one each step                                            */
+    uint32_t seed;           /* of the stochastic roundings: a new one each step, or with step on the host the same elements */
+                             /* go up and down each time, and what a step takes away is lost where they go up               */
 } a3po_adamw_options;
 
 /*

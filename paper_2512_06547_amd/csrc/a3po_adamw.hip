@@ -12,8 +12,9 @@
 // Memory bounds it: a thread reads 8 elements of everything, 16 bytes at a time, past the caches, and writes them back; 2,048 a
 // workgroup, as many workgroups as there are chunks (no element is read twice, so nothing is gained by fewer).  151,936 x 1,536
 // fp32 weights with bfloat16 gradients and copies: states in 32 bits 28 bytes an element, 1,270 us, 5.1 TB/s; in 8 bits 16.1 bytes, 707 us,
-// 5.3 TB/s (446 vector instructions a wavefront, 51 % of the cycles).  The gradients' norm reads them once more, 83 us: the step needs
-// it before its first element.
+// 5.3 TB/s (495 vector instructions a wavefront, 57 % of the cycles).  The gradients' norm reads them once more, 83 us: the step needs
+// it before its first element.  With the step's number on the device each thread computes the two powers of beta in 64 bits for itself: the
+// same weights 8 us more, with 8-bit states 49.
 #include "a3po_common.h"
 #include "a3po_launch.h"
 
@@ -49,7 +50,8 @@ struct AdamArgs {
 };
 static_assert(sizeof(AdamArgs) <= 4096, "launch arguments");
 
-// 32 bits of chance for every whole number: two multiplications between shifted sums without carry
+// 32 bits of chance for every whole number: two multiplications between shifted sums without carry.  Shifts and factors are those of a
+// published function, the last step of Austin Appleby's MurmurHash3 for 32 bits (public domain).
 __host__ __device__ __forceinline__ uint32_t mix(uint32_t x)
 {
     x ^= x >> 16;
@@ -245,6 +247,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a)
             // (where there has been no gradient yet and eps is 0, the mean over its root is 0 over 0: no update)
             p[i] = fmaf(p[i], decay, m[i] == 0.0f ? 0.0f : -size * (m[i] * __builtin_amdgcn_rcpf(below)));
         }
+        // (a bfloat16 weight is rounded by the upper 16 bits, exp_avg_sq by the lower 21: an element that has both shares five of them)
         uint32_t chance[kEach];
         if constexpr (BYTES || PT::kBytes == 2) {
             const uint32_t key = mix(a.seed + 0x9E3779B9u * (a.number + (uint32_t)k + 1u)) ^ salt ^ (uint32_t)(at >> 32) * 0x9E3779B9u;

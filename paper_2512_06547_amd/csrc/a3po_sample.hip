@@ -13,22 +13,25 @@
 //            border is in
 //   gather:  the entries down to that bin, where they are few, else that bin's alone: parts without any are not read again
 //   finish:  the border among those entries, and the token
-// Rows that this does not settle (borders among very many equal logits, or 2^-32 below the largest weight, 2^-128 under top-k) are gone
-// over by one workgroup as often as their cuts ask.
+// Cut rows that this does not settle are gone over by one workgroup as often as their cuts ask (passes): a border among more entries than
+// can be listed (kSampleFewest down to it, or kSampleListed in its bin; with top-k and top-p the former), one 2^-32 below the largest weight
+// (2^-128 under top-k), also where that leaves every entry, values off the grid; and all rows of more than 512 parts.
 //
 // Why parts: one row decodes alone as often as a thousand do together, so the row's passes are spread over as many compute units as it
 // has parts, and a part stays in registers from its maximum to its bins.  Why bins on a grid of absolute places: parts need not know the
 // row's maximum, and what they find adds up.  One read of the row is needed (38 MB of 64 x 151,936 fp32 logits take 8 us at a large
 // copy's 4.9 TB/s), a second one of the parts that hold entries down to the border.
 // Measured, us (all five or six kernels back to back; by kernel: parts / rows / gather / finish / rows with passes / bits):
-//     1 x  32,000 fp32, top-p 0.95                         30   (6.6 / 5.7 / 6.3 / 11.2 / 2.9: five launches in a row)
+//     1 x  32,000 fp32, top-p 0.95                         28 to 34   (7 / 6 / 6 / 11 / 3 to 4: five launches in a row, whose host time differs by call)
 //    64 x 151,936 fp32, top-p 0.95                         64   (19 / 8 / 16 / 20 / 4)
 //   300 x  50,001 fp32, top-k 50, top-p, min-p, bits       80   (29 / 8 / 20 / 18 / 5 / 4)
-//   256 x 151,936 bf16, top-p 0.9 of flat rows, bits      135   (37 / 9 / 36 / 30 / 6 / 18)
-//  1024 x 151,936 bf16, uncut                             112   (one pass over the rows 111, tokens 10; under the profiler)
+//   256 x 151,936 bf16, top-p 0.9 of flat rows, bits      136   (37 / 9 / 36 / 30 / 6 / 18)
+//  1024 x 151,936 bf16, uncut                             113   (one pass over the rows 114, tokens 11; under the profiler)
+//   1 / 64 / 512 x 151,936 fp32, uncut with bits          25 / 41 / 193   (parts, rows, bits; without bits 15 / 21 / 96)
 // What bounds them: vector instructions where there are many parts (uncut 21 an entry, 9 of them in 64 bits: active in 94 % of a
 // compute unit's busy cycles; parts of flat rows 26 an entry, 85 %), latencies in a row where there are few: a part's load, maximum, bins; a row's parts,
-// scan, border; list, border, part, token.
+// scan, border; list, border, part, token.  Spilled registers: finish 10 in either type, passes 5 in fp32 and 47 in bfloat16, gather 2 in
+// bfloat16, none elsewhere.
 //
 // In a bin, weights are relative to the bin's and added as whole numbers of 2^-36, their count above them in the same 64 bits: one
 // atomic an entry.  Everywhere else that entries are counted by atomics weights are multiples of 2^-shift of the row's largest, so many that
@@ -281,8 +284,8 @@ __device__ __forceinline__ float first_at(int p, double grid, double step, float
     while (place_of(z, grid, lowest) < p) z = nextafterf(z, kInf);
     return z;
 }
-// in a bin's sum: the count in the upper 14 bits, weights times 2^36 below (8,192 of them, each below 1.03, are below 2^50; the
-// bin's middle is 1)
+// in a bin's sum: the count in the upper 14 bits, weights times 2^36 below (the bin's middle is 1, its largest below 1.03, or 1.10 in bins of 1/4
+// power of two: 8,192 of them are below 2^50)
 constexpr int kWeightBits = 50;
 constexpr uint64_t kWeightMask = (1ull << kWeightBits) - 1;
 constexpr double kOne = 68719476736.0, kCounted = 5629499534213120.0;  // 2^36, 2^52 + 2^50
